@@ -254,6 +254,145 @@ dmoe_status dmoe_router_no_alloc_device_error(void* stream, int32_t* info);
  * applies). */
 dmoe_status dmoe_no_alloc_scratch(void** device_ptr, size_t* bytes);
 
+/* ---------------------------------------------------------------------------------------
+ * A MoE layer by its parts: tokens sorted by expert, their rows gathered and combined (with
+ * the gradients), and products with 4-bit expert weights. §3's "MoE includes routing and expert
+ * execution" with the steps between the two as calls of their own, for programs that bring
+ * their own expert products, train, or hold the weights in 4 bits.
+ *
+ * The conventions at the head of this file hold, and for these calls:
+ *  - R = T * k rows, one per (token, slot). T = 0 (no tokens) is valid everywhere; pointers to
+ *    tensors without elements may be NULL.
+ *  - Matrices of rows have a row stride in elements (ld), at least their width. Their bases
+ *    need only be aligned to their element (16-byte aligned bases and strides run fastest,
+ *    4-byte aligned ones next). A base of int32, fp32 gates or 4-bit weights is 16-byte aligned.
+ *  - Outputs do not overlap inputs, unless a call says so. Rows of an output that a stride
+ *    leaves gaps between keep what is in the gaps.
+ *  - `pos` entries outside [-R, R) and `rows` entries outside [0, T * k) are not followed: they
+ *    count as slots without an expert, and as rows of zeros.
+ * ------------------------------------------------------------------------------------- */
+
+typedef enum { DMOE_BF16 = 0, DMOE_FP16 = 1, DMOE_FP32 = 2 } dmoe_dtype;
+
+/* Bytes of the workspace of dmoe_sort_tokens (host only). 1 <= k <= 16, 1 <= E <= 256, T >= 0,
+ * T * k <= 2^30. */
+dmoe_status dmoe_sort_workspace_size(int64_t T, int32_t k, int32_t E, size_t* bytes /* host */);
+
+/* Tokens sorted by expert, for any number of tokens and with slots that have no expert (the
+ * padding of a batch, dropped pairs). The sort is stable: an expert's rows stand in the order of
+ * their (token, slot), and the slots without an expert stand behind the last expert's rows.
+ *   topk_idx  int32 [T, k]   expert of every slot; negative: none. The same expert may stand in
+ *                            several slots of a token. An id >= E counts as none and is
+ *                            recorded in the workspace (DMOE_ERR_DEVICE)
+ *   offsets   int32 [E + 1]  out: expert e has rows offsets[e] .. offsets[e+1]; offsets[E] is
+ *                            the number of slots with an expert
+ *   rows      int32 [R]      out: rows[r] = t*k + slot; -1 from row offsets[E] on
+ *   pos       int32 [R]      out: the row of every slot; ~row (negative) for a slot without an
+ *                            expert, whose row is one of those from offsets[E] on
+ *   workspace                as for the calls above (256-byte aligned, dmoe_workspace_init
+ *                            once), of dmoe_sort_workspace_size bytes */
+dmoe_status dmoe_sort_tokens(int64_t T, int32_t k, int32_t E, const int32_t* topk_idx,
+                             int32_t* offsets, int32_t* rows, int32_t* pos, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Token rows copied into sorted order: xs[pos[t,j]] = x[t], and zeros in row ~pos[t,j] of a slot
+ * without an expert.
+ *   x   [T, d] of dtype, row stride ldx    pos  int32 [R], as from dmoe_sort_tokens or
+ *   xs  [R, d] out, row stride ldxs             dmoe_dispatch
+ * 1 <= k <= 16, d >= 1, T * k <= 2^30. */
+dmoe_status dmoe_gather_rows(int32_t dtype, int64_t T, int32_t k, int32_t d, const void* x,
+                             int64_t ldx, const int32_t* pos, void* xs, int64_t ldxs,
+                             void* stream);
+
+/* Its gradient: dx[t] = sum over the slots j with an expert of dxs[pos[t,j]], in fp32 and in the
+ * order of the slots, rounded once; zeros for a token without any. dxs [R, d], dx [T, d] out. */
+dmoe_status dmoe_gather_rows_backward(int32_t dtype, int64_t T, int32_t k, int32_t d,
+                                      const void* dxs, int64_t lddxs, const int32_t* pos,
+                                      void* dx, int64_t lddx, void* stream);
+
+/* The experts' rows back to their tokens, weighted:
+ *   y[t] = add[t] + sum over the slots j with an expert of gates[t,j] * ys[pos[t,j]],
+ * in fp32 and in the order of the slots, rounded once. Slots without an expert are left out,
+ * whatever their gate and row hold.
+ *   ys    [R, d] of dtype, row stride ldys      pos  int32 [R]
+ *   gates fp32 [T, k], or NULL for ones         add  [T, d] of dtype (row stride ldadd), or NULL
+ *   y     [T, d] out, row stride ldy; may be `add` itself (with the same stride) */
+dmoe_status dmoe_combine_rows(int32_t dtype, int64_t T, int32_t k, int32_t d, const void* ys,
+                              int64_t ldys, const int32_t* pos, const float* gates,
+                              const void* add, int64_t ldadd, void* y, int64_t ldy,
+                              void* stream);
+
+/* Its gradient (the addend's is dy itself):
+ *   dys[pos[t,j]] = gates[t,j] * dy[t];  zeros in the row ~pos[t,j] of a slot without an expert
+ *   dgates[t,j]   = sum over d of dy[t] * ys[pos[t,j]], in fp32;  0 for a slot without an expert
+ *   dy  [T, d] of dtype, row stride lddy        ys  as above; read only for dgates (else NULL)
+ *   gates fp32 [T, k], or NULL for ones
+ *   dys [R, d] out (row stride lddys), or NULL  dgates fp32 [T, k] out, or NULL (one of the two
+ *                                               at least) */
+dmoe_status dmoe_combine_rows_backward(int32_t dtype, int64_t T, int32_t k, int32_t d,
+                                       const void* dy, int64_t lddy, const void* ys,
+                                       int64_t ldys, const int32_t* pos, const float* gates,
+                                       void* dys, int64_t lddys, float* dgates, void* stream);
+
+/* Expert matrices in 4 bits: n_experts matrices of n_out rows (outputs) and n_in columns
+ * (inputs), each row cut into groups of `group` inputs that share a scale.
+ * Limits: 1 <= n_experts <= 256; 1 <= n_out <= 65536; group 32, 64 or 128; n_in a multiple of
+ * group, at most 16384. */
+typedef struct {
+  int32_t n_experts;
+  int32_t n_out;
+  int32_t n_in;
+  int32_t group;
+} dmoe_q4_desc;
+
+/* Bytes of the codes and of the scales of such matrices (host only; the layout is the
+ * library's own: 16 rows x 64 inputs per 512 bytes of codes). */
+dmoe_status dmoe_q4_size(const dmoe_q4_desc* desc, size_t* codes_bytes /* host */,
+                         size_t* scales_bytes /* host */);
+
+/* bf16 weights to 4 bits. For each group with a = max |w|: scale s = a / 7 rounded to five
+ * significant bits (to nearest, ties to even), code c = w / s rounded to the nearest integer
+ * (ties to even), -7 <= c <= 7; the group stands for the values c * s, which bf16 holds exactly
+ * (three bits times five). A group whose a is below 2^-100 stands for zeros; one that holds an
+ * infinity or a NaN stands for NaNs.
+ *   w       bf16 [n_experts, n_out, n_in]   codes, scales  out, of dmoe_q4_size bytes */
+dmoe_status dmoe_q4_quantize(const dmoe_q4_desc* desc, const void* w, void* codes, void* scales,
+                             void* stream);
+
+/* The values that codes and scales stand for: w bf16 [n_experts, n_out, n_in] out. */
+dmoe_status dmoe_q4_dequantize(const dmoe_q4_desc* desc, const void* codes, const void* scales,
+                               void* w, void* stream);
+
+/* Products of sorted rows with their experts' 4-bit matrices: row r of group u has expert
+ * e = expert_ids[u] (or u) and
+ *   y[r, n] = sum over i of W[e][n, i] * x[src(r), i]      (fp32 sums, rounded once)
+ *   x          bf16 [T_x, n_in], row stride ldx, a multiple of 8, and a 16-byte aligned base: its
+ *              rows are read 16 bytes at a time
+ *   rows       int32 [R]: row r's source is src(r) = rows[r] / k; one outside [0, T_x) counts as a
+ *              row of zeros. NULL: src(r) = r (then T_x >= R)
+ *   offsets    int32 [n_groups + 1]: group u has rows offsets[u] .. offsets[u+1]. NULL: one group
+ *              of all R rows (n_groups = 1)
+ *   expert_ids int32 [n_groups] or NULL (group u is expert u, n_groups <= n_experts). With
+ *              dmoe_dispatch's offsets: its unique_ids. Groups with an id outside
+ *              [0, n_experts) are left out
+ *   y          [R, n_out] out, bf16 or fp32 (y_dtype), row stride ldy. Rows that are in no group
+ *              (from offsets[n_groups] on, the slots without an expert) are not written
+ * 0 <= R <= 2^30; 1 <= n_groups <= 256; offsets outside [0, R] are cut to it. */
+dmoe_status dmoe_q4_linear(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const void* x,
+                           int64_t ldx, int64_t T_x, const int32_t* rows, int32_t k,
+                           const int32_t* offsets, const int32_t* expert_ids,
+                           const void* codes, const void* scales, void* y, int64_t ldy,
+                           int32_t y_dtype, void* stream);
+
+/* Gate and up products with SwiGLU: y[r, n] = silu(Wg[e][n] . x[src(r)]) * (Wu[e][n] . x[src(r)]),
+ * rounded once. Both matrices have the shape `desc`; arguments otherwise as above. */
+dmoe_status dmoe_q4_swiglu(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const void* x,
+                           int64_t ldx, int64_t T_x, const int32_t* rows, int32_t k,
+                           const int32_t* offsets, const int32_t* expert_ids,
+                           const void* gate_codes, const void* gate_scales,
+                           const void* up_codes, const void* up_scales, void* y, int64_t ldy,
+                           int32_t y_dtype, void* stream);
+
 /* Synchronises `stream`, then reads and clears the fault code the kernels recorded in
  * `workspace`. Returns DMOE_OK if none, DMOE_ERR_TIMEOUT for a bounded wait that ran out,
  * DMOE_ERR_DEVICE for any other recorded fault, DMOE_ERR_CUDA if the sync failed.

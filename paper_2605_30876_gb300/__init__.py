@@ -20,6 +20,10 @@ __all__ = [
     "dmoe_layer_forward", "dmoe_get_device_error", "dmoe_status_string", "dmoe_abi_version",
     "dmoe_layer_forward_launches",
     "alloc_workspace", "LIB_PATH", "dmoe_set_profile_events", "KERNELS",
+    "dmoe_sort_workspace_size", "alloc_sort_workspace", "dmoe_sort_tokens", "dmoe_gather_rows",
+    "dmoe_gather_rows_backward", "dmoe_combine_rows", "dmoe_combine_rows_backward",
+    "Q4Desc", "make_q4_desc", "dmoe_q4_size", "alloc_q4", "dmoe_q4_quantize",
+    "dmoe_q4_dequantize", "dmoe_q4_linear", "dmoe_q4_swiglu",
 ]
 
 DMOE_ROUTE_TOKEN = 0
@@ -53,6 +57,16 @@ def make_desc(d_model, n_experts, top_k, d_ff, d_ff_shared, block_size, n_blocks
               mode=DMOE_ROUTE_BLOCK, top_p=0.0, block_top_k=0) -> LayerDesc:
     return LayerDesc(d_model, n_experts, top_k, d_ff, d_ff_shared, block_size, n_blocks,
                      mode, float(top_p), int(block_top_k))
+
+
+class Q4Desc(ctypes.Structure):
+    """dmoe_q4_desc (include/dmoe.h)."""
+    _fields_ = [("n_experts", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("n_in", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+def make_q4_desc(n_experts, n_out, n_in, group=64) -> Q4Desc:
+    return Q4Desc(n_experts, n_out, n_in, group)
 
 
 class DmoeError(RuntimeError):
@@ -106,6 +120,24 @@ def _load() -> ctypes.CDLL:
     lib.dmoe_router_no_alloc_device_error.restype = st
     lib.dmoe_no_alloc_scratch.argtypes = [ctypes.POINTER(P), ctypes.POINTER(ctypes.c_size_t)]
     lib.dmoe_no_alloc_scratch.restype = st
+    i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    Q = ctypes.POINTER(Q4Desc)
+    sizes = ctypes.POINTER(size)
+    products = [Q, i64, i32, P, i64, i64, P, i32, P, P]
+    for name, args in {
+            "dmoe_sort_workspace_size": [i64, i32, i32, sizes],
+            "dmoe_sort_tokens": [i64, i32, i32, P, P, P, P, P, size, P],
+            "dmoe_gather_rows": [i32, i64, i32, i32, P, i64, P, P, i64, P],
+            "dmoe_gather_rows_backward": [i32, i64, i32, i32, P, i64, P, P, i64, P],
+            "dmoe_combine_rows": [i32, i64, i32, i32, P, i64, P, P, P, i64, P, i64, P],
+            "dmoe_combine_rows_backward": [i32, i64, i32, i32, P, i64, P, i64, P, P, P, i64, P, P],
+            "dmoe_q4_size": [Q, sizes, sizes],
+            "dmoe_q4_quantize": [Q, P, P, P, P],
+            "dmoe_q4_dequantize": [Q, P, P, P, P],
+            "dmoe_q4_linear": products + [P] * 2 + [P, i64, i32, P],
+            "dmoe_q4_swiglu": products + [P] * 4 + [P, i64, i32, P]}.items():
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, st
     return lib
 
 
@@ -273,6 +305,217 @@ def dmoe_set_debug_hold(workspace, hold: int, stream=None) -> None:
     `hold` is nonzero (see include/dmoe.h); cleared by dmoe_get_device_error."""
     _check(_lib.dmoe_set_debug_hold(_ptr(workspace, torch.uint8, "workspace"), int(hold),
                                     _stream(stream)), "dmoe_set_debug_hold")
+
+
+# ---------------------------------------------------------------- a layer by its parts
+# (include/dmoe.h has the meaning of every argument). Matrices of rows are 2-D tensors whose rows
+# are contiguous; their stride may leave gaps between rows. All tensors of a call are on one device,
+# which need not be the current one.
+
+_DTYPE_IDS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _matrix(t, name, shape, dtype, device) -> Tuple[int, int]:
+    """(device pointer, row stride) of a 2-D CUDA tensor of contiguous rows."""
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name}: must be a CUDA tensor on the call's device")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    n, d = shape
+    if step != 1 and d > 1:
+        raise ValueError(f"{name}: its rows must be contiguous")
+    return t.data_ptr(), ld if n > 1 else d   # (one row: any stride)
+
+
+def _vector(t, name, numel, dtype, device) -> Optional[int]:
+    """Device pointer of a contiguous CUDA tensor of `numel` elements (None -> NULL)."""
+    if t is None:
+        return None
+    p = _ptr(t, dtype, name)
+    if not isinstance(t, _Tensor) or t.get_device() != device:
+        raise ValueError(f"{name}: must be a CUDA tensor on the call's device")
+    if t.numel() != numel:
+        raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
+    return p
+
+
+def _launch(name, device, stream, *args) -> None:
+    """Calls the library on the tensors' device, on its current stream unless one is given."""
+    fn = getattr(_lib, name)
+    if _current_device is not None and torch.cuda.is_initialized() and device == _current_device():
+        _check(fn(*args, _stream(stream)), name)
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, _stream(stream)), name)
+
+
+def _slots(tokens, pos, name="pos") -> int:
+    k, rest = divmod(pos.numel(), tokens) if tokens > 0 else (1, pos.numel())
+    if rest or k < 1:
+        raise ValueError(f"{name}: {pos.numel()} entries are no k slots for each of {tokens} tokens")
+    return k
+
+
+def _row_dtype(t, name) -> int:
+    if not isinstance(t, _Tensor) or t.dtype not in _DTYPE_IDS or t.dim() != 2:
+        raise TypeError(f"{name}: expected a 2-D bf16, fp16 or fp32 tensor")
+    return _DTYPE_IDS[t.dtype]
+
+
+def dmoe_sort_workspace_size(T: int, k: int, E: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.dmoe_sort_workspace_size(T, k, E, ctypes.byref(n)), "dmoe_sort_workspace_size")
+    return n.value
+
+
+def alloc_sort_workspace(T: int, k: int, E: int, device="cuda") -> torch.Tensor:
+    """A zeroed workspace for dmoe_sort_tokens of these sizes."""
+    ws = torch.empty(dmoe_sort_workspace_size(T, k, E), dtype=torch.uint8, device=device)
+    dmoe_workspace_init(ws)
+    return ws
+
+
+def dmoe_sort_tokens(topk_idx, E, offsets, rows, pos, workspace=None, stream=None) -> None:
+    """topk_idx int32 [T, k] (negative: no expert) -> offsets [E + 1], rows [T * k], pos [T * k]."""
+    if not isinstance(topk_idx, _Tensor) or topk_idx.dim() != 2:
+        raise TypeError("topk_idx: expected an int32 tensor [T, k]")
+    T, k = topk_idx.shape
+    dev, i32 = topk_idx.get_device(), torch.int32
+    ws, nb = _ws(workspace)
+    if workspace.get_device() != dev:
+        raise ValueError("workspace: must be on the call's device")
+    _launch("dmoe_sort_tokens", dev, stream, T, k, E, _vector(topk_idx, "topk_idx", T * k, i32, dev),
+            _vector(offsets, "offsets", E + 1, i32, dev), _vector(rows, "rows", T * k, i32, dev),
+            _vector(pos, "pos", T * k, i32, dev), ws, nb)
+
+
+def dmoe_gather_rows(x, pos, xs, stream=None) -> None:
+    """xs[pos[t, j]] = x[t]; zeros in the rows of slots without an expert."""
+    dt = _row_dtype(x, "x")
+    T, d = x.shape
+    R, dev = pos.numel(), x.get_device()
+    k = _slots(T, pos)
+    px, ldx = _matrix(x, "x", (T, d), x.dtype, dev)
+    po, ldo = _matrix(xs, "xs", (R, d), x.dtype, dev)
+    _launch("dmoe_gather_rows", dev, stream, dt, T, k, d, px, ldx,
+            _vector(pos, "pos", R, torch.int32, dev), po, ldo)
+
+
+def dmoe_gather_rows_backward(dxs, pos, dx, stream=None) -> None:
+    """dx[t] = sum over its slots of dxs[pos[t, j]]."""
+    dt = _row_dtype(dxs, "dxs")
+    R, d = dxs.shape
+    T, dev = dx.shape[0], dxs.get_device()
+    k = _slots(T, pos)
+    pi, ldi = _matrix(dxs, "dxs", (T * k if T else 0, d), dxs.dtype, dev)
+    po, ldo = _matrix(dx, "dx", (T, d), dxs.dtype, dev)
+    _launch("dmoe_gather_rows_backward", dev, stream, dt, T, k, d, pi, ldi,
+            _vector(pos, "pos", R, torch.int32, dev), po, ldo)
+
+
+def dmoe_combine_rows(ys, pos, gates, add, y, stream=None) -> None:
+    """y[t] = add[t] + sum over its slots of gates[t, j] * ys[pos[t, j]] (gates, add: or None)."""
+    dt = _row_dtype(ys, "ys")
+    R, d = ys.shape
+    T, dev = y.shape[0], ys.get_device()
+    k = _slots(T, pos)
+    pi, ldi = _matrix(ys, "ys", (T * k if T else 0, d), ys.dtype, dev)
+    pa, lda = (None, 0) if add is None else _matrix(add, "add", (T, d), ys.dtype, dev)
+    po, ldo = _matrix(y, "y", (T, d), ys.dtype, dev)
+    _launch("dmoe_combine_rows", dev, stream, dt, T, k, d, pi, ldi,
+            _vector(pos, "pos", R, torch.int32, dev),
+            _vector(gates, "gates", R, torch.float32, dev), pa, lda, po, ldo)
+
+
+def dmoe_combine_rows_backward(dy, ys, pos, gates, dys, dgates, stream=None) -> None:
+    """dys[pos[t, j]] = gates[t, j] * dy[t] and dgates[t, j] = <dy[t], ys[pos[t, j]]> (either of
+    dys and dgates may be None; ys is read for dgates only)."""
+    dt = _row_dtype(dy, "dy")
+    T, d = dy.shape
+    R, dev = pos.numel(), dy.get_device()
+    k = _slots(T, pos)
+    pd, ldd = _matrix(dy, "dy", (T, d), dy.dtype, dev)
+    py, ldy = (None, 0) if ys is None else _matrix(ys, "ys", (R, d), dy.dtype, dev)
+    po, ldo = (None, 0) if dys is None else _matrix(dys, "dys", (R, d), dy.dtype, dev)
+    f32 = torch.float32
+    _launch("dmoe_combine_rows_backward", dev, stream, dt, T, k, d, pd, ldd, py, ldy,
+            _vector(pos, "pos", R, torch.int32, dev), _vector(gates, "gates", R, f32, dev), po, ldo,
+            _vector(dgates, "dgates", R, f32, dev))
+
+
+def dmoe_q4_size(desc: Q4Desc) -> Tuple[int, int]:
+    """(bytes of the codes, bytes of the scales)."""
+    c, s = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib.dmoe_q4_size(ctypes.byref(desc), ctypes.byref(c), ctypes.byref(s)), "dmoe_q4_size")
+    return c.value, s.value
+
+
+def alloc_q4(desc: Q4Desc, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Buffers (uint8) for the codes and the scales of `desc`'s matrices."""
+    return tuple(torch.empty(n, dtype=torch.uint8, device=device) for n in dmoe_q4_size(desc))
+
+
+def _q4(desc, codes, scales, name, device) -> Tuple[int, int]:
+    if codes is None or scales is None:
+        raise TypeError(f"{name}: codes and scales are required")
+    nc, ns = dmoe_q4_size(desc)
+    return (_vector(codes, f"{name} codes", nc, torch.uint8, device),
+            _vector(scales, f"{name} scales", ns, torch.uint8, device))
+
+
+def _q4_convert(name, desc, w, codes, scales, stream):
+    if not isinstance(w, _Tensor):
+        raise TypeError("w: expected a torch.Tensor")
+    dev = w.get_device()
+    c, s = _q4(desc, codes, scales, "w", dev)
+    p = _vector(w, "w", desc.n_experts * desc.n_out * desc.n_in, torch.bfloat16, dev)
+    pw = (p, c, s) if name == "dmoe_q4_quantize" else (c, s, p)
+    _launch(name, dev, stream, ctypes.byref(desc), *pw)
+
+
+def dmoe_q4_quantize(desc, w, codes, scales, stream=None) -> None:
+    """w bf16 [n_experts, n_out, n_in] -> codes, scales (alloc_q4)."""
+    _q4_convert("dmoe_q4_quantize", desc, w, codes, scales, stream)
+
+
+def dmoe_q4_dequantize(desc, codes, scales, w, stream=None) -> None:
+    """codes, scales -> the bf16 values they stand for, w [n_experts, n_out, n_in]."""
+    _q4_convert("dmoe_q4_dequantize", desc, w, codes, scales, stream)
+
+
+def _q4_products(name, desc, x, offsets, weights, y, rows, k, expert_ids, stream):
+    if not isinstance(x, _Tensor) or x.dim() != 2 or not isinstance(y, _Tensor) or y.dim() != 2:
+        raise TypeError("x, y: expected 2-D tensors")
+    dev, (T, R) = x.get_device(), (x.shape[0], y.shape[0])
+    px, ldx = _matrix(x, "x", (T, desc.n_in), torch.bfloat16, dev)
+    ydt = torch.float32 if y.dtype is torch.float32 else torch.bfloat16
+    py, ldy = _matrix(y, "y", (R, desc.n_out), ydt, dev)
+    n = offsets.numel() - 1 if offsets is not None else 1
+    i32 = torch.int32
+    ptrs = [p for c, s in zip(weights[::2], weights[1::2]) for p in _q4(desc, c, s, "weights", dev)]
+    _launch(name, dev, stream, ctypes.byref(desc), R, n, px, ldx, T,
+            _vector(rows, "rows", R, i32, dev), k, _vector(offsets, "offsets", n + 1, i32, dev),
+            _vector(expert_ids, "expert_ids", n, i32, dev), *ptrs, py, ldy, _DTYPE_IDS[ydt])
+
+
+def dmoe_q4_linear(desc, x, offsets, codes, scales, y, rows=None, k=1, expert_ids=None,
+                   stream=None) -> None:
+    """y[r] = W[expert of r] x[rows[r] // k] (rows None: x[r]) for the rows of every group of
+    offsets (None: one group of all rows)."""
+    _q4_products("dmoe_q4_linear", desc, x, offsets, (codes, scales), y, rows, k, expert_ids,
+                 stream)
+
+
+def dmoe_q4_swiglu(desc, x, offsets, gate_codes, gate_scales, up_codes, up_scales, y, rows=None,
+                   k=1, expert_ids=None, stream=None) -> None:
+    """y[r] = silu(Wg x) * (Wu x), arguments as for dmoe_q4_linear."""
+    _q4_products("dmoe_q4_swiglu", desc, x, offsets, (gate_codes, gate_scales, up_codes, up_scales),
+                 y, rows, k, expert_ids, stream)
 
 
 KERNELS = {"router": 0, "dispatch": 1, "gather": 2, "experts": 3, "combine": 4}

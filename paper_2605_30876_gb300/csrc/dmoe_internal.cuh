@@ -36,7 +36,7 @@ enum DevErr : int32_t {
 };
 enum DevWhere : int32_t {
   kAtRouter = 1, kAtBlockRoute = 2, kAtDispatch = 3, kAtGateUp = 4, kAtDown = 5,
-  kAtCombine = 6, kAtGather = 7,
+  kAtCombine = 6, kAtGather = 7, kAtSort = 8,
 };
 constexpr int kRouteTickets = 256;
 constexpr int kRouteClusterCtas = 8;   // CTAs per cluster of the decode-size routing launch
@@ -309,6 +309,54 @@ constexpr int kSpecMaskWords = (kMaxExperts + 23) / 24;
 // every group, all tokens at once (no gather), then the combine.
 bool experts_decode_ok(int T, int d, int I, int Is);
 cudaError_t launch_experts_decode(const ExpertArgs& a, cudaStream_t s);
+
+// Tokens sorted by expert (sort_tokens.cu): the workspace is the fault record and the chunks' counts.
+size_t sort_workspace_bytes(int64_t R, int E);
+cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,
+                               int32_t* rows, int32_t* pos, void* ws, cudaStream_t s);
+
+// Rows of tokens into sorted order and back, and their gradients (rows.cu). Strides in elements.
+struct RowsArgs {
+  int dtype;             // dmoe_dtype
+  int64_t T;
+  int k, d;
+  const int32_t* pos;    // [T * k]
+  const float* gates;    // [T, k] or null
+  const void* tok;       // [T, d] read: x, the addend (or null), dy
+  int64_t ldtok;
+  const void* sorted;    // [T * k, d] read: ys or dxs (null: dgates is not wanted)
+  int64_t ldsorted;
+  void* tok_out;         // [T, d] written: y or dx
+  int64_t ldtok_out;
+  void* sorted_out;      // [T * k, d] written: xs or dys (or null)
+  int64_t ldsorted_out;
+  float* dgates;         // [T, k] or null
+};
+cudaError_t launch_gather_rows(const RowsArgs& a, cudaStream_t s);
+cudaError_t launch_combine_rows(const RowsArgs& a, cudaStream_t s);
+cudaError_t launch_combine_rows_backward(const RowsArgs& a, cudaStream_t s);
+
+// 4-bit matrices (q4_weights.cu, q4_linear.cu; the layout: q4.cuh)
+cudaError_t launch_q4_quantize(const dmoe_q4_desc& d, const void* w, void* codes, void* scales,
+                               cudaStream_t s);
+cudaError_t launch_q4_dequantize(const dmoe_q4_desc& d, const void* codes, const void* scales,
+                                 void* w, cudaStream_t s);
+struct Q4Args {
+  const __nv_bfloat16* x;      // [T_x, K]
+  int64_t ldx, T_x;
+  const int32_t* rows;         // [R] or null
+  int k;
+  const int32_t* offsets;      // [n_groups + 1] or null
+  const int32_t* expert_ids;   // [n_groups] or null
+  const void* codes[2];        // gate and up, or one matrix and null
+  const void* scales[2];
+  void* y;                     // [R, N]
+  int64_t ldy;
+  bool y_fp32;
+  int64_t R;
+  int n_groups, n_experts;
+};
+cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_t s);
 
 // profiling events (dmoe_set_profile_events), per host thread
 void prof_begin(int kernel, cudaStream_t s);

@@ -1,0 +1,175 @@
+// bf16 weights to 4-bit codes and group scales, and back. One warp takes 16 rows x 128 inputs
+// (whole groups of every size): 4 KB of weights, two tiles of codes. Bound by the bytes.
+#include "q4.cuh"
+
+namespace dmoe {
+namespace {
+
+constexpr int kQ4Threads = 256;
+
+struct Q4Block {   // a warp's 16 x 128 weights
+  int e, nt, kb;
+  bool ok;
+};
+__device__ __forceinline__ Q4Block q4_block(const Q4Shape& s, int n_experts) {
+  const int kbs = (s.k_tiles + 1) / 2;
+  int64_t i = (int64_t)blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5);
+  Q4Block b;
+  b.kb = (int)(i % kbs);
+  i /= kbs;
+  b.nt = (int)(i % s.row_tiles);
+  i /= s.row_tiles;
+  b.e = (int)i;
+  b.ok = i < n_experts;
+  return b;
+}
+
+// a / 7 to five significant bits, for a >= 2^-100 (the quotient is a normal number)
+__device__ __forceinline__ float q4_scale(float a) {
+  uint32_t u = __float_as_uint(a / 7.f);
+  u = (u + 0x3FFFFu + (u >> 19 & 1u)) & ~0x7FFFFu;
+  return __uint_as_float(u);
+}
+
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
+
+__global__ void __launch_bounds__(kQ4Threads)
+q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint4* __restrict__ codes,
+                   uint32_t* __restrict__ scales) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const Q4Block b = q4_block(s, n_experts);
+  if (!b.ok) return;
+  const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  uint4 v[2][4];       // rows g and g + 8; 32 inputs each
+  uint32_t top[2][4];  // the largest magnitude, as the bits of a bf16
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int n = b.nt * 16 + g + 8 * r, k = b.kb * 128 + c * 32 + q * 8;
+      v[r][c] = n < s.N && k < s.K
+                    ? __ldcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t m = 0x7FFF7FFFu;
+      uint32_t t = max2(max2(v[r][c].x & m, v[r][c].y & m), max2(v[r][c].z & m, v[r][c].w & m));
+      t = max2(t, __shfl_xor_sync(0xffffffffu, t, 1));
+      t = max2(t, __shfl_xor_sync(0xffffffffu, t, 2));
+      top[r][c] = max(t & 0xFFFFu, t >> 16);
+    }
+  const int per = s.group / 32;   // 32-input chunks per group: 1, 2 or 4
+  float scale[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (per >= 2) {
+      top[r][0] = top[r][1] = max(top[r][0], top[r][1]);
+      top[r][2] = top[r][3] = max(top[r][2], top[r][3]);
+    }
+    if (per == 4) top[r][0] = top[r][1] = top[r][2] = top[r][3] = max(top[r][0], top[r][2]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float a = __uint_as_float(top[r][c] << 16);
+      scale[r][c] = top[r][c] >= 0x7F80u ? __int_as_float(0x7FC00000) : a < 0x1p-100f ? 0.f : q4_scale(a);
+    }
+  }
+  uint32_t word[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t raw[4] = {v[r][c].x, v[r][c].y, v[r][c].z, v[r][c].w};
+      const bool plain = scale[r][c] > 0.f;
+      const float d = plain ? scale[r][c] : 1.f;
+      uint32_t o = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float lo = __uint_as_float(raw[i] << 16), hi = __uint_as_float(raw[i] & 0xFFFF0000u);
+        const int cl = plain ? __float2int_rn(lo / d) : 0, ch = plain ? __float2int_rn(hi / d) : 0;
+        o |= (uint32_t)(cl + 8) << (4 * i) | (uint32_t)(ch + 8) << (16 + 4 * i);
+      }
+      word[r][c] = o;
+    }
+  const size_t tile = (size_t)b.e * s.row_tiles + b.nt;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (b.kb * 2 + h < s.k_tiles)
+      codes[(tile * s.k_tiles + b.kb * 2 + h) * 32 + lane] =
+          make_uint4(word[0][2 * h], word[1][2 * h], word[0][2 * h + 1], word[1][2 * h + 1]);
+  uint32_t* sc = scales + (tile * 8 + g) * s.groups_pad;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int gi = (b.kb * 4 + c) / per;
+    if (q == c && c % per == 0 && gi < s.groups)
+      sc[gi] = __float_as_uint(scale[0][c]) >> 16 | (__float_as_uint(scale[1][c]) & 0xFFFF0000u);
+  }
+  if (b.kb == (s.k_tiles + 1) / 2 - 1 && q == 0)
+    for (int gi = s.groups; gi < s.groups_pad; ++gi) sc[gi] = 0u;
+}
+
+__global__ void __launch_bounds__(kQ4Threads)
+q4_dequantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ codes,
+                     const uint32_t* __restrict__ scales, uint4* __restrict__ w) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const Q4Block b = q4_block(s, n_experts);
+  if (!b.ok) return;
+  const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const size_t tile = (size_t)b.e * s.row_tiles + b.nt;
+  const uint32_t* sc = scales + (tile * 8 + g) * s.groups_pad;
+  const int per = s.group / 32;
+  uint32_t word[2][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint4 c = make_uint4(0, 0, 0, 0);
+    if (b.kb * 2 + h < s.k_tiles) c = __ldcs(codes + (tile * s.k_tiles + b.kb * 2 + h) * 32 + lane);
+    word[0][2 * h] = c.x;
+    word[1][2 * h] = c.y;
+    word[0][2 * h + 1] = c.z;
+    word[1][2 * h + 1] = c.w;
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int gi = (b.kb * 4 + c) / per, k = b.kb * 128 + c * 32 + q * 8;
+    if (k >= s.K) continue;
+    const uint32_t pair = __ldg(sc + gi);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int n = b.nt * 16 + g + 8 * r;
+      const uint32_t one = r == 0 ? pair & 0xFFFFu : pair >> 16, two = one | one << 16;
+      const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&two);
+      if (n < s.N)
+        __stcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8,
+               make_uint4(q4_value_pair(word[r][c], 0, v), q4_value_pair(word[r][c], 1, v),
+                          q4_value_pair(word[r][c], 2, v), q4_value_pair(word[r][c], 3, v)));
+    }
+  }
+}
+
+unsigned q4_ctas(const Q4Shape& s, int n_experts) {
+  const int64_t warps = (int64_t)n_experts * s.row_tiles * ((s.k_tiles + 1) / 2);
+  return (unsigned)((warps + kQ4Threads / 32 - 1) / (kQ4Threads / 32));
+}
+
+}  // namespace
+
+cudaError_t launch_q4_quantize(const dmoe_q4_desc& d, const void* w, void* codes, void* scales,
+                               cudaStream_t s) {
+  const Q4Shape sh = q4_shape(d);
+  return launch_ex(q4_quantize_kernel, dim3(q4_ctas(sh, d.n_experts)), dim3(kQ4Threads), 0, s, true,
+                   sh, d.n_experts, static_cast<const uint4*>(w), static_cast<uint4*>(codes),
+                   static_cast<uint32_t*>(scales));
+}
+
+cudaError_t launch_q4_dequantize(const dmoe_q4_desc& d, const void* codes, const void* scales,
+                                 void* w, cudaStream_t s) {
+  const Q4Shape sh = q4_shape(d);
+  return launch_ex(q4_dequantize_kernel, dim3(q4_ctas(sh, d.n_experts)), dim3(kQ4Threads), 0, s,
+                   true, sh, d.n_experts, static_cast<const uint4*>(codes),
+                   static_cast<const uint32_t*>(scales), static_cast<uint4*>(w));
+}
+
+}  // namespace dmoe

@@ -1,0 +1,314 @@
+// Token rows into the experts' order and back, and the gradients of both. All four are copies and
+// short sums: they are bound by the bytes of the rows (each read once and written once), so the work
+// is cut by tokens: a token's row is held in registers while its k sorted rows are written or
+// read, and no row of x or dy is read k times.
+#include <cuda_fp16.h>
+
+#include "block_reduce.cuh"
+#include "dmoe_internal.cuh"
+
+namespace dmoe {
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kSlotBatch = 8;   // slots whose rows are in flight together
+
+// VB bytes of a row as loaded and stored at once
+template <int VB> struct Raw;
+template <> struct Raw<16> { using type = uint4; };
+template <> struct Raw<4> { using type = uint32_t; };
+template <> struct Raw<2> { using type = uint16_t; };
+
+template <typename T, int VB>
+struct Piece {
+  static constexpr int n = VB / (int)sizeof(T);
+  using raw = typename Raw<VB>::type;
+  union {
+    raw r;
+    T e[n];
+  };
+  __device__ __forceinline__ Piece() {}
+};
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) {
+  return __float2bfloat16_rn(v);
+}
+
+template <typename T, int VB>
+__device__ __forceinline__ Piece<T, VB> load_piece(const T* row, int64_t v) {
+  Piece<T, VB> p;
+  p.r = *(reinterpret_cast<const typename Raw<VB>::type*>(row) + v);
+  return p;
+}
+template <typename T, int VB>
+__device__ __forceinline__ void store_piece(T* row, int64_t v, const Piece<T, VB>& p) {
+  *(reinterpret_cast<typename Raw<VB>::type*>(row) + v) = p.r;
+}
+
+// the sorted row that a pos entry names; -1: one that is not followed
+__device__ __forceinline__ int named_row(int p, int R) {
+  const int r = p < 0 ? ~p : p;
+  return r < R ? r : -1;
+}
+
+// gather: thread (v, token) copies piece v of the token's row to its k places
+template <typename T, int VB>
+__global__ void __launch_bounds__(kRowThreads)
+gather_rows_kernel(const T* __restrict__ x, int64_t ldx, const int32_t* __restrict__ pos,
+                   T* __restrict__ xs, int64_t ldxs, int64_t tokens, int k, int nv) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int v = blockIdx.y * blockDim.x + threadIdx.x;
+  if (t >= tokens || v >= nv) return;
+  const int R = (int)(tokens * k);
+  const Piece<T, VB> p = load_piece<T, VB>(x + t * ldx, v);
+  Piece<T, VB> zero;
+  zero.r = typename Raw<VB>::type{};
+  for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
+    int at[kSlotBatch];
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j) at[j] = j0 + j < k ? __ldg(pos + t * k + j0 + j) : R;
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j) {
+      const int r = named_row(at[j], R);
+      if (r >= 0) store_piece<T, VB>(xs + r * ldxs, v, at[j] < 0 ? zero : p);
+    }
+  }
+}
+
+// combine (and, with neither gates nor an addend, the gather's gradient): thread (v, token) adds up
+// piece v of the token's k rows in fp32, in the order of the slots
+template <typename T, int VB>
+__global__ void __launch_bounds__(kRowThreads)
+combine_rows_kernel(const T* __restrict__ ys, int64_t ldys, const int32_t* __restrict__ pos,
+                    const float* __restrict__ gates, const T* add, int64_t ldadd, T* y,
+                    int64_t ldy, int64_t tokens, int k, int nv) {
+  constexpr int n = Piece<T, VB>::n;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int v = blockIdx.y * blockDim.x + threadIdx.x;
+  if (t >= tokens || v >= nv) return;
+  const int R = (int)(tokens * k);
+  float acc[n];
+#pragma unroll
+  for (int i = 0; i < n; ++i) acc[i] = 0.f;
+  if (add != nullptr) {
+    const Piece<T, VB> p = load_piece<T, VB>(add + t * ldadd, v);
+#pragma unroll
+    for (int i = 0; i < n; ++i) acc[i] = to_f(p.e[i]);
+  }
+  for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
+    int at[kSlotBatch];
+    float g[kSlotBatch];
+    Piece<T, VB> p[kSlotBatch];
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j) {
+      at[j] = j0 + j < k ? __ldg(pos + t * k + j0 + j) : -1;
+      if (at[j] >= R) at[j] = -1;
+      g[j] = gates != nullptr && j0 + j < k ? __ldg(gates + t * k + j0 + j) : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j)
+      if (at[j] >= 0) p[j] = load_piece<T, VB>(ys + at[j] * ldys, v);
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j)
+      if (at[j] >= 0) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) acc[i] = fmaf(g[j], to_f(p[j].e[i]), acc[i]);
+      }
+  }
+  Piece<T, VB> out;
+#pragma unroll
+  for (int i = 0; i < n; ++i) out.e[i] = from_f<T>(acc[i]);
+  store_piece<T, VB>(y + t * ldy, v, out);
+}
+
+// Sums of kSlotBatch values over a warp's lanes: each step halves the values a lane keeps. The
+// lane's result is that of value slot_of(lane), the same in the four lanes that share it.
+__device__ __forceinline__ int slot_of(int lane) {
+  return (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
+}
+__device__ __forceinline__ float warp_sums(float (&a)[kSlotBatch], int lane) {
+#pragma unroll
+  for (int half = kSlotBatch / 2, o = 16; half > 0; half >>= 1, o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const float give = up ? a[i] : a[i + half], keep = up ? a[i + half] : a[i];
+      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  a[0] += __shfl_xor_sync(0xffffffffu, a[0], 2);
+  a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
+  return a[0];
+}
+
+// combine's gradient: the threads of a token (blockDim.x of them, whole warps) go over dy's row,
+// write gate * dy to its k rows and add up dy * ys for its k gates
+template <typename T, int VB>
+__global__ void __launch_bounds__(kRowThreads)
+combine_rows_backward_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ ys,
+                             int64_t ldys, const int32_t* __restrict__ pos,
+                             const float* __restrict__ gates, T* __restrict__ dys, int64_t lddys,
+                             float* __restrict__ dgates, int64_t tokens, int k, int nv) {
+  constexpr int n = Piece<T, VB>::n;
+  __shared__ float part[kRowThreads / 32][kSlotBatch];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int warp = (threadIdx.y * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+  const int R = (int)(tokens * k);
+  for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
+    int at[kSlotBatch];
+    float g[kSlotBatch], dot[kSlotBatch];
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j) {
+      const bool in = t < tokens && j0 + j < k;
+      at[j] = in ? __ldg(pos + t * k + j0 + j) : R;
+      g[j] = in && gates != nullptr ? __ldg(gates + t * k + j0 + j) : 1.f;
+      dot[j] = 0.f;
+    }
+    if (t < tokens)
+      for (int v = threadIdx.x; v < nv; v += blockDim.x) {
+        const Piece<T, VB> d = load_piece<T, VB>(dy + t * lddy, v);
+        Piece<T, VB> p[kSlotBatch];
+        if (dgates != nullptr) {
+#pragma unroll
+          for (int j = 0; j < kSlotBatch; ++j)
+            if (at[j] >= 0 && at[j] < R) p[j] = load_piece<T, VB>(ys + at[j] * ldys, v);
+        }
+        if (dys != nullptr) {
+#pragma unroll
+          for (int j = 0; j < kSlotBatch; ++j) {
+            const int r = named_row(at[j], R);
+            if (r < 0) continue;
+            Piece<T, VB> o;
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+              o.e[i] = at[j] < 0 ? from_f<T>(0.f) : from_f<T>(g[j] * to_f(d.e[i]));
+            store_piece<T, VB>(dys + r * lddys, v, o);
+          }
+        }
+        if (dgates != nullptr) {
+#pragma unroll
+          for (int j = 0; j < kSlotBatch; ++j)
+            if (at[j] >= 0 && at[j] < R) {
+#pragma unroll
+              for (int i = 0; i < n; ++i) dot[j] = fmaf(to_f(d.e[i]), to_f(p[j].e[i]), dot[j]);
+            }
+        }
+      }
+    if (dgates == nullptr) continue;   // (the same for all threads)
+    const float sum = warp_sums(dot, lane);
+    if ((lane & 3) == 0) part[warp][slot_of(lane)] = sum;
+    __syncthreads();
+    if (t < tokens && threadIdx.x < kSlotBatch && j0 + threadIdx.x < k) {
+      float s = 0.f;
+      for (int w = 0; w < (int)blockDim.x / 32; ++w) s += part[warp + w][threadIdx.x];
+      dgates[t * k + j0 + threadIdx.x] = s;
+    }
+    __syncthreads();
+  }
+}
+
+// pieces of a row, and the CTA's shape: `x` threads on a token's row (whole warps, at most a CTA)
+struct RowShape {
+  int nv;
+  dim3 block;
+};
+RowShape row_shape(int d, int per_piece) {
+  RowShape s;
+  s.nv = d / per_piece;
+  int bx = 32;
+  while (bx < s.nv && bx < kRowThreads) bx *= 2;
+  s.block = dim3(bx, kRowThreads / bx);
+  return s;
+}
+
+// the widest pieces that the rows' width, strides and bases allow
+int piece_bytes(int esize, int d, std::initializer_list<const void*> ptrs,
+                std::initializer_list<int64_t> lds) {
+  uint64_t bits = (uint64_t)d * esize;
+  for (const void* p : ptrs) bits |= reinterpret_cast<uint64_t>(p);
+  for (int64_t ld : lds) bits |= (uint64_t)ld * esize;
+  if (bits % 16 == 0) return 16;
+  return bits % 4 == 0 ? 4 : 2;
+}
+
+// calls f(T{}, pieces' bytes as a constant) for a dtype
+template <int V> struct Int { static constexpr int value = V; };
+template <typename F>
+cudaError_t with_type(int dtype, int vb, F f) {
+  switch (dtype) {
+    case DMOE_BF16:
+      return vb == 16 ? f(__nv_bfloat16{}, Int<16>{})
+                      : vb == 4 ? f(__nv_bfloat16{}, Int<4>{}) : f(__nv_bfloat16{}, Int<2>{});
+    case DMOE_FP16:
+      return vb == 16 ? f(__half{}, Int<16>{})
+                      : vb == 4 ? f(__half{}, Int<4>{}) : f(__half{}, Int<2>{});
+    default: return vb == 16 ? f(float{}, Int<16>{}) : f(float{}, Int<4>{});
+  }
+}
+
+int dtype_bytes(int dtype) { return dtype == DMOE_FP32 ? 4 : 2; }
+
+}  // namespace
+
+cudaError_t launch_gather_rows(const RowsArgs& a, cudaStream_t s) {
+  const int es = dtype_bytes(a.dtype);
+  const int vb = piece_bytes(es, a.d, {a.tok, a.sorted_out}, {a.ldtok, a.ldsorted_out});
+  return with_type(a.dtype, vb, [&](auto z, auto w) {
+    using T = decltype(z);
+    constexpr int VB = decltype(w)::value;
+    const RowShape sh = row_shape(a.d, VB / es);
+    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y),
+                    (sh.nv + sh.block.x - 1) / sh.block.x);
+    return launch_ex(gather_rows_kernel<T, VB>, grid, sh.block, 0, s, true,
+                     static_cast<const T*>(a.tok), a.ldtok, a.pos, static_cast<T*>(a.sorted_out),
+                     a.ldsorted_out, a.T, a.k, sh.nv);
+  });
+}
+
+cudaError_t launch_combine_rows(const RowsArgs& a, cudaStream_t s) {
+  const int es = dtype_bytes(a.dtype);
+  const int vb = piece_bytes(es, a.d, {a.sorted, a.tok, a.tok_out},
+                             {a.ldsorted, a.tok != nullptr ? a.ldtok : 0, a.ldtok_out});
+  return with_type(a.dtype, vb, [&](auto z, auto w) {
+    using T = decltype(z);
+    constexpr int VB = decltype(w)::value;
+    const RowShape sh = row_shape(a.d, VB / es);
+    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y),
+                    (sh.nv + sh.block.x - 1) / sh.block.x);
+    return launch_ex(combine_rows_kernel<T, VB>, grid, sh.block, 0, s, true,
+                     static_cast<const T*>(a.sorted), a.ldsorted, a.pos, a.gates,
+                     static_cast<const T*>(a.tok), a.ldtok, static_cast<T*>(a.tok_out),
+                     a.ldtok_out, a.T, a.k, sh.nv);
+  });
+}
+
+cudaError_t launch_combine_rows_backward(const RowsArgs& a, cudaStream_t s) {
+  const int es = dtype_bytes(a.dtype);
+  const int vb = piece_bytes(es, a.d, {a.tok, a.sorted, a.sorted_out},
+                             {a.ldtok, a.sorted != nullptr ? a.ldsorted : 0,
+                              a.sorted_out != nullptr ? a.ldsorted_out : 0});
+  return with_type(a.dtype, vb, [&](auto z, auto w) {
+    using T = decltype(z);
+    constexpr int VB = decltype(w)::value;
+    const RowShape sh = row_shape(a.d, VB / es);
+    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y));
+    return launch_ex(combine_rows_backward_kernel<T, VB>, grid, sh.block, 0, s, true,
+                     static_cast<const T*>(a.tok), a.ldtok, static_cast<const T*>(a.sorted),
+                     a.ldsorted, a.pos, a.gates, static_cast<T*>(a.sorted_out), a.ldsorted_out,
+                     a.dgates, a.T, a.k, sh.nv);
+  });
+}
+
+}  // namespace dmoe

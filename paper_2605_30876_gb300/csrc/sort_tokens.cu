@@ -1,0 +1,156 @@
+// Tokens sorted by expert: a stable counting sort of the R = T k (token, slot) pairs over E + 1
+// keys (the experts, and last the pairs without one).
+//   sort_count_kernel  pairs per key of each chunk of pairs, one CTA per chunk
+//   sort_place_kernel  every CTA adds up, per key, the pairs before its chunk and all of them, and
+//                      goes through its chunk kSortTile pairs at a time: per warp the pairs of each
+//                      key by ballots over the warp's lanes, a prefix over the warps, and each
+//                      pair's row is its key's base, the pairs of its key in the warps before its
+//                      own and those before it in its warp.
+// Up to kSortTile pairs take the second launch alone. Every count is an integer sum: the order does
+// not depend on the order of atomics.
+#include "block_reduce.cuh"
+#include "dmoe_internal.cuh"
+
+namespace dmoe {
+namespace {
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortRounds = 4;                          // pairs per thread and tile
+constexpr int kSortTile = kSortThreads * kSortRounds;   // 4096 pairs
+constexpr int kSortMaxChunks = 148;                     // every CTA of one wave takes one chunk
+constexpr int kMaxKeys = kMaxExperts + 1;
+
+__device__ __forceinline__ int sort_key(int id, int E) { return id < 0 || id >= E ? E : id; }
+
+__global__ void __launch_bounds__(kSortThreads)
+sort_count_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk,
+                  int32_t* __restrict__ counts) {
+  __shared__ int cnt[kMaxKeys];
+  const int tid = threadIdx.x;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (tid <= E) cnt[tid] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * chunk, end = begin + chunk < R ? begin + chunk : R;
+  for (int64_t i = begin + tid; i < end; i += kSortThreads)
+    atomicAdd(&cnt[sort_key(__ldcg(ids + i), E)], 1);
+  __syncthreads();
+  if (tid <= E) counts[(size_t)blockIdx.x * (E + 1) + tid] = cnt[tid];
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk, int nchunks,
+                  const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+                  int32_t* __restrict__ rows, int32_t* __restrict__ pos, DevErrRecord* err) {
+  __shared__ int cnt[kSortWarps][kMaxKeys];   // per warp and key: pairs, then the first row
+  __shared__ int base[kMaxKeys];              // per key: the next tile's first row
+  __shared__ int iscr[32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, keys = E + 1;
+  const int64_t begin = blockIdx.x * chunk, end = begin + chunk < R ? begin + chunk : R;
+  pdl_wait();
+  pdl_launch_dependents();
+  int all = 0, before = 0;   // of key tid
+  if (tid < keys)
+    for (int c = 0; c < nchunks; ++c) {
+      const int n = counts != nullptr ? __ldcg(counts + (size_t)c * keys + tid) : 0;
+      all += n;
+      before += c < (int)blockIdx.x ? n : 0;
+    }
+  for (int64_t t0 = begin; t0 == begin || t0 < end; t0 += kSortTile) {
+    for (int i = tid; i < kSortWarps * kMaxKeys; i += kSortThreads) (&cnt[0][0])[i] = 0;
+    // a warp's pairs are consecutive
+    int key[kSortRounds], rank[kSortRounds];
+    const int64_t w0 = t0 + warp * (32 * kSortRounds) + lane;
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+      const int64_t i = w0 + 32 * j;
+      key[j] = -1;
+      if (i < end) {
+        const int id = __ldcg(ids + i);
+        if (id >= E) record_error(err, kErrExpertId, kAtSort, (int)i);
+        key[j] = sort_key(id, E);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+      const uint32_t same = __match_any_sync(0xffffffffu, key[j]);
+      const int ahead = __popc(same & ((1u << lane) - 1u));
+      if (key[j] >= 0) rank[j] = cnt[warp][key[j]] + ahead;
+      __syncwarp();
+      if (key[j] >= 0 && ahead == 0) cnt[warp][key[j]] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    int mine = 0;   // this tile's pairs of key tid
+    if (tid < keys)
+      for (int w = 0; w < kSortWarps; ++w) mine += cnt[w][tid];
+    if (t0 == begin) {
+      int total;
+      const int n = tid < keys ? (nchunks == 0 ? mine : all) : 0;
+      const int first = block_exclusive_scan_i(n, iscr, &total);
+      if (tid < keys) {
+        base[tid] = first + before;
+        if (blockIdx.x == 0) offsets[tid] = first;
+      }
+    }
+    if (tid < keys) {
+      int r = base[tid];
+      base[tid] = r + mine;
+      for (int w = 0; w < kSortWarps; ++w) {
+        const int n = cnt[w][tid];
+        cnt[w][tid] = r;
+        r += n;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+      if (key[j] < 0) continue;
+      const int64_t i = w0 + 32 * j;
+      const int r = cnt[warp][key[j]] + rank[j];
+      const bool none = key[j] == E;
+      pos[i] = none ? ~r : r;
+      rows[r] = none ? -1 : (int)i;
+    }
+    __syncthreads();
+  }
+}
+
+// chunks of whole tiles, at most kSortMaxChunks of them; 0: one CTA places them without counts
+int sort_chunks(int64_t R, int64_t* chunk) {
+  const int64_t tiles = (R + kSortTile - 1) / kSortTile;
+  const int64_t per = (tiles + kSortMaxChunks - 1) / kSortMaxChunks;
+  *chunk = (per < 1 ? 1 : per) * kSortTile;
+  return tiles <= 1 ? 0 : (int)((R + *chunk - 1) / *chunk);
+}
+
+constexpr size_t kSortCounts = 256;   // offset of the counts: behind the fault record
+
+}  // namespace
+
+size_t sort_workspace_bytes(int64_t R, int E) {
+  int64_t chunk;
+  return kSortCounts + sizeof(int32_t) * (size_t)sort_chunks(R, &chunk) * (E + 1);
+}
+
+cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,
+                               int32_t* rows, int32_t* pos, void* ws, cudaStream_t s) {
+  int64_t chunk;
+  const int n = sort_chunks(R, &chunk);
+  DevErrRecord* err = static_cast<DevErrRecord*>(ws);
+  int32_t* counts = n > 0 ? reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + kSortCounts)
+                          : nullptr;
+  cudaError_t e = cudaSuccess;
+  if (n > 0)
+    e = launch_ex(sort_count_kernel, dim3(n), dim3(kSortThreads), 0, s, true, ids, R, E, chunk,
+                  counts);
+  if (e == cudaSuccess)
+    e = launch_ex(sort_place_kernel, dim3(n > 0 ? n : 1), dim3(kSortThreads), 0, s, true, ids, R,
+                  E, chunk, n, static_cast<const int32_t*>(counts), offsets, rows, pos, err);
+  if (e != cudaSuccess) return e;
+  return cudaGetLastError();
+}
+
+}  // namespace dmoe
