@@ -353,8 +353,8 @@ dmoe_status dmoe_q4_size(const dmoe_q4_desc* desc, size_t* codes_bytes /* host *
 /* bf16 weights to 4 bits. For each group with a = max |w|: scale s = a / 7 rounded to five
  * significant bits (to nearest, ties to even), code c = w / s rounded to the nearest integer
  * (ties to even), -7 <= c <= 7; the group stands for the values c * s, which bf16 holds exactly
- * (three bits times five). A group whose a is below 2^-100 stands for zeros; one that holds an
- * infinity or a NaN stands for NaNs.
+ * (three bits times five). A group whose a is below 2^-100 stands for zeros; one whose a is 2^120 or
+ * more, or that holds a NaN, stands for NaNs.
  *   w       bf16 [n_experts, n_out, n_in]   codes, scales  out, of dmoe_q4_size bytes */
 dmoe_status dmoe_q4_quantize(const dmoe_q4_desc* desc, const void* w, void* codes, void* scales,
                              void* stream);

@@ -5,9 +5,9 @@
 //   word 2h + s   row g + 8s, inputs 32h + 8q .. + 7 of the block
 // so a warp's 16-byte loads are whole lines, and a word is a lane's share of the A operand of
 // two 16 x 8 x 16 MMAs (with the inputs of each 32 taken in an order of their own, the same for
-// both operands: x is then read 16 bytes at a time). In a word, input 2i is the nibble at bit 4i
-// and input 2i + 1 the one at bit 16 + 4i: a shift and a mask leave a pair of them in the low
-// bits of two 16-bit halves. A nibble is the code + 8.
+// both operands: x is then read 16 bytes at a time). In a word, input 2i is the nibble at bit 4i + 3
+// and input 2i + 1 the one at bit 4i + 19, counted around the word's end: a rotation and a mask
+// leave a pair of them in the upper mantissa bits of two bf16 halves. A nibble is the code + 8.
 // Scales: per matrix and row tile, per g, the groups' scale pairs (row g, row g + 8) of bf16,
 // the groups padded to a multiple of four with zeros.
 // Rows behind n_out have scales of zero, inputs behind n_in codes of zero.
@@ -36,16 +36,35 @@ inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
   return s;
 }
 
-// Pair i of a word's inputs (2i, 2i + 1) as bf16 codes: 128 + nibble is exact in bf16's eight
-// bits, and so is the difference from 136.
-__device__ __forceinline__ __nv_bfloat162 q4_pair(uint32_t word, int i) {
-  const uint32_t u = ((word >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-  return __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), __float2bfloat162_rn(136.f));
+__device__ __forceinline__ uint32_t q4_pack_word(const int (&code)[8]) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w |= (uint32_t)(code[2 * i] + 8) << (4 * i) | (uint32_t)(code[2 * i + 1] + 8) << (16 + 4 * i);
+  return __funnelshift_l(w, w, 3);
 }
 
-// The same times the scale (five significant bits times three: exact).
-__device__ __forceinline__ uint32_t q4_value_pair(uint32_t word, int i, __nv_bfloat162 scale) {
-  const __nv_bfloat162 v = __hmul2(q4_pair(word, i), scale);
+// A row's scale as the two operands of the values' FMA: s and -24 s, in both halves.
+struct Q4Scale {
+  __nv_bfloat162 s, b;
+};
+__device__ __forceinline__ Q4Scale q4_scale_pair(uint32_t bits) {
+  Q4Scale r;
+  const uint32_t two = __byte_perm(bits, bits, 0x1010);
+  r.s = *reinterpret_cast<const __nv_bfloat162*>(&two);
+  r.b = __hmul2(r.s, __float2bfloat162_rn(-24.f));
+  return r;
+}
+
+// Pair i of a word's inputs, 2i and 2i + 1, as bf16 values. The nibble in the upper four mantissa
+// bits of 16 makes 16 + nibble; times s, less 24 s, it is s (nibble - 8). Every step is exact: 24 s
+// has 5 + 2 significant bits, the value 5 + 3, and bf16 holds eight; the FMA rounds once. With the
+// nibble in the lower bits (128 + nibble) the offset would be 136 s, 5 + 5 bits, and a
+// subtraction of its own were needed.
+__device__ __forceinline__ uint32_t q4_value_pair(uint32_t word, int i, const Q4Scale& s) {
+  const uint32_t r = i == 0 ? word : i == 3 ? __funnelshift_r(word, word, 12) : word >> (4 * i);
+  const uint32_t u = (r & 0x00780078u) | 0x41804180u;
+  const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&u), s.s, s.b);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 

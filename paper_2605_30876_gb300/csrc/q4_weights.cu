@@ -73,7 +73,9 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint4*
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const float a = __uint_as_float(top[r][c] << 16);
-      scale[r][c] = top[r][c] >= 0x7F80u ? __int_as_float(0x7FC00000) : a < 0x1p-100f ? 0.f : q4_scale(a);
+      // (the values' FMA holds 24 s: finite for a < 2^120)
+      scale[r][c] = top[r][c] >= (120u + 127u) << 7 ? __int_as_float(0x7FC00000)
+                                                    : a < 0x1p-100f ? 0.f : q4_scale(a);
     }
   }
   uint32_t word[2][4];
@@ -84,14 +86,14 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint4*
       const uint32_t raw[4] = {v[r][c].x, v[r][c].y, v[r][c].z, v[r][c].w};
       const bool plain = scale[r][c] > 0.f;
       const float d = plain ? scale[r][c] : 1.f;
-      uint32_t o = 0;
+      int code[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float lo = __uint_as_float(raw[i] << 16), hi = __uint_as_float(raw[i] & 0xFFFF0000u);
-        const int cl = plain ? __float2int_rn(lo / d) : 0, ch = plain ? __float2int_rn(hi / d) : 0;
-        o |= (uint32_t)(cl + 8) << (4 * i) | (uint32_t)(ch + 8) << (16 + 4 * i);
+        code[2 * i] = plain ? __float2int_rn(lo / d) : 0;
+        code[2 * i + 1] = plain ? __float2int_rn(hi / d) : 0;
       }
-      word[r][c] = o;
+      word[r][c] = q4_pack_word(code);
     }
   const size_t tile = (size_t)b.e * s.row_tiles + b.nt;
 #pragma unroll
@@ -139,8 +141,7 @@ q4_dequantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ codes,
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int n = b.nt * 16 + g + 8 * r;
-      const uint32_t one = r == 0 ? pair & 0xFFFFu : pair >> 16, two = one | one << 16;
-      const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&two);
+      const Q4Scale v = q4_scale_pair(r == 0 ? pair : pair >> 16);
       if (n < s.N)
         __stcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8,
                make_uint4(q4_value_pair(word[r][c], 0, v), q4_value_pair(word[r][c], 1, v),

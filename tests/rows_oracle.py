@@ -64,7 +64,7 @@ def q4_values(w, group):
     w = np.asarray(w, np.float64)
     v = w.reshape(*w.shape[:-1], w.shape[-1] // group, group)
     top = np.abs(v).max(-1)
-    fin = np.isfinite(v).all(-1)
+    fin = np.isfinite(v).all(-1) & (top < 2.0 ** 120)
     with np.errstate(all="ignore"):
         s = np.where(fin, np.where(top < 2.0 ** -100, 0.0, five_bits(np.where(fin, top, 0) / 7)), np.nan)
         c = np.where((s > 0)[..., None], np.rint(v / s[..., None]), 0.0)
