@@ -64,8 +64,9 @@ __device__ __forceinline__ void q4_groups(const Q4Args& a, Q4Groups& s, int* wco
 }
 
 // A warp's steps through its work: units (tile pairs) u0, u0 + stride, ... of the CTA, each in passes of
-// NT * 8 rows of its group, each over the warp's blocks of 64 inputs. Two cursors go the same way,
-// one that starts copies and, behind it, one that multiplies.
+// NT * 8 rows of its group, each over the warp's chunks of 256 inputs. Two cursors go the same
+// way, one that starts copies and, behind it, one that multiplies.
+constexpr int kChunk = 4;   // blocks of 64 inputs
 struct Q4Plan {
   int64_t units;
   int pairs, share, per, pass_rows;
@@ -108,12 +109,8 @@ struct Q4Cursor {
   __device__ __forceinline__ bool live() const { return r0 + p < r1; }
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void copy_small(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -121,42 +118,46 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The ring of a warp: a stage is a block's codes (2 x 512 bytes), scale pairs (2 x 256) and, up to 16
-// rows a pass, rows of x (2 NT x 512). Every lane reads what it copied itself: no barriers. The
-// CTA's shared memory is the rings and the warps' sums (two CTAs per SM: 4, 3 or 5 stages).
-constexpr int kMmaSmem = 100 * 1024;
-template <int NT>
+// The ring of a warp: a stage is a chunk's codes (2 matrices x 4 x 512 bytes) and scale pairs (2 x
+// 128 bytes, twice that in groups of 32). No other warp reads it.
+template <bool kG32>
 struct Q4Ring {
-  static constexpr bool kX = NT <= 2;   // (at 32 rows x is read directly: the stages would be too few)
-  static constexpr int stage = 1536 + (kX ? 2 * NT * 512 : 0);
-  static constexpr int red = kMmaWarps * NT * 8 * 32 * (int)sizeof(float);
-  static constexpr int stages = (kMmaSmem - red) / kMmaWarps / stage;
+  static constexpr int words = kG32 ? 2 : 1;   // 16-byte pieces of scale pairs per chunk
+  static constexpr int stage = 2 * kChunk * 512 + 2 * words * 128;
+  static constexpr int stages = 2;
+  static constexpr int bytes = kMmaWarps * stages * stage;
 };
-
+constexpr int kRedTiles = 2;   // tiles of 8 rows whose sums are exchanged at a time
 template <int NT>
-__device__ __forceinline__ const uint4* x_row(const Q4Args& a, int r, int r1, int q) {
-  int64_t src = -1;
-  if (r < r1) {
-    src = r;
-    if (a.rows != nullptr) {
-      const int i = __ldg(a.rows + r);
-      src = i >= 0 ? i / a.k : -1;
-    }
-  }
-  return src >= 0 && src < a.T_x ? reinterpret_cast<const uint4*>(a.x + src * a.ldx) + q : nullptr;
+constexpr int q4_red_bytes() {
+  return kMmaWarps * (NT < kRedTiles ? NT : kRedTiles) * 8 * 32 * (int)sizeof(float);
 }
 
-// The copying cursor: the current pass's addresses, advanced block by block.
-template <int NT, bool kGated, bool kG32>
+__device__ uint4 q4_zero_row[kMaxDModel / 8];   // stands in for sources that are not there
+
+// the row of x of sorted row r, from input 8 q on; behind the group's last row, that one's (its
+// products are not stored)
+__device__ __forceinline__ const uint4* x_row(const Q4Args& a, int r, int r1, int q) {
+  r = min(r, r1 - 1);
+  int64_t src = r;
+  if (a.rows != nullptr) {
+    const int i = __ldg(a.rows + r);
+    src = i >= 0 ? i / a.k : -1;
+  }
+  return (src >= 0 && src < a.T_x ? reinterpret_cast<const uint4*>(a.x + src * a.ldx) : q4_zero_row) + q;
+}
+
+// The copying cursor: the current unit's addresses, advanced chunk by chunk.
+template <bool kGated, bool kG32>
 struct Q4Copier {
+  using Ring = Q4Ring<kG32>;
   Q4Cursor<kGated> c;
   const uint4* codes[2];
   const uint32_t* scales[2];
-  const uint4* xrow[NT];
-  int kt, slot;
+  int ch, slot;
   __device__ __forceinline__ void enter_pass(const Q4Args& a, const Q4Shape& s, int first) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    kt = first;
+    const int lane = threadIdx.x & 31;
+    ch = first;
     if (c.done || !c.live()) return;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -165,57 +166,52 @@ struct Q4Copier {
                                                       // are behind n_out and not stored)
       const size_t tile = (size_t)c.e * s.row_tiles + nt;
       codes[m] = static_cast<const uint4*>(a.codes[kGated ? m : 0]) + tile * s.k_tiles * 32 + lane;
-      scales[m] = static_cast<const uint32_t*>(a.scales[kGated ? m : 0]) + (tile * 8 + g) * s.groups_pad;
+      scales[m] = static_cast<const uint32_t*>(a.scales[kGated ? m : 0]) +
+                  (tile * 8 + (lane >> 2)) * s.groups_pad;
     }
-    if (Q4Ring<NT>::kX)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) xrow[t] = x_row<NT>(a, c.r0 + c.p + t * 8 + g, c.r1, q);
   }
-  // starts the next block's copies, if there is one; always one group of copies
+  // starts the next chunk's copies, if there is one; always one group of copies
   __device__ __forceinline__ void copy(const Q4Args& a, const Q4Shape& s, const Q4Plan& pl,
-                                       const Q4Groups& gs, int warp, int first, uint32_t ring) {
-    while (!c.done && (!c.live() || kt >= s.k_tiles)) {
+                                       const Q4Groups& gs, int warp, int first, int chunks,
+                                       uint32_t ring) {
+    while (!c.done && (!c.live() || ch >= chunks)) {
       c.next(pl, gs, warp);
       enter_pass(a, s, first);
     }
     if (!c.done) {
       const int lane = threadIdx.x & 31;
-      const uint32_t dst = ring + slot * Q4Ring<NT>::stage;
+      const uint32_t dst = ring + slot * Ring::stage;
+      const int kt = ch * kChunk;
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        copy16(dst + m * 512 + lane * 16, codes[m] + (size_t)kt * 32, 16);
-        if (kG32) copy_small<8>(dst + 1024 + m * 256 + lane * 8, scales[m] + 2 * kt);   // (padded)
-        else copy_small<4>(dst + 1024 + m * 256 + lane * 8, scales[m] + (s.group == 64 ? kt : kt >> 1));
+        const uint4* src = codes[m] + kt * 32;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+          if (kt + i < s.k_tiles) copy16(dst + lane * 16 + (m * kChunk + i) * 512, src + i * 32);
+        const int gi = kG32 ? ch * 8 : s.group == 64 ? ch * 4 : (ch * 2) & ~3;
+#pragma unroll
+        for (int w = 0; w < Ring::words; ++w)
+          if ((lane & 3) == 0 && gi + 4 * w < s.groups_pad)
+            copy16(dst + 2 * kChunk * 512 + (m * Ring::words + w) * 128 + lane * 4, scales[m] + gi + 4 * w);
       }
-      if (Q4Ring<NT>::kX)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const bool ok = xrow[t] != nullptr && kt * 64 + h * 32 < s.K;   // (n_in is whole halves)
-            copy16(dst + 1536 + (h * NT + t) * 512 + lane * 16,
-                   ok ? static_cast<const void*>(xrow[t] + kt * 8 + h * 4) : codes[0], ok ? 16 : 0);
-          }
-      kt += pl.share;
-      slot = slot + 1 == Q4Ring<NT>::stages ? 0 : slot + 1;
+      ch += pl.share;
+      slot = slot + 1 == Ring::stages ? 0 : slot + 1;
     }
     copies_commit();
   }
 };
 
-template <int NT, bool kG32>
-__device__ __forceinline__ void mma_block(const uint8_t* st, const uint4 (&x)[2][NT],
-                                          float (&acc)[2][NT][4]) {
-  const int lane = threadIdx.x & 31;
+// One block of 64 inputs: st is the lane's place in the block's codes
+template <int NT>
+__device__ __forceinline__ void mma_block(const uint8_t* st, const uint32_t (&bits)[2][2],
+                                          const uint4 (&x)[2][NT], float (&acc)[2][NT][4]) {
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    const uint4 c = *reinterpret_cast<const uint4*>(st + m * 512 + lane * 16);
-    const uint2 sc = *reinterpret_cast<const uint2*>(st + 1024 + m * 256 + lane * 8);
+    const uint4 c = *reinterpret_cast<const uint4*>(st + m * kChunk * 512);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t lo = h == 0 ? c.x : c.z, hi = h == 0 ? c.y : c.w;
-      const uint32_t bits = kG32 && h == 1 ? sc.y : sc.x;
-      const Q4Scale slo = q4_scale_pair(bits), shi = q4_scale_pair(bits >> 16);
+      const Q4Scale slo = q4_scale_pair(bits[m][h]), shi = q4_scale_pair(bits[m][h] >> 16);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t a[4] = {q4_value_pair(lo, 2 * j, slo), q4_value_pair(hi, 2 * j, shi),
@@ -225,6 +221,47 @@ __device__ __forceinline__ void mma_block(const uint8_t* st, const uint4 (&x)[2]
           mma_16816(acc[m][t], a, j == 0 ? x[h][t].x : x[h][t].z, j == 0 ? x[h][t].y : x[h][t].w);
       }
     }
+  }
+}
+
+// A chunk: kFull has all its blocks and all of their inputs.
+template <int NT, bool kG32, bool kFull>
+__device__ __forceinline__ void mma_chunk(const Q4Shape& s, int ch, const uint8_t* st,
+                                          const uint4* const (&xrow)[NT], float (&acc)[2][NT][4]) {
+  const int lane = threadIdx.x & 31;
+  uint4 sc[2][Q4Ring<kG32>::words];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int w = 0; w < Q4Ring<kG32>::words; ++w)
+      sc[m][w] = *reinterpret_cast<const uint4*>(st + 2 * kChunk * 512 +
+                                                 (m * Q4Ring<kG32>::words + w) * 128 + (lane >> 2) * 16);
+  const bool g128 = s.group == 128, odd = ch & 1;
+#pragma unroll
+  for (int i = 0; i < kChunk; ++i) {
+    const int kt = ch * kChunk + i;
+    if (!kFull && kt >= s.k_tiles) break;
+    uint4 x[2][NT];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        x[h][t] = kFull || kt * 64 + h * 32 < s.K   // (n_in is whole halves)
+                      ? __ldg(xrow[t] + kt * 8 + h * 4) : make_uint4(0, 0, 0, 0);
+    uint32_t bits[2][2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const uint32_t v[4] = {sc[m][0].x, sc[m][0].y, sc[m][0].z, sc[m][0].w};
+      if (kG32) {
+        const uint4 o = sc[m][Q4Ring<kG32>::words - 1];
+        const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+        bits[m][0] = i < 2 ? v[2 * i & 3] : w[2 * i & 3];
+        bits[m][1] = i < 2 ? v[(2 * i + 1) & 3] : w[(2 * i + 1) & 3];
+      } else {
+        bits[m][0] = bits[m][1] = g128 ? (odd ? v[2 + i / 2] : v[i / 2]) : v[i];
+      }
+    }
+    mma_block<NT>(st + i * 512 + lane * 16, bits, x, acc);
   }
 }
 
@@ -253,55 +290,61 @@ __device__ __forceinline__ void unit_outputs(const Q4Args& a, const Q4Shape& s, 
       }
     return;
   }
-  // red[warp][row of the pass][output of the pair]
-  constexpr int kPer = NT * 8 * 32;
-  if (live) {
+  // red[warp][row of the part][output of the pair]
+  constexpr int kTiles = NT < kRedTiles ? NT : kRedTiles, kPer = kTiles * 8 * 32;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+  for (int t0 = 0; t0 < NT; t0 += kTiles) {
+    if (live) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          red[warp * kPer + (t * 8 + q * 2 + (i & 1)) * 32 + m * 16 + g + (i >> 1) * 8] = acc[m][t][i];
-  }
-  __syncthreads();
-  if (live) {
-    // the sharing warps take the pair's rows in turn; a lane has one output of the pair
-    const int w0 = warp / share * share;
-    for (int j = warp - w0; j < NT * 8; j += share) {
-      float v = 0.f;
-      for (int w = 0; w < share; ++w) v += red[(w0 + w) * kPer + j * 32 + lane];
-      const float up = __shfl_down_sync(0xffffffffu, v, 16);
-      const int r = r0 + j;
-      if (r >= r1) continue;
-      if (kGated) {
-        if (lane < 16 && pair * 16 + lane < s.N) store_y(a, r, pair * 16 + lane, silu_divide(v) * up);
-      } else {
-        if (pair * 32 + lane < s.N) store_y(a, r, pair * 32 + lane, v);
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            red[warp * kPer + (t * 8 + q * 2 + (i & 1)) * 32 + m * 16 + g + (i >> 1) * 8] =
+                acc[m][t0 + t][i];
+    }
+    __syncthreads();
+    if (live) {
+      // the sharing warps take the part's rows in turn; a lane has one output of the pair
+      const int w0 = warp / share * share;
+      for (int j = warp - w0; j < kTiles * 8; j += share) {
+        float v = 0.f;
+        for (int w = 0; w < share; ++w) v += red[(w0 + w) * kPer + j * 32 + lane];
+        const float up = __shfl_down_sync(0xffffffffu, v, 16);
+        const int r = r0 + t0 * 8 + j;
+        if (r >= r1) continue;
+        if (kGated) {
+          if (lane < 16 && pair * 16 + lane < s.N)
+            store_y(a, r, pair * 16 + lane, silu_divide(v) * up);
+        } else {
+          if (pair * 32 + lane < s.N) store_y(a, r, pair * 32 + lane, v);
+        }
       }
     }
+    __syncthreads();
   }
-  __syncthreads();
 }
 
 template <int NT, bool kGated, bool kG32>
 __device__ __forceinline__ void run_units(const Q4Args& a, const Q4Shape& s, Q4Plan pl,
                                           const Q4Groups& gs, uint8_t* smem) {
-  using Ring = Q4Ring<NT>;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  float* red = reinterpret_cast<float*>(smem);
-  uint8_t* ring = smem + Ring::red + warp * (Ring::stages * Ring::stage);
+  using Ring = Q4Ring<kG32>;
+  const int warp = threadIdx.x >> 5, g = (threadIdx.x & 31) >> 2, q = threadIdx.x & 3;
+  uint8_t* ring = smem + warp * (Ring::stages * Ring::stage);
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
-  const int first = warp % pl.share;
+  float* red = reinterpret_cast<float*>(smem + Ring::bytes);
+  const int first = warp % pl.share, chunks = (s.k_tiles + kChunk - 1) / kChunk;
+  const int full = s.K / (64 * kChunk);
   pl.pass_rows = NT * 8;
-  Q4Copier<NT, kGated, kG32> cp;
+  Q4Copier<kGated, kG32> cp;
   cp.c.u0 = (int64_t)blockIdx.x * pl.per;
   cp.c.enter(pl, gs, warp);
   cp.slot = 0;
   cp.enter_pass(a, s, first);
   Q4Cursor<kGated> c = cp.c;
 #pragma unroll 1
-  for (int i = 0; i < Ring::stages - 1; ++i) cp.copy(a, s, pl, gs, warp, first, ring_addr);
+  for (int i = 0; i < Ring::stages - 1; ++i) cp.copy(a, s, pl, gs, warp, first, chunks, ring_addr);
   int slot = 0;
   for (; !c.done; c.next(pl, gs, warp)) {
     float acc[2][NT][4];
@@ -314,29 +357,17 @@ __device__ __forceinline__ void run_units(const Q4Args& a, const Q4Shape& s, Q4P
     const int from = c.r0 + c.p;
     if (c.live()) {
       const uint4* xrow[NT];
-      if (!Ring::kX)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) xrow[t] = x_row<NT>(a, from + t * 8 + g, c.r1, q);
+      for (int t = 0; t < NT; ++t) xrow[t] = x_row(a, from + t * 8 + g, c.r1, q);
 #pragma unroll 1
-      for (int kt = first; kt < s.k_tiles; kt += pl.share) {
-        uint4 x[2][NT];
-        if (!Ring::kX)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-              x[h][t] = xrow[t] != nullptr && kt * 64 + h * 32 < s.K
-                            ? __ldg(xrow[t] + kt * 8 + h * 4) : make_uint4(0, 0, 0, 0);
-        cp.copy(a, s, pl, gs, warp, first, ring_addr);
+      for (int ch = first; ch < chunks; ch += pl.share) {
+        cp.copy(a, s, pl, gs, warp, first, chunks, ring_addr);
         copies_wait<Ring::stages - 1>();
+        __syncwarp();   // (scale pairs are read by the lanes beside the copying one)
         const uint8_t* st = ring + slot * Ring::stage;
-        if (Ring::kX)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-              x[h][t] = *reinterpret_cast<const uint4*>(st + 1536 + (h * NT + t) * 512 + lane * 16);
-        mma_block<NT, kG32>(st, x, acc);
+        if (ch < full) mma_chunk<NT, kG32, true>(s, ch, st, xrow, acc);
+        else mma_chunk<NT, kG32, false>(s, ch, st, xrow, acc);
+        __syncwarp();
         slot = slot + 1 == Ring::stages ? 0 : slot + 1;
       }
     }
@@ -357,13 +388,14 @@ q4_mma_kernel(Q4Args a, Q4Shape s) {
   Q4Plan pl;
   pl.pairs = kGated ? s.row_tiles : (s.row_tiles + 1) / 2;
   pl.units = (int64_t)groups.n * pl.pairs;
-  // Warps that share a tile pair's inputs: as many as give the least blocks per warp, where two
-  // blocks' time goes into an iteration's end.
+  // Warps that share a tile pair's inputs: as many as give the least chunks per warp, where half a
+  // chunk's time goes into an iteration's end.
+  const int chunks = (s.k_tiles + kChunk - 1) / kChunk;
   int64_t best = -1;
 #pragma unroll
   for (int c = 1; c <= kMmaWarps; c *= 2) {
     const int64_t slots = (int64_t)gridDim.x * (kMmaWarps / c);
-    const int64_t cost = (pl.units + slots - 1) / slots * ((s.k_tiles + c - 1) / c + 2);
+    const int64_t cost = (pl.units + slots - 1) / slots * (2 * ((chunks + c - 1) / c) + 1);
     if (best < 0 || cost < best) {
       best = cost;
       pl.share = c;
@@ -397,11 +429,15 @@ cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_
     for (auto* k : {q4_mma_kernel<true, true>, q4_mma_kernel<false, true>, q4_mma_kernel<true, false>,
                     q4_mma_kernel<false, false>})
       if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmaSmem);
+        e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 Q4Ring<true>::bytes + q4_red_bytes<4>());
     if (e == cudaSuccess) ready.fetch_or(bit, std::memory_order_release);
   }
   if (e != cudaSuccess) return e;
-  return launch_ex(kernel, dim3((unsigned)ctas), dim3(kMmaThreads), kMmaSmem, st, true, a, s);
+  // (a group has no more rows than there are: the sums' space for passes of 8, 16 or 32)
+  const size_t smem = (s.group == 32 ? Q4Ring<true>::bytes : Q4Ring<false>::bytes) +
+                      (a.R <= 8 ? q4_red_bytes<1>() : a.R <= 16 ? q4_red_bytes<2>() : q4_red_bytes<4>());
+  return launch_ex(kernel, dim3((unsigned)ctas), dim3(kMmaThreads), smem, st, true, a, s);
 }
 
 }  // namespace dmoe
