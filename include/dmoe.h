@@ -346,7 +346,7 @@ typedef struct {
 } dmoe_q4_desc;
 
 /* Bytes of the codes and of the scales of such matrices (host only; the layout is the
- * library's own: 16 rows x 64 inputs per 512 bytes of codes). */
+ * library's own, of n_out in whole sixteens and n_in in whole 64s). */
 dmoe_status dmoe_q4_size(const dmoe_q4_desc* desc, size_t* codes_bytes /* host */,
                          size_t* scales_bytes /* host */);
 
@@ -377,7 +377,7 @@ dmoe_status dmoe_q4_dequantize(const dmoe_q4_desc* desc, const void* codes, cons
  *              [0, n_experts) are left out
  *   y          [R, n_out] out, bf16 or fp32 (y_dtype), row stride ldy. Rows that are in no group
  *              (from offsets[n_groups] on, the slots without an expert) are not written
- * 0 <= R <= 2^30; 1 <= n_groups <= 256; offsets outside [0, R] are cut to it. */
+ * 0 <= R <= 2^26; 1 <= n_groups <= 256; offsets outside [0, R] are cut to it. */
 dmoe_status dmoe_q4_linear(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const void* x,
                            int64_t ldx, int64_t T_x, const int32_t* rows, int32_t k,
                            const int32_t* offsets, const int32_t* expert_ids,
@@ -392,6 +392,11 @@ dmoe_status dmoe_q4_swiglu(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups
                            const void* gate_codes, const void* gate_scales,
                            const void* up_codes, const void* up_scales, void* y, int64_t ldy,
                            int32_t y_dtype, void* stream);
+
+/* The fault record of the two calls above on the current device (they have no workspace: it lies
+ * in the library's own device memory and all of them share it): synchronises `stream`, then reads
+ * and clears it. Returns and fills `info` (host, 4 int32, or NULL) as dmoe_get_device_error does. */
+dmoe_status dmoe_q4_device_error(void* stream, int32_t* info);
 
 /* Synchronises `stream`, then reads and clears the fault code the kernels recorded in
  * `workspace`. Returns DMOE_OK if none, DMOE_ERR_TIMEOUT for a bounded wait that ran out,

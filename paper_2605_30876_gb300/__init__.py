@@ -24,6 +24,7 @@ __all__ = [
     "dmoe_gather_rows_backward", "dmoe_combine_rows", "dmoe_combine_rows_backward",
     "Q4Desc", "make_q4_desc", "dmoe_q4_size", "alloc_q4", "dmoe_q4_quantize",
     "dmoe_q4_dequantize", "dmoe_q4_linear", "dmoe_q4_swiglu",
+    "dmoe_q4_device_error",
 ]
 
 DMOE_ROUTE_TOKEN = 0
@@ -134,6 +135,7 @@ def _load() -> ctypes.CDLL:
             "dmoe_q4_size": [Q, sizes, sizes],
             "dmoe_q4_quantize": [Q, P, P, P, P],
             "dmoe_q4_dequantize": [Q, P, P, P, P],
+            "dmoe_q4_device_error": [P, ctypes.POINTER(i32)],
             "dmoe_q4_linear": products + [P] * 2 + [P, i64, i32, P],
             "dmoe_q4_swiglu": products + [P] * 4 + [P, i64, i32, P]}.items():
         fn = getattr(lib, name)
@@ -516,6 +518,14 @@ def dmoe_q4_swiglu(desc, x, offsets, gate_codes, gate_scales, up_codes, up_scale
     """y[r] = silu(Wg x) * (Wu x), arguments as for dmoe_q4_linear."""
     _q4_products("dmoe_q4_swiglu", desc, x, offsets, (gate_codes, gate_scales, up_codes, up_scales),
                  y, rows, k, expert_ids, stream)
+
+
+def dmoe_q4_device_error(stream=None) -> Tuple[int, Tuple[int, int, int]]:
+    """Synchronises the stream; returns (status, (code, where, value)) of the fault record of the
+    4-bit products on the current device and clears it."""
+    info = (ctypes.c_int32 * 4)()
+    st = _lib.dmoe_q4_device_error(_stream(stream), info)
+    return st, (info[0], info[1], info[2])
 
 
 KERNELS = {"router": 0, "dispatch": 1, "gather": 2, "experts": 3, "combine": 4}

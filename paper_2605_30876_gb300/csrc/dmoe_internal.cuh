@@ -36,7 +36,7 @@ enum DevErr : int32_t {
 };
 enum DevWhere : int32_t {
   kAtRouter = 1, kAtBlockRoute = 2, kAtDispatch = 3, kAtGateUp = 4, kAtDown = 5,
-  kAtCombine = 6, kAtGather = 7, kAtSort = 8,
+  kAtCombine = 6, kAtGather = 7, kAtSort = 8, kAtQ4 = 9,
 };
 constexpr int kRouteTickets = 256;
 constexpr int kRouteClusterCtas = 8;   // CTAs per cluster of the decode-size routing launch
@@ -357,6 +357,8 @@ struct Q4Args {
   int n_groups, n_experts;
 };
 cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_t s);
+// the products' fault record in the current device's memory
+cudaError_t q4_fault_address(void** p);
 
 // profiling events (dmoe_set_profile_events), per host thread
 void prof_begin(int kernel, cudaStream_t s);

@@ -8,6 +8,7 @@ using namespace dmoe;
 namespace {
 
 constexpr int64_t kMaxPairs = 1 << 30;
+constexpr int64_t kMaxQ4Rows = 1 << 26;   // units of 128 rows x 64 outputs are counted in 32 bits
 constexpr int kMaxRowWidth = 1 << 20;
 
 dmoe_status status_of(cudaError_t e) {
@@ -65,7 +66,7 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   if (R < 0 || T_x < 0 || n_groups <= 0 || k <= 0 || ldx < desc->n_in || ldy < desc->n_out ||
       (y_dtype != DMOE_BF16 && y_dtype != DMOE_FP32))
     return DMOE_ERR_INVALID_ARG;
-  if (R > kMaxPairs || n_groups > kMaxExperts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
+  if (R > kMaxQ4Rows || n_groups > kMaxExperts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
   if ((offsets == nullptr && n_groups != 1) ||
       (expert_ids == nullptr && n_groups > desc->n_experts) || (rows == nullptr && T_x < R))
     return DMOE_ERR_INVALID_ARG;
@@ -251,6 +252,12 @@ dmoe_status dmoe_q4_swiglu(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups
                            int32_t y_dtype, void* stream) {
   return run_q4(desc, R, n_groups, x, ldx, T_x, rows, k, offsets, expert_ids,
                 {gate_codes, gate_scales, up_codes, up_scales}, y, ldy, y_dtype, stream);
+}
+
+dmoe_status dmoe_q4_device_error(void* stream, int32_t* info) {
+  void* record = nullptr;
+  const cudaError_t e = q4_fault_address(&record);
+  return e != cudaSuccess ? status_of(e) : dmoe_get_device_error(record, stream, info);
 }
 
 }  // extern "C"

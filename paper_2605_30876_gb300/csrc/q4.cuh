@@ -1,15 +1,13 @@
 // 4-bit expert matrices: the layout shared by the kernels that write and read it.
 //
-// Codes: per matrix, row tiles of 16 rows; per row tile, blocks of 64 inputs of 512 bytes: lane
-// (g, q) = (lane / 4, lane % 4) of a warp has 16 bytes, four words:
-//   word 2h + s   row g + 8s, inputs 32h + 8q .. + 7 of the block
-// so a warp's 16-byte loads are whole lines, and a word is a lane's share of the A operand of
-// two 16 x 8 x 16 MMAs (with the inputs of each 32 taken in an order of their own, the same for
-// both operands: x is then read 16 bytes at a time). In a word, input 2i is the nibble at bit 4i + 3
-// and input 2i + 1 the one at bit 4i + 19, counted around the word's end: a rotation and a mask
-// leave a pair of them in the upper mantissa bits of two bf16 halves. A nibble is the code + 8.
-// Scales: per matrix and row tile, per g, the groups' scale pairs (row g, row g + 8) of bf16,
-// the groups padded to a multiple of four with zeros.
+// Codes: per matrix, tiles of 128 rows (the last one of as many as are left, in sixteens); per tile,
+// blocks of 64 inputs: first every row's inputs 0 .. 31 of the block, 16 bytes a row, then every
+// row's 32 .. 63. A warp whose lanes have 32 neighbouring rows reads whole lines, and a lane
+// has a row's inputs: what a lane of tensor memory takes. Word w of the 16 bytes has inputs 8w ..
+// 8w + 7. In a word, input 2i is the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19,
+// counted around the word's end: a rotation and a mask leave a pair of them in the upper mantissa
+// bits of two bf16 halves. A nibble is the code + 8.
+// Scales: bf16, per row its groups, padded with zeros to a multiple of eight (16 bytes).
 // Rows behind n_out have scales of zero, inputs behind n_in codes of zero.
 #pragma once
 
@@ -19,9 +17,19 @@ namespace dmoe {
 
 struct Q4Shape {
   int N, K, group;
-  int row_tiles, k_tiles, groups, groups_pad;
-  __host__ __device__ size_t code_bytes() const { return (size_t)row_tiles * k_tiles * 512; }
-  __host__ __device__ size_t scale_bytes() const { return (size_t)row_tiles * 8 * groups_pad * 4; }
+  int rows, k_tiles, groups, groups_pad;   // rows: n_out in whole sixteens
+  __host__ __device__ size_t code_bytes() const { return (size_t)rows * k_tiles * 32; }
+  __host__ __device__ size_t scale_bytes() const { return (size_t)rows * groups_pad * 2; }
+  // rows of the 128-row tile that has row n
+  __host__ __device__ int tile_rows(int n) const {
+    const int left = rows - n / 128 * 128;
+    return left < 128 ? left : 128;
+  }
+  // byte offset of row n's 16 bytes of block kt, half h, in its matrix
+  __host__ __device__ size_t code_at(int n, int kt, int h) const {
+    const int tile = n / 128 * 128;
+    return (size_t)tile * k_tiles * 32 + ((size_t)kt * 2 + h) * tile_rows(n) * 16 + (n - tile) * 16;
+  }
 };
 
 inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
@@ -29,10 +37,10 @@ inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
   s.N = d.n_out;
   s.K = d.n_in;
   s.group = d.group;
-  s.row_tiles = (d.n_out + 15) / 16;
+  s.rows = (d.n_out + 15) / 16 * 16;
   s.k_tiles = (d.n_in + 63) / 64;
   s.groups = d.n_in / d.group;
-  s.groups_pad = (s.groups + 3) / 4 * 4;
+  s.groups_pad = (s.groups + 7) / 8 * 8;
   return s;
 }
 
@@ -44,13 +52,13 @@ __device__ __forceinline__ uint32_t q4_pack_word(const int (&code)[8]) {
   return __funnelshift_l(w, w, 3);
 }
 
-// A row's scale as the two operands of the values' FMA: s and -24 s, in both halves.
+// A scale as the two operands of the values' FMA: s and -24 s, in both halves.
 struct Q4Scale {
   __nv_bfloat162 s, b;
 };
-__device__ __forceinline__ Q4Scale q4_scale_pair(uint32_t bits) {
+__device__ __forceinline__ Q4Scale q4_scale_pair(uint32_t bits) {   // (the lower half's)
   Q4Scale r;
-  const uint32_t two = __byte_perm(bits, bits, 0x1010);
+  const uint32_t two = __byte_perm(bits, 0u, 0x1010);
   r.s = *reinterpret_cast<const __nv_bfloat162*>(&two);
   r.b = __hmul2(r.s, __float2bfloat162_rn(-24.f));
   return r;

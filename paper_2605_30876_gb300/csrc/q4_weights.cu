@@ -1,5 +1,5 @@
 // bf16 weights to 4-bit codes and group scales, and back. One warp takes 16 rows x 128 inputs
-// (whole groups of every size): 4 KB of weights, two tiles of codes. Bound by the bytes.
+// (whole groups of every size): 4 KB of weights. Bound by the bytes.
 #include "q4.cuh"
 
 namespace dmoe {
@@ -17,8 +17,9 @@ __device__ __forceinline__ Q4Block q4_block(const Q4Shape& s, int n_experts) {
   Q4Block b;
   b.kb = (int)(i % kbs);
   i /= kbs;
-  b.nt = (int)(i % s.row_tiles);
-  i /= s.row_tiles;
+  const int tiles = s.rows / 16;
+  b.nt = (int)(i % tiles);
+  i /= tiles;
   b.e = (int)i;
   b.ok = i < n_experts;
   return b;
@@ -34,8 +35,8 @@ __device__ __forceinline__ float q4_scale(float a) {
 __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
 
 __global__ void __launch_bounds__(kQ4Threads)
-q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint4* __restrict__ codes,
-                   uint32_t* __restrict__ scales) {
+q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_t* __restrict__ codes,
+                   uint16_t* __restrict__ scales) {
   pdl_wait();
   pdl_launch_dependents();
   const Q4Block b = q4_block(s, n_experts);
@@ -95,63 +96,65 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint4*
       }
       word[r][c] = q4_pack_word(code);
     }
-  const size_t tile = (size_t)b.e * s.row_tiles + b.nt;
+  uint8_t* to = codes + b.e * s.code_bytes();
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    if (b.kb * 2 + h < s.k_tiles)
-      codes[(tile * s.k_tiles + b.kb * 2 + h) * 32 + lane] =
-          make_uint4(word[0][2 * h], word[1][2 * h], word[0][2 * h + 1], word[1][2 * h + 1]);
-  uint32_t* sc = scales + (tile * 8 + g) * s.groups_pad;
+  for (int c = 0; c < 4; ++c)
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int gi = (b.kb * 4 + c) / per;
-    if (q == c && c % per == 0 && gi < s.groups)
-      sc[gi] = __float_as_uint(scale[0][c]) >> 16 | (__float_as_uint(scale[1][c]) & 0xFFFF0000u);
+    for (int r = 0; r < 2; ++r)
+      if (b.kb * 2 + c / 2 < s.k_tiles)
+        *reinterpret_cast<uint32_t*>(to + s.code_at(b.nt * 16 + g + 8 * r, b.kb * 2 + c / 2, c & 1) +
+                                     4 * q) = word[r][c];
+  uint16_t* sc = scales + ((size_t)b.e * s.rows + b.nt * 16 + g) * s.groups_pad;
+#pragma unroll
+  for (int r = 0; r < 2; ++r, sc += 8 * s.groups_pad) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int gi = (b.kb * 4 + c) / per;
+      if (q == c && c % per == 0 && gi < s.groups)
+        sc[gi] = (uint16_t)(__float_as_uint(scale[r][c]) >> 16);
+    }
+    if (b.kb == (s.k_tiles + 1) / 2 - 1 && q == 0)
+      for (int gi = s.groups; gi < s.groups_pad; ++gi) sc[gi] = 0;
   }
-  if (b.kb == (s.k_tiles + 1) / 2 - 1 && q == 0)
-    for (int gi = s.groups; gi < s.groups_pad; ++gi) sc[gi] = 0u;
 }
 
 __global__ void __launch_bounds__(kQ4Threads)
-q4_dequantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ codes,
-                     const uint32_t* __restrict__ scales, uint4* __restrict__ w) {
+q4_dequantize_kernel(Q4Shape s, int n_experts, const uint8_t* __restrict__ codes,
+                     const uint16_t* __restrict__ scales, uint4* __restrict__ w) {
   pdl_wait();
   pdl_launch_dependents();
   const Q4Block b = q4_block(s, n_experts);
   if (!b.ok) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const size_t tile = (size_t)b.e * s.row_tiles + b.nt;
-  const uint32_t* sc = scales + (tile * 8 + g) * s.groups_pad;
   const int per = s.group / 32;
-  uint32_t word[2][4];
+  const uint8_t* from = codes + b.e * s.code_bytes();
+  uint32_t word[2][4], bits[2][4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint4 c = make_uint4(0, 0, 0, 0);
-    if (b.kb * 2 + h < s.k_tiles) c = __ldcs(codes + (tile * s.k_tiles + b.kb * 2 + h) * 32 + lane);
-    word[0][2 * h] = c.x;
-    word[1][2 * h] = c.y;
-    word[0][2 * h + 1] = c.z;
-    word[1][2 * h + 1] = c.w;
-  }
+  for (int r = 0; r < 2; ++r)
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int gi = (b.kb * 4 + c) / per, k = b.kb * 128 + c * 32 + q * 8;
-    if (k >= s.K) continue;
-    const uint32_t pair = __ldg(sc + gi);
+    for (int c = 0; c < 4; ++c) {
+      const int n = b.nt * 16 + g + 8 * r, kt = b.kb * 2 + c / 2, gi = (b.kb * 4 + c) / per;
+      word[r][c] = 0;
+      bits[r][c] = 0;
+      if (kt < s.k_tiles)
+        word[r][c] = __ldcs(reinterpret_cast<const uint32_t*>(from + s.code_at(n, kt, c & 1) + 4 * q));
+      if (gi < s.groups) bits[r][c] = __ldg(scales + ((size_t)b.e * s.rows + n) * s.groups_pad + gi);
+    }
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int n = b.nt * 16 + g + 8 * r;
-      const Q4Scale v = q4_scale_pair(r == 0 ? pair : pair >> 16);
-      if (n < s.N)
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int n = b.nt * 16 + g + 8 * r, k = b.kb * 128 + c * 32 + q * 8;
+      const Q4Scale v = q4_scale_pair(bits[r][c]);
+      if (n < s.N && k < s.K)
         __stcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8,
                make_uint4(q4_value_pair(word[r][c], 0, v), q4_value_pair(word[r][c], 1, v),
                           q4_value_pair(word[r][c], 2, v), q4_value_pair(word[r][c], 3, v)));
     }
-  }
 }
 
 unsigned q4_ctas(const Q4Shape& s, int n_experts) {
-  const int64_t warps = (int64_t)n_experts * s.row_tiles * ((s.k_tiles + 1) / 2);
+  const int64_t warps = (int64_t)n_experts * (s.rows / 16) * ((s.k_tiles + 1) / 2);
   return (unsigned)((warps + kQ4Threads / 32 - 1) / (kQ4Threads / 32));
 }
 
@@ -161,16 +164,16 @@ cudaError_t launch_q4_quantize(const dmoe_q4_desc& d, const void* w, void* codes
                                cudaStream_t s) {
   const Q4Shape sh = q4_shape(d);
   return launch_ex(q4_quantize_kernel, dim3(q4_ctas(sh, d.n_experts)), dim3(kQ4Threads), 0, s, true,
-                   sh, d.n_experts, static_cast<const uint4*>(w), static_cast<uint4*>(codes),
-                   static_cast<uint32_t*>(scales));
+                   sh, d.n_experts, static_cast<const uint4*>(w), static_cast<uint8_t*>(codes),
+                   static_cast<uint16_t*>(scales));
 }
 
 cudaError_t launch_q4_dequantize(const dmoe_q4_desc& d, const void* codes, const void* scales,
                                  void* w, cudaStream_t s) {
   const Q4Shape sh = q4_shape(d);
   return launch_ex(q4_dequantize_kernel, dim3(q4_ctas(sh, d.n_experts)), dim3(kQ4Threads), 0, s,
-                   true, sh, d.n_experts, static_cast<const uint4*>(codes),
-                   static_cast<const uint32_t*>(scales), static_cast<uint4*>(w));
+                   true, sh, d.n_experts, static_cast<const uint8_t*>(codes),
+                   static_cast<const uint16_t*>(scales), static_cast<uint4*>(w));
 }
 
 }  // namespace dmoe
