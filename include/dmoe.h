@@ -366,10 +366,10 @@ dmoe_status dmoe_q4_dequantize(const dmoe_q4_desc* desc, const void* codes, cons
 /* Products of sorted rows with their experts' 4-bit matrices: row r of group u has expert
  * e = expert_ids[u] (or u) and
  *   y[r, n] = sum over i of W[e][n, i] * x[src(r), i]      (fp32 sums, rounded once)
- *   x          bf16 [T_x, n_in], row stride ldx, a multiple of 8, and a 16-byte aligned base: its
- *              rows are read 16 bytes at a time
- *   rows       int32 [R]: row r's source is src(r) = rows[r] / k; one outside [0, T_x) counts as a
- *              row of zeros. NULL: src(r) = r (then T_x >= R)
+ *   x          bf16 [T_x, n_in], 1 <= T_x < 2^31, row stride ldx, a multiple of 8, and a 16-byte
+ *              aligned base: its rows are read 16 bytes at a time
+ *   rows       int32 [R]: row r's source is src(r) = rows[r] / k; one outside [0, T_x) gives a
+ *              row of zeros in y. NULL: src(r) = r (then T_x >= R)
  *   offsets    int32 [n_groups + 1]: group u has rows offsets[u] .. offsets[u+1]. NULL: one group
  *              of all R rows (n_groups = 1)
  *   expert_ids int32 [n_groups] or NULL (group u is expert u, n_groups <= n_experts). With

@@ -73,11 +73,12 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   if (R == 0) return DMOE_OK;
   for (const void* w : weights)
     if (!given16(w)) return DMOE_ERR_INVALID_ARG;
-  if (!null_or16(rows) || !null_or16(offsets) || !null_or16(expert_ids) ||
-      (T_x > 0 && x == nullptr) || y == x || !matrix(y, ldy, y_dtype, desc->n_out))
+  if (!null_or16(rows) || !null_or16(offsets) || !null_or16(expert_ids) || T_x == 0 ||
+      x == nullptr || y == x || !matrix(y, ldy, y_dtype, desc->n_out))
     return DMOE_ERR_INVALID_ARG;
-  // rows of x are read 16 bytes at a time
+  // rows of x are read 16 bytes at a time, their indices held in 32 bits
   if (!aligned(x, 16) || ldx % 8 != 0) return DMOE_ERR_INVALID_ARG;
+  if (T_x > (int64_t)INT32_MAX || ldx >= (int64_t)1 << 39) return DMOE_ERR_UNSUPPORTED;
   Q4Args a{};
   a.x = static_cast<const __nv_bfloat16*>(x);
   a.ldx = ldx;

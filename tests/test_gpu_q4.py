@@ -183,6 +183,13 @@ def test_rows_of_a_group(rows, gated):
 
 
 @pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows", [20, 70, 90, 128, 300])
+def test_long_sums_over_several_tiles(rows, gated):
+    """More inputs than any ring of stages holds, many times over."""
+    check_products(2, 300, 8192, 128, np.array([rows, 3]), gated=gated, seed=rows)
+
+
+@pytest.mark.parametrize("gated", [False, True])
 def test_groups_with_their_own_experts(gated):
     ids = np.array([3, 3, -1, 0, 6, 2, 2 ** 31 - 1], np.int32)         # twice the same; three left out
     sizes = np.array([5, 2, 4, 0, 3, 40, 6])

@@ -173,6 +173,9 @@ def test_q4_product_refusals(dm, lib):
         assert call(fn, x=None) == 1
         assert call(fn, T_x=7) == 1                   # fewer rows of x than R, without a list
         assert call(fn, T_x=-1) == 1
+        assert call(fn, T_x=0, rows=FAKE) == 1        # no row of x at all
+        assert call(fn, T_x=2 ** 31) == 2
+        assert call(fn, ldx=2 ** 39) == 2
         assert call(fn, ldy=23) == 1
         assert call(fn, ydt=1) == 1
         assert call(fn, y=None) == 1
