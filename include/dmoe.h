@@ -346,7 +346,7 @@ typedef struct {
 } dmoe_q4_desc;
 
 /* Bytes of the codes and of the scales of such matrices (host only; the layout is the
- * library's own, of n_out in whole sixteens and n_in in whole 64s). */
+ * library's own, of n_out in whole 32s and n_in in whole 128s). */
 dmoe_status dmoe_q4_size(const dmoe_q4_desc* desc, size_t* codes_bytes /* host */,
                          size_t* scales_bytes /* host */);
 

@@ -1,35 +1,28 @@
 // 4-bit expert matrices: the layout shared by the kernels that write and read it.
 //
-// Codes: per matrix, tiles of 128 rows (the last one of as many as are left, in sixteens); per tile,
-// blocks of 64 inputs: first every row's inputs 0 .. 31 of the block, 16 bytes a row, then every
-// row's 32 .. 63. A warp whose lanes have 32 neighbouring rows reads whole lines, and a lane
-// has a row's inputs: what a lane of tensor memory takes. Word w of the 16 bytes has inputs 8w ..
-// 8w + 7. In a word, input 2i is the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19,
+// A matrix is cut into tiles of 32 rows, a tile into blocks of 128 inputs: 2048 bytes of codes, which
+// one bulk copy brings to the warp whose lanes have the rows. In them every row's inputs 0 .. 31
+// come first, 16 bytes a row, then every row's 32 .. 63, and so on. Word w of the 16 bytes has inputs
+// 8w .. 8w + 7: input 2i of them is the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19,
 // counted around the word's end: a rotation and a mask leave a pair of them in the upper mantissa
 // bits of two bf16 halves. A nibble is the code + 8.
-// Scales: bf16, per row its groups, padded with zeros to a multiple of eight (16 bytes).
-// Rows behind n_out have scales of zero, inputs behind n_in codes of zero.
+// Scales: bf16, per tile and block every row's groups of the block (4, 2 or 1).
+// Rows behind n_out and inputs behind n_in have codes and scales of zero.
 #pragma once
 
 #include "dmoe_internal.cuh"
 
 namespace dmoe {
 
+constexpr int kQ4Rows = 32, kQ4Inputs = 128, kQ4CodeBytes = kQ4Rows * kQ4Inputs / 2;
+
 struct Q4Shape {
   int N, K, group;
-  int rows, k_tiles, groups, groups_pad;   // rows: n_out in whole sixteens
-  __host__ __device__ size_t code_bytes() const { return (size_t)rows * k_tiles * 32; }
-  __host__ __device__ size_t scale_bytes() const { return (size_t)rows * groups_pad * 2; }
-  // rows of the 128-row tile that has row n
-  __host__ __device__ int tile_rows(int n) const {
-    const int left = rows - n / 128 * 128;
-    return left < 128 ? left : 128;
-  }
-  // byte offset of row n's 16 bytes of block kt, half h, in its matrix
-  __host__ __device__ size_t code_at(int n, int kt, int h) const {
-    const int tile = n / 128 * 128;
-    return (size_t)tile * k_tiles * 32 + ((size_t)kt * 2 + h) * tile_rows(n) * 16 + (n - tile) * 16;
-  }
+  int tiles, blocks;   // of a matrix, and of a tile
+  int groups;          // of a row in a block
+  __host__ __device__ size_t code_bytes() const { return (size_t)tiles * blocks * kQ4CodeBytes; }
+  __host__ __device__ int scale_block() const { return kQ4Rows * groups * 2; }   // bytes
+  __host__ __device__ size_t scale_bytes() const { return (size_t)tiles * blocks * scale_block(); }
 };
 
 inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
@@ -37,10 +30,9 @@ inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
   s.N = d.n_out;
   s.K = d.n_in;
   s.group = d.group;
-  s.rows = (d.n_out + 15) / 16 * 16;
-  s.k_tiles = (d.n_in + 63) / 64;
-  s.groups = d.n_in / d.group;
-  s.groups_pad = (s.groups + 7) / 8 * 8;
+  s.tiles = (d.n_out + kQ4Rows - 1) / kQ4Rows;
+  s.blocks = (d.n_in + kQ4Inputs - 1) / kQ4Inputs;
+  s.groups = kQ4Inputs / d.group;
   return s;
 }
 

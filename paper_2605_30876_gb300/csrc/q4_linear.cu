@@ -1,20 +1,21 @@
 // Products of sorted rows with their experts' 4-bit matrices, plain or gate and up with SwiGLU:
 // y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 128 rows of a group.
 //
-// A persistent CTA per SM, in roles:
-//   dequantising warps (four sets of four, in turn): a lane has a row of W. Its codes come by
-//       asynchronous copies into a ring of its own, become bf16 values by one exact FMA per pair
+// A persistent CTA per SM, in roles, by stages of 128 inputs:
+//   dequantising warps (four sets of four, a stage each in turn): a lane has a row of W. A bulk copy
+//       brings the codes of a warp's 32 rows; they become bf16 values by one exact FMA per pair
 //       and go to tensor memory: the A operand of the MMAs. Through shared memory they would take
-//       four times the codes' bytes twice, and 4 KB of codes have 184 cycles of an SM's share of
-//       HBM's rate, in which shared memory moves 23 KB.
+//       four times the codes' bytes twice, and 8 KB of codes have 368 cycles of an SM's share of
+//       HBM's rate, in which shared memory moves 46 KB.
 //   loading warps: the rows of x that the group names, a stage each in turn, by copies of 16 bytes
-//       into shared memory (B). Between the copies and the tensor pipe's reads is a fence of 350
-//       to 1000 cycles, so as many stages are under way as there are loading warps. (TMA gathers of
-//       four rows need no fence, but took 80 cycles each: 64 rows 2500 cycles a stage.)
+//       into shared memory (B). Between the copies and the tensor pipe's reads is a fence of 200
+//       cycles and more, so several stages are under way. (TMA gathers of four rows need no fence,
+//       but took 80 cycles each: for 64 rows 2500 cycles a stage.)
 //   an issuing warp: tcgen05.mma, M = 128 outputs, N = the unit's rows in sixteens
 //   epilogue warps: sums from tensor memory, SwiGLU, y
-// Few rows: the weights' bytes are the bound, and the arithmetic on the codes is close to it (32
-// pairs a row and 64 inputs, 2.75 operations each). Many rows: the tensor pipe.
+// Few rows: the weights' bytes are the bound, and the instructions per code are close to it: 64 pairs
+// a lane and stage at 2.75, of the 368 that each scheduler issues in that time. Many rows: the
+// tensor pipe, and the copies of x.
 // Every wait has a limit of one second. One that runs out is recorded (dmoe_q4_device_error) and ends
 // its role; the others' waits run out after it, and the CTA gives its tensor memory back.
 #include "q4.cuh"
@@ -28,14 +29,12 @@ constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 4;
 constexpr int kLoadWarp = kEpiWarps + kDeqWarps, kMmaWarp = kLoadWarp + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kUnitRows = 128;             // rows of a group per unit, at most
-// A stage is 128 inputs: two blocks of 64.
-constexpr int kASlots = 4;                 // stages of A in tensor memory, 64 columns each
-constexpr int kBRing = 128 * 1024;         // bytes of the ring of x's stages
+constexpr int kASlots = kSets;             // stages of A in tensor memory, 64 columns each
+constexpr int kBRing = 96 * 1024;          // bytes of the ring of x's stages
 constexpr int kBSlotsMax = 8;
-constexpr int kCodeSlots = 2;              // stages of codes per set, one of them in use
+constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of them in use
 constexpr int kAcc0 = kASlots * 64;        // first column of the sums: two buffers of 128
 constexpr uint64_t kWaitNs = 1000000000ull;
-
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
 
 __device__ DevErrRecord q4_fault;          // of every call on the device
@@ -52,13 +51,18 @@ struct __align__(16) Unit {
   int r0, n;      // rows
 };
 
+struct CodeSlot {
+  uint4 codes[4][kQ4Rows];       // [32 inputs][row]
+  uint16_t scales[kQ4Rows * 4];  // [row][group]
+};
+
 struct Smem {
-  uint8_t b[kBRing];                                       // 1024-byte aligned
-  uint4 codes[kSets][kCodeSlots][4][128];                      // [set][slot][32 inputs][row]
-  uint4 scales[kSets][kCodeSlots][128];                    // eight groups of a row
-  float swap[2][2][64][9];                                 // ups and gates between epilogue warps
-  Unit sched[kSched];                                      // the CTA's units, in its order
+  uint8_t b[kBRing];                         // 1024-byte aligned
+  CodeSlot code[kDeqWarps][kCodeSlots];
+  float swap[2][2][64][9];                   // ups and gates between epilogue warps
+  Unit sched[kSched];                        // the CTA's units, in its order
   Groups groups;
+  uint64_t code_full[kDeqWarps][kCodeSlots];
   uint64_t a_full[kASlots], a_empty[kASlots];
   uint64_t b_full[kBSlotsMax], b_empty[kBSlotsMax];
   uint64_t d_full[2], d_empty[2], drain;
@@ -145,13 +149,124 @@ __device__ __forceinline__ int units_of_cta(const Groups& s) {
   return s.units > (int)blockIdx.x ? (s.units - (int)blockIdx.x - 1) / (int)gridDim.x + 1 : 0;
 }
 
+// Waits with pauses, or, for the issuing warp (kPause 0), without.
+template <int kPause>
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, int where) {
-  if (ptx::mbar_wait_long(bar, parity, kWaitNs)) return true;
+  if (ptx::mbar_wait_paused(bar, parity, kWaitNs, kPause)) return true;
   record_error(&q4_fault, kErrTimeout, kAtQ4, where);
   return false;
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes = 16) {
+// A slot of a ring and the parity of its turn, one step on.
+struct Slot {
+  int i = 0;
+  uint32_t turn = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++i == n) {
+      i = 0;
+      turn ^= 1u;
+    }
+  }
+};
+
+// ------------------------------------------------------------------ dequantising
+template <bool kGated>
+__device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
+                                           uint32_t tmem) {
+  const int warp = threadIdx.x / 32 - kEpiWarps, set = warp >> 2, lane = threadIdx.x & 31;
+  const int units = units_of_cta(sm.groups), scale_block = s.scale_block();
+  CodeSlot* const ring = sm.code[warp];
+  uint64_t* const full = sm.code_full[warp];
+
+  // The copies run ahead of the values by kCodeSlots - 1 blocks of this warp, over the ends of units.
+  // base: stages of the units before; the set takes the stages whose number is set mod kSets.
+  int unit = 0, base = 0, st = set, copied = 0;
+  const uint8_t *codes = nullptr, *scales = nullptr;
+  bool there = false;   // the warp's rows of this unit are in the matrix
+  auto enter = [&]() {
+    if (unit >= units) return;
+    const Unit u = unit_at(sm, m_tiles, unit);
+    const int m = kGated ? (warp & 3) >> 1 : 0;
+    const int tile = kGated ? u.mt * 2 + (warp & 1) : u.mt * 4 + (warp & 3);
+    there = tile < s.tiles;
+    const size_t block = ((size_t)u.e * s.tiles + tile) * s.blocks + st;
+    codes = static_cast<const uint8_t*>(a.codes[m]) + block * kQ4CodeBytes;
+    scales = static_cast<const uint8_t*>(a.scales[m]) + block * scale_block;
+  };
+  Slot to;
+  auto copy = [&]() {
+    while (st >= s.blocks && unit < units) {
+      base += s.blocks;
+      ++unit;
+      st = (set - base) & (kSets - 1);
+      if (st < s.blocks) enter();
+    }
+    if (unit >= units) return;
+    if (lane == 0) {
+      ptx::mbar_arrive_expect_tx(&full[to.i], there ? kQ4CodeBytes + scale_block : 0);
+      if (there) {
+        ptx::bulk_load(ring[to.i].codes, codes, kQ4CodeBytes, &full[to.i]);
+        ptx::bulk_load(ring[to.i].scales, scales, scale_block, &full[to.i]);
+      }
+    }
+    codes += kSets * kQ4CodeBytes;
+    scales += kSets * scale_block;
+    st += kSets;
+    ++copied;
+    to.next(kCodeSlots);
+  };
+  if (st < s.blocks) enter();
+  for (int i = 0; i < kCodeSlots - 1; ++i) copy();
+
+  const uint32_t at = tmem + set * 64 + ((uint32_t)(warp & 3) << 21);   // (A's slot is the set's)
+  Slot from;
+  uint32_t a_turn = 1;
+  int done = 0;
+  for (;; ++done) {
+    copy();
+    if (done == copied) break;   // (copies are ahead until there are none)
+    if (!__all_sync(0xffffffffu, wait<0>(&full[from.i], from.turn, 8))) break;
+    const CodeSlot& slot = ring[from.i];
+    // the scales of the stage's four 32 inputs
+    uint32_t s01, s23;
+    if (s.groups == 4) {
+      const uint2 v = reinterpret_cast<const uint2*>(slot.scales)[lane];
+      s01 = v.x;
+      s23 = v.y;
+    } else if (s.groups == 2) {
+      const uint32_t v = reinterpret_cast<const uint32_t*>(slot.scales)[lane];
+      s01 = __byte_perm(v, 0u, 0x1010);
+      s23 = __byte_perm(v, 0u, 0x3232);
+    } else {
+      s01 = s23 = slot.scales[lane] * 0x10001u;
+    }
+    if (!__all_sync(0xffffffffu, wait<20>(&sm.a_empty[set], a_turn, 1))) break;
+    ptx::tc_fence_after();
+#pragma unroll 1
+    for (int h = 0; h < 4; h += 2) {
+      const uint32_t pair = h == 0 ? s01 : s23;
+      const Q4Scale s0 = q4_scale_pair(pair), s1 = q4_scale_pair(pair >> 16);
+      const uint4 c0 = slot.codes[h][lane], c1 = slot.codes[h + 1][lane];
+      const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+      uint32_t v[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = q4_value_pair(w[i / 4], i & 3, i < 16 ? s0 : s1);
+      ptx::tmem_st32(at + h * 16, v);
+    }
+    ptx::tmem_st_wait();
+    ptx::tc_fence_before();
+    __syncwarp();   // (the slot has been read, too)
+    if (lane == 0) ptx::mbar_arrive(&sm.a_full[set]);
+    a_turn ^= 1u;
+    from.next(kCodeSlots);
+  }
+  // no copy is left in flight behind a wait that ran out
+  for (; done < copied; ++done, from.next(kCodeSlots))
+    if (!ptx::mbar_wait_paused(&full[from.i], from.turn, kWaitNs, 0)) break;
+}
+
+// ------------------------------------------------------------------ loading x
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
                : "memory");
 }
@@ -161,131 +276,6 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ int stages_of(const Q4Shape& s) { return (s.k_tiles + 1) / 2; }
-
-// ------------------------------------------------------------------ dequantising
-// The place of a row's next codes and scales: copies run ahead of the values by kCodeSlots - 1 stages
-// of the set, over the ends of units.
-template <bool kGated>
-struct CodeCursor {
-  int unit, st, base;   // unit of the CTA; base: stages of the units before this one
-  int piece;            // of eight groups' scales, of the stage before
-  const uint8_t* codes; // of this row, stage st
-  const uint8_t* scales;
-  int half;             // bytes from half block to half block
-  bool row;             // this row is there
-  __device__ __forceinline__ void enter(const Q4Args& a, const Q4Shape& s, const Smem& sm, int units,
-                                        int m_tiles, int set, int lane_row) {
-    st = (set - base) & (kSets - 1);
-    piece = -1;
-    if (unit >= units) return;
-    const Unit u = unit_at(sm, m_tiles, unit);
-    const int m = kGated ? lane_row >> 6 : 0;
-    const int n = kGated ? u.mt * 64 + (lane_row & 63) : u.mt * 128 + lane_row;
-    row = n < s.rows;
-    if (!row) return;
-    half = s.tile_rows(n) * 16;
-    codes = static_cast<const uint8_t*>(a.codes[m]) + u.e * s.code_bytes() + s.code_at(n, 2 * st, 0);
-    scales = static_cast<const uint8_t*>(a.scales[m]) + ((size_t)u.e * s.rows + n) * s.groups_pad * 2;
-  }
-};
-
-template <bool kGated>
-__device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
-                                           uint32_t tmem) {
-  const int warp = threadIdx.x / 32 - kEpiWarps, set = warp >> 2;
-  const int lane_row = threadIdx.x & 127;   // (each set: lanes 0 .. 127 of tensor memory)
-  const int stages = stages_of(s), units = units_of_cta(sm.groups);
-  const int per_piece = s.group == 32 ? 1 : s.group == 64 ? 2 : 3;   // log2 of stages per piece
-  const uint32_t codes_at = ptx::smem_addr(&sm.codes[set][0][0][lane_row]);
-  const uint32_t scales_at = ptx::smem_addr(&sm.scales[set][0][lane_row]);
-  constexpr int kSlot = sizeof(sm.codes[0][0]), kHalf = sizeof(sm.codes[0][0][0]);
-  CodeCursor<kGated> c;
-  c.unit = 0;
-  c.base = 0;
-  c.enter(a, s, sm, units, m_tiles, set, lane_row);
-  int copy_slot = 0, copy_piece = 0;
-  auto copy = [&]() {
-    while (c.unit < units && c.st >= stages) {
-      c.base += stages;
-      ++c.unit;
-      c.enter(a, s, sm, units, m_tiles, set, lane_row);
-    }
-    if (c.unit < units) {
-      const int piece = c.st >> per_piece;
-      if (c.row) {
-        const uint32_t dst = codes_at + copy_slot * kSlot;
-        copy16(dst, c.codes);
-        copy16(dst + kHalf, c.codes + c.half);
-        if (2 * c.st + 1 < s.k_tiles) {
-          copy16(dst + 2 * kHalf, c.codes + 2 * c.half);
-          copy16(dst + 3 * kHalf, c.codes + 3 * c.half);
-        }
-        if (piece != c.piece) copy16(scales_at + copy_piece * kHalf, c.scales + piece * 16);
-        c.codes += kSets * 4 * c.half;
-      }
-      if (piece != c.piece) copy_piece = (copy_piece + 1) % kCodeSlots;
-      c.piece = piece;
-      copy_slot = (copy_slot + 1) % kCodeSlots;
-      c.st += kSets;
-    }
-    copies_commit();
-  };
-  for (int i = 0; i < kCodeSlots - 1; ++i) copy();
-  int base = 0, slot = 0, next_piece = 0;
-  bool ok = true;
-  for (int unit = 0; ok && unit < units; ++unit, base += stages) {
-    int piece = -1;
-    uint4 sc = make_uint4(0, 0, 0, 0);
-    for (int st = (set - base) & (kSets - 1); st < stages; st += kSets) {
-      copy();
-      copies_wait<kCodeSlots - 1>();
-      if (st >> per_piece != piece) {
-        piece = st >> per_piece;
-        sc = sm.scales[set][next_piece][lane_row];
-        next_piece = (next_piece + 1) % kCodeSlots;
-      }
-      // the scales of the stage's four halves of blocks, in pairs
-      uint32_t p0, p1;
-      if (s.group == 32) {
-        p0 = st & 1 ? sc.z : sc.x;
-        p1 = st & 1 ? sc.w : sc.y;
-      } else {
-        const int w = s.group == 64 ? st & 3 : (st & 7) >> 1;
-        const uint32_t pair = w & 2 ? (w & 1 ? sc.w : sc.z) : (w & 1 ? sc.y : sc.x);
-        p0 = __byte_perm(pair, 0u, s.group == 128 && (st & 1) ? 0x3232 : 0x1010);
-        p1 = s.group == 64 ? __byte_perm(pair, 0u, 0x3232) : p0;
-      }
-      const int stage = base + st, as = stage % kASlots;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (b == 1 && 2 * st + 1 >= s.k_tiles) break;
-        const uint4 c0 = sm.codes[set][slot][2 * b][lane_row], c1 = sm.codes[set][slot][2 * b + 1][lane_row];
-        const Q4Scale s0 = q4_scale_pair(b == 0 ? p0 : p1), s1 = q4_scale_pair((b == 0 ? p0 : p1) >> 16);
-        const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-        uint32_t v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = q4_value_pair(w[i / 4], i & 3, i < 16 ? s0 : s1);
-        if (b == 0) {
-          ok = wait(&sm.a_empty[as], ((stage / kASlots) & 1) ^ 1, 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          ptx::tc_fence_after();
-        }
-        ptx::tmem_st32(tmem + as * 64 + b * 32 + ((uint32_t)(warp & 3) << 21), v);
-      }
-      if (!ok) break;
-      slot = (slot + 1) % kCodeSlots;
-      ptx::tmem_st_wait();
-      ptx::tc_fence_before();
-      __syncwarp();
-      if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&sm.a_full[as]);
-    }
-  }
-  copies_wait<0>();
-}
-
-// ------------------------------------------------------------------ loading x
 // The source row of sorted row r, or -1.
 __device__ __forceinline__ int source(const Q4Args& a, int r) {
   if (a.rows == nullptr) return r;
@@ -293,95 +283,114 @@ __device__ __forceinline__ int source(const Q4Args& a, int r) {
   return t < a.T_x ? t : -1;
 }
 
-__device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
-                                       int b_slots) {
+// The ring's slots: 8, or as many as there is room for. A slot's stages are one warp's, so that no warp
+// waits for a slot two turns ahead of another: with 8 slots, a warp has two.
+__device__ __forceinline__ int b_slots_of(int widest) { return widest <= 48 ? 8 : widest <= 96 ? 4 : 3; }
+static_assert(8 * 48 * 256 <= kBRing && 4 * 96 * 256 <= kBRing && 3 * 128 * 256 <= kBRing &&
+                  kLoadWarps == 4, "ring of x");
+
+__device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm) {
   const int warp = threadIdx.x / 32 - kLoadWarp, lane = threadIdx.x & 31;
   const int chunk = lane & 7, sub = lane >> 3;   // 16 bytes of a row's 128, row of four
-  const int stages = stages_of(s), units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
+  const int units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
+  const int slots = b_slots_of(sm.groups.widest), warps = slots < kLoadWarps ? slots : kLoadWarps;
+  const bool lag = slots > kLoadWarps;   // a stage's copies are waited for after the next one's start
   const uint32_t ring = ptx::smem_addr(sm.b);
-  int stage = 0;
-  bool ok = true;
-  for (int unit = 0; ok && unit < units; ++unit) {
-    const int base = stage;
-    stage += stages;
-    int st = (warp - base) & (kLoadWarps - 1);   // this warp's first stage of the unit
-    if (st >= stages) continue;
+  if (warp >= warps) return;
+  int first = warp, slot = warp, pending = -1;   // this warp's next stage, counted from the unit's start
+  uint32_t turn = 1;
+  auto publish = [&](int i) {   // this warp's stage in slot i, for the tensor pipe to see
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sm.b_full[i]);
+  };
+  for (int unit = 0; unit < units; ++unit, first -= s.blocks) {
+    if (first >= s.blocks) continue;
     const Unit u = unit_at(sm, m_tiles, unit);
     int src[kUnitRows / 32];                     // of rows lane, lane + 32, ...
 #pragma unroll
     for (int j = 0; j < kUnitRows / 32; ++j)
       src[j] = 32 * j < u.n ? max(source(a, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
-    for (; st < stages; st += kLoadWarps) {
-      const int bs = (base + st) % b_slots;
-      ok = __all_sync(0xffffffffu, wait(&sm.b_empty[bs], (((base + st) / b_slots) & 1) ^ 1, 2));
-      if (!ok) break;
+    for (; first < s.blocks; first += warps) {
+      if (!__all_sync(0xffffffffu, wait<20>(&sm.b_empty[slot], turn, 2))) {
+        copies_wait<0>();
+        return;
+      }
       // (row r's 16-byte piece c is at r * 128 + (c ^ r % 8) * 16)
-      const uint32_t dst = ring + bs * 2 * block_bytes + sub * 128;
-      const __nv_bfloat16* x = a.x + st * 128 + chunk * 8;
-      const uint32_t in0 = st * 128 + chunk * 8 < s.K ? 16u : 0u;        // (zeros behind n_in)
-      const uint32_t in1 = st * 128 + 64 + chunk * 8 < s.K ? 16u : 0u;
+      const uint32_t dst = ring + slot * 2 * block_bytes;
+      const int k = first * 128 + chunk * 8;
+      const __nv_bfloat16* x = a.x + k;
+      const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
 #pragma unroll
       for (int j = 0; j < kUnitRows / 32; ++j) {
-        if (32 * j >= u.n) break;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 32 * j + 4 * i + sub;
-          const int64_t at = __shfl_sync(0xffffffffu, src[j], 4 * i + sub) * a.ldx;
-          if (r < u.n) {
-            const uint32_t to = dst + (32 * j + 4 * i) * 128 + ((chunk ^ ((4 * i + sub) & 7)) << 4);
+        const int n = min(u.n - 32 * j, 32);
+#pragma unroll 1
+        for (int i = 0; i < n; i += 4) {
+          const int r = i + sub;
+          const int64_t at = __shfl_sync(0xffffffffu, src[j], r) * a.ldx;
+          if (r < n) {
+            const uint32_t to = dst + (32 * j + r) * 128 + ((chunk ^ (r & 7)) << 4);
             copy16(to, in0 ? x + at : a.x, in0);
-            if (2 * st + 1 < s.k_tiles) copy16(to + block_bytes, in1 ? x + at + 64 : a.x, in1);
+            copy16(to + block_bytes, in1 ? x + at + 64 : a.x, in1);
           }
         }
       }
       copies_commit();
-      copies_wait<0>();
-      ptx::fence_proxy_async_smem();   // (the tensor pipe reads them)
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&sm.b_full[bs]);
+      if (!lag) {
+        copies_wait<0>();
+        publish(slot);
+      } else {
+        copies_wait<1>();
+        if (pending >= 0) publish(pending);
+        pending = slot;
+      }
+      slot += warps;
+      if (slot >= slots) {
+        slot = warp;
+        turn ^= 1u;
+      }
     }
   }
+  copies_wait<0>();
+  if (pending >= 0) publish(pending);
 }
 
 // ------------------------------------------------------------------ issuing the MMAs
-__device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem,
-                                      int b_slots) {
-  const int stages = stages_of(s), units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
-  const uint32_t ring = ptx::smem_addr(sm.b);
-  int stage = 0;
+__device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem) {
+  const int units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
+  const int slots = b_slots_of(sm.groups.widest);
+  const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b));
+  const uint32_t block16 = block_bytes >> 4;   // (a descriptor's address is in units of 16 bytes)
+  Slot as, bs, ds;
   bool ok = true;
-  for (int turn = 0; ok && turn < units; ++turn) {
+  for (int turn = 0; ok && turn < units; ++turn, ds.next(2)) {
     const Unit u = unit_at(sm, m_tiles, turn);
     const uint32_t idesc = ptx::idesc_bf16(128, (u.n + 15) / 16 * 16);
-    const int buf = turn & 1;
-    const uint32_t d = tmem + kAcc0 + buf * 128;
-    ok = __all_sync(0xffffffffu, wait(&sm.d_empty[buf], ((turn >> 1) & 1) ^ 1, 3));
-    for (int st = 0; ok && st < stages; ++st, ++stage) {
-      const int as = stage % kASlots, bs = stage % b_slots;
-      ok = wait(&sm.b_full[bs], (stage / b_slots) & 1, 4) && wait(&sm.a_full[as], (stage / kASlots) & 1, 5);
+    const uint32_t d = tmem + kAcc0 + ds.i * 128;
+    ok = __all_sync(0xffffffffu, wait<0>(&sm.d_empty[ds.i], ds.turn ^ 1u, 3));
+    for (int st = 0; ok && st < s.blocks; ++st) {
+      ok = wait<0>(&sm.b_full[bs.i], bs.turn, 4) && wait<0>(&sm.a_full[as.i], as.turn, 5);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       ptx::tc_fence_after();
-      const uint64_t b0 = ptx::sdesc_k_sw128(ring + bs * 2 * block_bytes);
       if (ptx::elect_one()) {
+        const uint64_t b0 = ring + bs.i * 2 * block16;
+        const uint32_t a0 = tmem + as.i * 64;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          if (b == 1 && 2 * st + 1 >= s.k_tiles) break;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)   // (a descriptor's address is in units of 16 bytes)
-            ptx::mma_bf16_ta(d, tmem + as * 64 + b * 32 + j * 8, b0 + b * (block_bytes >> 4) + j * 2, idesc,
-                             (st | b | j) != 0);
-        }
-        ptx::mma_commit(&sm.a_empty[as]);
-        ptx::mma_commit(&sm.b_empty[bs]);
-        if (st == stages - 1) ptx::mma_commit(&sm.d_full[buf]);
+        for (int j = 0; j < 8; ++j)
+          ptx::mma_bf16_ta(d, a0 + j * 8, b0 + (j & 4 ? block16 : 0u) + (j & 3) * 2, idesc, (st | j) != 0);
+        ptx::mma_commit(&sm.a_empty[as.i]);
+        ptx::mma_commit(&sm.b_empty[bs.i]);
+        if (st == s.blocks - 1) ptx::mma_commit(&sm.d_full[ds.i]);
       }
       __syncwarp();
+      as.next(kASlots);
+      bs.next(slots);
     }
   }
   // everything issued has been done before the CTA gives its memory back
   if (ptx::elect_one()) ptx::mma_commit(&sm.drain);
-  wait(&sm.drain, 0, 6);
+  wait<0>(&sm.drain, 0, 6);
 }
 
 // ------------------------------------------------------------------ epilogue
@@ -407,7 +416,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         missing[j] = __ballot_sync(0xffffffffu, r < u.n && source(a, u.r0 + r) < 0);
       }
     }
-    if (!ptx::epi_all(wait(&sm.d_full[buf], (turn >> 1) & 1, 7))) break;
+    if (!ptx::epi_all(wait<100>(&sm.d_full[buf], (turn >> 1) & 1, 7))) break;
     ptx::tc_fence_after();
     const uint32_t from = tmem + kAcc0 + buf * 128 + ((uint32_t)warp << 21);
     const int n = kGated ? u.mt * 64 + (row & 63) : u.mt * 128 + row;
@@ -458,8 +467,9 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
     ptx::tmem_relinquish();
   }
   if (threadIdx.x == 0) {
+    for (int i = 0; i < kDeqWarps * kCodeSlots; ++i) ptx::mbar_init(&sm.code_full[0][0] + i, 1);
     for (int i = 0; i < kASlots; ++i) {
-      ptx::mbar_init(&sm.a_full[i], kDeqWarps / kSets);
+      ptx::mbar_init(&sm.a_full[i], 4);
       ptx::mbar_init(&sm.a_empty[i], 1);
     }
     for (int i = 0; i < kBSlotsMax; ++i) {
@@ -483,14 +493,10 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  // (a multiple of the loading warps: a slot's stages are one warp's, so that no warp waits for a
-  // slot two turns ahead of another)
-  static_assert(kBRing == kBSlotsMax * 64 * 256 && kBSlotsMax == 2 * kLoadWarps && kASlots == kSets, "rings");
-  const int b_slots = sm.groups.widest <= 64 ? kBSlotsMax : kBSlotsMax / 2;
   if (warp < kEpiWarps) epilogue<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, m_tiles, sm, tmem);
-  else if (warp == kMmaWarp) issue(s, m_tiles, sm, tmem, b_slots);
-  else load_x(a, s, m_tiles, sm, b_slots);
+  else if (warp == kMmaWarp) issue(s, m_tiles, sm, tmem);
+  else load_x(a, s, m_tiles, sm);
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();

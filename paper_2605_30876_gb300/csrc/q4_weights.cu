@@ -12,14 +12,12 @@ struct Q4Block {   // a warp's 16 x 128 weights
   bool ok;
 };
 __device__ __forceinline__ Q4Block q4_block(const Q4Shape& s, int n_experts) {
-  const int kbs = (s.k_tiles + 1) / 2;
   int64_t i = (int64_t)blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5);
   Q4Block b;
-  b.kb = (int)(i % kbs);
-  i /= kbs;
-  const int tiles = s.rows / 16;
-  b.nt = (int)(i % tiles);
-  i /= tiles;
+  b.kb = (int)(i % s.blocks);
+  i /= s.blocks;
+  b.nt = (int)(i % (2 * s.tiles));
+  i /= 2 * s.tiles;
   b.e = (int)i;
   b.ok = i < n_experts;
   return b;
@@ -96,26 +94,18 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_
       }
       word[r][c] = q4_pack_word(code);
     }
-  uint8_t* to = codes + b.e * s.code_bytes();
+  const size_t block = ((size_t)b.e * s.tiles + b.nt / 2) * s.blocks + b.kb;
+  const int row = b.nt % 2 * 16 + g;   // of the tile, and the one 8 behind it
+  uint8_t* to = codes + block * kQ4CodeBytes + row * 16 + 4 * q;
+  uint16_t* sc = scales + (block * kQ4Rows + row) * s.groups;
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      if (b.kb * 2 + c / 2 < s.k_tiles)
-        *reinterpret_cast<uint32_t*>(to + s.code_at(b.nt * 16 + g + 8 * r, b.kb * 2 + c / 2, c & 1) +
-                                     4 * q) = word[r][c];
-  uint16_t* sc = scales + ((size_t)b.e * s.rows + b.nt * 16 + g) * s.groups_pad;
-#pragma unroll
-  for (int r = 0; r < 2; ++r, sc += 8 * s.groups_pad) {
+  for (int r = 0; r < 2; ++r)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int gi = (b.kb * 4 + c) / per;
-      if (q == c && c % per == 0 && gi < s.groups)
-        sc[gi] = (uint16_t)(__float_as_uint(scale[r][c]) >> 16);
+      *reinterpret_cast<uint32_t*>(to + c * kQ4Rows * 16 + r * 8 * 16) = word[r][c];
+      if (q == c && c % per == 0)
+        sc[r * 8 * s.groups + c / per] = (uint16_t)(__float_as_uint(scale[r][c]) >> 16);
     }
-    if (b.kb == (s.k_tiles + 1) / 2 - 1 && q == 0)
-      for (int gi = s.groups; gi < s.groups_pad; ++gi) sc[gi] = 0;
-  }
 }
 
 __global__ void __launch_bounds__(kQ4Threads)
@@ -127,18 +117,17 @@ q4_dequantize_kernel(Q4Shape s, int n_experts, const uint8_t* __restrict__ codes
   if (!b.ok) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int per = s.group / 32;
-  const uint8_t* from = codes + b.e * s.code_bytes();
+  const size_t block = ((size_t)b.e * s.tiles + b.nt / 2) * s.blocks + b.kb;
+  const int row = b.nt % 2 * 16 + g;
+  const uint8_t* from = codes + block * kQ4CodeBytes + row * 16 + 4 * q;
+  const uint16_t* sc = scales + (block * kQ4Rows + row) * s.groups;
   uint32_t word[2][4], bits[2][4];
 #pragma unroll
   for (int r = 0; r < 2; ++r)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int n = b.nt * 16 + g + 8 * r, kt = b.kb * 2 + c / 2, gi = (b.kb * 4 + c) / per;
-      word[r][c] = 0;
-      bits[r][c] = 0;
-      if (kt < s.k_tiles)
-        word[r][c] = __ldcs(reinterpret_cast<const uint32_t*>(from + s.code_at(n, kt, c & 1) + 4 * q));
-      if (gi < s.groups) bits[r][c] = __ldg(scales + ((size_t)b.e * s.rows + n) * s.groups_pad + gi);
+      word[r][c] = __ldcs(reinterpret_cast<const uint32_t*>(from + c * kQ4Rows * 16 + r * 8 * 16));
+      bits[r][c] = __ldg(sc + r * 8 * s.groups + c / per);
     }
 #pragma unroll
   for (int r = 0; r < 2; ++r)
@@ -154,7 +143,7 @@ q4_dequantize_kernel(Q4Shape s, int n_experts, const uint8_t* __restrict__ codes
 }
 
 unsigned q4_ctas(const Q4Shape& s, int n_experts) {
-  const int64_t warps = (int64_t)n_experts * (s.rows / 16) * ((s.k_tiles + 1) / 2);
+  const int64_t warps = (int64_t)n_experts * 2 * s.tiles * s.blocks;
   return (unsigned)((warps + kQ4Threads / 32 - 1) / (kQ4Threads / 32));
 }
 

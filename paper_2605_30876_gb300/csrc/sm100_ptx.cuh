@@ -65,24 +65,21 @@ __device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// The same for a wait that is expected to be long: the thread may be suspended for up to `hint_ns` at a
-// time, and takes no issue slots meanwhile.
-__device__ __forceinline__ bool mbar_try_wait_long(uint64_t* bar, uint32_t parity, uint32_t hint_ns) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_addr(bar)), "r"(parity), "r"(hint_ns)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_long(uint64_t* bar, uint32_t parity, uint64_t timeout_ns) {
+// The same, with a pause of `pause_ns` after each poll (0: none), so that a warp that waits long takes
+// few issue slots from the others. The time is read every 256 polls only: reading it takes
+// as long as some polls.
+__device__ __forceinline__ bool mbar_wait_paused(uint64_t* bar, uint32_t parity, uint64_t timeout_ns,
+                                                 uint32_t pause_ns) {
   if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = globaltimer_ns();
-  while (!mbar_try_wait_long(bar, parity, 20000u))
-    if (globaltimer_ns() - t0 > timeout_ns) return false;
+  uint64_t t0 = 0;
+  for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
+    if (pause_ns > 0) __nanosleep(pause_ns);
+    if ((i & 255u) == 0u) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > timeout_ns) return false;
+    }
+  }
   return true;
 }
 // one lane of a converged warp
@@ -124,6 +121,14 @@ __device__ __forceinline__ uint64_t policy_evict_last() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
   return p;
+}
+// `bytes` of global memory into shared memory (16-byte aligned both, and the size)
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_addr(bar))
+      : "memory");
 }
 // 2-D tiled load of the box at (x = inner coordinate, y = row) into shared memory; the
 // transaction bytes are signalled on `bar`.

@@ -141,10 +141,10 @@ def test_q4_desc_refusals(dm, lib, kw, status):
 
 
 def test_q4_sizes(dm):
-    # 4 bits a weight and 16 a group, where rows, inputs and groups are whole sixteens, 64s and eights
+    # 4 bits a weight and 16 a group, where rows are whole 32s and inputs whole 128s
     assert dm.dmoe_q4_size(dm.make_q4_desc(3, 32, 512, 64)) == (3 * 32 * 256, 3 * 32 * 8 * 2)
-    # 17 rows: 32; 96 inputs: two blocks of 64; three groups: eight
-    assert dm.dmoe_q4_size(dm.make_q4_desc(1, 17, 96, 32)) == (32 * 2 * 32, 32 * 8 * 2)
+    # 33 rows: 64; 160 inputs: 256
+    assert dm.dmoe_q4_size(dm.make_q4_desc(1, 33, 160, 32)) == (64 * 128, 64 * 8 * 2)
 
 
 def test_q4_product_refusals(dm, lib):
