@@ -61,9 +61,20 @@ __device__ __forceinline__ Q4Scale q4_scale_pair(uint32_t bits) {   // (the lowe
 // has 5 + 2 significant bits, the value 5 + 3, and bf16 holds eight; the FMA rounds once. With the
 // nibble in the lower bits (128 + nibble) the offset would be 136 s, 5 + 5 bits, and a
 // subtraction of its own were needed.
-__device__ __forceinline__ uint32_t q4_value_pair(uint32_t word, int i, const Q4Scale& s) {
+// The mask and the exponent bits of a pair are held in registers by the caller (an instruction takes one
+// immediate: given both, the compiler makes two of the AND and the OR).
+struct Q4Bits {
+  uint32_t mask, sixteen;
+  __device__ __forceinline__ Q4Bits() {
+    asm volatile("mov.u32 %0, 0x00780078;" : "=r"(mask));
+    asm volatile("mov.u32 %0, 0x41804180;" : "=r"(sixteen));
+  }
+};
+__device__ __forceinline__ uint32_t q4_value_pair(uint32_t word, int i, const Q4Scale& s,
+                                                  const Q4Bits& bits) {
   const uint32_t r = i == 0 ? word : i == 3 ? __funnelshift_r(word, word, 12) : word >> (4 * i);
-  const uint32_t u = (r & 0x00780078u) | 0x41804180u;
+  uint32_t u;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(r), "r"(bits.mask), "r"(bits.sixteen));   // and, or
   const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&u), s.s, s.b);
   return *reinterpret_cast<const uint32_t*>(&v);
 }

@@ -1,5 +1,5 @@
 // Products of sorted rows with their experts' 4-bit matrices, plain or gate and up with SwiGLU:
-// y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 128 rows of a group.
+// y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 96 rows of a group.
 //
 // A persistent CTA per SM, in roles, by stages of 128 inputs:
 //   dequantising warps (four sets of four, a stage each in turn): a lane has a row of W. A bulk copy
@@ -28,12 +28,14 @@ namespace {
 constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 4;
 constexpr int kLoadWarp = kEpiWarps + kDeqWarps, kMmaWarp = kLoadWarp + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
-constexpr int kUnitRows = 128;             // rows of a group per unit, at most
-constexpr int kASlots = kSets;             // stages of A in tensor memory, 64 columns each
-constexpr int kBRing = 96 * 1024;          // bytes of the ring of x's stages
-constexpr int kBSlotsMax = 8;
+constexpr int kUnitRows = 96;              // rows of a group per unit, at most
+// The ring of stages: A in tensor memory, 64 columns a slot, and B in shared memory. A slot is a set's
+// and a loading warp's, and one pair of barriers serves both operands: the issuing thread's waits
+// and commits take as long as the MMAs of few rows (100 to 150 cycles each).
+constexpr int kSlots = 4;
 constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of them in use
-constexpr int kAcc0 = kASlots * 64;        // first column of the sums: two buffers of 128
+constexpr int kAcc0 = kSlots * 64;         // first column of the sums: two buffers of 128
+static_assert(kSets == kSlots && kLoadWarps == kSlots, "a set and a loading warp per slot");
 constexpr uint64_t kWaitNs = 1000000000ull;
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
 
@@ -42,7 +44,6 @@ __device__ DevErrRecord q4_fault;          // of every call on the device
 // The groups that have rows and an expert, in order, and their first units.
 struct Groups {
   int n, units;
-  int widest;   // rows of the widest unit, in sixteens
   int e[kMaxExperts], r0[kMaxExperts], r1[kMaxExperts], first[kMaxExperts];
 };
 
@@ -57,14 +58,13 @@ struct CodeSlot {
 };
 
 struct Smem {
-  uint8_t b[kBRing];                         // 1024-byte aligned
+  uint8_t b[kSlots][2][kUnitRows * 128];     // [slot][64 inputs], 1024-byte aligned
   CodeSlot code[kDeqWarps][kCodeSlots];
   float swap[2][2][64][9];                   // ups and gates between epilogue warps
   Unit sched[kSched];                        // the CTA's units, in its order
   Groups groups;
   uint64_t code_full[kDeqWarps][kCodeSlots];
-  uint64_t a_full[kASlots], a_empty[kASlots];
-  uint64_t b_full[kBSlotsMax], b_empty[kBSlotsMax];
+  uint64_t full[kSlots], empty[kSlots];      // of the ring's stages
   uint64_t d_full[2], d_empty[2], drain;
   uint32_t tmem;
   int wcount[kThreads / 32];
@@ -92,7 +92,6 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
     const int v = __shfl_up_sync(0xffffffffu, before, o);
     if (lane >= o) before += v;
   }
-  if (u == 0) s.widest = 16;
   if (lane == 31) {
     sm.wcount[warp] = before;
     if (warp < kMaxExperts / 32) s.first[warp] = __popc(m);   // (for the moment)
@@ -113,8 +112,6 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
     s.r0[at] = r0;
     s.r1[at] = r1;
     s.first[at] = before - units;
-    const int per = (r1 - r0 + tiles - 1) / tiles;
-    atomicMax(&s.widest, (per + 15) / 16 * 16);
   }
   if (u == 0) {
     s.n = n;
@@ -218,9 +215,10 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
   if (st < s.blocks) enter();
   for (int i = 0; i < kCodeSlots - 1; ++i) copy();
 
-  const uint32_t at = tmem + set * 64 + ((uint32_t)(warp & 3) << 21);   // (A's slot is the set's)
+  const uint32_t at = tmem + set * 64 + ((uint32_t)(warp & 3) << 21);   // (the set's slot)
+  const Q4Bits bits;
   Slot from;
-  uint32_t a_turn = 1;
+  uint32_t turn = 1;
   int done = 0;
   for (;; ++done) {
     copy();
@@ -240,7 +238,7 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
     } else {
       s01 = s23 = slot.scales[lane] * 0x10001u;
     }
-    if (!__all_sync(0xffffffffu, wait<20>(&sm.a_empty[set], a_turn, 1))) break;
+    if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[set], turn, 1))) break;
     ptx::tc_fence_after();
 #pragma unroll 1
     for (int h = 0; h < 4; h += 2) {
@@ -250,14 +248,14 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
       const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       uint32_t v[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = q4_value_pair(w[i / 4], i & 3, i < 16 ? s0 : s1);
+      for (int i = 0; i < 32; ++i) v[i] = q4_value_pair(w[i / 4], i & 3, i < 16 ? s0 : s1, bits);
       ptx::tmem_st32(at + h * 16, v);
     }
     ptx::tmem_st_wait();
     ptx::tc_fence_before();
     __syncwarp();   // (the slot has been read, too)
-    if (lane == 0) ptx::mbar_arrive(&sm.a_full[set]);
-    a_turn ^= 1u;
+    if (lane == 0) ptx::mbar_arrive(&sm.full[set]);
+    turn ^= 1u;
     from.next(kCodeSlots);
   }
   // no copy is left in flight behind a wait that ran out
@@ -283,110 +281,98 @@ __device__ __forceinline__ int source(const Q4Args& a, int r) {
   return t < a.T_x ? t : -1;
 }
 
-// The ring's slots: 8, or as many as there is room for. A slot's stages are one warp's, so that no warp
-// waits for a slot two turns ahead of another: with 8 slots, a warp has two.
-__device__ __forceinline__ int b_slots_of(int widest) { return widest <= 48 ? 8 : widest <= 96 ? 4 : 3; }
-static_assert(8 * 48 * 256 <= kBRing && 4 * 96 * 256 <= kBRing && 3 * 128 * 256 <= kBRing &&
-                  kLoadWarps == 4, "ring of x");
-
 __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm) {
   const int warp = threadIdx.x / 32 - kLoadWarp, lane = threadIdx.x & 31;
   const int chunk = lane & 7, sub = lane >> 3;   // 16 bytes of a row's 128, row of four
-  const int units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
-  const int slots = b_slots_of(sm.groups.widest), warps = slots < kLoadWarps ? slots : kLoadWarps;
-  const bool lag = slots > kLoadWarps;   // a stage's copies are waited for after the next one's start
-  const uint32_t ring = ptx::smem_addr(sm.b);
-  if (warp >= warps) return;
-  int first = warp, slot = warp, pending = -1;   // this warp's next stage, counted from the unit's start
+  const int units = units_of_cta(sm.groups);
+  // (row r's 16-byte piece c is at r * 128 + (c ^ r % 8) * 16)
+  const uint32_t dst = ptx::smem_addr(sm.b[warp][0]) + sub * 128;
   uint32_t turn = 1;
-  auto publish = [&](int i) {   // this warp's stage in slot i, for the tensor pipe to see
-    ptx::fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(&sm.b_full[i]);
-  };
-  for (int unit = 0; unit < units; ++unit, first -= s.blocks) {
-    if (first >= s.blocks) continue;
+  int st = warp;   // this warp's next stage, counted from the unit's start
+  for (int unit = 0; unit < units; ++unit, st -= s.blocks) {
+    if (st >= s.blocks) continue;
     const Unit u = unit_at(sm, m_tiles, unit);
     int src[kUnitRows / 32];                     // of rows lane, lane + 32, ...
 #pragma unroll
     for (int j = 0; j < kUnitRows / 32; ++j)
       src[j] = 32 * j < u.n ? max(source(a, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
-    for (; first < s.blocks; first += warps) {
-      if (!__all_sync(0xffffffffu, wait<20>(&sm.b_empty[slot], turn, 2))) {
-        copies_wait<0>();
-        return;
-      }
-      // (row r's 16-byte piece c is at r * 128 + (c ^ r % 8) * 16)
-      const uint32_t dst = ring + slot * 2 * block_bytes;
-      const int k = first * 128 + chunk * 8;
+    for (; st < s.blocks; st += kSlots) {
+      const int k = st * 128 + chunk * 8;
       const __nv_bfloat16* x = a.x + k;
       const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
+      if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[warp], turn, 2))) return;
+      turn ^= 1u;
 #pragma unroll
       for (int j = 0; j < kUnitRows / 32; ++j) {
         const int n = min(u.n - 32 * j, 32);
 #pragma unroll 1
         for (int i = 0; i < n; i += 4) {
-          const int r = i + sub;
-          const int64_t at = __shfl_sync(0xffffffffu, src[j], r) * a.ldx;
-          if (r < n) {
-            const uint32_t to = dst + (32 * j + r) * 128 + ((chunk ^ (r & 7)) << 4);
+          const int64_t at = __shfl_sync(0xffffffffu, src[j], i + sub) * a.ldx;
+          if (i + sub < n) {
+            const uint32_t to = dst + (32 * j + i) * 128 + ((chunk ^ ((i + sub) & 7)) << 4);
             copy16(to, in0 ? x + at : a.x, in0);
-            copy16(to + block_bytes, in1 ? x + at + 64 : a.x, in1);
+            copy16(to + kUnitRows * 128, in1 ? x + at + 64 : a.x, in1);
           }
         }
       }
       copies_commit();
-      if (!lag) {
-        copies_wait<0>();
-        publish(slot);
-      } else {
-        copies_wait<1>();
-        if (pending >= 0) publish(pending);
-        pending = slot;
-      }
-      slot += warps;
-      if (slot >= slots) {
-        slot = warp;
-        turn ^= 1u;
-      }
+      copies_wait<0>();
+      ptx::fence_proxy_async_smem();   // (the tensor pipe reads them)
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&sm.full[warp]);
     }
   }
-  copies_wait<0>();
-  if (pending >= 0) publish(pending);
 }
 
 // ------------------------------------------------------------------ issuing the MMAs
+// The whole warp goes through the stages and elects the lane that issues: with one lane in a branch of
+// its own the operands were not uniform, and eight MMAs took 600 cycles to issue instead of 150. One
+// warp's instructions take five cycles and more each here, and this warp's are the ring's
+// pace: the slots are unrolled, so that addresses are constants.
 __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem) {
-  const int units = units_of_cta(sm.groups), block_bytes = sm.groups.widest * 128;
-  const int slots = b_slots_of(sm.groups.widest);
   const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b));
-  const uint32_t block16 = block_bytes >> 4;   // (a descriptor's address is in units of 16 bytes)
-  Slot as, bs, ds;
+  constexpr uint32_t kBlock16 = kUnitRows * 128 / 16;   // (a descriptor's address is in units of 16 bytes)
+  const int units = units_of_cta(sm.groups);
+  int unit = 0, left = 0;   // stages left of the unit
+  uint32_t d = 0, idesc = 0, full_turn = 0;
+  Slot acc;
   bool ok = true;
-  for (int turn = 0; ok && turn < units; ++turn, ds.next(2)) {
-    const Unit u = unit_at(sm, m_tiles, turn);
-    const uint32_t idesc = ptx::idesc_bf16(128, (u.n + 15) / 16 * 16);
-    const uint32_t d = tmem + kAcc0 + ds.i * 128;
-    ok = __all_sync(0xffffffffu, wait<0>(&sm.d_empty[ds.i], ds.turn ^ 1u, 3));
-    for (int st = 0; ok && st < s.blocks; ++st) {
-      ok = wait<0>(&sm.b_full[bs.i], bs.turn, 4) && wait<0>(&sm.a_full[as.i], as.turn, 5);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
+  while (ok) {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      bool first = false;
+      if (left == 0) {
+        if (unit == units) {
+          ok = false;
+          break;
+        }
+        idesc = ptx::idesc_bf16(128, (unit_at(sm, m_tiles, unit).n + 15) / 16 * 16);
+        d = tmem + kAcc0 + acc.i * 128;
+        if (!__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
+          ok = false;
+          break;
+        }
+        ++unit;
+        left = s.blocks;
+        first = true;
+      }
+      if (!__all_sync(0xffffffffu, wait<0>(&sm.full[i], full_turn, 4))) {
+        ok = false;
+        break;
+      }
       ptx::tc_fence_after();
       if (ptx::elect_one()) {
-        const uint64_t b0 = ring + bs.i * 2 * block16;
-        const uint32_t a0 = tmem + as.i * 64;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          ptx::mma_bf16_ta(d, a0 + j * 8, b0 + (j & 4 ? block16 : 0u) + (j & 3) * 2, idesc, (st | j) != 0);
-        ptx::mma_commit(&sm.a_empty[as.i]);
-        ptx::mma_commit(&sm.b_empty[bs.i]);
-        if (st == s.blocks - 1) ptx::mma_commit(&sm.d_full[ds.i]);
+          ptx::mma_bf16_ta(d, tmem + i * 64 + j * 8,
+                           ring + (i * 2 + j / 4) * kBlock16 + (j & 3) * 2, idesc, !first || j != 0);
+        ptx::mma_commit(&sm.empty[i]);
+        if (left == 1) ptx::mma_commit(&sm.d_full[acc.i]);
       }
       __syncwarp();
-      as.next(kASlots);
-      bs.next(slots);
+      if (--left == 0) acc.next(2);
     }
+    full_turn ^= 1u;
   }
   // everything issued has been done before the CTA gives its memory back
   if (ptx::elect_one()) ptx::mma_commit(&sm.drain);
@@ -408,10 +394,10 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
   for (int turn = 0; turn < units; ++turn) {
     const Unit u = unit_at(sm, m_tiles, turn);
     const int buf = turn & 1;
-    uint32_t missing[4] = {0, 0, 0, 0};   // rows without a source: zeros
+    uint32_t missing[kUnitRows / 32] = {};   // rows without a source: zeros
     if (a.rows != nullptr) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kUnitRows / 32; ++j) {
         const int r = 32 * j + (row & 31);
         missing[j] = __ballot_sync(0xffffffffu, r < u.n && source(a, u.r0 + r) < 0);
       }
@@ -424,8 +410,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
       float v[16];
       ptx::tmem_ld16(from + c0, v);
       ptx::tmem_ld_wait();
-      const uint32_t miss = c0 < 64 ? (c0 < 32 ? missing[0] : missing[1])
-                                    : (c0 < 96 ? missing[2] : missing[3]);
+      const uint32_t miss = c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2];
       if (miss >> (c0 & 16) & 0xFFFFu) {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -468,13 +453,9 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < kDeqWarps * kCodeSlots; ++i) ptx::mbar_init(&sm.code_full[0][0] + i, 1);
-    for (int i = 0; i < kASlots; ++i) {
-      ptx::mbar_init(&sm.a_full[i], 4);
-      ptx::mbar_init(&sm.a_empty[i], 1);
-    }
-    for (int i = 0; i < kBSlotsMax; ++i) {
-      ptx::mbar_init(&sm.b_full[i], 1);
-      ptx::mbar_init(&sm.b_empty[i], 1);
+    for (int i = 0; i < kSlots; ++i) {
+      ptx::mbar_init(&sm.full[i], 4 + 1);   // the set's warps and the loading one
+      ptx::mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&sm.d_full[i], 1);
@@ -495,8 +476,8 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   const uint32_t tmem = sm.tmem;
   if (warp < kEpiWarps) epilogue<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, m_tiles, sm, tmem);
-  else if (warp == kMmaWarp) issue(s, m_tiles, sm, tmem);
-  else load_x(a, s, m_tiles, sm);
+  else if (warp < kMmaWarp) load_x(a, s, m_tiles, sm);
+  else issue(s, m_tiles, sm, tmem);
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();

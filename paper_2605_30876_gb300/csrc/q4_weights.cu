@@ -121,6 +121,7 @@ q4_dequantize_kernel(Q4Shape s, int n_experts, const uint8_t* __restrict__ codes
   const int row = b.nt % 2 * 16 + g;
   const uint8_t* from = codes + block * kQ4CodeBytes + row * 16 + 4 * q;
   const uint16_t* sc = scales + (block * kQ4Rows + row) * s.groups;
+  const Q4Bits pair_bits;
   uint32_t word[2][4], bits[2][4];
 #pragma unroll
   for (int r = 0; r < 2; ++r)
@@ -137,8 +138,8 @@ q4_dequantize_kernel(Q4Shape s, int n_experts, const uint8_t* __restrict__ codes
       const Q4Scale v = q4_scale_pair(bits[r][c]);
       if (n < s.N && k < s.K)
         __stcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8,
-               make_uint4(q4_value_pair(word[r][c], 0, v), q4_value_pair(word[r][c], 1, v),
-                          q4_value_pair(word[r][c], 2, v), q4_value_pair(word[r][c], 3, v)));
+               make_uint4(q4_value_pair(word[r][c], 0, v, pair_bits), q4_value_pair(word[r][c], 1, v, pair_bits),
+                          q4_value_pair(word[r][c], 2, v, pair_bits), q4_value_pair(word[r][c], 3, v, pair_bits)));
     }
 }
 
