@@ -1,7 +1,7 @@
 // 4-bit expert matrices: the layout shared by the kernels that write and read it.
 //
-// A matrix is cut into tiles of 32 rows, a tile into blocks of 128 inputs: 2048 bytes of codes, which
-// one bulk copy brings to the warp whose lanes have the rows. In them every row's inputs 0 .. 31
+// A matrix is cut into tiles of 32 rows, a tile into blocks of 128 inputs: 2048 bytes of codes, for
+// a warp whose lanes have the rows. In them every row's inputs 0 .. 31
 // come first, 16 bytes a row, then every row's 32 .. 63, and so on. Word w of the 16 bytes has inputs
 // 8w .. 8w + 7: input 2i of them is the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19,
 // counted around the word's end: a rotation and a mask leave a pair of them in the upper mantissa

@@ -2,8 +2,8 @@
 // y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 96 rows of a group.
 //
 // A persistent CTA per SM, in roles, by stages of 128 inputs:
-//   dequantising warps (four sets of four, a stage each in turn): a lane has a row of W. A bulk copy
-//       brings the codes of a warp's 32 rows; they become bf16 values by one exact FMA per pair
+//   dequantising warps (four sets of four, a stage each in turn): a lane has a row of W. Its codes come
+//       by asynchronous copies (a bulk copy per warp took longer to start); they become bf16 values by one exact FMA per pair
 //       and go to tensor memory: the A operand of the MMAs. Through shared memory they would take
 //       four times the codes' bytes twice, and 8 KB of codes have 368 cycles of an SM's share of
 //       HBM's rate, in which shared memory moves 46 KB.
@@ -11,7 +11,7 @@
 //       into shared memory (B). Between the copies and the tensor pipe's reads is a fence of 200
 //       cycles and more, so several stages are under way. (TMA gathers of four rows need no fence,
 //       but took 80 cycles each: for 64 rows 2500 cycles a stage.)
-//   an issuing warp: tcgen05.mma, M = 128 outputs, N = the unit's rows in sixteens
+//   two issuing warps: tcgen05.mma, M = 128 outputs, N = the unit's rows in sixteens
 //   epilogue warps: sums from tensor memory, SwiGLU, y
 // Few rows: the weights' bytes are the bound, and the instructions per code are close to it: 64 pairs
 // a lane and stage at 2.75, of the 368 that each scheduler issues in that time. Many rows: the
@@ -25,16 +25,18 @@
 namespace dmoe {
 namespace {
 
-constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 4;
+constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 4, kMmaWarps = 2;
 constexpr int kLoadWarp = kEpiWarps + kDeqWarps, kMmaWarp = kLoadWarp + kLoadWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kUnitRows = 96;              // rows of a group per unit, at most
 // The ring of stages: A in tensor memory, 64 columns a slot, and B in shared memory. A slot is a set's
-// and a loading warp's, and one pair of barriers serves both operands: the issuing thread's waits
-// and commits take as long as the MMAs of few rows (100 to 150 cycles each).
+// and a loading warp's, and one pair of barriers serves both operands: an issuing warp's waits
+// and commits take as long as the MMAs of few rows (100 to 150 cycles each). There are two issuing
+// warps for the same reason, with the even and the odd stages of a unit and sums of their own,
+// which the epilogue adds (even plus odd whichever warp has which: the same sums at any place).
 constexpr int kSlots = 4;
 constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of them in use
-constexpr int kAcc0 = kSlots * 64;         // first column of the sums: two buffers of 128
+constexpr int kAcc0 = kSlots * 64;         // first column of the sums
 static_assert(kSets == kSlots && kLoadWarps == kSlots, "a set and a loading warp per slot");
 constexpr uint64_t kWaitNs = 1000000000ull;
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
@@ -44,6 +46,7 @@ __device__ DevErrRecord q4_fault;          // of every call on the device
 // The groups that have rows and an expert, in order, and their first units.
 struct Groups {
   int n, units;
+  int widest;   // rows of the widest unit
   int e[kMaxExperts], r0[kMaxExperts], r1[kMaxExperts], first[kMaxExperts];
 };
 
@@ -63,9 +66,8 @@ struct Smem {
   float swap[2][2][64][9];                   // ups and gates between epilogue warps
   Unit sched[kSched];                        // the CTA's units, in its order
   Groups groups;
-  uint64_t code_full[kDeqWarps][kCodeSlots];
   uint64_t full[kSlots], empty[kSlots];      // of the ring's stages
-  uint64_t d_full[2], d_empty[2], drain;
+  uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
   uint32_t tmem;
   int wcount[kThreads / 32];
 };
@@ -92,6 +94,7 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
     const int v = __shfl_up_sync(0xffffffffu, before, o);
     if (lane >= o) before += v;
   }
+  if (u == 0) s.widest = 0;
   if (lane == 31) {
     sm.wcount[warp] = before;
     if (warp < kMaxExperts / 32) s.first[warp] = __popc(m);   // (for the moment)
@@ -112,6 +115,7 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
     s.r0[at] = r0;
     s.r1[at] = r1;
     s.first[at] = before - units;
+    atomicMax(&s.widest, (r1 - r0 + tiles - 1) / tiles);
   }
   if (u == 0) {
     s.n = n;
@@ -166,65 +170,76 @@ struct Slot {
   }
 };
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // ------------------------------------------------------------------ dequantising
 template <bool kGated>
 __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
                                            uint32_t tmem) {
   const int warp = threadIdx.x / 32 - kEpiWarps, set = warp >> 2, lane = threadIdx.x & 31;
   const int units = units_of_cta(sm.groups), scale_block = s.scale_block();
-  CodeSlot* const ring = sm.code[warp];
-  uint64_t* const full = sm.code_full[warp];
+  const int pieces = scale_block / 16;   // of the scales: a lane copies one, the first lanes
+  const uint32_t ring = ptx::smem_addr(&sm.code[warp][0]) + lane * 16;
+  constexpr uint32_t kSlot = sizeof(CodeSlot), kScales = offsetof(CodeSlot, scales);
 
   // The copies run ahead of the values by kCodeSlots - 1 blocks of this warp, over the ends of units.
   // base: stages of the units before; the set takes the stages whose number is set mod kSets.
-  int unit = 0, base = 0, st = set, copied = 0;
+  int unit = 0, base = 0, st = set;
   const uint8_t *codes = nullptr, *scales = nullptr;
   bool there = false;   // the warp's rows of this unit are in the matrix
   auto enter = [&]() {
-    if (unit >= units) return;
     const Unit u = unit_at(sm, m_tiles, unit);
     const int m = kGated ? (warp & 3) >> 1 : 0;
     const int tile = kGated ? u.mt * 2 + (warp & 1) : u.mt * 4 + (warp & 3);
     there = tile < s.tiles;
     const size_t block = ((size_t)u.e * s.tiles + tile) * s.blocks + st;
-    codes = static_cast<const uint8_t*>(a.codes[m]) + block * kQ4CodeBytes;
-    scales = static_cast<const uint8_t*>(a.scales[m]) + block * scale_block;
+    codes = static_cast<const uint8_t*>(a.codes[m]) + block * kQ4CodeBytes + lane * 16;
+    scales = static_cast<const uint8_t*>(a.scales[m]) + block * scale_block + lane * 16;
   };
-  Slot to;
-  auto copy = [&]() {
+  uint32_t to = ring;
+  auto copy = [&]() {   // the next block's copies, if there is one; always one group of copies
     while (st >= s.blocks && unit < units) {
       base += s.blocks;
       ++unit;
       st = (set - base) & (kSets - 1);
-      if (st < s.blocks) enter();
+      if (st < s.blocks && unit < units) enter();
     }
-    if (unit >= units) return;
-    if (lane == 0) {
-      ptx::mbar_arrive_expect_tx(&full[to.i], there ? kQ4CodeBytes + scale_block : 0);
-      if (there) {
-        ptx::bulk_load(ring[to.i].codes, codes, kQ4CodeBytes, &full[to.i]);
-        ptx::bulk_load(ring[to.i].scales, scales, scale_block, &full[to.i]);
-      }
+    if (unit < units && there) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) copy16(to + h * kQ4Rows * 16, codes + h * kQ4Rows * 16, 16);
+      if (lane < pieces) copy16(to + kScales, scales, 16);
     }
+    copies_commit();
     codes += kSets * kQ4CodeBytes;
     scales += kSets * scale_block;
     st += kSets;
-    ++copied;
-    to.next(kCodeSlots);
+    to = to == ring + (kCodeSlots - 1) * kSlot ? ring : to + kSlot;
   };
-  if (st < s.blocks) enter();
+  if (st < s.blocks && units > 0) enter();
+#pragma unroll 1
   for (int i = 0; i < kCodeSlots - 1; ++i) copy();
 
   const uint32_t at = tmem + set * 64 + ((uint32_t)(warp & 3) << 21);   // (the set's slot)
   const Q4Bits bits;
-  Slot from;
   uint32_t turn = 1;
-  int done = 0;
-  for (;; ++done) {
+  int from = 0;
+  // this set's stages: of units * blocks, those whose number is set mod kSets
+  const int64_t all = (int64_t)units * s.blocks;
+  const int visits = all > set ? (int)((all - set - 1) / kSets) + 1 : 0;
+#pragma unroll 1
+  for (int i = 0; i < visits; ++i) {
     copy();
-    if (done == copied) break;   // (copies are ahead until there are none)
-    if (!__all_sync(0xffffffffu, wait<0>(&full[from.i], from.turn, 8))) break;
-    const CodeSlot& slot = ring[from.i];
+    copies_wait<kCodeSlots - 1>();
+    __syncwarp();   // (scales are copied by other lanes)
+    const CodeSlot& slot = sm.code[warp][from];
     // the scales of the stage's four 32 inputs
     uint32_t s01, s23;
     if (s.groups == 4) {
@@ -248,7 +263,7 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
       const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       uint32_t v[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = q4_value_pair(w[i / 4], i & 3, i < 16 ? s0 : s1, bits);
+      for (int j = 0; j < 32; ++j) v[j] = q4_value_pair(w[j / 4], j & 3, j < 16 ? s0 : s1, bits);
       ptx::tmem_st32(at + h * 16, v);
     }
     ptx::tmem_st_wait();
@@ -256,24 +271,12 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
     __syncwarp();   // (the slot has been read, too)
     if (lane == 0) ptx::mbar_arrive(&sm.full[set]);
     turn ^= 1u;
-    from.next(kCodeSlots);
+    from = from == kCodeSlots - 1 ? 0 : from + 1;
   }
-  // no copy is left in flight behind a wait that ran out
-  for (; done < copied; ++done, from.next(kCodeSlots))
-    if (!ptx::mbar_wait_paused(&full[from.i], from.turn, kWaitNs, 0)) break;
+  copies_wait<0>();
 }
 
 // ------------------------------------------------------------------ loading x
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // The source row of sorted row r, or -1.
 __device__ __forceinline__ int source(const Q4Args& a, int r) {
   if (a.rows == nullptr) return r;
@@ -325,38 +328,50 @@ __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_
 }
 
 // ------------------------------------------------------------------ issuing the MMAs
-// The whole warp goes through the stages and elects the lane that issues: with one lane in a branch of
+// The sums' place: with at most 64 rows two buffers of both warps' sums, else one.
+__device__ __forceinline__ int acc_buffers(int widest) { return widest <= 64 ? 2 : 1; }
+__device__ __forceinline__ uint32_t acc_column(int buffers, int buffer, int warp) {
+  return kAcc0 + (buffers == 2 ? (buffer * 2 + warp) * 64 : warp * 128);
+}
+
+// The whole warp goes through its stages and elects the lane that issues: with one lane in a branch of
 // its own the operands were not uniform, and eight MMAs took 600 cycles to issue instead of 150. One
-// warp's instructions take five cycles and more each here, and this warp's are the ring's
+// warp's instructions take five cycles and more each here, and these warps' are the ring's
 // pace: the slots are unrolled, so that addresses are constants.
-__device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem) {
-  const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b));
+__device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem, int warp) {
+  const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b[warp]));
   constexpr uint32_t kBlock16 = kUnitRows * 128 / 16;   // (a descriptor's address is in units of 16 bytes)
-  const int units = units_of_cta(sm.groups);
-  int unit = 0, left = 0;   // stages left of the unit
+  const int units = units_of_cta(sm.groups), buffers = acc_buffers(sm.groups.widest);
+  const uint32_t a0 = tmem + warp * 64;
+  uint64_t* const full = sm.full + warp;
+  uint64_t* const empty = sm.empty + warp;
+  int unit = 0, left = 0;   // this warp's stages left of the unit
   uint32_t d = 0, idesc = 0, full_turn = 0;
+  bool odd = false, ok = true;   // odd: the units before this one have an odd number of stages
   Slot acc;
-  bool ok = true;
+  uint64_t* d_full = nullptr;
   while (ok) {
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
+    for (int i = 0; i < kSlots; i += kMmaWarps) {
       bool first = false;
-      if (left == 0) {
-        if (unit == units) {
+      while (left == 0) {   // (a unit of one stage may have none of this warp's)
+        if (unit == units || !__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
           ok = false;
           break;
         }
         idesc = ptx::idesc_bf16(128, (unit_at(sm, m_tiles, unit).n + 15) / 16 * 16);
-        d = tmem + kAcc0 + acc.i * 128;
-        if (!__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
-          ok = false;
-          break;
-        }
-        ++unit;
-        left = s.blocks;
+        d = tmem + acc_column(buffers, acc.i, warp);
+        d_full = &sm.d_full[acc.i];
+        left = (s.blocks + ((warp != 0) == odd ? 1 : 0)) / 2;
+        odd ^= s.blocks & 1;
         first = true;
+        ++unit;
+        acc.next(buffers);
+        if (left == 0 && ptx::elect_one()) ptx::mbar_arrive(d_full);
+        __syncwarp();
       }
-      if (!__all_sync(0xffffffffu, wait<0>(&sm.full[i], full_turn, 4))) {
+      if (!ok) break;
+      if (!__all_sync(0xffffffffu, wait<0>(full + i, full_turn, 4))) {
         ok = false;
         break;
       }
@@ -364,19 +379,19 @@ __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, u
       if (ptx::elect_one()) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          ptx::mma_bf16_ta(d, tmem + i * 64 + j * 8,
+          ptx::mma_bf16_ta(d, a0 + i * 64 + j * 8,
                            ring + (i * 2 + j / 4) * kBlock16 + (j & 3) * 2, idesc, !first || j != 0);
-        ptx::mma_commit(&sm.empty[i]);
-        if (left == 1) ptx::mma_commit(&sm.d_full[acc.i]);
+        ptx::mma_commit(empty + i);
+        if (left == 1) ptx::mma_commit(d_full);
       }
       __syncwarp();
-      if (--left == 0) acc.next(2);
+      --left;
     }
     full_turn ^= 1u;
   }
   // everything issued has been done before the CTA gives its memory back
-  if (ptx::elect_one()) ptx::mma_commit(&sm.drain);
-  wait<0>(&sm.drain, 0, 6);
+  if (ptx::elect_one()) ptx::mma_commit(&sm.drain[warp]);
+  wait<0>(&sm.drain[warp], 0, 6);
 }
 
 // ------------------------------------------------------------------ epilogue
@@ -390,10 +405,12 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
                                          uint32_t tmem) {
   const int warp = threadIdx.x >> 5, row = threadIdx.x;   // lane of tensor memory
   const int units = units_of_cta(sm.groups);
+  const int buffers = acc_buffers(sm.groups.widest);
   int swap = 0;
-  for (int turn = 0; turn < units; ++turn) {
+  Slot acc;
+  bool odd = false;   // the units before have an odd number of stages
+  for (int turn = 0; turn < units; ++turn, acc.next(buffers), odd ^= s.blocks & 1) {
     const Unit u = unit_at(sm, m_tiles, turn);
-    const int buf = turn & 1;
     uint32_t missing[kUnitRows / 32] = {};   // rows without a source: zeros
     if (a.rows != nullptr) {
 #pragma unroll
@@ -402,14 +419,23 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         missing[j] = __ballot_sync(0xffffffffu, r < u.n && source(a, u.r0 + r) < 0);
       }
     }
-    if (!ptx::epi_all(wait<100>(&sm.d_full[buf], (turn >> 1) & 1, 7))) break;
+    if (!ptx::epi_all(wait<100>(&sm.d_full[acc.i], acc.turn, 7))) break;
     ptx::tc_fence_after();
-    const uint32_t from = tmem + kAcc0 + buf * 128 + ((uint32_t)warp << 21);
+    const uint32_t from = tmem + acc_column(buffers, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
+    const uint32_t other = acc_column(buffers, 0, 1) - acc_column(buffers, 0, 0);
     const int n = kGated ? u.mt * 64 + (row & 63) : u.mt * 128 + row;
     for (int c0 = 0; c0 < u.n; c0 += 16) {
       float v[16];
       ptx::tmem_ld16(from + c0, v);
-      ptx::tmem_ld_wait();
+      if (s.blocks > 1) {
+        float w[16];
+        ptx::tmem_ld16(from + other + c0, w);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] += w[j];
+      } else {
+        ptx::tmem_ld_wait();
+      }
       const uint32_t miss = c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2];
       if (miss >> (c0 & 16) & 0xFFFFu) {
 #pragma unroll
@@ -424,10 +450,10 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         ptx::named_bar_sync(1, 32 * kEpiWarps);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float other = sm.swap[swap][up ^ 1][row & 63][j], mine = up ? v[8 + j] : v[j];
+          const float theirs = sm.swap[swap][up ^ 1][row & 63][j], mine = up ? v[8 + j] : v[j];
           if (c0 + first + j < u.n && n < s.N)
             store_y(a, u.r0 + c0 + first + j, n,
-                    up ? silu_divide(other) * mine : silu_divide(mine) * other);
+                    up ? silu_divide(theirs) * mine : silu_divide(mine) * theirs);
         }
         swap ^= 1;
       } else {
@@ -437,7 +463,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
       }
     }
     ptx::tc_fence_before();
-    ptx::mbar_arrive(&sm.d_empty[buf]);
+    ptx::mbar_arrive(&sm.d_empty[acc.i]);
   }
 }
 
@@ -452,16 +478,15 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
     ptx::tmem_relinquish();
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kDeqWarps * kCodeSlots; ++i) ptx::mbar_init(&sm.code_full[0][0] + i, 1);
     for (int i = 0; i < kSlots; ++i) {
       ptx::mbar_init(&sm.full[i], 4 + 1);   // the set's warps and the loading one
       ptx::mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(&sm.d_full[i], 1);
+      ptx::mbar_init(&sm.d_full[i], kMmaWarps);
       ptx::mbar_init(&sm.d_empty[i], 32 * kEpiWarps);
     }
-    ptx::mbar_init(&sm.drain, 1);
+    for (int i = 0; i < kMmaWarps; ++i) ptx::mbar_init(&sm.drain[i], 1);
     ptx::fence_mbarrier_init();
   }
   ptx::tc_fence_before();
@@ -477,7 +502,7 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   if (warp < kEpiWarps) epilogue<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kMmaWarp) load_x(a, s, m_tiles, sm);
-  else issue(s, m_tiles, sm, tmem);
+  else issue(s, m_tiles, sm, tmem, warp - kMmaWarp);
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();
