@@ -25,19 +25,19 @@
 namespace dmoe {
 namespace {
 
-constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 4, kMmaWarps = 2;
+constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 8, kMmaWarps = 2;
 constexpr int kLoadWarp = kEpiWarps + kDeqWarps, kMmaWarp = kLoadWarp + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kUnitRows = 96;              // rows of a group per unit, at most
 // The ring of stages: A in tensor memory, 64 columns a slot, and B in shared memory. A slot is a set's
-// and a loading warp's, and one pair of barriers serves both operands: an issuing warp's waits
+// and two loading warps', and one pair of barriers serves both operands: an issuing warp's waits
 // and commits take as long as the MMAs of few rows (100 to 150 cycles each). There are two issuing
 // warps for the same reason, with the even and the odd stages of a unit and sums of their own,
 // which the epilogue adds (even plus odd whichever warp has which: the same sums at any place).
 constexpr int kSlots = 4;
 constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of them in use
 constexpr int kAcc0 = kSlots * 64;         // first column of the sums
-static_assert(kSets == kSlots && kLoadWarps == kSlots, "a set and a loading warp per slot");
+static_assert(kSets == kSlots && kLoadWarps == 2 * kSlots, "a set and two loading warps per slot");
 constexpr uint64_t kWaitNs = 1000000000ull;
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
 
@@ -180,11 +180,15 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// The warp's number, as a value that the compiler knows to be the warp's: what depends on it (cursors,
+// turns, loops) then takes the uniform datapath, not the pipe that the codes keep busy.
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0); }
+
 // ------------------------------------------------------------------ dequantising
 template <bool kGated>
 __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
                                            uint32_t tmem) {
-  const int warp = threadIdx.x / 32 - kEpiWarps, set = warp >> 2, lane = threadIdx.x & 31;
+  const int warp = warp_number() - kEpiWarps, set = warp >> 2, lane = threadIdx.x & 31;
   const int units = units_of_cta(sm.groups), scale_block = s.scale_block();
   const int pieces = scale_block / 16;   // of the scales: a lane copies one, the first lanes
   const uint32_t ring = ptx::smem_addr(&sm.code[warp][0]) + lane * 16;
@@ -255,7 +259,7 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
     }
     if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[set], turn, 1))) break;
     ptx::tc_fence_after();
-#pragma unroll 1
+#pragma unroll
     for (int h = 0; h < 4; h += 2) {
       const uint32_t pair = h == 0 ? s01 : s23;
       const Q4Scale s0 = q4_scale_pair(pair), s1 = q4_scale_pair(pair >> 16);
@@ -285,36 +289,39 @@ __device__ __forceinline__ int source(const Q4Args& a, int r) {
 }
 
 __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm) {
-  const int warp = threadIdx.x / 32 - kLoadWarp, lane = threadIdx.x & 31;
-  const int chunk = lane & 7, sub = lane >> 3;   // 16 bytes of a row's 128, row of four
+  const int warp = warp_number() - kLoadWarp, slot = warp % kSlots, lane = threadIdx.x & 31;
+  // 16 bytes of a row's 128, row of eight (the slot's warps have four of them each)
+  const int chunk = lane & 7, sub = (lane >> 3) + warp / kSlots * 4;
   const int units = units_of_cta(sm.groups);
   // (row r's 16-byte piece c is at r * 128 + (c ^ r % 8) * 16)
-  const uint32_t dst = ptx::smem_addr(sm.b[warp][0]) + sub * 128;
+  const uint32_t dst = ptx::smem_addr(sm.b[slot][0]) + sub * 128 + ((chunk ^ sub) << 4);
   uint32_t turn = 1;
-  int st = warp;   // this warp's next stage, counted from the unit's start
+  int st = slot;   // this warp's next stage, counted from the unit's start
   for (int unit = 0; unit < units; ++unit, st -= s.blocks) {
     if (st >= s.blocks) continue;
     const Unit u = unit_at(sm, m_tiles, unit);
-    int src[kUnitRows / 32];                     // of rows lane, lane + 32, ...
+    // this lane's rows: sub, sub + 8, ... (kept as the sources of rows lane, lane + 32, ...)
+    int src[kUnitRows / 32];
 #pragma unroll
     for (int j = 0; j < kUnitRows / 32; ++j)
       src[j] = 32 * j < u.n ? max(source(a, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
     for (; st < s.blocks; st += kSlots) {
       const int k = st * 128 + chunk * 8;
-      const __nv_bfloat16* x = a.x + k;
       const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
-      if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[warp], turn, 2))) return;
+      // (where there is nothing to read, any address of x)
+      const __nv_bfloat16 *x0 = a.x + (in0 ? k : 0), *x1 = a.x + (in1 ? k + 64 : 0);
+      if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[slot], turn, 2))) return;
       turn ^= 1u;
 #pragma unroll
       for (int j = 0; j < kUnitRows / 32; ++j) {
-        const int n = min(u.n - 32 * j, 32);
-#pragma unroll 1
-        for (int i = 0; i < n; i += 4) {
-          const int64_t at = __shfl_sync(0xffffffffu, src[j], i + sub) * a.ldx;
-          if (i + sub < n) {
-            const uint32_t to = dst + (32 * j + i) * 128 + ((chunk ^ ((i + sub) & 7)) << 4);
-            copy16(to, in0 ? x + at : a.x, in0);
-            copy16(to + kUnitRows * 128, in1 ? x + at + 64 : a.x, in1);
+        if (32 * j >= u.n) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * i + sub;
+          const int64_t at = __shfl_sync(0xffffffffu, src[j], r) * a.ldx;
+          if (32 * j + r < u.n) {
+            copy16(dst + (32 * j + 8 * i) * 128, x0 + at, in0);
+            copy16(dst + (32 * j + 8 * i) * 128 + kUnitRows * 128, x1 + at, in1);
           }
         }
       }
@@ -322,26 +329,28 @@ __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_
       copies_wait<0>();
       ptx::fence_proxy_async_smem();   // (the tensor pipe reads them)
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&sm.full[warp]);
+      if (lane == 0) ptx::mbar_arrive(&sm.full[slot]);
     }
   }
 }
 
 // ------------------------------------------------------------------ issuing the MMAs
-// The sums' place: with at most 64 rows two buffers of both warps' sums, else one.
-__device__ __forceinline__ int acc_buffers(int widest) { return widest <= 64 ? 2 : 1; }
-__device__ __forceinline__ uint32_t acc_column(int buffers, int buffer, int warp) {
-  return kAcc0 + (buffers == 2 ? (buffer * 2 + warp) * 64 : warp * 128);
+// Issuing warps: with more than 64 rows the MMAs take longer than their issue, and one warp does all (two
+// buffers of both warps' sums would not fit).
+__device__ __forceinline__ int mma_warps(int widest) { return widest <= 64 ? 2 : 1; }
+__device__ __forceinline__ uint32_t acc_column(int warps, int buffer, int warp) {
+  return kAcc0 + buffer * 128 + (warps == 2 ? warp * 64 : 0);
 }
 
 // The whole warp goes through its stages and elects the lane that issues: with one lane in a branch of
 // its own the operands were not uniform, and eight MMAs took 600 cycles to issue instead of 150. One
 // warp's instructions take five cycles and more each here, and these warps' are the ring's
 // pace: the slots are unrolled, so that addresses are constants.
+template <int kWarps>
 __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem, int warp) {
   const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b[warp]));
   constexpr uint32_t kBlock16 = kUnitRows * 128 / 16;   // (a descriptor's address is in units of 16 bytes)
-  const int units = units_of_cta(sm.groups), buffers = acc_buffers(sm.groups.widest);
+  const int units = units_of_cta(sm.groups);
   const uint32_t a0 = tmem + warp * 64;
   uint64_t* const full = sm.full + warp;
   uint64_t* const empty = sm.empty + warp;
@@ -352,7 +361,7 @@ __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, u
   uint64_t* d_full = nullptr;
   while (ok) {
 #pragma unroll
-    for (int i = 0; i < kSlots; i += kMmaWarps) {
+    for (int i = 0; i < kSlots; i += kWarps) {
       bool first = false;
       while (left == 0) {   // (a unit of one stage may have none of this warp's)
         if (unit == units || !__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
@@ -360,13 +369,13 @@ __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, u
           break;
         }
         idesc = ptx::idesc_bf16(128, (unit_at(sm, m_tiles, unit).n + 15) / 16 * 16);
-        d = tmem + acc_column(buffers, acc.i, warp);
+        d = tmem + acc_column(kWarps, acc.i, warp);
         d_full = &sm.d_full[acc.i];
-        left = (s.blocks + ((warp != 0) == odd ? 1 : 0)) / 2;
+        left = kWarps == 1 ? s.blocks : (s.blocks + ((warp != 0) == odd ? 1 : 0)) / 2;
         odd ^= s.blocks & 1;
         first = true;
         ++unit;
-        acc.next(buffers);
+        acc.next(2);
         if (left == 0 && ptx::elect_one()) ptx::mbar_arrive(d_full);
         __syncwarp();
       }
@@ -405,11 +414,11 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
                                          uint32_t tmem) {
   const int warp = threadIdx.x >> 5, row = threadIdx.x;   // lane of tensor memory
   const int units = units_of_cta(sm.groups);
-  const int buffers = acc_buffers(sm.groups.widest);
+  const int warps = mma_warps(sm.groups.widest);
   int swap = 0;
   Slot acc;
   bool odd = false;   // the units before have an odd number of stages
-  for (int turn = 0; turn < units; ++turn, acc.next(buffers), odd ^= s.blocks & 1) {
+  for (int turn = 0; turn < units; ++turn, acc.next(2), odd ^= s.blocks & 1) {
     const Unit u = unit_at(sm, m_tiles, turn);
     uint32_t missing[kUnitRows / 32] = {};   // rows without a source: zeros
     if (a.rows != nullptr) {
@@ -421,15 +430,15 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
     }
     if (!ptx::epi_all(wait<100>(&sm.d_full[acc.i], acc.turn, 7))) break;
     ptx::tc_fence_after();
-    const uint32_t from = tmem + acc_column(buffers, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
-    const uint32_t other = acc_column(buffers, 0, 1) - acc_column(buffers, 0, 0);
+    const uint32_t from =
+        tmem + acc_column(warps, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
     const int n = kGated ? u.mt * 64 + (row & 63) : u.mt * 128 + row;
     for (int c0 = 0; c0 < u.n; c0 += 16) {
       float v[16];
       ptx::tmem_ld16(from + c0, v);
-      if (s.blocks > 1) {
+      if (warps == 2 && s.blocks > 1) {
         float w[16];
-        ptx::tmem_ld16(from + other + c0, w);
+        ptx::tmem_ld16(from + 64 + c0, w);
         ptx::tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 16; ++j) v[j] += w[j];
@@ -472,18 +481,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   extern __shared__ __align__(1024) uint8_t raw[];
   Smem& sm = *reinterpret_cast<Smem*>(raw);
-  const int warp = threadIdx.x >> 5;
+  const int warp = warp_number();
   if (warp == kMmaWarp) {
     ptx::tmem_alloc(&sm.tmem, 512);
     ptx::tmem_relinquish();
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
-      ptx::mbar_init(&sm.full[i], 4 + 1);   // the set's warps and the loading one
+      ptx::mbar_init(&sm.full[i], 4 + 2);   // the set's warps and the loading ones
       ptx::mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(&sm.d_full[i], kMmaWarps);
       ptx::mbar_init(&sm.d_empty[i], 32 * kEpiWarps);
     }
     for (int i = 0; i < kMmaWarps; ++i) ptx::mbar_init(&sm.drain[i], 1);
@@ -496,13 +504,19 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   find_groups(a, m_tiles, sm);   // (synchronises the CTA)
   if ((int)threadIdx.x < min(kSched, units_of_cta(sm.groups)))
     sm.sched[threadIdx.x] = find_unit(sm.groups, m_tiles, blockIdx.x + threadIdx.x * gridDim.x);
+  const int issuers = mma_warps(sm.groups.widest);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) ptx::mbar_init(&sm.d_full[i], issuers);
+    ptx::fence_mbarrier_init();
+  }
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = sm.tmem;
   if (warp < kEpiWarps) epilogue<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, m_tiles, sm, tmem);
   else if (warp < kMmaWarp) load_x(a, s, m_tiles, sm);
-  else issue(s, m_tiles, sm, tmem, warp - kMmaWarp);
+  else if (issuers == 2) issue<2>(s, m_tiles, sm, tmem, warp - kMmaWarp);
+  else if (warp == kMmaWarp) issue<1>(s, m_tiles, sm, tmem, 0);
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();
