@@ -39,6 +39,7 @@ constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of t
 constexpr int kAcc0 = kSlots * 64;         // first column of the sums
 static_assert(kSets == kSlots && kLoadWarps == 2 * kSlots, "a set and two loading warps per slot");
 constexpr uint64_t kWaitNs = 1000000000ull;
+constexpr int kSources = 1024;             // sorted rows whose sources are looked up once, together
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
 
 __device__ DevErrRecord q4_fault;          // of every call on the device
@@ -55,6 +56,12 @@ struct __align__(16) Unit {
   int r0, n;      // rows
 };
 
+// The source row of sorted row r, or -1: with its index divided, and from the table.
+__device__ __forceinline__ int find_source(const Q4Args& a, int r) {
+  const int p = __ldg(a.rows + r), t = p >= 0 ? p / a.k : -1;
+  return t < a.T_x ? t : -1;
+}
+
 struct CodeSlot {
   uint4 codes[4][kQ4Rows];       // [32 inputs][row]
   uint16_t scales[kQ4Rows * 4];  // [row][group]
@@ -63,14 +70,19 @@ struct CodeSlot {
 struct Smem {
   uint8_t b[kSlots][2][kUnitRows * 128];     // [slot][64 inputs], 1024-byte aligned
   CodeSlot code[kDeqWarps][kCodeSlots];
-  float swap[2][2][64][9];                   // ups and gates between epilogue warps
+  float swap[2][64][17];                     // gates and ups of the epilogue warps
   Unit sched[kSched];                        // the CTA's units, in its order
   Groups groups;
   uint64_t full[kSlots], empty[kSlots];      // of the ring's stages
   uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
   uint32_t tmem;
   int wcount[kThreads / 32];
+  int source[kSources];                      // row of x of the first sorted rows, or -1
 };
+
+__device__ __forceinline__ int source(const Q4Args& a, const Smem& sm, int r) {
+  return a.rows == nullptr ? r : r < kSources ? sm.source[r] : find_source(a, r);
+}
 
 __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& sm) {
   Groups& s = sm.groups;
@@ -80,11 +92,15 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
   if (u < a.n_groups) {
     r1 = R;
     if (a.offsets != nullptr) {
-      r0 = max(__ldg(a.offsets + u), 0);
-      r1 = min(__ldg(a.offsets + u + 1), R);
+      r0 = __ldg(a.offsets + u);
+      r1 = __ldg(a.offsets + u + 1);
     }
     if (a.expert_ids != nullptr) e = __ldg(a.expert_ids + u);
   }
+  if (a.rows != nullptr)   // (while those loads are under way)
+    for (int r = u; r < min(R, kSources); r += kThreads) sm.source[r] = find_source(a, r);
+  r0 = max(r0, 0);
+  r1 = min(r1, R);
   const bool live = r0 < r1 && e >= 0 && e < a.n_experts;
   const int tiles = live ? (r1 - r0 + kUnitRows - 1) / kUnitRows : 0;
   const uint32_t m = __ballot_sync(0xffffffffu, live);
@@ -281,13 +297,6 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
 }
 
 // ------------------------------------------------------------------ loading x
-// The source row of sorted row r, or -1.
-__device__ __forceinline__ int source(const Q4Args& a, int r) {
-  if (a.rows == nullptr) return r;
-  const int p = __ldg(a.rows + r), t = p >= 0 ? p / a.k : -1;
-  return t < a.T_x ? t : -1;
-}
-
 __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm) {
   const int warp = warp_number() - kLoadWarp, slot = warp % kSlots, lane = threadIdx.x & 31;
   // 16 bytes of a row's 128, row of eight (the slot's warps have four of them each)
@@ -304,7 +313,7 @@ __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_
     int src[kUnitRows / 32];
 #pragma unroll
     for (int j = 0; j < kUnitRows / 32; ++j)
-      src[j] = 32 * j < u.n ? max(source(a, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
+      src[j] = 32 * j < u.n ? max(source(a, sm, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
     for (; st < s.blocks; st += kSlots) {
       const int k = st * 128 + chunk * 8;
       const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
@@ -404,9 +413,9 @@ __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, u
 }
 
 // ------------------------------------------------------------------ epilogue
-__device__ __forceinline__ void store_y(const Q4Args& a, int64_t r, int n, float v) {
-  if (a.y_fp32) static_cast<float*>(a.y)[r * a.ldy + n] = v;
-  else static_cast<__nv_bfloat16*>(a.y)[r * a.ldy + n] = __float2bfloat16_rn(v);
+__device__ __forceinline__ void store_y(uint8_t* y, bool fp32, float v) {
+  if (fp32) *reinterpret_cast<float*>(y) = v;
+  else *reinterpret_cast<__nv_bfloat16*>(y) = __float2bfloat16_rn(v);
 }
 
 template <bool kGated>
@@ -415,7 +424,8 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
   const int warp = threadIdx.x >> 5, row = threadIdx.x;   // lane of tensor memory
   const int units = units_of_cta(sm.groups);
   const int warps = mma_warps(sm.groups.widest);
-  int swap = 0;
+  const int size = a.y_fp32 ? 4 : 2;
+  const int64_t step = a.ldy * size;
   Slot acc;
   bool odd = false;   // the units before have an odd number of stages
   for (int turn = 0; turn < units; ++turn, acc.next(2), odd ^= s.blocks & 1) {
@@ -425,7 +435,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
 #pragma unroll
       for (int j = 0; j < kUnitRows / 32; ++j) {
         const int r = 32 * j + (row & 31);
-        missing[j] = __ballot_sync(0xffffffffu, r < u.n && source(a, u.r0 + r) < 0);
+        missing[j] = __ballot_sync(0xffffffffu, r < u.n && source(a, sm, u.r0 + r) < 0);
       }
     }
     if (!ptx::epi_all(wait<100>(&sm.d_full[acc.i], acc.turn, 7))) break;
@@ -433,7 +443,9 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
     const uint32_t from =
         tmem + acc_column(warps, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
     const int n = kGated ? u.mt * 64 + (row & 63) : u.mt * 128 + row;
+    const bool there = n < s.N;
     for (int c0 = 0; c0 < u.n; c0 += 16) {
+      const int count = min(16, u.n - c0);   // (few rows: what is done is cut to fours of them)
       float v[16];
       ptx::tmem_ld16(from + c0, v);
       if (warps == 2 && s.blocks > 1) {
@@ -445,30 +457,29 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
       } else {
         ptx::tmem_ld_wait();
       }
-      const uint32_t miss = c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2];
-      if (miss >> (c0 & 16) & 0xFFFFu) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (miss >> ((c0 & 16) + j) & 1u) v[j] = 0.f;
-      }
+      const uint32_t zero = (c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2]) >> (c0 & 16);
+      uint8_t* y = static_cast<uint8_t*>(a.y) + ((int64_t)(u.r0 + c0) * a.ldy + n) * size;
       if (kGated) {
-        // lanes 0 .. 63 are gates, 64 .. 127 ups: the gates' lanes do eight rows, the ups' the others
-        const int up = row >> 6, first = up * 8;
+        // lanes 0 .. 63 are gates, 64 .. 127 ups; then the first do the even rows, the others the odd
+        const int up = row >> 6;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sm.swap[swap][up][row & 63][j] = up ? v[j] : v[8 + j];
-        ptx::named_bar_sync(1, 32 * kEpiWarps);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float theirs = sm.swap[swap][up ^ 1][row & 63][j], mine = up ? v[8 + j] : v[j];
-          if (c0 + first + j < u.n && n < s.N)
-            store_y(a, u.r0 + c0 + first + j, n,
-                    up ? silu_divide(theirs) * mine : silu_divide(mine) * theirs);
+        for (int j = 0; j < 16; ++j) {
+          if ((j & 3) == 0 && j >= count) break;
+          sm.swap[up][row & 63][j] = v[j];
         }
-        swap ^= 1;
+        ptx::named_bar_sync(1, 32 * kEpiWarps);
+        y += up * step;
+        for (int j = up; j < count; j += 2, y += 2 * step) {
+          const float o = silu_divide(sm.swap[0][row & 63][j]) * sm.swap[1][row & 63][j];
+          if (there) store_y(y, a.y_fp32, zero >> j & 1u ? 0.f : o);
+        }
+        ptx::named_bar_sync(1, 32 * kEpiWarps);
       } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (c0 + j < u.n && n < s.N) store_y(a, u.r0 + c0 + j, n, v[j]);
+        for (int j = 0; j < 16; ++j, y += step) {
+          if ((j & 3) == 0 && j >= count) break;
+          if (j < count && there) store_y(y, a.y_fp32, zero >> j & 1u ? 0.f : v[j]);
+        }
       }
     }
     ptx::tc_fence_before();
