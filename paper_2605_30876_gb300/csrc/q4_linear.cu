@@ -469,9 +469,18 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         }
         ptx::named_bar_sync(1, 32 * kEpiWarps);
         y += up * step;
-        for (int j = up; j < count; j += 2, y += 2 * step) {
-          const float o = silu_divide(sm.swap[0][row & 63][j]) * sm.swap[1][row & 63][j];
-          if (there) store_y(y, a.y_fp32, zero >> j & 1u ? 0.f : o);
+#pragma unroll 1
+        for (int j0 = up; j0 < count; j0 += 8) {   // four rows of this half at a time
+          float g[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) g[j] = j0 + 2 * j < count ? sm.swap[0][row & 63][j0 + 2 * j] : 0.f;
+          silu_all(g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j, y += 2 * step) {
+            const int r = j0 + 2 * j;
+            if (r < count && there)
+              store_y(y, a.y_fp32, zero >> r & 1u ? 0.f : g[j] * sm.swap[1][row & 63][r]);
+          }
         }
         ptx::named_bar_sync(1, 32 * kEpiWarps);
       } else {
