@@ -70,7 +70,7 @@ struct CodeSlot {
 struct Smem {
   uint8_t b[kSlots][2][kUnitRows * 128];     // [slot][64 inputs], 1024-byte aligned
   CodeSlot code[kDeqWarps][kCodeSlots];
-  float swap[2][64][17];                     // gates and ups of the epilogue warps
+  float swap[2][16][66];                     // gates and ups of 16 rows, between the epilogue warps
   Unit sched[kSched];                        // the CTA's units, in its order
   Groups groups;
   uint64_t full[kSlots], empty[kSlots];      // of the ring's stages
@@ -421,11 +421,12 @@ __device__ __forceinline__ void store_y(uint8_t* y, bool fp32, float v) {
 template <bool kGated>
 __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
                                          uint32_t tmem) {
-  const int warp = threadIdx.x >> 5, row = threadIdx.x;   // lane of tensor memory
+  const int warp = warp_number(), lane = threadIdx.x & 31, row = threadIdx.x;   // row: lane of tensor memory
   const int units = units_of_cta(sm.groups);
   const int warps = mma_warps(sm.groups.widest);
   const int size = a.y_fp32 ? 4 : 2;
   const int64_t step = a.ldy * size;
+  const bool pairs = ((reinterpret_cast<uintptr_t>(a.y) | (uint64_t)step) & (2 * size - 1)) == 0;
   Slot acc;
   bool odd = false;   // the units before have an odd number of stages
   for (int turn = 0; turn < units; ++turn, acc.next(2), odd ^= s.blocks & 1) {
@@ -442,8 +443,6 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
     ptx::tc_fence_after();
     const uint32_t from =
         tmem + acc_column(warps, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
-    const int n = kGated ? u.mt * 64 + (row & 63) : u.mt * 128 + row;
-    const bool there = n < s.N;
     for (int c0 = 0; c0 < u.n; c0 += 16) {
       const int count = min(16, u.n - c0);   // (few rows: what is done is cut to fours of them)
       float v[16];
@@ -458,32 +457,45 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         ptx::tmem_ld_wait();
       }
       const uint32_t zero = (c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2]) >> (c0 & 16);
-      uint8_t* y = static_cast<uint8_t*>(a.y) + ((int64_t)(u.r0 + c0) * a.ldy + n) * size;
       if (kGated) {
-        // lanes 0 .. 63 are gates, 64 .. 127 ups; then the first do the even rows, the others the odd
+        // lanes 0 .. 63 are gates, 64 .. 127 ups; then a warp does every fourth row, a lane two outputs
         const int up = row >> 6;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           if ((j & 3) == 0 && j >= count) break;
-          sm.swap[up][row & 63][j] = v[j];
+          sm.swap[up][j][row & 63] = v[j];
         }
         ptx::named_bar_sync(1, 32 * kEpiWarps);
-        y += up * step;
-#pragma unroll 1
-        for (int j0 = up; j0 < count; j0 += 8) {   // four rows of this half at a time
-          float g[4];
+        float g[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) g[j] = j0 + 2 * j < count ? sm.swap[0][row & 63][j0 + 2 * j] : 0.f;
-          silu_all(g);
+        for (int i = 0; i < 4; ++i) {
+          float2 p = make_float2(0.f, 0.f);
+          if (warp + 4 * i < count) p = *reinterpret_cast<const float2*>(&sm.swap[0][warp + 4 * i][2 * lane]);
+          g[2 * i] = p.x;
+          g[2 * i + 1] = p.y;
+        }
+        silu_all(g);
+        const int first = u.mt * 64 + 2 * lane;
+        uint8_t* y = static_cast<uint8_t*>(a.y) + (int64_t)(u.r0 + c0 + warp) * step + (int64_t)first * size;
 #pragma unroll
-          for (int j = 0; j < 4; ++j, y += 2 * step) {
-            const int r = j0 + 2 * j;
-            if (r < count && there)
-              store_y(y, a.y_fp32, zero >> r & 1u ? 0.f : g[j] * sm.swap[1][row & 63][r]);
+        for (int i = 0; i < 4; ++i, y += 4 * step) {
+          const int r = warp + 4 * i;
+          if (r >= count) break;
+          const float2 p = *reinterpret_cast<const float2*>(&sm.swap[1][r][2 * lane]);
+          const bool none = zero >> r & 1u;
+          const float o0 = none ? 0.f : g[2 * i] * p.x, o1 = none ? 0.f : g[2 * i + 1] * p.y;
+          if (pairs && first + 1 < s.N) {
+            if (a.y_fp32) *reinterpret_cast<float2*>(y) = make_float2(o0, o1);
+            else *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(o0, o1);
+          } else {
+            if (first < s.N) store_y(y, a.y_fp32, o0);
+            if (first + 1 < s.N) store_y(y + size, a.y_fp32, o1);
           }
         }
         ptx::named_bar_sync(1, 32 * kEpiWarps);
       } else {
+        uint8_t* y = static_cast<uint8_t*>(a.y) + (int64_t)(u.r0 + c0) * step + (int64_t)(u.mt * 128 + row) * size;
+        const bool there = u.mt * 128 + row < s.N;
 #pragma unroll
         for (int j = 0; j < 16; ++j, y += step) {
           if ((j & 3) == 0 && j >= count) break;
