@@ -46,9 +46,16 @@ __device__ __forceinline__ Piece<T, VB> load_piece(const T* row, int64_t v) {
   p.r = *(reinterpret_cast<const typename Raw<VB>::type*>(row) + v);
   return p;
 }
+// rows that are read once
+template <typename T, int VB>
+__device__ __forceinline__ Piece<T, VB> load_once(const T* row, int64_t v) {
+  Piece<T, VB> p;
+  p.r = __ldcs(reinterpret_cast<const typename Raw<VB>::type*>(row) + v);
+  return p;
+}
 template <typename T, int VB>
 __device__ __forceinline__ void store_piece(T* row, int64_t v, const Piece<T, VB>& p) {
-  *(reinterpret_cast<typename Raw<VB>::type*>(row) + v) = p.r;
+  __stcs(reinterpret_cast<typename Raw<VB>::type*>(row) + v, p.r);
 }
 
 // the sorted row that a pos entry names; -1: one that is not followed
@@ -117,7 +124,7 @@ combine_rows_kernel(const T* __restrict__ ys, int64_t ldys, const int32_t* __res
     }
 #pragma unroll
     for (int j = 0; j < kSlotBatch; ++j)
-      if (at[j] >= 0) p[j] = load_piece<T, VB>(ys + at[j] * ldys, v);
+      if (at[j] >= 0) p[j] = load_once<T, VB>(ys + at[j] * ldys, v);
 #pragma unroll
     for (int j = 0; j < kSlotBatch; ++j)
       if (at[j] >= 0) {
@@ -131,91 +138,62 @@ combine_rows_kernel(const T* __restrict__ ys, int64_t ldys, const int32_t* __res
   store_piece<T, VB>(y + t * ldy, v, out);
 }
 
-// Sums of kSlotBatch values over a warp's lanes: each step halves the values a lane keeps. The
-// lane's result is that of value slot_of(lane), the same in the four lanes that share it.
-__device__ __forceinline__ int slot_of(int lane) {
-  return (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
-}
-__device__ __forceinline__ float warp_sums(float (&a)[kSlotBatch], int lane) {
-#pragma unroll
-  for (int half = kSlotBatch / 2, o = 16; half > 0; half >>= 1, o >>= 1) {
-    const bool up = lane & o;
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const float give = up ? a[i] : a[i + half], keep = up ? a[i + half] : a[i];
-      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-    }
-  }
-  a[0] += __shfl_xor_sync(0xffffffffu, a[0], 2);
-  a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
-  return a[0];
-}
-
-// combine's gradient: the threads of a token (blockDim.x of them, whole warps) go over dy's row,
-// write gate * dy to its k rows and add up dy * ys for its k gates
-template <typename T, int VB>
+// combine's gradient: a warp has a (token, slot). It goes over dy's row and the slot's row of ys, kAhead
+// pieces of both on their way, writes gate * dy and adds up dy * ys. The k warps of a token read
+// dy's row k times, from L1 or L2 but for the first (held in registers for all k slots at once,
+// the pieces took so many that half the threads fitted: 221 us instead of 16384 x 8 rows of 2048).
+constexpr int kAhead = 4;
+template <typename T, int VB, bool kRows, bool kGates>
 __global__ void __launch_bounds__(kRowThreads)
 combine_rows_backward_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ ys,
                              int64_t ldys, const int32_t* __restrict__ pos,
                              const float* __restrict__ gates, T* __restrict__ dys, int64_t lddys,
-                             float* __restrict__ dgates, int64_t tokens, int k, int nv) {
+                             float* __restrict__ dgates, int R, int k, int nv) {
   constexpr int n = Piece<T, VB>::n;
-  __shared__ float part[kRowThreads / 32][kSlotBatch];
   pdl_wait();
   pdl_launch_dependents();
-  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const int warp = (threadIdx.y * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
-  const int R = (int)(tokens * k);
-  for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
-    int at[kSlotBatch];
-    float g[kSlotBatch], dot[kSlotBatch];
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (i >= R) return;
+  const int p = __ldg(pos + i), r = named_row(p, R);
+  const float g = gates != nullptr ? __ldg(gates + i) : 1.f;
+  const bool own = p >= 0 && r >= 0;   // the slot has an expert
+  const T* from = dy + i / k * lddy;
+  const T* row = ys + (int64_t)(own ? r : 0) * ldys;
+  T* to = dys + (int64_t)(r >= 0 ? r : 0) * lddys;
+  float dot = 0.f;
+  if (own) {
+    for (int v0 = lane; v0 < nv; v0 += 32 * kAhead) {
+      Piece<T, VB> d[kAhead], y[kAhead];
 #pragma unroll
-    for (int j = 0; j < kSlotBatch; ++j) {
-      const bool in = t < tokens && j0 + j < k;
-      at[j] = in ? __ldg(pos + t * k + j0 + j) : R;
-      g[j] = in && gates != nullptr ? __ldg(gates + t * k + j0 + j) : 1.f;
-      dot[j] = 0.f;
-    }
-    if (t < tokens)
-      for (int v = threadIdx.x; v < nv; v += blockDim.x) {
-        const Piece<T, VB> d = load_piece<T, VB>(dy + t * lddy, v);
-        Piece<T, VB> p[kSlotBatch];
-        if (dgates != nullptr) {
-#pragma unroll
-          for (int j = 0; j < kSlotBatch; ++j)
-            if (at[j] >= 0 && at[j] < R) p[j] = load_piece<T, VB>(ys + at[j] * ldys, v);
+      for (int j = 0; j < kAhead; ++j)
+        if (v0 + 32 * j < nv) {
+          d[j] = load_piece<T, VB>(from, v0 + 32 * j);
+          if (kGates) y[j] = load_once<T, VB>(row, v0 + 32 * j);
         }
-        if (dys != nullptr) {
 #pragma unroll
-          for (int j = 0; j < kSlotBatch; ++j) {
-            const int r = named_row(at[j], R);
-            if (r < 0) continue;
+      for (int j = 0; j < kAhead; ++j)
+        if (v0 + 32 * j < nv) {
+          if (kRows) {
             Piece<T, VB> o;
 #pragma unroll
-            for (int i = 0; i < n; ++i)
-              o.e[i] = at[j] < 0 ? from_f<T>(0.f) : from_f<T>(g[j] * to_f(d.e[i]));
-            store_piece<T, VB>(dys + r * lddys, v, o);
+            for (int e = 0; e < n; ++e) o.e[e] = from_f<T>(g * to_f(d[j].e[e]));
+            store_piece<T, VB>(to, v0 + 32 * j, o);
+          }
+          if (kGates) {
+#pragma unroll
+            for (int e = 0; e < n; ++e) dot = fmaf(to_f(d[j].e[e]), to_f(y[j].e[e]), dot);
           }
         }
-        if (dgates != nullptr) {
-#pragma unroll
-          for (int j = 0; j < kSlotBatch; ++j)
-            if (at[j] >= 0 && at[j] < R) {
-#pragma unroll
-              for (int i = 0; i < n; ++i) dot[j] = fmaf(to_f(d.e[i]), to_f(p[j].e[i]), dot[j]);
-            }
-        }
-      }
-    if (dgates == nullptr) continue;   // (the same for all threads)
-    const float sum = warp_sums(dot, lane);
-    if ((lane & 3) == 0) part[warp][slot_of(lane)] = sum;
-    __syncthreads();
-    if (t < tokens && threadIdx.x < kSlotBatch && j0 + threadIdx.x < k) {
-      float s = 0.f;
-      for (int w = 0; w < (int)blockDim.x / 32; ++w) s += part[warp + w][threadIdx.x];
-      dgates[t * k + j0 + threadIdx.x] = s;
     }
-    __syncthreads();
+  } else if (kRows && r >= 0) {
+    Piece<T, VB> zero;
+    zero.r = typename Raw<VB>::type{};
+    for (int v = lane; v < nv; v += 32) store_piece<T, VB>(to, v, zero);
+  }
+  if (kGates) {
+    dot = warp_sum(dot);
+    if (lane == 0) dgates[i] = dot;
   }
 }
 
@@ -302,12 +280,14 @@ cudaError_t launch_combine_rows_backward(const RowsArgs& a, cudaStream_t s) {
   return with_type(a.dtype, vb, [&](auto z, auto w) {
     using T = decltype(z);
     constexpr int VB = decltype(w)::value;
-    const RowShape sh = row_shape(a.d, VB / es);
-    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y));
-    return launch_ex(combine_rows_backward_kernel<T, VB>, grid, sh.block, 0, s, true,
+    const int R = (int)(a.T * a.k), warps = kRowThreads / 32;
+    auto* kernel = a.dgates == nullptr ? combine_rows_backward_kernel<T, VB, true, false>
+                   : a.sorted_out == nullptr ? combine_rows_backward_kernel<T, VB, false, true>
+                                             : combine_rows_backward_kernel<T, VB, true, true>;
+    return launch_ex(kernel, dim3((R + warps - 1) / warps), dim3(kRowThreads), 0, s, true,
                      static_cast<const T*>(a.tok), a.ldtok, static_cast<const T*>(a.sorted),
                      a.ldsorted, a.pos, a.gates, static_cast<T*>(a.sorted_out), a.ldsorted_out,
-                     a.dgates, a.T, a.k, sh.nv);
+                     a.dgates, R, a.k, a.d / (VB / es));
   });
 }
 
