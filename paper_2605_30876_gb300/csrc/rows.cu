@@ -64,20 +64,28 @@ __device__ __forceinline__ int named_row(int p, int R) {
   return r < R ? r : -1;
 }
 
-// gather: thread (v, token) copies piece v of the token's row to its k places
+// Pieces of a row that a thread has in flight: narrow ones in numbers, or the bytes on their way are
+// too few (one 2-byte piece a thread: 8192 x 6 rows of 1001 were combined in 82 us).
+template <int VB>
+constexpr int pieces_ahead() { return VB == 16 ? 1 : 4; }
+
+// gather: a thread copies its pieces of the token's row to their k places
 template <typename T, int VB>
 __global__ void __launch_bounds__(kRowThreads)
 gather_rows_kernel(const T* __restrict__ x, int64_t ldx, const int32_t* __restrict__ pos,
                    T* __restrict__ xs, int64_t ldxs, int64_t tokens, int k, int nv) {
+  constexpr int kU = pieces_ahead<VB>();
   pdl_wait();
   pdl_launch_dependents();
   const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const int v = blockIdx.y * blockDim.x + threadIdx.x;
-  if (t >= tokens || v >= nv) return;
+  const int v0 = blockIdx.y * blockDim.x * kU + threadIdx.x;
+  if (t >= tokens || v0 >= nv) return;
   const int R = (int)(tokens * k);
-  const Piece<T, VB> p = load_piece<T, VB>(x + t * ldx, v);
-  Piece<T, VB> zero;
+  Piece<T, VB> p[kU], zero;
   zero.r = typename Raw<VB>::type{};
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+    if (v0 + u * (int)blockDim.x < nv) p[u] = load_once<T, VB>(x + t * ldx, v0 + u * (int)blockDim.x);
   for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
     int at[kSlotBatch];
 #pragma unroll
@@ -85,71 +93,87 @@ gather_rows_kernel(const T* __restrict__ x, int64_t ldx, const int32_t* __restri
 #pragma unroll
     for (int j = 0; j < kSlotBatch; ++j) {
       const int r = named_row(at[j], R);
-      if (r >= 0) store_piece<T, VB>(xs + r * ldxs, v, at[j] < 0 ? zero : p);
+      if (r < 0) continue;
+      T* to = xs + r * ldxs;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (v0 + u * (int)blockDim.x < nv)
+          store_piece<T, VB>(to, v0 + u * (int)blockDim.x, at[j] < 0 ? zero : p[u]);
     }
   }
 }
 
-// combine (and, with neither gates nor an addend, the gather's gradient): thread (v, token) adds up
-// piece v of the token's k rows in fp32, in the order of the slots
+// combine (and, with neither gates nor an addend, the gather's gradient): a thread adds up its pieces of
+// the token's k rows in fp32, in the order of the slots. The slots' positions have to be read before
+// the rows; four CTAs per SM (64 registers a thread) hide it: 16384 x 8 rows of 2048 took 99 us with
+// three, and 117 with CTAs that go on from token to token and read positions ahead (two per SM).
 template <typename T, int VB>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 4)
 combine_rows_kernel(const T* __restrict__ ys, int64_t ldys, const int32_t* __restrict__ pos,
                     const float* __restrict__ gates, const T* add, int64_t ldadd, T* y,
                     int64_t ldy, int64_t tokens, int k, int nv) {
-  constexpr int n = Piece<T, VB>::n;
+  constexpr int n = Piece<T, VB>::n, kU = pieces_ahead<VB>();
   pdl_wait();
   pdl_launch_dependents();
   const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const int v = blockIdx.y * blockDim.x + threadIdx.x;
-  if (t >= tokens || v >= nv) return;
+  const int bx = blockDim.x, v0 = blockIdx.y * bx * kU + threadIdx.x;
+  if (t >= tokens || v0 >= nv) return;
   const int R = (int)(tokens * k);
-  float acc[n];
+  float acc[kU][n];
 #pragma unroll
-  for (int i = 0; i < n; ++i) acc[i] = 0.f;
-  if (add != nullptr) {
-    const Piece<T, VB> p = load_piece<T, VB>(add + t * ldadd, v);
+  for (int u = 0; u < kU; ++u) {
+    Piece<T, VB> p;
+    p.r = typename Raw<VB>::type{};
+    if (add != nullptr && v0 + u * bx < nv) p = load_piece<T, VB>(add + t * ldadd, v0 + u * bx);
 #pragma unroll
-    for (int i = 0; i < n; ++i) acc[i] = to_f(p.e[i]);
+    for (int i = 0; i < n; ++i) acc[u][i] = to_f(p.e[i]);
   }
   for (int j0 = 0; j0 < k; j0 += kSlotBatch) {
     int at[kSlotBatch];
-    float g[kSlotBatch];
-    Piece<T, VB> p[kSlotBatch];
+    Piece<T, VB> p[kSlotBatch][kU];
+    uint32_t own = 0;
+#pragma unroll
+    for (int j = 0; j < kSlotBatch; ++j) at[j] = j0 + j < k ? __ldg(pos + t * k + j0 + j) : -1;
 #pragma unroll
     for (int j = 0; j < kSlotBatch; ++j) {
-      at[j] = j0 + j < k ? __ldg(pos + t * k + j0 + j) : -1;
-      if (at[j] >= R) at[j] = -1;
-      g[j] = gates != nullptr && j0 + j < k ? __ldg(gates + t * k + j0 + j) : 1.f;
+      if (at[j] < 0 || at[j] >= R) continue;
+      own |= 1u << j;
+      const T* row = ys + at[j] * ldys;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (v0 + u * bx < nv) p[j][u] = load_once<T, VB>(row, v0 + u * bx);
     }
 #pragma unroll
     for (int j = 0; j < kSlotBatch; ++j)
-      if (at[j] >= 0) p[j] = load_once<T, VB>(ys + at[j] * ldys, v);
+      if (own >> j & 1u) {
+        const float w = gates != nullptr ? __ldg(gates + t * k + j0 + j) : 1.f;
 #pragma unroll
-    for (int j = 0; j < kSlotBatch; ++j)
-      if (at[j] >= 0) {
+        for (int u = 0; u < kU; ++u)
 #pragma unroll
-        for (int i = 0; i < n; ++i) acc[i] = fmaf(g[j], to_f(p[j].e[i]), acc[i]);
+          for (int i = 0; i < n; ++i) acc[u][i] = fmaf(w, to_f(p[j][u].e[i]), acc[u][i]);
       }
   }
-  Piece<T, VB> out;
 #pragma unroll
-  for (int i = 0; i < n; ++i) out.e[i] = from_f<T>(acc[i]);
-  store_piece<T, VB>(y + t * ldy, v, out);
+  for (int u = 0; u < kU; ++u)
+    if (v0 + u * bx < nv) {
+      Piece<T, VB> out;
+#pragma unroll
+      for (int i = 0; i < n; ++i) out.e[i] = from_f<T>(acc[u][i]);
+      store_piece<T, VB>(y + t * ldy, v0 + u * bx, out);
+    }
 }
 
-// combine's gradient: a warp has a (token, slot). It goes over dy's row and the slot's row of ys, kAhead
-// pieces of both on their way, writes gate * dy and adds up dy * ys. The k warps of a token read
+// combine's gradient: a warp has a (token, slot). It goes over dy's row and the slot's row of ys, four
+// pieces of both on their way (more where they are narrow), writes gate * dy and adds up dy * ys. The k warps of a token read
 // dy's row k times, from L1 or L2 but for the first (held in registers for all k slots at once,
 // the pieces took so many that half the threads fitted: 221 us instead of 16384 x 8 rows of 2048).
-constexpr int kAhead = 4;
 template <typename T, int VB, bool kRows, bool kGates>
 __global__ void __launch_bounds__(kRowThreads)
 combine_rows_backward_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ ys,
                              int64_t ldys, const int32_t* __restrict__ pos,
                              const float* __restrict__ gates, T* __restrict__ dys, int64_t lddys,
                              float* __restrict__ dgates, int R, int k, int nv) {
-  constexpr int n = Piece<T, VB>::n;
+  constexpr int n = Piece<T, VB>::n, kAhead = VB == 16 ? 4 : VB == 4 ? 8 : 16;
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
@@ -197,17 +221,18 @@ combine_rows_backward_kernel(const T* __restrict__ dy, int64_t lddy, const T* __
   }
 }
 
-// pieces of a row, and the CTA's shape: `x` threads on a token's row (whole warps, at most a CTA)
+// pieces of a row, and the CTA's shape: `block.x` threads on a token's row, `ahead` pieces each
 struct RowShape {
   int nv;
-  dim3 block;
+  dim3 block, grid;
 };
-RowShape row_shape(int d, int per_piece) {
+RowShape row_shape(int64_t tokens, int d, int per_piece, int ahead) {
   RowShape s;
   s.nv = d / per_piece;
   int bx = 32;
-  while (bx < s.nv && bx < kRowThreads) bx *= 2;
+  while (bx * ahead < s.nv && bx < kRowThreads) bx *= 2;
   s.block = dim3(bx, kRowThreads / bx);
+  s.grid = dim3((unsigned)((tokens + s.block.y - 1) / s.block.y), (s.nv + bx * ahead - 1) / (bx * ahead));
   return s;
 }
 
@@ -246,10 +271,8 @@ cudaError_t launch_gather_rows(const RowsArgs& a, cudaStream_t s) {
   return with_type(a.dtype, vb, [&](auto z, auto w) {
     using T = decltype(z);
     constexpr int VB = decltype(w)::value;
-    const RowShape sh = row_shape(a.d, VB / es);
-    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y),
-                    (sh.nv + sh.block.x - 1) / sh.block.x);
-    return launch_ex(gather_rows_kernel<T, VB>, grid, sh.block, 0, s, true,
+    const RowShape sh = row_shape(a.T, a.d, VB / es, pieces_ahead<VB>());
+    return launch_ex(gather_rows_kernel<T, VB>, sh.grid, sh.block, 0, s, true,
                      static_cast<const T*>(a.tok), a.ldtok, a.pos, static_cast<T*>(a.sorted_out),
                      a.ldsorted_out, a.T, a.k, sh.nv);
   });
@@ -262,10 +285,8 @@ cudaError_t launch_combine_rows(const RowsArgs& a, cudaStream_t s) {
   return with_type(a.dtype, vb, [&](auto z, auto w) {
     using T = decltype(z);
     constexpr int VB = decltype(w)::value;
-    const RowShape sh = row_shape(a.d, VB / es);
-    const dim3 grid((unsigned)((a.T + sh.block.y - 1) / sh.block.y),
-                    (sh.nv + sh.block.x - 1) / sh.block.x);
-    return launch_ex(combine_rows_kernel<T, VB>, grid, sh.block, 0, s, true,
+    const RowShape sh = row_shape(a.T, a.d, VB / es, pieces_ahead<VB>());
+    return launch_ex(combine_rows_kernel<T, VB>, sh.grid, sh.block, 0, s, true,
                      static_cast<const T*>(a.sorted), a.ldsorted, a.pos, a.gates,
                      static_cast<const T*>(a.tok), a.ldtok, static_cast<T*>(a.tok_out),
                      a.ldtok_out, a.T, a.k, sh.nv);
