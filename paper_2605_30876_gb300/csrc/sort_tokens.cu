@@ -3,7 +3,7 @@
 //   sort_count_kernel  pairs per key of each chunk of pairs, one CTA per chunk
 //   sort_place_kernel  every CTA adds up, per key, the pairs before its chunk and all of them, and
 //                      goes through its chunk kSortTile pairs at a time: per warp the pairs of each
-//                      key by ballots over the warp's lanes, a prefix over the warps, and each
+//                      key by matches over the warp's lanes, a prefix over the warps, and each
 //                      pair's row is its key's base, the pairs of its key in the warps before its
 //                      own and those before it in its warp.
 // Up to kSortTile pairs take the second launch alone. Every count is an integer sum: the order does
@@ -33,48 +33,79 @@ sort_count_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
   if (tid <= E) cnt[tid] = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * chunk, end = begin + chunk < R ? begin + chunk : R;
-  for (int64_t i = begin + tid; i < end; i += kSortThreads)
-    atomicAdd(&cnt[sort_key(__ldcg(ids + i), E)], 1);
+  for (int64_t i0 = begin + tid; i0 < end; i0 += kSortTile) {
+    int id[kSortRounds];
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j)
+      id[j] = i0 + j * kSortThreads < end ? __ldcg(ids + i0 + j * kSortThreads) : 0;
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j)
+      if (i0 + j * kSortThreads < end) atomicAdd(&cnt[sort_key(id[j], E)], 1);
+  }
   __syncthreads();
   if (tid <= E) counts[(size_t)blockIdx.x * (E + 1) + tid] = cnt[tid];
 }
 
+// A key's counts over the chunks: [0] all of them, [1] those before this CTA's. Three groups of threads
+// take a third of the chunks each, 16 loads at a time.
+constexpr int kSumGroups = 3;
+static_assert(kSumGroups * kMaxKeys <= kSortThreads, "a thread per key and group");
+
+// `rounds` pairs a thread and tile (the tile has rounds * blockDim.x pairs, a warp's are consecutive)
 __global__ void __launch_bounds__(kSortThreads)
 sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk, int nchunks,
-                  const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+                  int rounds, const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
                   int32_t* __restrict__ rows, int32_t* __restrict__ pos, DevErrRecord* err) {
   __shared__ int cnt[kSortWarps][kMaxKeys];   // per warp and key: pairs, then the first row
   __shared__ int base[kMaxKeys];              // per key: the next tile's first row
+  __shared__ int sums[2][kMaxKeys];           // per key: pairs of all chunks, and of those before
   __shared__ int iscr[32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, keys = E + 1;
+  const int threads = blockDim.x, warps = threads >> 5;
   const int64_t begin = blockIdx.x * chunk, end = begin + chunk < R ? begin + chunk : R;
+  for (int i = tid; i < 2 * kMaxKeys; i += threads) (&sums[0][0])[i] = 0;
+  for (int i = lane; i < keys; i += 32) cnt[warp][i] = 0;
   pdl_wait();
   pdl_launch_dependents();
-  int all = 0, before = 0;   // of key tid
-  if (tid < keys)
-    for (int c = 0; c < nchunks; ++c) {
-      const int n = counts != nullptr ? __ldcg(counts + (size_t)c * keys + tid) : 0;
-      all += n;
-      before += c < (int)blockIdx.x ? n : 0;
+  if (nchunks > 0) {
+    __syncthreads();
+    const int group = tid / keys, key = tid - group * keys;
+    if (group < kSumGroups) {
+      const int per = (nchunks + kSumGroups - 1) / kSumGroups, c1 = min(nchunks, (group + 1) * per);
+      int all = 0, before = 0;
+      for (int c0 = group * per; c0 < c1; c0 += 16) {
+        int n[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          n[j] = c0 + j < c1 ? __ldcg(counts + (size_t)(c0 + j) * keys + key) : 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          all += n[j];
+          before += c0 + j < (int)blockIdx.x ? n[j] : 0;
+        }
+      }
+      atomicAdd(&sums[0][key], all);
+      atomicAdd(&sums[1][key], before);
     }
-  for (int64_t t0 = begin; t0 == begin || t0 < end; t0 += kSortTile) {
-    for (int i = tid; i < kSortWarps * kMaxKeys; i += kSortThreads) (&cnt[0][0])[i] = 0;
-    // a warp's pairs are consecutive
+  }
+  const int64_t tile = (int64_t)rounds * threads;
+  for (int64_t t0 = begin; t0 == begin || t0 < end; t0 += tile) {
     int key[kSortRounds], rank[kSortRounds];
-    const int64_t w0 = t0 + warp * (32 * kSortRounds) + lane;
+    const int64_t w0 = t0 + (int64_t)warp * (32 * rounds) + lane;
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
       const int64_t i = w0 + 32 * j;
       key[j] = -1;
-      if (i < end) {
+      if (j < rounds && i < end) {
         const int id = __ldcg(ids + i);
         if (id >= E) record_error(err, kErrExpertId, kAtSort, (int)i);
         key[j] = sort_key(id, E);
       }
     }
-    __syncthreads();
+    __syncwarp();   // (each warp has cleared its own counters)
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
+      if (j >= rounds) break;
       const uint32_t same = __match_any_sync(0xffffffffu, key[j]);
       const int ahead = __popc(same & ((1u << lane) - 1u));
       if (key[j] >= 0) rank[j] = cnt[warp][key[j]] + ahead;
@@ -83,25 +114,28 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
       __syncwarp();
     }
     __syncthreads();
-    int mine = 0;   // this tile's pairs of key tid
-    if (tid < keys)
-      for (int w = 0; w < kSortWarps; ++w) mine += cnt[w][tid];
-    if (t0 == begin) {
-      int total;
-      const int n = tid < keys ? (nchunks == 0 ? mine : all) : 0;
-      const int first = block_exclusive_scan_i(n, iscr, &total);
-      if (tid < keys) {
-        base[tid] = first + before;
-        if (blockIdx.x == 0) offsets[tid] = first;
+    // each key's first row in every warp: the warps' counts are summed up in place
+    int mine = 0;
+    if (tid < keys) {
+      for (int w = 0; w < warps; w += 8) {
+        int n[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[j] = w + j < warps ? cnt[w + j][tid] : 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (w + j < warps) {
+            cnt[w + j][tid] = mine;
+            mine += n[j];
+          }
       }
     }
-    if (tid < keys) {
-      int r = base[tid];
-      base[tid] = r + mine;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const int n = cnt[w][tid];
-        cnt[w][tid] = r;
-        r += n;
+    if (t0 == begin) {
+      int total;
+      const int n = tid < keys ? (nchunks == 0 ? mine : sums[0][tid]) : 0;
+      const int first = block_exclusive_scan_i(n, iscr, &total);
+      if (tid < keys) {
+        base[tid] = first + (nchunks == 0 ? 0 : sums[1][tid]);
+        if (blockIdx.x == 0) offsets[tid] = first;
       }
     }
     __syncthreads();
@@ -109,11 +143,15 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
     for (int j = 0; j < kSortRounds; ++j) {
       if (key[j] < 0) continue;
       const int64_t i = w0 + 32 * j;
-      const int r = cnt[warp][key[j]] + rank[j];
+      const int r = base[key[j]] + cnt[warp][key[j]] + rank[j];
       const bool none = key[j] == E;
       pos[i] = none ? ~r : r;
       rows[r] = none ? -1 : (int)i;
     }
+    if (t0 + tile >= end) break;
+    __syncthreads();
+    if (tid < keys) base[tid] += mine;
+    for (int i = lane; i < keys; i += 32) cnt[warp][i] = 0;
     __syncthreads();
   }
 }
@@ -146,9 +184,18 @@ cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* of
   if (n > 0)
     e = launch_ex(sort_count_kernel, dim3(n), dim3(kSortThreads), 0, s, true, ids, R, E, chunk,
                   counts);
+  // one CTA takes as few pairs a thread as there are threads for, and no more warps than it needs: the
+  // counts are added up over the warps (256 pairs: 6.9 us with 32 warps of four rounds)
+  int threads = kSortThreads, rounds = kSortRounds;
+  if (n == 0) {
+    rounds = R <= kSortThreads ? 1 : (int)((R + kSortThreads - 1) / kSortThreads);
+    const int64_t need = (R + rounds - 1) / rounds;
+    threads = (int)((need > E + 1 ? need : E + 1) + 31) / 32 * 32;
+  }
   if (e == cudaSuccess)
-    e = launch_ex(sort_place_kernel, dim3(n > 0 ? n : 1), dim3(kSortThreads), 0, s, true, ids, R,
-                  E, chunk, n, static_cast<const int32_t*>(counts), offsets, rows, pos, err);
+    e = launch_ex(sort_place_kernel, dim3(n > 0 ? n : 1), dim3(threads), 0, s, true, ids, R, E,
+                  n > 0 ? chunk : (R > 0 ? R : 1), n, rounds, static_cast<const int32_t*>(counts),
+                  offsets, rows, pos, err);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
