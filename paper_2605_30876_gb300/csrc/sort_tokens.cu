@@ -2,11 +2,11 @@
 // keys (the experts, and last the pairs without one).
 //   sort_count_kernel  pairs per key of each chunk of pairs, one CTA per chunk
 //   sort_place_kernel  every CTA adds up, per key, the pairs before its chunk and all of them, and
-//                      goes through its chunk kSortTile pairs at a time: per warp the pairs of each
+//                      goes through its chunk a tile of pairs at a time: per warp the pairs of each
 //                      key by matches over the warp's lanes, a prefix over the warps, and each
 //                      pair's row is its key's base, the pairs of its key in the warps before its
 //                      own and those before it in its warp.
-// Up to kSortTile pairs take the second launch alone. Every count is an integer sum: the order does
+// Up to 1024 pairs take the second launch alone. Every count is an integer sum: the order does
 // not depend on the order of atomics.
 #include "block_reduce.cuh"
 #include "dmoe_internal.cuh"
@@ -16,8 +16,8 @@ namespace {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortRounds = 4;                          // pairs per thread and tile
-constexpr int kSortTile = kSortThreads * kSortRounds;   // 4096 pairs
+constexpr int kSortRounds = 4;                          // pairs per thread and tile, at most
+constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxChunks = 148;                     // every CTA of one wave takes one chunk
 constexpr int kMaxKeys = kMaxExperts + 1;
 
@@ -156,12 +156,29 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
   }
 }
 
-// chunks of whole tiles, at most kSortMaxChunks of them; 0: one CTA places them without counts
-int sort_chunks(int64_t R, int64_t* chunk) {
-  const int64_t tiles = (R + kSortTile - 1) / kSortTile;
-  const int64_t per = (tiles + kSortMaxChunks - 1) / kSortMaxChunks;
-  *chunk = (per < 1 ? 1 : per) * kSortTile;
-  return tiles <= 1 ? 0 : (int)((R + *chunk - 1) / *chunk);
+// How R pairs are cut: up to 1024 go to one CTA, without counts (chunks 0); more are cut into chunks of
+// whole tiles, a CTA each and no more than run at once, with as few pairs a thread as that
+// allows (the matches within a warp are what takes time: 4096 pairs took 11.6 us in one CTA).
+struct SortPlan {
+  int chunks, rounds, threads;
+  int64_t chunk;
+};
+SortPlan sort_plan(int64_t R, int E) {
+  SortPlan p;
+  if (R <= kSortThreads) {
+    p.chunks = 0;
+    p.rounds = 1;
+    p.threads = (int)((R > E + 1 ? R : E + 1) + 31) / 32 * 32;
+    p.chunk = R > 0 ? R : 1;
+    return p;
+  }
+  const int64_t pieces = (R + kSortThreads - 1) / kSortThreads;
+  const int64_t per = (pieces + kSortMaxChunks - 1) / kSortMaxChunks;   // of a thread's pairs, per chunk
+  p.rounds = per < kSortRounds ? (int)per : kSortRounds;
+  p.threads = kSortThreads;
+  p.chunk = (per + p.rounds - 1) / p.rounds * p.rounds * kSortThreads;
+  p.chunks = (int)((R + p.chunk - 1) / p.chunk);
+  return p;
 }
 
 constexpr size_t kSortCounts = 256;   // offset of the counts: behind the fault record
@@ -169,32 +186,23 @@ constexpr size_t kSortCounts = 256;   // offset of the counts: behind the fault 
 }  // namespace
 
 size_t sort_workspace_bytes(int64_t R, int E) {
-  int64_t chunk;
-  return kSortCounts + sizeof(int32_t) * (size_t)sort_chunks(R, &chunk) * (E + 1);
+  return kSortCounts + sizeof(int32_t) * (size_t)sort_plan(R, E).chunks * (E + 1);
 }
 
 cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,
                                int32_t* rows, int32_t* pos, void* ws, cudaStream_t s) {
-  int64_t chunk;
-  const int n = sort_chunks(R, &chunk);
+  const SortPlan p = sort_plan(R, E);
   DevErrRecord* err = static_cast<DevErrRecord*>(ws);
-  int32_t* counts = n > 0 ? reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + kSortCounts)
-                          : nullptr;
+  int32_t* counts = p.chunks > 0
+                        ? reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + kSortCounts)
+                        : nullptr;
   cudaError_t e = cudaSuccess;
-  if (n > 0)
-    e = launch_ex(sort_count_kernel, dim3(n), dim3(kSortThreads), 0, s, true, ids, R, E, chunk,
-                  counts);
-  // one CTA takes as few pairs a thread as there are threads for, and no more warps than it needs: the
-  // counts are added up over the warps (256 pairs: 6.9 us with 32 warps of four rounds)
-  int threads = kSortThreads, rounds = kSortRounds;
-  if (n == 0) {
-    rounds = R <= kSortThreads ? 1 : (int)((R + kSortThreads - 1) / kSortThreads);
-    const int64_t need = (R + rounds - 1) / rounds;
-    threads = (int)((need > E + 1 ? need : E + 1) + 31) / 32 * 32;
-  }
+  if (p.chunks > 0)
+    e = launch_ex(sort_count_kernel, dim3(p.chunks), dim3(kSortThreads), 0, s, true, ids, R, E,
+                  p.chunk, counts);
   if (e == cudaSuccess)
-    e = launch_ex(sort_place_kernel, dim3(n > 0 ? n : 1), dim3(threads), 0, s, true, ids, R, E,
-                  n > 0 ? chunk : (R > 0 ? R : 1), n, rounds, static_cast<const int32_t*>(counts),
+    e = launch_ex(sort_place_kernel, dim3(p.chunks > 0 ? p.chunks : 1), dim3(p.threads), 0, s, true,
+                  ids, R, E, p.chunk, p.chunks, p.rounds, static_cast<const int32_t*>(counts),
                   offsets, rows, pos, err);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
