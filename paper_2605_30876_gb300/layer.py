@@ -1,13 +1,15 @@
-"""A resident MoE layer: device weights, workspace and output buffers around
-dmoe_layer_forward (argument marshalling only; the forward runs in libdmoe's kernels)."""
+"""Resident MoE layers: device weights, workspace and output buffers around the library's calls
+(argument marshalling only; the forwards run in libdmoe's kernels). MoELayer holds bf16 weights,
+MoELayerQ4 the same layer's experts in 4 bits."""
 from __future__ import annotations
 
 from typing import Dict, Optional
 
 import torch
 
-from . import (DMOE_ROUTE_BLOCK, LayerDesc, alloc_workspace, dmoe_layer_forward,
-               dmoe_router_prepare, make_desc)
+from . import (DMOE_ROUTE_BLOCK, LayerDesc, alloc_q4, alloc_workspace, dmoe_combine_rows,
+               dmoe_dispatch, dmoe_layer_forward, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_swiglu,
+               dmoe_router, dmoe_router_prepare, make_desc, make_q4_desc)
 
 WEIGHT_KEYS = ("w_r", "bias", "w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
 
@@ -54,4 +56,79 @@ class MoELayer:
                            w["ws_gate"], w["ws_up"], w["ws_down"], out, self.topk_idx,
                            self.topk_gate, self.n_unique, self.unique_ids, workspace=self.ws,
                            stream=stream)
+        return out
+
+
+class Q4Weight:
+    """Matrices in 4 bits with group scales: codes and scales of `desc`, quantised from bf16 [n_experts,
+    n_out, n_in] (or [n_out, n_in]: one matrix)."""
+
+    def __init__(self, w: torch.Tensor, group: int = 64, stream=None):
+        w = w.unsqueeze(0) if w.dim() == 2 else w
+        self.desc = make_q4_desc(*w.shape, group)
+        self.codes, self.scales = alloc_q4(self.desc, w.device)
+        dmoe_q4_quantize(self.desc, w.contiguous(), self.codes, self.scales, stream=stream)
+
+
+class MoELayerQ4:
+    """MoELayer with its experts (and its shared expert) in 4 bits, a bf16 scale per `group` inputs: the
+    weights that a forward reads are a quarter. The router stays fp32; the routing, the unique
+    experts and the rows are those of MoELayer, the experts' outputs those of the quantised
+    weights, with the SwiGLU intermediate and the rows per (token, slot) rounded to bf16.
+
+    weights: as for MoELayer (the bf16 expert weights are not kept).
+    """
+
+    def __init__(self, desc: LayerDesc, weights: Dict[str, Optional[torch.Tensor]],
+                 device="cuda", workspace: Optional[torch.Tensor] = None, group: int = 64):
+        self.desc = desc
+        self.device = torch.device(device)
+        T, k, E, d, I = desc.T, desc.top_k, desc.n_experts, desc.d_model, desc.d_ff
+        Is = desc.d_ff_shared
+        self.w_r, self.bias = weights["w_r"], weights.get("bias")
+        self.gate, self.up, self.down = (Q4Weight(weights[n], group)
+                                         for n in ("w_gate", "w_up", "w_down"))
+        self.shared = tuple(Q4Weight(weights[n], group)
+                            for n in ("ws_gate", "ws_up", "ws_down")) if Is > 0 else None
+        self.ws = workspace if workspace is not None else alloc_workspace(desc, self.device)
+
+        def new(*shape, dtype=torch.bfloat16):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        i32 = torch.int32
+        self.topk_idx, self.topk_gate = new(T, k, dtype=i32), new(T, k, dtype=torch.float32)
+        self.n_unique, self.unique_ids = new(1, dtype=i32), new(E, dtype=i32)
+        self.offsets = new(E + 1, dtype=i32)
+        self.rows, self.pos = new(T * k, dtype=i32), new(T * k, dtype=i32)
+        self.h, self.ys, self.y = new(T * k, I), new(T * k, d), new(T, d)
+        self.hs, self.y_shared = (new(T, Is), new(T, d)) if Is > 0 else (None, None)
+        self.prepare()
+
+    def prepare(self, stream=None) -> None:
+        dmoe_router_prepare(self.desc, self.w_r, self.ws, stream=stream)
+
+    @classmethod
+    def from_shape(cls, shape, weights, device="cuda", workspace=None, group=64) -> "MoELayerQ4":
+        desc = make_desc(shape.d_model, shape.n_experts, shape.top_k, shape.d_ff,
+                         shape.d_ff_shared, shape.block_size, shape.n_blocks,
+                         getattr(shape, "mode", DMOE_ROUTE_BLOCK), getattr(shape, "top_p", 0.0),
+                         getattr(shape, "block_top_k", 0))
+        return cls(desc, weights, device, workspace, group)
+
+    def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        out, k = self.y if y is None else y, self.desc.top_k
+        dmoe_router(self.desc, x, self.w_r, self.bias, self.topk_idx, self.topk_gate,
+                    workspace=self.ws, stream=stream)
+        dmoe_dispatch(self.desc, self.topk_idx, self.n_unique, self.unique_ids, self.offsets,
+                      self.rows, self.pos, workspace=self.ws, stream=stream)
+        g, u, d = self.gate, self.up, self.down
+        dmoe_q4_swiglu(g.desc, x, self.offsets, g.codes, g.scales, u.codes, u.scales, self.h,
+                       rows=self.rows, k=k, expert_ids=self.unique_ids, stream=stream)
+        dmoe_q4_linear(d.desc, self.h, self.offsets, d.codes, d.scales, self.ys,
+                       expert_ids=self.unique_ids, stream=stream)
+        if self.shared is not None:
+            g, u, d = self.shared
+            dmoe_q4_swiglu(g.desc, x, None, g.codes, g.scales, u.codes, u.scales, self.hs,
+                           stream=stream)
+            dmoe_q4_linear(d.desc, self.hs, None, d.codes, d.scales, self.y_shared, stream=stream)
+        dmoe_combine_rows(self.ys, self.pos, self.topk_gate, self.y_shared, out, stream=stream)
         return out
