@@ -317,18 +317,17 @@ def dmoe_set_debug_hold(workspace, hold: int, stream=None) -> None:
 _DTYPE_IDS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-def _matrix(t, name, shape, dtype, device) -> Tuple[int, int]:
-    """(device pointer, row stride) of a 2-D CUDA tensor of contiguous rows."""
+def _matrix(t, name, n, d, dtype, device) -> Tuple[int, int]:
+    """(device pointer, row stride) of an [n, d] CUDA tensor of contiguous rows."""
     if not isinstance(t, _Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.get_device() != device or device < 0:
+    if device < 0 or t.get_device() != device:
         raise ValueError(f"{name}: must be a CUDA tensor on the call's device")
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape != (n, d):
+        raise ValueError(f"{name}: expected shape {(n, d)}, got {tuple(t.shape)}")
     ld, step = t.stride()
-    n, d = shape
     if step != 1 and d > 1:
         raise ValueError(f"{name}: its rows must be contiguous")
     return t.data_ptr(), ld if n > 1 else d   # (one row: any stride)
@@ -338,22 +337,28 @@ def _vector(t, name, numel, dtype, device) -> Optional[int]:
     """Device pointer of a contiguous CUDA tensor of `numel` elements (None -> NULL)."""
     if t is None:
         return None
-    p = _ptr(t, dtype, name)
-    if not isinstance(t, _Tensor) or t.get_device() != device:
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if device < 0 or t.get_device() != device:
         raise ValueError(f"{name}: must be a CUDA tensor on the call's device")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
     if t.numel() != numel:
         raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
-    return p
+    return t.data_ptr()
 
 
-def _launch(name, device, stream, *args) -> None:
+def _launch(fn, device, stream, *args) -> None:
     """Calls the library on the tensors' device, on its current stream unless one is given."""
-    fn = getattr(_lib, name)
-    if _current_device is not None and torch.cuda.is_initialized() and device == _current_device():
-        _check(fn(*args, _stream(stream)), name)
-        return
-    with torch.cuda.device(device):
-        _check(fn(*args, _stream(stream)), name)
+    if _raw_stream is not None and device == _current_device():
+        status = fn(*args, _raw_stream(device) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _stream(stream))
+    if status != DMOE_OK:
+        _check(status, fn.__name__)
 
 
 def _slots(tokens, pos, name="pos") -> int:
@@ -391,7 +396,7 @@ def dmoe_sort_tokens(topk_idx, E, offsets, rows, pos, workspace=None, stream=Non
     ws, nb = _ws(workspace)
     if workspace.get_device() != dev:
         raise ValueError("workspace: must be on the call's device")
-    _launch("dmoe_sort_tokens", dev, stream, T, k, E, _vector(topk_idx, "topk_idx", T * k, i32, dev),
+    _launch(_lib.dmoe_sort_tokens, dev, stream, T, k, E, _vector(topk_idx, "topk_idx", T * k, i32, dev),
             _vector(offsets, "offsets", E + 1, i32, dev), _vector(rows, "rows", T * k, i32, dev),
             _vector(pos, "pos", T * k, i32, dev), ws, nb)
 
@@ -402,9 +407,9 @@ def dmoe_gather_rows(x, pos, xs, stream=None) -> None:
     T, d = x.shape
     R, dev = pos.numel(), x.get_device()
     k = _slots(T, pos)
-    px, ldx = _matrix(x, "x", (T, d), x.dtype, dev)
-    po, ldo = _matrix(xs, "xs", (R, d), x.dtype, dev)
-    _launch("dmoe_gather_rows", dev, stream, dt, T, k, d, px, ldx,
+    px, ldx = _matrix(x, "x", T, d, x.dtype, dev)
+    po, ldo = _matrix(xs, "xs", R, d, x.dtype, dev)
+    _launch(_lib.dmoe_gather_rows, dev, stream, dt, T, k, d, px, ldx,
             _vector(pos, "pos", R, torch.int32, dev), po, ldo)
 
 
@@ -414,9 +419,9 @@ def dmoe_gather_rows_backward(dxs, pos, dx, stream=None) -> None:
     R, d = dxs.shape
     T, dev = dx.shape[0], dxs.get_device()
     k = _slots(T, pos)
-    pi, ldi = _matrix(dxs, "dxs", (T * k if T else 0, d), dxs.dtype, dev)
-    po, ldo = _matrix(dx, "dx", (T, d), dxs.dtype, dev)
-    _launch("dmoe_gather_rows_backward", dev, stream, dt, T, k, d, pi, ldi,
+    pi, ldi = _matrix(dxs, "dxs", T * k if T else 0, d, dxs.dtype, dev)
+    po, ldo = _matrix(dx, "dx", T, d, dxs.dtype, dev)
+    _launch(_lib.dmoe_gather_rows_backward, dev, stream, dt, T, k, d, pi, ldi,
             _vector(pos, "pos", R, torch.int32, dev), po, ldo)
 
 
@@ -426,10 +431,10 @@ def dmoe_combine_rows(ys, pos, gates, add, y, stream=None) -> None:
     R, d = ys.shape
     T, dev = y.shape[0], ys.get_device()
     k = _slots(T, pos)
-    pi, ldi = _matrix(ys, "ys", (T * k if T else 0, d), ys.dtype, dev)
-    pa, lda = (None, 0) if add is None else _matrix(add, "add", (T, d), ys.dtype, dev)
-    po, ldo = _matrix(y, "y", (T, d), ys.dtype, dev)
-    _launch("dmoe_combine_rows", dev, stream, dt, T, k, d, pi, ldi,
+    pi, ldi = _matrix(ys, "ys", T * k if T else 0, d, ys.dtype, dev)
+    pa, lda = (None, 0) if add is None else _matrix(add, "add", T, d, ys.dtype, dev)
+    po, ldo = _matrix(y, "y", T, d, ys.dtype, dev)
+    _launch(_lib.dmoe_combine_rows, dev, stream, dt, T, k, d, pi, ldi,
             _vector(pos, "pos", R, torch.int32, dev),
             _vector(gates, "gates", R, torch.float32, dev), pa, lda, po, ldo)
 
@@ -441,11 +446,11 @@ def dmoe_combine_rows_backward(dy, ys, pos, gates, dys, dgates, stream=None) -> 
     T, d = dy.shape
     R, dev = pos.numel(), dy.get_device()
     k = _slots(T, pos)
-    pd, ldd = _matrix(dy, "dy", (T, d), dy.dtype, dev)
-    py, ldy = (None, 0) if ys is None else _matrix(ys, "ys", (R, d), dy.dtype, dev)
-    po, ldo = (None, 0) if dys is None else _matrix(dys, "dys", (R, d), dy.dtype, dev)
+    pd, ldd = _matrix(dy, "dy", T, d, dy.dtype, dev)
+    py, ldy = (None, 0) if ys is None else _matrix(ys, "ys", R, d, dy.dtype, dev)
+    po, ldo = (None, 0) if dys is None else _matrix(dys, "dys", R, d, dy.dtype, dev)
     f32 = torch.float32
-    _launch("dmoe_combine_rows_backward", dev, stream, dt, T, k, d, pd, ldd, py, ldy,
+    _launch(_lib.dmoe_combine_rows_backward, dev, stream, dt, T, k, d, pd, ldd, py, ldy,
             _vector(pos, "pos", R, torch.int32, dev), _vector(gates, "gates", R, f32, dev), po, ldo,
             _vector(dgates, "dgates", R, f32, dev))
 
@@ -462,22 +467,28 @@ def alloc_q4(desc: Q4Desc, device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
     return tuple(torch.empty(n, dtype=torch.uint8, device=device) for n in dmoe_q4_size(desc))
 
 
-def _q4(desc, codes, scales, name, device) -> Tuple[int, int]:
+def _q4_bytes(desc) -> Tuple[int, int]:
+    """dmoe_q4_size without the call (a product checks it every time): tiles of 32 rows, blocks of 128
+    inputs. The library refuses what is no valid desc."""
+    blocks = desc.n_experts * (-(-desc.n_out // 32)) * (-(-desc.n_in // 128))
+    return 2048 * blocks, 64 * (128 // max(desc.group, 1)) * blocks
+
+
+def _q4(sizes, codes, scales, name, device) -> Tuple[int, int]:
     if codes is None or scales is None:
         raise TypeError(f"{name}: codes and scales are required")
-    nc, ns = dmoe_q4_size(desc)
-    return (_vector(codes, f"{name} codes", nc, torch.uint8, device),
-            _vector(scales, f"{name} scales", ns, torch.uint8, device))
+    return (_vector(codes, f"{name} codes", sizes[0], torch.uint8, device),
+            _vector(scales, f"{name} scales", sizes[1], torch.uint8, device))
 
 
 def _q4_convert(name, desc, w, codes, scales, stream):
     if not isinstance(w, _Tensor):
         raise TypeError("w: expected a torch.Tensor")
     dev = w.get_device()
-    c, s = _q4(desc, codes, scales, "w", dev)
+    c, s = _q4(_q4_bytes(desc), codes, scales, "w", dev)
     p = _vector(w, "w", desc.n_experts * desc.n_out * desc.n_in, torch.bfloat16, dev)
     pw = (p, c, s) if name == "dmoe_q4_quantize" else (c, s, p)
-    _launch(name, dev, stream, ctypes.byref(desc), *pw)
+    _launch(getattr(_lib, name), dev, stream, ctypes.byref(desc), *pw)
 
 
 def dmoe_q4_quantize(desc, w, codes, scales, stream=None) -> None:
@@ -490,18 +501,19 @@ def dmoe_q4_dequantize(desc, codes, scales, w, stream=None) -> None:
     _q4_convert("dmoe_q4_dequantize", desc, w, codes, scales, stream)
 
 
-def _q4_products(name, desc, x, offsets, weights, y, rows, k, expert_ids, stream):
+def _q4_products(fn, desc, x, offsets, weights, y, rows, k, expert_ids, stream):
     if not isinstance(x, _Tensor) or x.dim() != 2 or not isinstance(y, _Tensor) or y.dim() != 2:
         raise TypeError("x, y: expected 2-D tensors")
-    dev, (T, R) = x.get_device(), (x.shape[0], y.shape[0])
-    px, ldx = _matrix(x, "x", (T, desc.n_in), torch.bfloat16, dev)
+    dev, T, R = x.get_device(), x.shape[0], y.shape[0]
+    px, ldx = _matrix(x, "x", T, desc.n_in, torch.bfloat16, dev)
     ydt = torch.float32 if y.dtype is torch.float32 else torch.bfloat16
-    py, ldy = _matrix(y, "y", (R, desc.n_out), ydt, dev)
+    py, ldy = _matrix(y, "y", R, desc.n_out, ydt, dev)
     n = offsets.numel() - 1 if offsets is not None else 1
-    i32 = torch.int32
-    ptrs = [p for c, s in zip(weights[::2], weights[1::2]) for p in _q4(desc, c, s, "weights", dev)]
-    _launch(name, dev, stream, ctypes.byref(desc), R, n, px, ldx, T,
-            _vector(rows, "rows", R, i32, dev), k, _vector(offsets, "offsets", n + 1, i32, dev),
+    i32, sizes, ptrs = torch.int32, _q4_bytes(desc), []
+    for i in range(0, len(weights), 2):
+        ptrs += _q4(sizes, weights[i], weights[i + 1], "weights", dev)
+    _launch(fn, dev, stream, ctypes.byref(desc), R, n, px, ldx, T, _vector(rows, "rows", R, i32, dev),
+            k, _vector(offsets, "offsets", n + 1, i32, dev),
             _vector(expert_ids, "expert_ids", n, i32, dev), *ptrs, py, ldy, _DTYPE_IDS[ydt])
 
 
@@ -509,14 +521,14 @@ def dmoe_q4_linear(desc, x, offsets, codes, scales, y, rows=None, k=1, expert_id
                    stream=None) -> None:
     """y[r] = W[expert of r] x[rows[r] // k] (rows None: x[r]) for the rows of every group of
     offsets (None: one group of all rows)."""
-    _q4_products("dmoe_q4_linear", desc, x, offsets, (codes, scales), y, rows, k, expert_ids,
+    _q4_products(_lib.dmoe_q4_linear, desc, x, offsets, (codes, scales), y, rows, k, expert_ids,
                  stream)
 
 
 def dmoe_q4_swiglu(desc, x, offsets, gate_codes, gate_scales, up_codes, up_scales, y, rows=None,
                    k=1, expert_ids=None, stream=None) -> None:
     """y[r] = silu(Wg x) * (Wu x), arguments as for dmoe_q4_linear."""
-    _q4_products("dmoe_q4_swiglu", desc, x, offsets, (gate_codes, gate_scales, up_codes, up_scales),
+    _q4_products(_lib.dmoe_q4_swiglu, desc, x, offsets, (gate_codes, gate_scales, up_codes, up_scales),
                  y, rows, k, expert_ids, stream)
 
 
