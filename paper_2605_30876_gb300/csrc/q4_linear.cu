@@ -16,6 +16,11 @@
 // Few rows: the weights' bytes are the bound, and the instructions per code are close to it: 64 pairs
 // a lane and stage at 2.75, of the 368 that each scheduler issues in that time. Many rows: the
 // tensor pipe, and the copies of x.
+// With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
+// CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
+// its own. One row times 8192 x K, alone and in pairs: K = 2048 8.4 and 8.5 us, 4096 12.1 and 10.5,
+// 8192 19.4 and 14.4; the pairs' launch, barriers and exchange take 2 us. (Also 0.5 to 1 us where
+// they share nothing.) So pairs are for kPairStages stages and more, and fewer tiles than CTAs.
 // Every wait has a limit of one second. One that runs out is recorded (dmoe_q4_device_error) and ends
 // its role; the others' waits run out after it, and the CTA gives its tensor memory back.
 #include "q4.cuh"
@@ -40,6 +45,7 @@ constexpr int kAcc0 = kSlots * 64;         // first column of the sums
 static_assert(kSets == kSlots && kLoadWarps == 2 * kSlots, "a set and two loading warps per slot");
 constexpr uint64_t kWaitNs = 1000000000ull;
 constexpr int kSources = 1024;             // sorted rows whose sources are looked up once, together
+constexpr int kPairStages = 24;
 constexpr int kSched = 256;                // units of a CTA that are looked up once, together
 
 __device__ DevErrRecord q4_fault;          // of every call on the device
@@ -49,6 +55,12 @@ struct Groups {
   int n, units;
   int widest;   // rows of the widest unit
   int e[kMaxExperts], r0[kMaxExperts], r1[kMaxExperts], first[kMaxExperts];
+};
+
+// What this CTA does: its units, and of their stages those from `first` on.
+struct Work {
+  int units, first, blocks;
+  int rank;      // in a pair that shares its unit: 0 or 1; else -1
 };
 
 struct __align__(16) Unit {
@@ -75,6 +87,7 @@ struct Smem {
   Groups groups;
   uint64_t full[kSlots], empty[kSlots];      // of the ring's stages
   uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
+  uint64_t pair_ready, pair_full;            // the first CTA has room for the second's sums; has them
   uint32_t tmem;
   int wcount[kThreads / 32];
   int source[kSources];                      // row of x of the first sorted rows, or -1
@@ -162,8 +175,21 @@ __device__ __forceinline__ Unit find_unit(const Groups& s, int m_tiles, int unit
 __device__ __forceinline__ Unit unit_at(const Smem& sm, int m_tiles, int i) {
   return i < kSched ? sm.sched[i] : find_unit(sm.groups, m_tiles, blockIdx.x + i * gridDim.x);
 }
-__device__ __forceinline__ int units_of_cta(const Groups& s) {
-  return s.units > (int)blockIdx.x ? (s.units - (int)blockIdx.x - 1) / (int)gridDim.x + 1 : 0;
+__device__ __forceinline__ Work work_of_cta(const Groups& g, int blocks, bool paired) {
+  Work w;
+  const int ctas = gridDim.x, cta = blockIdx.x;
+  if (paired && 2 * g.units <= ctas) {
+    w.rank = cta & 1;   // (CTAs 2p and 2p + 1 are a cluster)
+    w.units = cta / 2 < g.units ? 1 : 0;
+    w.first = w.rank == 0 ? 0 : (blocks + 1) / 2;
+    w.blocks = w.rank == 0 ? (blocks + 1) / 2 : blocks / 2;
+  } else {
+    w.rank = -1;
+    w.units = g.units > cta ? (g.units - cta - 1) / ctas + 1 : 0;
+    w.first = 0;
+    w.blocks = blocks;
+  }
+  return w;
 }
 
 // Waits with pauses, or, for the issuing warp (kPause 0), without.
@@ -202,10 +228,10 @@ __device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, t
 
 // ------------------------------------------------------------------ dequantising
 template <bool kGated>
-__device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
-                                           uint32_t tmem) {
+__device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, const Work& w, int m_tiles,
+                                           Smem& sm, uint32_t tmem) {
   const int warp = warp_number() - kEpiWarps, set = warp >> 2, lane = threadIdx.x & 31;
-  const int units = units_of_cta(sm.groups), scale_block = s.scale_block();
+  const int units = w.units, scale_block = s.scale_block();
   const int pieces = scale_block / 16;   // of the scales: a lane copies one, the first lanes
   const uint32_t ring = ptx::smem_addr(&sm.code[warp][0]) + lane * 16;
   constexpr uint32_t kSlot = sizeof(CodeSlot), kScales = offsetof(CodeSlot, scales);
@@ -220,17 +246,17 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
     const int m = kGated ? (warp & 3) >> 1 : 0;
     const int tile = kGated ? u.mt * 2 + (warp & 1) : u.mt * 4 + (warp & 3);
     there = tile < s.tiles;
-    const size_t block = ((size_t)u.e * s.tiles + tile) * s.blocks + st;
+    const size_t block = ((size_t)u.e * s.tiles + tile) * s.blocks + w.first + st;
     codes = static_cast<const uint8_t*>(a.codes[m]) + block * kQ4CodeBytes + lane * 16;
     scales = static_cast<const uint8_t*>(a.scales[m]) + block * scale_block + lane * 16;
   };
   uint32_t to = ring;
   auto copy = [&]() {   // the next block's copies, if there is one; always one group of copies
-    while (st >= s.blocks && unit < units) {
-      base += s.blocks;
+    while (st >= w.blocks && unit < units) {
+      base += w.blocks;
       ++unit;
       st = (set - base) & (kSets - 1);
-      if (st < s.blocks && unit < units) enter();
+      if (st < w.blocks && unit < units) enter();
     }
     if (unit < units && there) {
 #pragma unroll
@@ -243,7 +269,7 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
     st += kSets;
     to = to == ring + (kCodeSlots - 1) * kSlot ? ring : to + kSlot;
   };
-  if (st < s.blocks && units > 0) enter();
+  if (st < w.blocks && units > 0) enter();
 #pragma unroll 1
   for (int i = 0; i < kCodeSlots - 1; ++i) copy();
 
@@ -252,7 +278,7 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
   uint32_t turn = 1;
   int from = 0;
   // this set's stages: of units * blocks, those whose number is set mod kSets
-  const int64_t all = (int64_t)units * s.blocks;
+  const int64_t all = (int64_t)units * w.blocks;
   const int visits = all > set ? (int)((all - set - 1) / kSets) + 1 : 0;
 #pragma unroll 1
   for (int i = 0; i < visits; ++i) {
@@ -280,10 +306,10 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
       const uint32_t pair = h == 0 ? s01 : s23;
       const Q4Scale s0 = q4_scale_pair(pair), s1 = q4_scale_pair(pair >> 16);
       const uint4 c0 = slot.codes[h][lane], c1 = slot.codes[h + 1][lane];
-      const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+      const uint32_t word[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       uint32_t v[32];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = q4_value_pair(w[j / 4], j & 3, j < 16 ? s0 : s1, bits);
+      for (int j = 0; j < 32; ++j) v[j] = q4_value_pair(word[j / 4], j & 3, j < 16 ? s0 : s1, bits);
       ptx::tmem_st32(at + h * 16, v);
     }
     ptx::tmem_st_wait();
@@ -297,25 +323,25 @@ __device__ __forceinline__ void dequantise(const Q4Args& a, const Q4Shape& s, in
 }
 
 // ------------------------------------------------------------------ loading x
-__device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm) {
+__device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, const Work& w, int m_tiles,
+                                       Smem& sm) {
   const int warp = warp_number() - kLoadWarp, slot = warp % kSlots, lane = threadIdx.x & 31;
   // 16 bytes of a row's 128, row of eight (the slot's warps have four of them each)
   const int chunk = lane & 7, sub = (lane >> 3) + warp / kSlots * 4;
-  const int units = units_of_cta(sm.groups);
   // (row r's 16-byte piece c is at r * 128 + (c ^ r % 8) * 16)
   const uint32_t dst = ptx::smem_addr(sm.b[slot][0]) + sub * 128 + ((chunk ^ sub) << 4);
   uint32_t turn = 1;
   int st = slot;   // this warp's next stage, counted from the unit's start
-  for (int unit = 0; unit < units; ++unit, st -= s.blocks) {
-    if (st >= s.blocks) continue;
+  for (int unit = 0; unit < w.units; ++unit, st -= w.blocks) {
+    if (st >= w.blocks) continue;
     const Unit u = unit_at(sm, m_tiles, unit);
     // this lane's rows: sub, sub + 8, ... (kept as the sources of rows lane, lane + 32, ...)
     int src[kUnitRows / 32];
 #pragma unroll
     for (int j = 0; j < kUnitRows / 32; ++j)
       src[j] = 32 * j < u.n ? max(source(a, sm, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
-    for (; st < s.blocks; st += kSlots) {
-      const int k = st * 128 + chunk * 8;
+    for (; st < w.blocks; st += kSlots) {
+      const int k = (w.first + st) * 128 + chunk * 8;
       const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
       // (where there is nothing to read, any address of x)
       const __nv_bfloat16 *x0 = a.x + (in0 ? k : 0), *x1 = a.x + (in1 ? k + 64 : 0);
@@ -356,10 +382,9 @@ __device__ __forceinline__ uint32_t acc_column(int warps, int buffer, int warp) 
 // warp's instructions take five cycles and more each here, and these warps' are the ring's
 // pace: the slots are unrolled, so that addresses are constants.
 template <int kWarps>
-__device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, uint32_t tmem, int warp) {
+__device__ __forceinline__ void issue(const Work& w, int m_tiles, Smem& sm, uint32_t tmem, int warp) {
   const uint64_t ring = ptx::sdesc_k_sw128(ptx::smem_addr(sm.b[warp]));
   constexpr uint32_t kBlock16 = kUnitRows * 128 / 16;   // (a descriptor's address is in units of 16 bytes)
-  const int units = units_of_cta(sm.groups);
   const uint32_t a0 = tmem + warp * 64;
   uint64_t* const full = sm.full + warp;
   uint64_t* const empty = sm.empty + warp;
@@ -373,15 +398,15 @@ __device__ __forceinline__ void issue(const Q4Shape& s, int m_tiles, Smem& sm, u
     for (int i = 0; i < kSlots; i += kWarps) {
       bool first = false;
       while (left == 0) {   // (a unit of one stage may have none of this warp's)
-        if (unit == units || !__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
+        if (unit == w.units || !__all_sync(0xffffffffu, wait<0>(&sm.d_empty[acc.i], acc.turn ^ 1u, 3))) {
           ok = false;
           break;
         }
         idesc = ptx::idesc_bf16(128, (unit_at(sm, m_tiles, unit).n + 15) / 16 * 16);
         d = tmem + acc_column(kWarps, acc.i, warp);
         d_full = &sm.d_full[acc.i];
-        left = kWarps == 1 ? s.blocks : (s.blocks + ((warp != 0) == odd ? 1 : 0)) / 2;
-        odd ^= s.blocks & 1;
+        left = kWarps == 1 ? w.blocks : (w.blocks + ((warp != 0) == odd ? 1 : 0)) / 2;
+        odd ^= w.blocks & 1;
         first = true;
         ++unit;
         acc.next(2);
@@ -418,18 +443,32 @@ __device__ __forceinline__ void store_y(uint8_t* y, bool fp32, float v) {
   else *reinterpret_cast<__nv_bfloat16*>(y) = __float2bfloat16_rn(v);
 }
 
+// Waits for the pair's other CTA (once per launch).
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, int where) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1; !ptx::mbar_try_wait_cluster(bar, 0); ++i)
+    if ((i & 255u) == 0u) {
+      const uint64_t now = ptx::globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > kWaitNs) {
+        record_error(&q4_fault, kErrTimeout, kAtQ4, where);
+        return false;
+      }
+    }
+  return true;
+}
+
 template <bool kGated>
-__device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int m_tiles, Smem& sm,
-                                         uint32_t tmem) {
+__device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, const Work& w, int m_tiles,
+                                         Smem& sm, uint32_t tmem) {
   const int warp = warp_number(), lane = threadIdx.x & 31, row = threadIdx.x;   // row: lane of tensor memory
-  const int units = units_of_cta(sm.groups);
   const int warps = mma_warps(sm.groups.widest);
   const int size = a.y_fp32 ? 4 : 2;
   const int64_t step = a.ldy * size;
   const bool pairs = ((reinterpret_cast<uintptr_t>(a.y) | (uint64_t)step) & (2 * size - 1)) == 0;
   Slot acc;
   bool odd = false;   // the units before have an odd number of stages
-  for (int turn = 0; turn < units; ++turn, acc.next(2), odd ^= s.blocks & 1) {
+  for (int turn = 0; turn < w.units; ++turn, acc.next(2), odd ^= w.blocks & 1) {
     const Unit u = unit_at(sm, m_tiles, turn);
     uint32_t missing[kUnitRows / 32] = {};   // rows without a source: zeros
     if (a.rows != nullptr) {
@@ -441,20 +480,44 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
     }
     if (!ptx::epi_all(wait<100>(&sm.d_full[acc.i], acc.turn, 7))) break;
     ptx::tc_fence_after();
+    // A shared unit: x's ring, whose stages have all been used, takes the other CTA's sums, [row][output].
+    float* const theirs = reinterpret_cast<float*>(sm.b);
+    if (w.rank == 0) {
+      if (row == 0) ptx::mbar_arrive_cluster(ptx::peer_smem(&sm.pair_ready, 1));
+      if (!ptx::epi_all(wait_pair(&sm.pair_full, 9))) break;
+    } else if (w.rank == 1) {
+      if (!ptx::epi_all(wait_pair(&sm.pair_ready, 10))) break;
+    }
+    const uint32_t to = w.rank == 1 ? ptx::peer_smem(theirs, 0) + row * 4 : 0u;
     const uint32_t from =
-        tmem + acc_column(warps, acc.i, s.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
+        tmem + acc_column(warps, acc.i, w.blocks == 1 && odd ? 1 : 0) + ((uint32_t)warp << 21);
     for (int c0 = 0; c0 < u.n; c0 += 16) {
       const int count = min(16, u.n - c0);   // (few rows: what is done is cut to fours of them)
       float v[16];
       ptx::tmem_ld16(from + c0, v);
-      if (warps == 2 && s.blocks > 1) {
-        float w[16];
-        ptx::tmem_ld16(from + 64 + c0, w);
+      if (warps == 2 && w.blocks > 1) {
+        float o[16];
+        ptx::tmem_ld16(from + 64 + c0, o);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] += w[j];
+        for (int j = 0; j < 16; ++j) v[j] += o[j];
       } else {
         ptx::tmem_ld_wait();
+      }
+      if (w.rank == 1) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if ((j & 3) == 0 && j >= count) break;
+          ptx::st_cluster_f32(to + (c0 + j) * 512, v[j]);
+        }
+        continue;
+      }
+      if (w.rank == 0) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if ((j & 3) == 0 && j >= count) break;
+          v[j] += theirs[(c0 + j) * 128 + row];
+        }
       }
       const uint32_t zero = (c0 < 32 ? missing[0] : c0 < 64 ? missing[1] : missing[2]) >> (c0 & 16);
       if (kGated) {
@@ -503,6 +566,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
         }
       }
     }
+    if (w.rank == 1) ptx::mbar_arrive_cluster(ptx::peer_smem(&sm.pair_full, 0));
     ptx::tc_fence_before();
     ptx::mbar_arrive(&sm.d_empty[acc.i]);
   }
@@ -510,7 +574,7 @@ __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, int 
 
 template <bool kGated>
 __global__ void __launch_bounds__(kThreads, 1)
-q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
+q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, const bool paired) {
   extern __shared__ __align__(1024) uint8_t raw[];
   Smem& sm = *reinterpret_cast<Smem*>(raw);
   const int warp = warp_number();
@@ -527,6 +591,8 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
       ptx::mbar_init(&sm.d_empty[i], 32 * kEpiWarps);
     }
     for (int i = 0; i < kMmaWarps; ++i) ptx::mbar_init(&sm.drain[i], 1);
+    ptx::mbar_init(&sm.pair_ready, 1);
+    ptx::mbar_init(&sm.pair_full, 32 * kEpiWarps);
     ptx::fence_mbarrier_init();
   }
   ptx::tc_fence_before();
@@ -534,25 +600,37 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s) {
   pdl_launch_dependents();
   const int m_tiles = kGated ? (s.N + 63) / 64 : (s.N + 127) / 128;
   find_groups(a, m_tiles, sm);   // (synchronises the CTA)
-  if ((int)threadIdx.x < min(kSched, units_of_cta(sm.groups)))
-    sm.sched[threadIdx.x] = find_unit(sm.groups, m_tiles, blockIdx.x + threadIdx.x * gridDim.x);
+  const Work w = work_of_cta(sm.groups, s.blocks, paired);
+  if ((int)threadIdx.x < min(kSched, w.units))
+    sm.sched[threadIdx.x] =
+        find_unit(sm.groups, m_tiles, w.rank >= 0 ? blockIdx.x / 2 : blockIdx.x + threadIdx.x * gridDim.x);
   const int issuers = mma_warps(sm.groups.widest);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) ptx::mbar_init(&sm.d_full[i], issuers);
     ptx::fence_mbarrier_init();
   }
-  __syncthreads();
+  // (a pair's barriers are there before the other CTA arrives on them, and until it has)
+  if (w.rank >= 0) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  } else {
+    __syncthreads();
+  }
   ptx::tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  if (warp < kEpiWarps) epilogue<kGated>(a, s, m_tiles, sm, tmem);
-  else if (warp < kLoadWarp) dequantise<kGated>(a, s, m_tiles, sm, tmem);
-  else if (warp < kMmaWarp) load_x(a, s, m_tiles, sm);
-  else if (issuers == 2) issue<2>(s, m_tiles, sm, tmem, warp - kMmaWarp);
-  else if (warp == kMmaWarp) issue<1>(s, m_tiles, sm, tmem, 0);
+  if (warp < kEpiWarps) epilogue<kGated>(a, s, w, m_tiles, sm, tmem);
+  else if (warp < kLoadWarp) dequantise<kGated>(a, s, w, m_tiles, sm, tmem);
+  else if (warp < kMmaWarp) load_x(a, s, w, m_tiles, sm);
+  else if (issuers == 2) issue<2>(w, m_tiles, sm, tmem, warp - kMmaWarp);
+  else if (warp == kMmaWarp) issue<1>(w, m_tiles, sm, tmem, 0);
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) ptx::tmem_dealloc(tmem, 512);
+  if (w.rank >= 0) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  }
 }
 
 }  // namespace
@@ -571,12 +649,17 @@ cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_
     if (e == cudaSuccess) ready.fetch_or(bit, std::memory_order_release);
   }
   if (e != cudaSuccess) return e;
-  // at most as many CTAs as units there can be
+  // at most as many CTAs as units there can be, and as run at once
   const int64_t groups = a.n_groups < a.R ? a.n_groups : a.R;
-  const int64_t units = (groups + a.R / kUnitRows) * (gated ? (s.N + 63) / 64 : (s.N + 127) / 128);
+  const int64_t tiles = gated ? (s.N + 63) / 64 : (s.N + 127) / 128;
+  const int64_t units = (groups + a.R / kUnitRows) * tiles;
   const int sms = device_sm_count();
-  return launch_ex(gated ? q4_kernel<true> : q4_kernel<false>, dim3((unsigned)(units < sms ? units : sms)),
-                   dim3(kThreads), sizeof(Smem), st, true, a, s);
+  auto* kernel = gated ? q4_kernel<true> : q4_kernel<false>;
+  if (s.blocks >= kPairStages && 2 * tiles <= sms)
+    return launch_cluster(kernel, dim3((unsigned)(2 * (units < sms / 2 ? units : sms / 2))),
+                          dim3(kThreads), sizeof(Smem), st, 2, true, a, s, true);
+  return launch_ex(kernel, dim3((unsigned)(units < sms ? units : sms)), dim3(kThreads), sizeof(Smem),
+                   st, true, a, s, false);
 }
 
 cudaError_t q4_fault_address(void** p) { return cudaGetSymbolAddress(p, q4_fault); }

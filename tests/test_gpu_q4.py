@@ -183,10 +183,65 @@ def test_rows_of_a_group(rows, gated):
 
 
 @pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("rows", [20, 70, 90, 128, 300])
-def test_long_sums_over_several_tiles(rows, gated):
-    """More inputs than any ring of stages holds, many times over."""
-    check_products(2, 300, 8192, 128, np.array([rows, 3]), gated=gated, seed=rows)
+@pytest.mark.parametrize("rows", [1, 20, 70, 90, 128, 300])
+@pytest.mark.parametrize("K", [2944, 3200, 8192])        # 23 stages (a CTA's), 25 and 64 (a pair's)
+def test_long_sums_over_several_tiles(rows, K, gated):
+    """More inputs than any ring of stages holds, many times over; the same result every time."""
+    sizes = np.array([rows, 3])
+    _, y = check_products(2, 300, K, 128, sizes, gated=gated, seed=rows, gap=8)
+    for _ in range(3):
+        assert torch.equal(check_products(2, 300, K, 128, sizes, gated=gated, seed=rows, gap=8)[1], y)
+
+
+def test_long_sums_of_more_units_than_pairs():
+    check_many_units(40, 640, 3200, 64, np.full(40, 3), True)
+    check_many_units(40, 640, 3200, 64, np.full(40, 3), False)
+
+
+def check_many_units(E, N, K, g, sizes, gated, seed=0):
+    """The products of more units than CTAs, against torch in 64 bits on the dequantised weights (which
+    tests of their own hold to the definition)."""
+    m = P.dm()
+    desc = m.make_q4_desc(E, N, K, g)
+    R = int(sizes.sum())
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int32, device="cuda")
+    packed, vals = [], []
+    for _ in range(2 if gated else 1):
+        w = torch.empty((E, N, K), dtype=BF16, device="cuda")
+        for e in range(E):
+            w[e] = torch.randn((N, K), generator=gen, device="cuda") * 0.02
+        packed += pack(desc, w)
+        m.dmoe_q4_dequantize(desc, packed[-2], packed[-1], w)
+        vals.append(w)
+    x = torch.randn((R, K), generator=gen, device="cuda").to(BF16)
+    y = torch.full((R, N), 3.0, dtype=BF16, device="cuda")
+    (m.dmoe_q4_swiglu if gated else m.dmoe_q4_linear)(desc, x, offsets, *packed, y)
+    for e in np.flatnonzero(sizes):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        xe = x[lo:hi].double()
+        s = [(xe @ v[e].double().T, xe.abs() @ v[e].double().abs().T) for v in vals]
+        s = [(a.cpu().numpy(), b.cpu().numpy()) for a, b in s]
+        if gated:
+            want, tol = swiglu_bounds(*s[0], *s[1], K, BF16)
+        else:
+            want, tol = s[0][0], bounds(*s[0], K, BF16)[1]
+        assert (np.abs(f64(y[lo:hi]) - want) <= tol).all(), e
+    assert m.dmoe_q4_device_error()[0] == 0
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("K", [128, 256, 384, 1408])     # one stage a unit, two, three, eleven
+@pytest.mark.parametrize("most", [5, 50, 90, 250])       # up to 16, 64, 96 rows a unit; several units
+def test_more_units_than_ctas(K, most, gated):
+    rng = np.random.default_rng(K + most)
+    sizes = rng.integers(0, 6, 100)
+    sizes[rng.integers(0, 100, 5)] = rng.integers(most // 2, most + 1, 5)
+    check_many_units(100, 320, K, 64, sizes, gated, seed=K)
+
+
+def test_more_units_than_a_cta_looks_up_at_once():
+    check_many_units(256, 32768, 128, 128, np.full(256, 1), False)
 
 
 @pytest.mark.parametrize("gated", [False, True])
