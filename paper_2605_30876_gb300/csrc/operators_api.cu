@@ -8,7 +8,6 @@ using namespace dmoe;
 namespace {
 
 constexpr int64_t kMaxPairs = 1 << 30;
-constexpr int64_t kMaxQ4Rows = 1 << 26;   // units of 128 rows x 64 outputs are counted in 32 bits
 constexpr int kMaxRowWidth = 1 << 20;
 
 dmoe_status status_of(cudaError_t e) {
@@ -66,7 +65,9 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   if (R < 0 || T_x < 0 || n_groups <= 0 || k <= 0 || ldx < desc->n_in || ldy < desc->n_out ||
       (y_dtype != DMOE_BF16 && y_dtype != DMOE_FP32))
     return DMOE_ERR_INVALID_ARG;
-  if (R > kMaxQ4Rows || n_groups > kMaxExperts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
+  if (R > kMaxPairs || n_groups > kMaxExperts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
+  // the kernel counts its units (96 rows x 64 outputs of a group) in 32 bits, whatever the offsets hold
+  if ((R / 96 + 1) * ((desc->n_out + 63) / 64) * n_groups > INT32_MAX) return DMOE_ERR_UNSUPPORTED;
   if ((offsets == nullptr && n_groups != 1) ||
       (expert_ids == nullptr && n_groups > desc->n_experts) || (rows == nullptr && T_x < R))
     return DMOE_ERR_INVALID_ARG;

@@ -52,7 +52,7 @@ __device__ DevErrRecord q4_fault;          // of every call on the device
 
 // The groups that have rows and an expert, in order, and their first units.
 struct Groups {
-  int n, units;
+  int n;
   int widest;   // rows of the widest unit
   int e[kMaxExperts], r0[kMaxExperts], r1[kMaxExperts], first[kMaxExperts];
 };
@@ -89,7 +89,7 @@ struct Smem {
   uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
   uint64_t pair_ready, pair_full;            // the first CTA has room for the second's sums; has them
   uint32_t tmem;
-  int wcount[kThreads / 32];
+  int2 warp_groups[kMaxExperts / 32];        // of 32 groups: those with rows, and their units
   int source[kSources];                      // row of x of the first sorted rows, or -1
 };
 
@@ -97,10 +97,24 @@ __device__ __forceinline__ int source(const Q4Args& a, const Smem& sm, int r) {
   return a.rows == nullptr ? r : r < kSources ? sm.source[r] : find_source(a, r);
 }
 
-__device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& sm) {
+// A group's rows are cut into parts of about the same size, each a unit per tile of outputs.
+__device__ __forceinline__ Unit make_unit(int e, int r0, int r1, int parts, int m_tiles, int local) {
+  const int part = local / m_tiles, per = (r1 - r0 + parts - 1) / parts;
+  Unit u;
+  u.e = e;
+  u.mt = local - part * m_tiles;
+  u.r0 = r0 + part * per;
+  u.n = min(per, r1 - u.r0);
+  return u;
+}
+
+// The groups with rows and an expert, this CTA's work, and its first units. Every thread has a group, and
+// writes down those of its units that are this CTA's. (The caller synchronises the CTA after it.)
+__device__ __forceinline__ Work find_work(const Q4Args& a, int m_tiles, int blocks, bool paired, Smem& sm) {
   Groups& s = sm.groups;
   const int u = threadIdx.x, lane = u & 31, warp = u >> 5, R = (int)a.R;
-  static_assert(kThreads >= kMaxExperts && kThreads >= kSched, "a thread per group, and per unit");
+  static_assert(kThreads >= kMaxExperts, "a thread per group");
+  constexpr int kWarps = kMaxExperts / 32;
   int e = u, r0 = 0, r1 = 0;
   if (u < a.n_groups) {
     r1 = R;
@@ -115,81 +129,71 @@ __device__ __forceinline__ void find_groups(const Q4Args& a, int m_tiles, Smem& 
   r0 = max(r0, 0);
   r1 = min(r1, R);
   const bool live = r0 < r1 && e >= 0 && e < a.n_experts;
-  const int tiles = live ? (r1 - r0 + kUnitRows - 1) / kUnitRows : 0;
+  const int parts = live ? (r1 - r0 + kUnitRows - 1) / kUnitRows : 0;
   const uint32_t m = __ballot_sync(0xffffffffu, live);
-  int units = tiles * m_tiles, before = units;   // inclusive sum over the warp
+  const int units = parts * m_tiles;   // (their sum over the groups fits: checked on the host)
+  int end = units;                     // inclusive sum over the warp
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += v;
+    const int v = __shfl_up_sync(0xffffffffu, end, o);
+    if (lane >= o) end += v;
   }
   if (u == 0) s.widest = 0;
-  if (lane == 31) {
-    sm.wcount[warp] = before;
-    if (warp < kMaxExperts / 32) s.first[warp] = __popc(m);   // (for the moment)
-  }
+  if (lane == 31 && warp < kWarps) sm.warp_groups[warp] = make_int2(__popc(m), end);
   __syncthreads();
   int at = __popc(m & ((1u << lane) - 1u)), n = 0, all = 0;
-  for (int w = 0; w < kMaxExperts / 32; ++w) {
-    if (w < warp) {
-      at += s.first[w];
-      before += sm.wcount[w];
-    }
-    n += s.first[w];
-    all += sm.wcount[w];
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const int2 v = sm.warp_groups[w];
+    at += w < warp ? v.x : 0;
+    end += w < warp ? v.y : 0;
+    n += v.x;
+    all += v.y;
   }
-  __syncthreads();
+  Work w;
+  const int ctas = gridDim.x, cta = blockIdx.x;
+  int first = cta;   // this CTA's first unit; the others are `ctas` apart
+  if (paired && 2 * all <= ctas) {
+    w.rank = cta & 1;   // (CTAs 2p and 2p + 1 are a cluster)
+    first = cta / 2;
+    w.units = first < all ? 1 : 0;
+    w.first = w.rank == 0 ? 0 : (blocks + 1) / 2;
+    w.blocks = w.rank == 0 ? (blocks + 1) / 2 : blocks / 2;
+  } else {
+    w.rank = -1;
+    w.units = all > cta ? (all - cta - 1) / ctas + 1 : 0;
+    w.first = 0;
+    w.blocks = blocks;
+  }
   if (live) {
+    const int begin = end - units;
     s.e[at] = e;
     s.r0[at] = r0;
     s.r1[at] = r1;
-    s.first[at] = before - units;
-    atomicMax(&s.widest, (r1 - r0 + tiles - 1) / tiles);
+    s.first[at] = begin;
+    atomicMax(&s.widest, (r1 - r0 + parts - 1) / parts);
+    for (int i = begin > first ? (begin - first + ctas - 1) / ctas : 0; i < min(kSched, w.units); ++i) {
+      if (first + i * ctas >= end) break;
+      sm.sched[i] = make_unit(e, r0, r1, parts, m_tiles, first + i * ctas - begin);
+    }
   }
-  if (u == 0) {
-    s.n = n;
-    s.units = all;
-  }
-  __syncthreads();
+  if (u == 0) s.n = n;
+  return w;
 }
 
-__device__ __forceinline__ Unit find_unit(const Groups& s, int m_tiles, int unit) {
+// the i-th unit of this CTA, which is there
+__device__ __forceinline__ Unit unit_at(const Smem& sm, int m_tiles, int i) {
+  if (i < kSched) return sm.sched[i];
+  const Groups& s = sm.groups;
+  const int unit = blockIdx.x + i * gridDim.x;
   int lo = 0, hi = s.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (s.first[mid] <= unit) lo = mid;
     else hi = mid - 1;
   }
-  const int local = unit - s.first[lo], part = local / m_tiles;
-  const int rows = s.r1[lo] - s.r0[lo], parts = (rows + kUnitRows - 1) / kUnitRows;
-  const int per = (rows + parts - 1) / parts;
-  Unit u;
-  u.e = s.e[lo];
-  u.mt = local - part * m_tiles;
-  u.r0 = s.r0[lo] + part * per;
-  u.n = min(per, s.r1[lo] - u.r0);
-  return u;
-}
-
-// the i-th unit of this CTA, which is there
-__device__ __forceinline__ Unit unit_at(const Smem& sm, int m_tiles, int i) {
-  return i < kSched ? sm.sched[i] : find_unit(sm.groups, m_tiles, blockIdx.x + i * gridDim.x);
-}
-__device__ __forceinline__ Work work_of_cta(const Groups& g, int blocks, bool paired) {
-  Work w;
-  const int ctas = gridDim.x, cta = blockIdx.x;
-  if (paired && 2 * g.units <= ctas) {
-    w.rank = cta & 1;   // (CTAs 2p and 2p + 1 are a cluster)
-    w.units = cta / 2 < g.units ? 1 : 0;
-    w.first = w.rank == 0 ? 0 : (blocks + 1) / 2;
-    w.blocks = w.rank == 0 ? (blocks + 1) / 2 : blocks / 2;
-  } else {
-    w.rank = -1;
-    w.units = g.units > cta ? (g.units - cta - 1) / ctas + 1 : 0;
-    w.first = 0;
-    w.blocks = blocks;
-  }
-  return w;
+  return make_unit(s.e[lo], s.r0[lo], s.r1[lo], (s.r1[lo] - s.r0[lo] + kUnitRows - 1) / kUnitRows,
+                   m_tiles, unit - s.first[lo]);
 }
 
 // Waits with pauses, or, for the issuing warp (kPause 0), without.
@@ -410,7 +414,8 @@ __device__ __forceinline__ void issue(const Work& w, int m_tiles, Smem& sm, uint
         first = true;
         ++unit;
         acc.next(2);
-        if (left == 0 && ptx::elect_one()) ptx::mbar_arrive(d_full);
+        // (for the other warp's part of the sums, or for none)
+        if ((left == 0 || kWarps == 1) && ptx::elect_one()) ptx::mbar_arrive(d_full);
         __syncwarp();
       }
       if (!ok) break;
@@ -588,6 +593,7 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, c
       ptx::mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&sm.d_full[i], kMmaWarps);
       ptx::mbar_init(&sm.d_empty[i], 32 * kEpiWarps);
     }
     for (int i = 0; i < kMmaWarps; ++i) ptx::mbar_init(&sm.drain[i], 1);
@@ -599,16 +605,7 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, c
   pdl_wait();
   pdl_launch_dependents();
   const int m_tiles = kGated ? (s.N + 63) / 64 : (s.N + 127) / 128;
-  find_groups(a, m_tiles, sm);   // (synchronises the CTA)
-  const Work w = work_of_cta(sm.groups, s.blocks, paired);
-  if ((int)threadIdx.x < min(kSched, w.units))
-    sm.sched[threadIdx.x] =
-        find_unit(sm.groups, m_tiles, w.rank >= 0 ? blockIdx.x / 2 : blockIdx.x + threadIdx.x * gridDim.x);
-  const int issuers = mma_warps(sm.groups.widest);
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) ptx::mbar_init(&sm.d_full[i], issuers);
-    ptx::fence_mbarrier_init();
-  }
+  const Work w = find_work(a, m_tiles, s.blocks, paired, sm);
   // (a pair's barriers are there before the other CTA arrives on them, and until it has)
   if (w.rank >= 0) {
     ptx::cluster_arrive();
@@ -618,6 +615,7 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, c
   }
   ptx::tc_fence_after();
   const uint32_t tmem = sm.tmem;
+  const int issuers = mma_warps(sm.groups.widest);
   if (warp < kEpiWarps) epilogue<kGated>(a, s, w, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, w, m_tiles, sm, tmem);
   else if (warp < kMmaWarp) load_x(a, s, w, m_tiles, sm);

@@ -181,7 +181,9 @@ def test_q4_product_refusals(dm, lib):
         assert call(fn, y=None) == 1
         assert call(fn, y=FAKE) == 1                  # in place
         assert call(fn, y=FAKE * 2 + 2, ydt=2) == 1
-        assert call(fn, R=2 ** 30 + 1, T_x=2 ** 40) == 2
+        assert call(fn, R=2 ** 30 + 1, T_x=2 ** 30 + 1) == 2
+        # more units than 32 bits count
+        assert call(fn, R=2 ** 30, T_x=2 ** 30, groups=256, ids=FAKE) == 2
         for a in ("rows", "offsets", "ids"):
             assert call(fn, **{a: FAKE + 4}) == 1
         for i in range(n):
