@@ -23,18 +23,21 @@ __device__ __forceinline__ Q4Block q4_block(const Q4Shape& s, int n_experts) {
   return b;
 }
 
-// a / 7 to five significant bits, for a >= 2^-100 (the quotient is a normal number)
+// a / 7 to five significant bits, for a bf16 a of 2^-100 and more. A quotient of eight significant bits
+// by 7 is a tie of two such numbers or 2^-9 of itself and more away from one; the product with 1 / 7,
+// off by less than 2^-22, is brought back to a tie by a first rounding to 17 bits.
 __device__ __forceinline__ float q4_scale(float a) {
-  uint32_t u = __float_as_uint(a / 7.f);
+  uint32_t u = __float_as_uint(a * (1.f / 7.f));
+  u = (u + 0x40u) & ~0x7Fu;
   u = (u + 0x3FFFFu + (u >> 19 & 1u)) & ~0x7FFFFu;
   return __uint_as_float(u);
 }
 
-// rint(w / s) + 8 in the lower four bits, from inv = 1 / s rounded. The quotient of eight significant
+// rint(w / s) + 8 in the lower four bits, from inv = 1 / s within 2^-21. The quotient of eight significant
 // bits by five is a tie of two integers or 2^-9 and more away from one, and w * inv is off by less
 // than 2^-20: the sum with 384, rounded to 2^-15, brings a tie back to it and passes no other one.
-// The second sum rounds to an integer, ties to even. A zero inv gives 8, the code of zero. (With a
-// division for each weight, 134 M weights and back took 335 us.)
+// The second sum rounds to an integer, ties to even. A zero inv gives 8, the code of zero. (With
+// divisions for each weight and scale, 268 M weights and back took 335 us.)
 __device__ __forceinline__ uint32_t q4_nibble(float w, float inv) {
   return __float_as_uint(__fadd_rn(__fmaf_rn(w, inv, 384.f), 12582912.f + 8.f - 384.f));
 }
@@ -70,20 +73,27 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_
       top[r][c] = max(t & 0xFFFFu, t >> 16);
     }
   const int per = s.group / 32;   // 32-input chunks per group: 1, 2 or 4
-  float scale[2][4];
+  float scale[2][4], inv[2][4];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (per >= 2) {
-      top[r][0] = top[r][1] = max(top[r][0], top[r][1]);
-      top[r][2] = top[r][3] = max(top[r][2], top[r][3]);
+      top[r][0] = max(top[r][0], top[r][1]);
+      top[r][2] = max(top[r][2], top[r][3]);
     }
-    if (per == 4) top[r][0] = top[r][1] = top[r][2] = top[r][3] = max(top[r][0], top[r][2]);
+    if (per == 4) top[r][0] = max(top[r][0], top[r][2]);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
+      if (c % per != 0) {   // the same group as chunk 0, or chunk 2
+        const bool two = c == 3 && per == 2;
+        scale[r][c] = two ? scale[r][2] : scale[r][0];
+        inv[r][c] = two ? inv[r][2] : inv[r][0];
+        continue;
+      }
       const float a = __uint_as_float(top[r][c] << 16);
       // (the values' FMA holds 24 s: finite for a < 2^120)
-      scale[r][c] = top[r][c] >= (120u + 127u) << 7 ? __int_as_float(0x7FC00000)
-                                                    : a < 0x1p-100f ? 0.f : q4_scale(a);
+      const bool nan = top[r][c] >= (120u + 127u) << 7, zero = a < 0x1p-100f;
+      scale[r][c] = nan ? __int_as_float(0x7FC00000) : zero ? 0.f : q4_scale(a);
+      inv[r][c] = nan || zero ? 0.f : __fdividef(1.f, scale[r][c]);
     }
   }
   uint32_t word[2][4];
@@ -92,12 +102,11 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const uint32_t raw[4] = {v[r][c].x, v[r][c].y, v[r][c].z, v[r][c].w};
-      const float inv = scale[r][c] > 0.f ? 1.f / scale[r][c] : 0.f;
       uint32_t nibble[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        nibble[2 * i] = q4_nibble(__uint_as_float(raw[i] << 16), inv);
-        nibble[2 * i + 1] = q4_nibble(__uint_as_float(raw[i] & 0xFFFF0000u), inv);
+        nibble[2 * i] = q4_nibble(__uint_as_float(raw[i] << 16), inv[r][c]);
+        nibble[2 * i + 1] = q4_nibble(__uint_as_float(raw[i] & 0xFFFF0000u), inv[r][c]);
       }
       word[r][c] = q4_pack_word(nibble);
     }
