@@ -51,7 +51,9 @@ class _Gather(torch.autograd.Function):
 class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ys, pos, gates, add, tokens):
-        ctx.save_for_backward(ys, pos, gates)
+        # (the rows are needed for the gates' gradient only)
+        ctx.save_for_backward(ys if ctx.needs_input_grad[2] else None, pos, gates)
+        ctx.shape = ys.shape
         y = ys.new_empty((tokens, ys.shape[1]))
         dmoe_combine_rows(_rows(ys), pos, gates, None if add is None else _rows(add), y)
         return y
@@ -61,7 +63,7 @@ class _Combine(torch.autograd.Function):
     def backward(ctx, dy):
         ys, pos, gates = ctx.saved_tensors
         rows, gate = ctx.needs_input_grad[0], ctx.needs_input_grad[2]
-        dys = dy.new_empty(ys.shape) if rows else None
+        dys = dy.new_empty(ctx.shape) if rows else None
         dgates = torch.empty_like(gates) if gate else None
         if rows or gate:
             dmoe_combine_rows_backward(_rows(dy), _rows(ys) if gate else None, pos, gates, dys, dgates)
