@@ -49,7 +49,7 @@ dmoe_status check_q4(const dmoe_q4_desc* d) {
   if (d->n_experts <= 0 || d->n_out <= 0 || d->n_in <= 0 || d->group <= 0)
     return DMOE_ERR_INVALID_ARG;
   if (d->group != 32 && d->group != 64 && d->group != 128) return DMOE_ERR_UNSUPPORTED;
-  if (d->n_experts > kMaxExperts || d->n_out > 65536 || d->n_in > kMaxDModel ||
+  if (d->n_experts > kMaxQ4Experts || d->n_out > 65536 || d->n_in > kMaxDModel ||
       d->n_in % d->group != 0)
     return DMOE_ERR_UNSUPPORTED;
   return DMOE_OK;
@@ -65,7 +65,7 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   if (R < 0 || T_x < 0 || n_groups <= 0 || k <= 0 || ldx < desc->n_in || ldy < desc->n_out ||
       (y_dtype != DMOE_BF16 && y_dtype != DMOE_FP32))
     return DMOE_ERR_INVALID_ARG;
-  if (R > kMaxPairs || n_groups > kMaxExperts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
+  if (R > kMaxPairs || n_groups > kMaxQ4Experts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
   // the kernel counts its units (96 rows x 64 outputs of a group) in 32 bits, whatever the offsets hold
   if ((R / 96 + 1) * ((desc->n_out + 63) / 64) * n_groups > INT32_MAX) return DMOE_ERR_UNSUPPORTED;
   if ((offsets == nullptr && n_groups != 1) ||

@@ -14,6 +14,7 @@
 
 namespace dmoe {
 
+constexpr int kMaxQ4Experts = 512;   // (256 routed ones and a shared one are one set)
 constexpr int kQ4Rows = 32, kQ4Inputs = 128, kQ4CodeBytes = kQ4Rows * kQ4Inputs / 2;
 
 struct Q4Shape {

@@ -46,7 +46,7 @@ static_assert(kSets == kSlots && kLoadWarps == 2 * kSlots, "a set and two loadin
 constexpr uint64_t kWaitNs = 1000000000ull;
 constexpr int kSources = 1024;             // sorted rows whose sources are looked up once, together
 constexpr int kPairStages = 24;
-constexpr int kSched = 256;                // units of a CTA that are looked up once, together
+constexpr int kSched = 128;                // units of a CTA that are looked up once, together
 
 __device__ DevErrRecord q4_fault;          // of every call on the device
 
@@ -54,7 +54,7 @@ __device__ DevErrRecord q4_fault;          // of every call on the device
 struct Groups {
   int n;
   int widest;   // rows of the widest unit
-  int e[kMaxExperts], r0[kMaxExperts], r1[kMaxExperts], first[kMaxExperts];
+  int e[kMaxQ4Experts], r0[kMaxQ4Experts], r1[kMaxQ4Experts], first[kMaxQ4Experts];
 };
 
 // What this CTA does: its units, and of their stages those from `first` on.
@@ -89,9 +89,10 @@ struct Smem {
   uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
   uint64_t pair_ready, pair_full;            // the first CTA has room for the second's sums; has them
   uint32_t tmem;
-  int2 warp_groups[kMaxExperts / 32];        // of 32 groups: those with rows, and their units
+  int2 warp_groups[kMaxQ4Experts / 32];      // of 32 groups: those with rows, and their units
   int source[kSources];                      // row of x of the first sorted rows, or -1
 };
+static_assert(sizeof(Smem) <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ int source(const Q4Args& a, const Smem& sm, int r) {
   return a.rows == nullptr ? r : r < kSources ? sm.source[r] : find_source(a, r);
@@ -113,8 +114,8 @@ __device__ __forceinline__ Unit make_unit(int e, int r0, int r1, int parts, int 
 __device__ __forceinline__ Work find_work(const Q4Args& a, int m_tiles, int blocks, bool paired, Smem& sm) {
   Groups& s = sm.groups;
   const int u = threadIdx.x, lane = u & 31, warp = u >> 5, R = (int)a.R;
-  static_assert(kThreads >= kMaxExperts, "a thread per group");
-  constexpr int kWarps = kMaxExperts / 32;
+  static_assert(kThreads >= kMaxQ4Experts, "a thread per group");
+  constexpr int kWarps = kMaxQ4Experts / 32;
   int e = u, r0 = 0, r1 = 0;
   if (u < a.n_groups) {
     r1 = R;

@@ -8,8 +8,8 @@ from typing import Dict, Optional
 import torch
 
 from . import (DMOE_ROUTE_BLOCK, LayerDesc, alloc_q4, alloc_workspace, dmoe_combine_rows,
-               dmoe_dispatch, dmoe_layer_forward, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_swiglu,
-               dmoe_router, dmoe_router_prepare, make_desc, make_q4_desc)
+               dmoe_dispatch, dmoe_layer_forward, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_size,
+               dmoe_q4_swiglu, dmoe_router, dmoe_router_prepare, make_desc, make_q4_desc)
 
 WEIGHT_KEYS = ("w_r", "bias", "w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
 
@@ -61,13 +61,19 @@ class MoELayer:
 
 class Q4Weight:
     """Matrices in 4 bits with group scales: codes and scales of `desc`, quantised from bf16 [n_experts,
-    n_out, n_in] (or [n_out, n_in]: one matrix)."""
+    n_out, n_in]. `more` ([n_out, n_in], a shared expert's) is one more expert behind them."""
 
-    def __init__(self, w: torch.Tensor, group: int = 64, stream=None):
-        w = w.unsqueeze(0) if w.dim() == 2 else w
-        self.desc = make_q4_desc(*w.shape, group)
+    def __init__(self, w: torch.Tensor, group: int = 64, more: Optional[torch.Tensor] = None,
+                 stream=None):
+        E, n_out, n_in = w.shape
+        self.desc = make_q4_desc(E + (more is not None), n_out, n_in, group)
         self.codes, self.scales = alloc_q4(self.desc, w.device)
-        dmoe_q4_quantize(self.desc, w.contiguous(), self.codes, self.scales, stream=stream)
+        first = make_q4_desc(E, n_out, n_in, group)
+        nc, ns = dmoe_q4_size(first)
+        dmoe_q4_quantize(first, w.contiguous(), self.codes[:nc], self.scales[:ns], stream=stream)
+        if more is not None:
+            dmoe_q4_quantize(make_q4_desc(1, n_out, n_in, group), more.contiguous(), self.codes[nc:],
+                             self.scales[ns:], stream=stream)
 
 
 class MoELayerQ4:
@@ -86,21 +92,34 @@ class MoELayerQ4:
         T, k, E, d, I = desc.T, desc.top_k, desc.n_experts, desc.d_model, desc.d_ff
         Is = desc.d_ff_shared
         self.w_r, self.bias = weights["w_r"], weights.get("bias")
-        self.gate, self.up, self.down = (Q4Weight(weights[n], group)
-                                         for n in ("w_gate", "w_up", "w_down"))
-        self.shared = tuple(Q4Weight(weights[n], group)
-                            for n in ("ws_gate", "ws_up", "ws_down")) if Is > 0 else None
+        # A shared expert of the routed ones' size is one of them, with a group of all tokens behind the
+        # routed groups; one of another size has products of its own.
+        self.joined = Is == I
+        self.gate, self.up, self.down = (
+            Q4Weight(weights["w_" + n], group, weights["ws_" + n] if self.joined else None)
+            for n in ("gate", "up", "down"))
+        self.shared = tuple(Q4Weight(weights[n].unsqueeze(0), group)
+                            for n in ("ws_gate", "ws_up", "ws_down")) if Is > 0 and not self.joined else None
         self.ws = workspace if workspace is not None else alloc_workspace(desc, self.device)
 
         def new(*shape, dtype=torch.bfloat16):
             return torch.empty(shape, dtype=dtype, device=self.device)
-        i32 = torch.int32
+        i32, R = torch.int32, T * k
         self.topk_idx, self.topk_gate = new(T, k, dtype=i32), new(T, k, dtype=torch.float32)
-        self.n_unique, self.unique_ids = new(1, dtype=i32), new(E, dtype=i32)
-        self.offsets = new(E + 1, dtype=i32)
-        self.rows, self.pos = new(T * k, dtype=i32), new(T * k, dtype=i32)
-        self.h, self.ys, self.y = new(T * k, I), new(T * k, d), new(T, d)
-        self.hs, self.y_shared = (new(T, Is), new(T, d)) if Is > 0 else (None, None)
+        self.n_unique = new(1, dtype=i32)
+        # the dispatch's outputs, and behind them the shared expert's group
+        more = 1 if self.joined else 0
+        self.groups, self.ids = new(E + 1 + more, dtype=i32), new(E + more, dtype=i32)
+        self.all_rows = new(R + more * T, dtype=i32)
+        self.offsets, self.unique_ids = self.groups[:E + 1], self.ids[:E]
+        self.rows, self.pos = self.all_rows[:R], new(R, dtype=i32)
+        if self.joined:
+            self.groups[E + 1:].fill_(R + T)
+            self.ids[E:].fill_(E)
+            self.all_rows[R:] = torch.arange(0, R, k, dtype=i32, device=self.device)
+        self.h, self.ys, self.y = new(R + more * T, I), new(R + more * T, d), new(T, d)
+        self.hs = new(T, Is) if self.shared is not None else None
+        self.y_shared = self.ys[R:] if self.joined else new(T, d) if Is > 0 else None
         self.prepare()
 
     def prepare(self, stream=None) -> None:
@@ -121,14 +140,15 @@ class MoELayerQ4:
         dmoe_dispatch(self.desc, self.topk_idx, self.n_unique, self.unique_ids, self.offsets,
                       self.rows, self.pos, workspace=self.ws, stream=stream)
         g, u, d = self.gate, self.up, self.down
-        dmoe_q4_swiglu(g.desc, x, self.offsets, g.codes, g.scales, u.codes, u.scales, self.h,
-                       rows=self.rows, k=k, expert_ids=self.unique_ids, stream=stream)
-        dmoe_q4_linear(d.desc, self.h, self.offsets, d.codes, d.scales, self.ys,
-                       expert_ids=self.unique_ids, stream=stream)
+        dmoe_q4_swiglu(g.desc, x, self.groups, g.codes, g.scales, u.codes, u.scales, self.h,
+                       rows=self.all_rows, k=k, expert_ids=self.ids, stream=stream)
+        dmoe_q4_linear(d.desc, self.h, self.groups, d.codes, d.scales, self.ys,
+                       expert_ids=self.ids, stream=stream)
         if self.shared is not None:
             g, u, d = self.shared
             dmoe_q4_swiglu(g.desc, x, None, g.codes, g.scales, u.codes, u.scales, self.hs,
                            stream=stream)
             dmoe_q4_linear(d.desc, self.hs, None, d.codes, d.scales, self.y_shared, stream=stream)
-        dmoe_combine_rows(self.ys, self.pos, self.topk_gate, self.y_shared, out, stream=stream)
+        dmoe_combine_rows(self.ys[:self.desc.T * k], self.pos, self.topk_gate, self.y_shared, out,
+                          stream=stream)
         return out

@@ -165,6 +165,8 @@ def layer_bounds(shape, host, vals, svals, idx, gates):
 SHAPES = {"tiny": (TINY.with_(top_p=0.6), 32),
           "tiny token": (TINY.with_(mode=ROUTE_TOKEN), 64),
           "shared": (TINY.with_(d_ff_shared=128, block_size=24, n_blocks=3), 64),
+          "shared, larger": (TINY.with_(d_ff_shared=256, block_size=24, n_blocks=3), 64),
+          "one token": (TINY.with_(d_ff_shared=128, block_size=1, n_blocks=1, mode=ROUTE_TOKEN), 32),
           "block of 32": (LAYER.with_(n_experts=32), 128),
           "token routing": (LAYER.with_(n_experts=32, mode=ROUTE_TOKEN), 64)}
 

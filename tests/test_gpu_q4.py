@@ -251,6 +251,12 @@ def test_groups_with_their_own_experts(gated):
     check_products(6, 64, 128, 32, sizes, ids=ids, gated=gated)
 
 
+def test_as_many_groups_as_there_can_be():
+    check_many_units(512, 48, 128, 64, np.arange(512) % 3, True)
+    ids = np.random.default_rng(0).integers(-1, 8, 512).astype(np.int32)
+    check_products(7, 40, 128, 32, np.arange(512) % 3, ids=ids)
+
+
 @pytest.mark.parametrize("R", [1, 3, 40, 300])
 def test_dense(R):
     m = P.dm()

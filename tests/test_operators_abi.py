@@ -125,7 +125,7 @@ def test_row_refusals(lib, name):
 @pytest.mark.parametrize("kw,status", [
     (dict(n_experts=0), 1), (dict(n_out=0), 1), (dict(n_in=0), 1), (dict(group=0), 1),
     (dict(group=16), 2), (dict(group=96), 2), (dict(n_in=96, group=64), 2),
-    (dict(n_in=16384 + 64), 2), (dict(n_experts=257), 2), (dict(n_out=65537), 2)])
+    (dict(n_in=16384 + 64), 2), (dict(n_experts=513), 2), (dict(n_out=65537), 2)])
 def test_q4_desc_refusals(dm, lib, kw, status):
     a = dict(n_experts=4, n_out=24, n_in=128, group=64)
     a.update(kw)
@@ -162,7 +162,7 @@ def test_q4_product_refusals(dm, lib):
         assert call(fn, R=0) == 0                     # no rows: nothing to do
         assert call(fn, R=-1) == 1
         assert call(fn, groups=0) == 1
-        assert call(fn, groups=257, ids=FAKE) == 2
+        assert call(fn, groups=513, ids=FAKE) == 2
         assert call(fn, groups=5) == 1                # more groups than experts, without ids
         assert call(fn, groups=2, offsets=None) == 1
         assert call(fn, k=0) == 1
