@@ -377,7 +377,7 @@ dmoe_status dmoe_q4_dequantize(const dmoe_q4_desc* desc, const void* codes, cons
  *              [0, n_experts) are left out
  *   y          [R, n_out] out, bf16 or fp32 (y_dtype), row stride ldy. Rows that are in no group
  *              (from offsets[n_groups] on, the slots without an expert) are not written
- * 0 <= R <= 2^30; 1 <= n_groups <= 512; (R / 96 + 1) * ceil(n_out / 64) * n_groups < 2^31; offsets
+ * 0 <= R <= 2^30; 1 <= n_groups <= 512; (R / 64 + 1) * ceil(n_out / 64) * n_groups < 2^31; offsets
  * outside [0, R] are cut to it. */
 dmoe_status dmoe_q4_linear(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const void* x,
                            int64_t ldx, int64_t T_x, const int32_t* rows, int32_t k,

@@ -66,8 +66,8 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
       (y_dtype != DMOE_BF16 && y_dtype != DMOE_FP32))
     return DMOE_ERR_INVALID_ARG;
   if (R > kMaxPairs || n_groups > kMaxQ4Experts || k > kMaxTopK) return DMOE_ERR_UNSUPPORTED;
-  // the kernel counts its units (96 rows x 64 outputs of a group) in 32 bits, whatever the offsets hold
-  if ((R / 96 + 1) * ((desc->n_out + 63) / 64) * n_groups > INT32_MAX) return DMOE_ERR_UNSUPPORTED;
+  // the kernel counts its units (64 rows x 64 outputs of a group) in 32 bits, whatever the offsets hold
+  if ((R / 64 + 1) * ((desc->n_out + 63) / 64) * n_groups > INT32_MAX) return DMOE_ERR_UNSUPPORTED;
   if ((offsets == nullptr && n_groups != 1) ||
       (expert_ids == nullptr && n_groups > desc->n_experts) || (rows == nullptr && T_x < R))
     return DMOE_ERR_INVALID_ARG;

@@ -33,7 +33,10 @@ namespace {
 constexpr int kEpiWarps = 4, kSets = 4, kDeqWarps = 4 * kSets, kLoadWarps = 8, kMmaWarps = 2;
 constexpr int kLoadWarp = kEpiWarps + kDeqWarps, kMmaWarp = kLoadWarp + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + kMmaWarps);
-constexpr int kUnitRows = 96;              // rows of a group per unit, at most
+// Rows of a group per unit, at most: a launch has one of the two limits. With the smaller one a stage
+// takes two thirds to four fifths of the time; which one is better goes by the CTAs' turns
+// (unit_limit).
+constexpr int kUnitRows = 96, kSmallUnitRows = 64;
 // The ring of stages: A in tensor memory, 64 columns a slot, and B in shared memory. A slot is a set's
 // and two loading warps', and one pair of barriers serves both operands: an issuing warp's waits
 // and commits take as long as the MMAs of few rows (100 to 150 cycles each). There are two issuing
@@ -53,7 +56,7 @@ __device__ DevErrRecord q4_fault;          // of every call on the device
 // The groups that have rows and an expert, in order, and their first units.
 struct Groups {
   int n;
-  int widest;   // rows of the widest unit
+  int limit;    // rows of a unit, at most
   int e[kMaxQ4Experts], r0[kMaxQ4Experts], r1[kMaxQ4Experts], first[kMaxQ4Experts];
 };
 
@@ -89,13 +92,32 @@ struct Smem {
   uint64_t d_full[2], d_empty[2], drain[kMmaWarps];
   uint64_t pair_ready, pair_full;            // the first CTA has room for the second's sums; has them
   uint32_t tmem;
-  int2 warp_groups[kMaxQ4Experts / 32];      // of 32 groups: those with rows, and their units
+  int4 warp_groups[kMaxQ4Experts / 32];      // of 32 groups: those with rows; rows; units by either limit
   int source[kSources];                      // row of x of the first sorted rows, or -1
 };
 static_assert(sizeof(Smem) <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ int source(const Q4Args& a, const Smem& sm, int r) {
   return a.rows == nullptr ? r : r < kSources ? sm.source[r] : find_source(a, r);
+}
+
+// Where there are at most half as many units as CTAs, a pair of CTAs shares one.
+__device__ __forceinline__ bool share_units(int units, int ctas, bool paired) {
+  return paired && units <= ctas / 2;
+}
+// The limit of a launch, from the units that there are with either (of `rows` rows and tiles in all): a
+// stage of n rows takes about as long as (100 + n) / 0.44 ns, so the limit is the one whose turns
+// (halves, in pairs) times that are less. (256 rows times 8192 x 8192, two turns with either: 51 us
+// with 64 and 55 with 96. 2048 rows times 4096 x 4096, seven and five turns: 86 and 74.)
+__device__ __forceinline__ float unit_cost(float rows, int units, int ctas, bool paired) {
+  const uint32_t halves = share_units(units, ctas, paired) ? 1u : 2u * ((uint32_t)(units - 1) / (uint32_t)ctas + 1u);
+  return (float)halves * (100.f + __fdividef(rows, (float)units));
+}
+__device__ __forceinline__ int unit_limit(float rows, int small_units, int large_units, int ctas,
+                                          bool paired) {
+  return small_units == large_units ||
+                 unit_cost(rows, small_units, ctas, paired) <= unit_cost(rows, large_units, ctas, paired)
+             ? kSmallUnitRows : kUnitRows;
 }
 
 // A group's rows are cut into parts of about the same size, each a unit per tile of outputs.
@@ -130,31 +152,41 @@ __device__ __forceinline__ Work find_work(const Q4Args& a, int m_tiles, int bloc
   r0 = max(r0, 0);
   r1 = min(r1, R);
   const bool live = r0 < r1 && e >= 0 && e < a.n_experts;
-  const int parts = live ? (r1 - r0 + kUnitRows - 1) / kUnitRows : 0;
+  const int size = live ? r1 - r0 : 0;
   const uint32_t m = __ballot_sync(0xffffffffu, live);
-  const int units = parts * m_tiles;   // (their sum over the groups fits: checked on the host)
-  int end = units;                     // inclusive sum over the warp
+  // (the sums of the units over the groups fit: checked on the host)
+  const int small_units = (size + kSmallUnitRows - 1) / kSmallUnitRows * m_tiles;
+  const int large_units = (size + kUnitRows - 1) / kUnitRows * m_tiles;
+  const int warp_small = __reduce_add_sync(0xffffffffu, small_units);
+  const int warp_large = __reduce_add_sync(0xffffffffu, large_units);
+  const int warp_rows = __reduce_add_sync(0xffffffffu, size);
+  if (lane == 0 && warp < kWarps)
+    sm.warp_groups[warp] = make_int4(__popc(m), warp_rows, warp_small, warp_large);
+  __syncthreads();
+  const int4 v = sm.warp_groups[lane & (kWarps - 1)];   // every warp adds them up
+  const uint32_t all_lanes = 0xffffffffu;
+  static_assert(kWarps <= 32 && (kWarps & (kWarps - 1)) == 0, "a lane per warp of groups");
+  const bool counts = lane < kWarps, before = counts && lane < warp;
+  const int all_small = __reduce_add_sync(all_lanes, counts ? v.z : 0);
+  const int all_large = __reduce_add_sync(all_lanes, counts ? v.w : 0);
+  const int rows = __reduce_add_sync(all_lanes, counts ? v.y : 0);
+  const int limit = unit_limit((float)rows * (float)m_tiles, all_small, all_large, gridDim.x, paired);
+  const bool small = limit == kSmallUnitRows;
+  const int all = small ? all_small : all_large, units = small ? small_units : large_units;
+  const int parts = (size + limit - 1) / limit;
+  const int n = __reduce_add_sync(all_lanes, counts ? v.x : 0);
+  const int at = __reduce_add_sync(all_lanes, before ? v.x : 0) + __popc(m & ((1u << lane) - 1u));
+  int end = units;   // inclusive sum over the groups
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, end, o);
-    if (lane >= o) end += v;
+    const int k = __shfl_up_sync(all_lanes, end, o);
+    if (lane >= o) end += k;
   }
-  if (u == 0) s.widest = 0;
-  if (lane == 31 && warp < kWarps) sm.warp_groups[warp] = make_int2(__popc(m), end);
-  __syncthreads();
-  int at = __popc(m & ((1u << lane) - 1u)), n = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const int2 v = sm.warp_groups[w];
-    at += w < warp ? v.x : 0;
-    end += w < warp ? v.y : 0;
-    n += v.x;
-    all += v.y;
-  }
+  end += __reduce_add_sync(all_lanes, before ? small ? v.z : v.w : 0);
   Work w;
   const int ctas = gridDim.x, cta = blockIdx.x;
   int first = cta;   // this CTA's first unit; the others are `ctas` apart
-  if (paired && 2 * all <= ctas) {
+  if (share_units(all, ctas, paired)) {
     w.rank = cta & 1;   // (CTAs 2p and 2p + 1 are a cluster)
     first = cta / 2;
     w.units = first < all ? 1 : 0;
@@ -172,13 +204,15 @@ __device__ __forceinline__ Work find_work(const Q4Args& a, int m_tiles, int bloc
     s.r0[at] = r0;
     s.r1[at] = r1;
     s.first[at] = begin;
-    atomicMax(&s.widest, (r1 - r0 + parts - 1) / parts);
     for (int i = begin > first ? (begin - first + ctas - 1) / ctas : 0; i < min(kSched, w.units); ++i) {
       if (first + i * ctas >= end) break;
       sm.sched[i] = make_unit(e, r0, r1, parts, m_tiles, first + i * ctas - begin);
     }
   }
-  if (u == 0) s.n = n;
+  if (u == 0) {
+    s.n = n;
+    s.limit = limit;
+  }
   return w;
 }
 
@@ -193,8 +227,8 @@ __device__ __forceinline__ Unit unit_at(const Smem& sm, int m_tiles, int i) {
     if (s.first[mid] <= unit) lo = mid;
     else hi = mid - 1;
   }
-  return make_unit(s.e[lo], s.r0[lo], s.r1[lo], (s.r1[lo] - s.r0[lo] + kUnitRows - 1) / kUnitRows,
-                   m_tiles, unit - s.first[lo]);
+  return make_unit(s.e[lo], s.r0[lo], s.r1[lo], (s.r1[lo] - s.r0[lo] + s.limit - 1) / s.limit, m_tiles,
+                   unit - s.first[lo]);
 }
 
 // Waits with pauses, or, for the issuing warp (kPause 0), without.
@@ -376,8 +410,9 @@ __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, const 
 
 // ------------------------------------------------------------------ issuing the MMAs
 // Issuing warps: with more than 64 rows the MMAs take longer than their issue, and one warp does all (two
-// buffers of both warps' sums would not fit).
-__device__ __forceinline__ int mma_warps(int widest) { return widest <= 64 ? 2 : 1; }
+// buffers of both warps' sums would not fit). With one for few rows too, 256 rows for 104 experts
+// took 22.8 us, not 21.3, and 64 rows times 8192 x 8192 24.4, not 24.1.
+__device__ __forceinline__ int mma_warps(int limit) { return limit == kSmallUnitRows ? 2 : 1; }
 __device__ __forceinline__ uint32_t acc_column(int warps, int buffer, int warp) {
   return kAcc0 + buffer * 128 + (warps == 2 ? warp * 64 : 0);
 }
@@ -468,7 +503,7 @@ template <bool kGated>
 __device__ __forceinline__ void epilogue(const Q4Args& a, const Q4Shape& s, const Work& w, int m_tiles,
                                          Smem& sm, uint32_t tmem) {
   const int warp = warp_number(), lane = threadIdx.x & 31, row = threadIdx.x;   // row: lane of tensor memory
-  const int warps = mma_warps(sm.groups.widest);
+  const int warps = mma_warps(sm.groups.limit);
   const int size = a.y_fp32 ? 4 : 2;
   const int64_t step = a.ldy * size;
   const bool pairs = ((reinterpret_cast<uintptr_t>(a.y) | (uint64_t)step) & (2 * size - 1)) == 0;
@@ -616,7 +651,7 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, c
   }
   ptx::tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  const int issuers = mma_warps(sm.groups.widest);
+  const int issuers = mma_warps(sm.groups.limit);
   if (warp < kEpiWarps) epilogue<kGated>(a, s, w, m_tiles, sm, tmem);
   else if (warp < kLoadWarp) dequantise<kGated>(a, s, w, m_tiles, sm, tmem);
   else if (warp < kMmaWarp) load_x(a, s, w, m_tiles, sm);
@@ -651,7 +686,7 @@ cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_
   // at most as many CTAs as units there can be, and as run at once
   const int64_t groups = a.n_groups < a.R ? a.n_groups : a.R;
   const int64_t tiles = gated ? (s.N + 63) / 64 : (s.N + 127) / 128;
-  const int64_t units = (groups + a.R / kUnitRows) * tiles;
+  const int64_t units = (groups + a.R / kSmallUnitRows) * tiles;
   const int sms = device_sm_count();
   auto* kernel = gated ? q4_kernel<true> : q4_kernel<false>;
   if (s.blocks >= kPairStages && 2 * tiles <= sms)

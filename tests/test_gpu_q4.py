@@ -245,6 +245,15 @@ def test_more_units_than_a_cta_looks_up_at_once():
 
 
 @pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n,N,K", [(30, 320, 128), (61, 320, 256), (3, 4224, 256), (12, 8192, 128),
+                                   (1, 4224, 3200), (1, 8192, 3200)])
+def test_groups_between_the_two_limits(n, N, K, gated):
+    """Groups of 65 to 96 rows, of one unit or two for each tile of outputs, in one turn of the CTAs or
+    more, and in pairs."""
+    check_many_units(n, N, K, 64, np.random.default_rng(n).integers(65, 97, n), gated, seed=n)
+
+
+@pytest.mark.parametrize("gated", [False, True])
 def test_groups_with_their_own_experts(gated):
     ids = np.array([3, 3, -1, 0, 6, 2, 2 ** 31 - 1], np.int32)         # twice the same; three left out
     sizes = np.array([5, 2, 4, 0, 3, 40, 6])
