@@ -375,3 +375,30 @@ def test_on_another_stream_and_replayed():
     again = y.clone()
     m.dmoe_q4_swiglu(desc, x, off, *packed, y)
     assert torch.equal(y, again)
+
+
+def test_offsets_past_32_bits():
+    """Matrices whose last one lies behind 2^31 bytes of codes, and rows behind 2^31 elements: the same
+    values as alone and close together."""
+    m = P.dm()
+    E, N, K, g, R = 20, 16384, 16384, 64, 12
+    desc, one = m.make_q4_desc(E, N, K, g), m.make_q4_desc(1, N, K, g)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    w = torch.zeros((E, N, K), dtype=BF16, device="cuda")
+    w[-1] = torch.randn((N, K), generator=gen, device="cuda", dtype=BF16) * 0.02
+    packed, alone = pack(desc, w), pack(one, w[-1:])
+    values = torch.empty_like(w[-1:])
+    m.dmoe_q4_dequantize(one, *alone, values)
+    m.dmoe_q4_dequantize(desc, *packed, w)
+    assert torch.equal(w[-1:], values) and not w[:-1].any()
+    del w, values
+    x = torch.randn((R, K), generator=gen, device="cuda").to(BF16)
+    near = torch.empty((R, N), dtype=BF16, device="cuda")
+    far_x, far_y = (torch.empty((R, 1 << 28), dtype=BF16, device="cuda")[:, :n] for n in (K, N))
+    far_x.copy_(x)
+    ids = torch.tensor([E - 1], dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, R], dtype=torch.int32, device="cuda")
+    m.dmoe_q4_linear(one, x, None, *alone, near)
+    m.dmoe_q4_linear(desc, far_x, offsets, *packed, far_y, expert_ids=ids)
+    assert near.any() and torch.equal(far_y, near)
+    assert m.dmoe_q4_device_error()[0] == 0

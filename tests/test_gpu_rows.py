@@ -295,3 +295,36 @@ def test_on_another_stream_and_replayed():
         want = O.sort_tokens(idx.cpu().numpy(), E)
         assert np.array_equal(got[2].cpu().numpy(), want[2])
         assert np.array_equal(f64(got[3]), O.gather(f64(x), want[2], k))
+
+
+def test_offsets_past_32_bits():
+    """Rows so far apart that the last ones lie behind 2^31 elements: the same values as close together."""
+    m = P.dm()
+    T, k, d, E = 6, 2, 80, 5
+    idx = make_idx(T, k, E, 0)
+    idx[4, 1] = -1
+    pos = sort(idx, E)[0][2]
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    far_t, far_r, far_o = (torch.empty((n, 1 << 28 << (n == T)), dtype=torch.bfloat16, device="cuda")[:, :d]
+                           for n in (T, T * k, T * k))
+    x, ys, dy = (torch.randn((n, d), generator=gen, device="cuda").to(torch.bfloat16)
+                 for n in (T, T * k, T))
+    gates = torch.rand((T, k), generator=gen, device="cuda")
+
+    near = torch.empty_like(ys)
+    m.dmoe_gather_rows(x, pos, near)
+    far_t.copy_(x)
+    m.dmoe_gather_rows(far_t, pos, far_r)
+    assert torch.equal(far_r, near)
+
+    near = torch.empty_like(x)
+    m.dmoe_combine_rows(ys, pos, gates, None, near)
+    far_r.copy_(ys)
+    m.dmoe_combine_rows(far_r, pos, gates, None, far_t)
+    assert torch.equal(far_t, near)
+
+    near, dgates, far_gates = torch.empty_like(ys), torch.empty_like(gates), torch.empty_like(gates)
+    m.dmoe_combine_rows_backward(dy, ys, pos, gates, near, dgates)
+    far_t.copy_(dy)
+    m.dmoe_combine_rows_backward(far_t, far_r, pos, gates, far_o, far_gates)
+    assert torch.equal(far_o, near) and torch.equal(far_gates, dgates)
