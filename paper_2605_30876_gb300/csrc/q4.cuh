@@ -1,11 +1,11 @@
 // 4-bit expert matrices: the layout shared by the kernels that write and read it.
 //
-// A matrix is cut into tiles of 32 rows, a tile into blocks of 128 inputs: 2048 bytes of codes, for
-// a warp whose lanes have the rows. In them every row's inputs 0 .. 31
-// come first, 16 bytes a row, then every row's 32 .. 63, and so on. Word w of the 16 bytes has inputs
-// 8w .. 8w + 7: input 2i of them is the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19,
-// counted around the word's end: a rotation and a mask leave a pair of them in the upper mantissa
-// bits of two bf16 halves. A nibble is the code + 8.
+// A matrix is cut into tiles of 32 rows, a tile into blocks of 128 inputs: 2048 bytes of codes, for a
+// warp whose lanes have the rows. In them every row's inputs 0 .. 31 come first, 16 bytes a row, then
+// every row's 32 .. 63, and so on. Word w of the 16 bytes has inputs 8w .. 8w + 7: input 2i of them is
+// the nibble at bit 4i + 3 and input 2i + 1 the one at bit 4i + 19, counted around the word's end:
+// a rotation and a mask leave a pair of them in the upper mantissa bits of two bf16 halves. A nibble
+// is the code + 8.
 // Scales: bf16, per tile and block every row's groups of the block (4, 2 or 1).
 // Rows behind n_out and inputs behind n_in have codes and scales of zero.
 #pragma once
@@ -14,7 +14,7 @@
 
 namespace dmoe {
 
-constexpr int kMaxQ4Experts = 512;   // (256 routed ones and a shared one are one set)
+constexpr int kMaxQ4Experts = 512;   // (256 routed experts and a shared one are one set)
 constexpr int kQ4Rows = 32, kQ4Inputs = 128, kQ4CodeBytes = kQ4Rows * kQ4Inputs / 2;
 
 struct Q4Shape {

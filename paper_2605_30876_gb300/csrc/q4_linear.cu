@@ -1,21 +1,31 @@
 // Products of sorted rows with their experts' 4-bit matrices, plain or gate and up with SwiGLU:
-// y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 96 rows of a group.
+// y^T = W x^T, per unit of 128 outputs (or 64 gate and 64 up outputs) and at most 64 or 96 rows of a
+// group.
 //
 // A persistent CTA per SM, in roles, by stages of 128 inputs:
 //   dequantising warps (four sets of four, a stage each in turn): a lane has a row of W. Its codes come
-//       by asynchronous copies (a bulk copy per warp took longer to start); they become bf16 values by one exact FMA per pair
-//       and go to tensor memory: the A operand of the MMAs. Through shared memory they would take
-//       four times the codes' bytes twice, and 8 KB of codes have 368 cycles of an SM's share of
-//       HBM's rate, in which shared memory moves 46 KB.
+//       by asynchronous copies (bulk copies, one per warp and stage, were slower); they become bf16
+//       values by one exact FMA per pair and go to tensor memory: the A operand of the MMAs. Through
+//       shared memory they would take four times the codes' bytes twice, and 8 KB of codes have
+//       368 cycles of an SM's share of HBM's rate, in which shared memory moves 46 KB.
 //   loading warps: the rows of x that the group names, a stage each in turn, by copies of 16 bytes
 //       into shared memory (B). Between the copies and the tensor pipe's reads is a fence of 200
 //       cycles and more, so several stages are under way. (TMA gathers of four rows need no fence,
 //       but took 80 cycles each: for 64 rows 2500 cycles a stage.)
 //   two issuing warps: tcgen05.mma, M = 128 outputs, N = the unit's rows in sixteens
 //   epilogue warps: sums from tensor memory, SwiGLU, y
-// Few rows: the weights' bytes are the bound, and the instructions per code are close to it: 64 pairs
-// a lane and stage at 2.75, of the 368 that each scheduler issues in that time. Many rows: the
-// tensor pipe, and the copies of x.
+//
+// Few rows: the weights' bytes are the bound, and the instructions per code are close to it (64 pairs a
+// lane and stage at 2.75 instructions, of the 368 that a scheduler issues in an SM's share of the
+// time). Measured with cold weights in a graph, floors at 6.8 TB/s: 256 rows for 104 experts,
+// 512 x 2048, 20.8 us (62 MB, 9.2 us): issue slots 65 % busy, the ALUs 56 %, DRAM 45 %; one row
+// times 8192 x 8192 17.2 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
+// 61 us (36.6 us: 4.1 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
+// look-up of groups and rows and the first bytes' way from HBM are about half.
+// Many rows: the issue slots, which the values, the copies of x and the epilogue share; the MMAs of 96
+// rows take about as long. 2048 rows times 4096 x 4096 75 us (920 TFLOP/s), 2048 x 8 rows for 256
+// experts, gate and up of 2048 x 512, 119 us (580 TFLOP/s; 64 rows an expert).
+//
 // With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
 // CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
 // its own. One row times 8192 x K, alone and in pairs: K = 2048 8.4 and 8.5 us, 4096 12.1 and 10.5,

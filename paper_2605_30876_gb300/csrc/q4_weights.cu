@@ -1,5 +1,8 @@
 // bf16 weights to 4-bit codes and group scales, and back. One warp takes 16 rows x 128 inputs
-// (whole groups of every size): 4 KB of weights. Bound by the bytes.
+// (whole groups of every size): 4 KB of weights. 268 M weights (256 matrices of 512 x 2048, groups of
+// 64): quantising 133 us, the values back 100 us (both 232 us, cold, with 200 us of bytes at 6.8 TB/s).
+// Quantising is bound by its instructions (issue slots 84 % busy, DRAM about three quarters), the way
+// back by the bytes (DRAM 79 %).
 #include "q4.cuh"
 
 namespace dmoe {

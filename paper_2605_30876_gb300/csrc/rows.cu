@@ -1,7 +1,11 @@
 // Token rows into the experts' order and back, and the gradients of both. All four are copies and
 // short sums: they are bound by the bytes of the rows (each read once and written once), so the work
-// is cut by tokens: a token's row is held in registers while its k sorted rows are written or
-// read, and no row of x or dy is read k times.
+// is cut by tokens: a token's row is held in registers while its k sorted rows are written or read.
+// Rows of bf16 2048 wide, 16384 tokens of eight slots, a tenth without an expert, cold: gather 92 us
+// (6.6 TB/s), its gradient 88 (6.25), combine with an addend 99 (6.25), its gradient 164 (6.65);
+// of the 6.8 TB/s that a copy reaches. Widths that only allow 2-byte pieces are bound by their loads'
+// number: 8192 tokens of four slots, 1001 wide: gather 21.5 us (3.8 TB/s), combine's gradient 42
+// (3.4).
 #include <cuda_fp16.h>
 
 #include "block_reduce.cuh"
@@ -164,9 +168,10 @@ combine_rows_kernel(const T* __restrict__ ys, int64_t ldys, const int32_t* __res
 }
 
 // combine's gradient: a warp has a (token, slot). It goes over dy's row and the slot's row of ys, four
-// pieces of both on their way (more where they are narrow), writes gate * dy and adds up dy * ys. The k warps of a token read
-// dy's row k times, from L1 or L2 but for the first (held in registers for all k slots at once,
-// the pieces took so many that half the threads fitted: 221 us instead of 16384 x 8 rows of 2048).
+// pieces of both on their way (more where they are narrow), writes gate * dy and adds up dy * ys. The
+// k warps of a token read dy's row k times, from L1 or L2 but for the first. (With dy's pieces held
+// in registers for all k slots at once half as many threads fitted: 221 us, not 164, for 16384
+// tokens of eight slots, 2048 wide.)
 template <typename T, int VB, bool kRows, bool kGates>
 __global__ void __launch_bounds__(kRowThreads)
 combine_rows_backward_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ ys,
