@@ -37,15 +37,6 @@ inline Q4Shape q4_shape(const dmoe_q4_desc& d) {
   return s;
 }
 
-// A word of eight nibbles, given in the lower bits.
-__device__ __forceinline__ uint32_t q4_pack_word(const uint32_t (&nibble)[8]) {
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w |= (nibble[2 * i] & 15u) << (4 * i) | (nibble[2 * i + 1] & 15u) << (16 + 4 * i);
-  return __funnelshift_l(w, w, 3);
-}
-
 // A scale as the two operands of the values' FMA: s and -24 s, in both halves.
 struct Q4Scale {
   __nv_bfloat162 s, b;

@@ -1,8 +1,8 @@
 // bf16 weights to 4-bit codes and group scales, and back. One warp takes 16 rows x 128 inputs
-// (whole groups of every size): 4 KB of weights. 268 M weights (256 matrices of 512 x 2048, groups of
-// 64): quantising 133 us, the values back 100 us (both 232 us, cold, with 200 us of bytes at 6.8 TB/s).
-// Quantising is bound by its instructions (issue slots 84 % busy, DRAM about three quarters), the way
-// back by the bytes (DRAM 79 %).
+// (whole groups of every size): 4 KB of weights. Bound by the bytes: 268 M weights (256 matrices of
+// 512 x 2048, groups of 64) are quantised in 104 us and brought back in 98.5 (DRAM 76 and 80 % busy;
+// both in a row 200 us, what their bytes take at 6.8 TB/s). Quantising is close to its instructions,
+// too (issue slots 66 %): each lane finds the scale of a quarter of the rows' groups.
 #include "q4.cuh"
 
 namespace dmoe {
@@ -14,15 +14,15 @@ struct Q4Block {   // a warp's 16 x 128 weights
   int e, nt, kb;
   bool ok;
 };
+// (At most 2^28 warps, and 32-bit divisions: with 64-bit ones quantising took 3 us more.)
 __device__ __forceinline__ Q4Block q4_block(const Q4Shape& s, int n_experts) {
-  int64_t i = (int64_t)blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5);
+  const uint32_t i = blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5), blocks = s.blocks,
+                 tiles = 2 * s.tiles, j = i / blocks, e = j / tiles;
   Q4Block b;
-  b.kb = (int)(i % s.blocks);
-  i /= s.blocks;
-  b.nt = (int)(i % (2 * s.tiles));
-  i /= 2 * s.tiles;
-  b.e = (int)i;
-  b.ok = i < n_experts;
+  b.kb = (int)(i - j * blocks);
+  b.nt = (int)(j - e * tiles);
+  b.e = (int)e;
+  b.ok = b.e < n_experts;
   return b;
 }
 
@@ -36,16 +36,56 @@ __device__ __forceinline__ float q4_scale(float a) {
   return __uint_as_float(u);
 }
 
-// rint(w / s) + 8 in the lower four bits, from inv = 1 / s within 2^-21. The quotient of eight significant
-// bits by five is a tie of two integers or 2^-9 and more away from one, and w * inv is off by less
-// than 2^-20: the sum with 384, rounded to 2^-15, brings a tie back to it and passes no other one.
-// The second sum rounds to an integer, ties to even. A zero inv gives 8, the code of zero. (With
-// divisions for each weight and scale, 268 M weights and back took 335 us.)
-__device__ __forceinline__ uint32_t q4_nibble(float w, float inv) {
-  return __float_as_uint(__fadd_rn(__fmaf_rn(w, inv, 384.f), 12582912.f + 8.f - 384.f));
+// rint(w / s) + 8 in the lower bits, for a pair of weights, from inv = 1 / s within 2^-21. The quotient of
+// eight significant bits by five is a tie of two integers or 2^-9 and more away from one, and w * inv
+// is off by less than 2^-20: the sum with 384, rounded to 2^-15, brings a tie back to it and passes
+// no other one. The second sum rounds to an integer, ties to even: kNibble's bits and 1 .. 15 more
+// (a zero inv gives 8, the code of zero). With divisions for each weight and scale, 268 M weights
+// and back took 335 us; with sums of one weight at a time, their lower bits masked, shifted and
+// joined, 232 (144 of them quantising, bound by the ALUs).
+constexpr uint32_t kNibble = 0x4B400000u;   // 1.5 * 2^23
+__device__ __forceinline__ uint2 q4_nibble_pair(uint32_t two_bf16, float inv) {
+  uint2 r;
+  asm("{\n\t"
+      ".reg .b64 w, i, s, m;\n\t"
+      "mov.b64 w, {%2, %3};\n\t"
+      "mov.b64 i, {%4, %4};\n\t"
+      "mov.b64 s, {%5, %5};\n\t"
+      "mov.b64 m, {%6, %6};\n\t"
+      "fma.rn.f32x2 w, w, i, s;\n\t"
+      "add.rn.f32x2 w, w, m;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t"
+      "}"
+      : "=r"(r.x), "=r"(r.y)
+      : "r"(two_bf16 << 16), "r"(two_bf16 & 0xFFFF0000u), "r"(__float_as_uint(inv)),
+        "r"(__float_as_uint(384.f)), "r"(__float_as_uint(12582912.f + 8.f - 384.f)));
+  return r;
+}
+// Four such pairs as a word of codes. The products shift the nibbles to their places, and the sum starts
+// from minus what kNibble's bits come to there. (A NaN fills its word; its group's values are NaNs.)
+__device__ __forceinline__ uint32_t q4_word(const uint4& w, float inv) {
+  const uint32_t two[4] = {w.x, w.y, w.z, w.w};
+  uint32_t sum = 0u - kNibble * 0x11111111u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint2 n = q4_nibble_pair(two[i], inv);
+    sum += n.x * (1u << 4 * i);
+    sum += n.y * (1u << (16 + 4 * i));
+  }
+  return __funnelshift_l(sum, sum, 3);
 }
 
-__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
+// the larger magnitudes of eight weights' four pairs
+__device__ __forceinline__ uint32_t max8(const uint4& w) {
+  const uint32_t m = 0x7FFF7FFFu;
+  return __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m));
+}
+
+// of both halves, with what the lane kLane away sends
+template <int kLane>
+__device__ __forceinline__ uint32_t max_with(uint32_t mine, uint32_t sent) {
+  return __vmaxu2(mine, __shfl_xor_sync(0xffffffffu, sent, kLane));
+}
 
 __global__ void __launch_bounds__(kQ4Threads)
 q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_t* __restrict__ codes,
@@ -56,7 +96,6 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_
   if (!b.ok) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   uint4 v[2][4];       // rows g and g + 8; 32 inputs each
-  uint32_t top[2][4];  // the largest magnitude, as the bits of a bf16
 #pragma unroll
   for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -65,66 +104,43 @@ q4_quantize_kernel(Q4Shape s, int n_experts, const uint4* __restrict__ w, uint8_
       v[r][c] = n < s.N && k < s.K
                     ? __ldcs(w + (((size_t)b.e * s.N + n) * s.K + k) / 8) : make_uint4(0, 0, 0, 0);
     }
+  // the largest magnitudes of the 32 inputs, as the bits of two bf16 (row g's the lower)
+  uint32_t top[4];
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t m = 0x7FFF7FFFu;
-      uint32_t t = max2(max2(v[r][c].x & m, v[r][c].y & m), max2(v[r][c].z & m, v[r][c].w & m));
-      t = max2(t, __shfl_xor_sync(0xffffffffu, t, 1));
-      t = max2(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      top[r][c] = max(t & 0xFFFFu, t >> 16);
-    }
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t low = max8(v[0][c]), high = max8(v[1][c]);
+    top[c] = __vmaxu2(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
+  }
+  // over the four lanes of the rows: lane q gets those of chunk q, then of its group
+  const bool upper = (q & 2) != 0, odd = (q & 1) != 0;
+  const uint32_t even = max_with<2>(upper ? top[2] : top[0], upper ? top[0] : top[2]),
+                 other = max_with<2>(upper ? top[3] : top[1], upper ? top[1] : top[3]);
+  uint32_t mine = max_with<1>(odd ? other : even, odd ? even : other);
   const int per = s.group / 32;   // 32-input chunks per group: 1, 2 or 4
-  float scale[2][4], inv[2][4];
+  if (per >= 2) mine = max_with<1>(mine, mine);
+  if (per == 4) mine = max_with<2>(mine, mine);
+  float scale[2], inv[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    if (per >= 2) {
-      top[r][0] = max(top[r][0], top[r][1]);
-      top[r][2] = max(top[r][2], top[r][3]);
-    }
-    if (per == 4) top[r][0] = max(top[r][0], top[r][2]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (c % per != 0) {   // the same group as chunk 0, or chunk 2
-        const bool two = c == 3 && per == 2;
-        scale[r][c] = two ? scale[r][2] : scale[r][0];
-        inv[r][c] = two ? inv[r][2] : inv[r][0];
-        continue;
-      }
-      const float a = __uint_as_float(top[r][c] << 16);
-      // (the values' FMA holds 24 s: finite for a < 2^120)
-      const bool nan = top[r][c] >= (120u + 127u) << 7, zero = a < 0x1p-100f;
-      scale[r][c] = nan ? __int_as_float(0x7FC00000) : zero ? 0.f : q4_scale(a);
-      inv[r][c] = nan || zero ? 0.f : __fdividef(1.f, scale[r][c]);
-    }
+    const float a = __uint_as_float(r == 0 ? mine << 16 : mine & 0xFFFF0000u);
+    // (the values' FMA holds 24 s: finite for a < 2^120)
+    const bool nan = !(a < 0x1p120f), zero = a < 0x1p-100f;
+    scale[r] = nan ? __int_as_float(0x7FC00000) : zero ? 0.f : q4_scale(a);
+    inv[r] = nan || zero ? 0.f : __fdividef(1.f, scale[r]);
   }
-  uint32_t word[2][4];
-#pragma unroll
-  for (int r = 0; r < 2; ++r)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t raw[4] = {v[r][c].x, v[r][c].y, v[r][c].z, v[r][c].w};
-      uint32_t nibble[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        nibble[2 * i] = q4_nibble(__uint_as_float(raw[i] << 16), inv[r][c]);
-        nibble[2 * i + 1] = q4_nibble(__uint_as_float(raw[i] & 0xFFFF0000u), inv[r][c]);
-      }
-      word[r][c] = q4_pack_word(nibble);
-    }
   const size_t block = ((size_t)b.e * s.tiles + b.nt / 2) * s.blocks + b.kb;
   const int row = b.nt % 2 * 16 + g;   // of the tile, and the one 8 behind it
   uint8_t* to = codes + block * kQ4CodeBytes + row * 16 + 4 * q;
   uint16_t* sc = scales + (block * kQ4Rows + row) * s.groups;
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
+  for (int r = 0; r < 2; ++r) {
+    if (q % per == 0)
+      sc[r * 8 * s.groups + q / per] = (uint16_t)(__float_as_uint(scale[r]) >> 16);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      *reinterpret_cast<uint32_t*>(to + c * kQ4Rows * 16 + r * 8 * 16) = word[r][c];
-      if (q == c && c % per == 0)
-        sc[r * 8 * s.groups + c / per] = (uint16_t)(__float_as_uint(scale[r][c]) >> 16);
-    }
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<uint32_t*>(to + c * kQ4Rows * 16 + r * 8 * 16) =
+          q4_word(v[r][c], __shfl_sync(0xffffffffu, inv[r], lane - q + c));
+  }
 }
 
 __global__ void __launch_bounds__(kQ4Threads)
