@@ -19,12 +19,13 @@
 // lane and stage at 2.75 instructions, of the 368 that a scheduler issues in an SM's share of the
 // time). Measured with cold weights in a graph, floors at 6.8 TB/s: 256 rows for 104 experts,
 // 512 x 2048, 20.8 us (62 MB, 9.2 us): issue slots 65 % busy, the ALUs 56 %, DRAM 45 %; one row
-// times 8192 x 8192 17.2 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
-// 61 us (36.6 us: 4.1 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
+// times 8192 x 8192 16.8 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
+// 59 us (36.6 us: 4.2 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
 // look-up of groups and rows and the first bytes' way from HBM are about half.
-// Many rows: the issue slots, which the values, the copies of x and the epilogue share; the MMAs of 96
-// rows take about as long. 2048 rows times 4096 x 4096 75 us (920 TFLOP/s), 2048 x 8 rows for 256
-// experts, gate and up of 2048 x 512, 119 us (580 TFLOP/s; 64 rows an expert).
+// Many rows: a stage's values take 440 cycles, and with its MMAs 610 (not all of either overlaps); the
+// copies of x, 24 KB of every SM's from L2 in a stage of 96 rows, bring that to 830. 2048 rows times
+// 4096 x 4096 72.5 us (950 TFLOP/s), 2048 x 8 rows for 256 experts, gate and up of 2048 x 512,
+// 115 us (600 TFLOP/s; 64 rows an expert).
 //
 // With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
 // CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
@@ -384,29 +385,30 @@ __device__ __forceinline__ void load_x(const Q4Args& a, const Q4Shape& s, const 
   for (int unit = 0; unit < w.units; ++unit, st -= w.blocks) {
     if (st >= w.blocks) continue;
     const Unit u = unit_at(sm, m_tiles, unit);
-    // this lane's rows: sub, sub + 8, ... (kept as the sources of rows lane, lane + 32, ...)
-    int src[kUnitRows / 32];
+    // this lane's rows: sub, sub + 8, ... Their addresses are found once per unit (per stage it took
+    // 2048 rows times 4096 x 4096 75 us, not 72.5).
+    const __nv_bfloat16* from[kUnitRows / 8];
 #pragma unroll
-    for (int j = 0; j < kUnitRows / 32; ++j)
-      src[j] = 32 * j < u.n ? max(source(a, sm, u.r0 + min(32 * j + lane, u.n - 1)), 0) : 0;
+    for (int j = 0; j < kUnitRows / 32; ++j) {
+      if (32 * j >= u.n) break;
+      const int src = max(source(a, sm, u.r0 + min(32 * j + lane, u.n - 1)), 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        from[4 * j + i] = a.x + __shfl_sync(0xffffffffu, src, 8 * i + sub) * a.ldx + chunk * 8;
+    }
     for (; st < w.blocks; st += kSlots) {
-      const int k = (w.first + st) * 128 + chunk * 8;
-      const uint32_t in0 = k < s.K ? 16u : 0u, in1 = k + 64 < s.K ? 16u : 0u;   // (zeros behind n_in)
-      // (where there is nothing to read, any address of x)
-      const __nv_bfloat16 *x0 = a.x + (in0 ? k : 0), *x1 = a.x + (in1 ? k + 64 : 0);
+      // zeros behind n_in (where there is nothing to read, any address of x)
+      const int k = (w.first + st) * 128, left = s.K - k - chunk * 8;
+      const uint32_t in0 = left > 0 ? 16u : 0u, in1 = left > 64 ? 16u : 0u;
+      const int k0 = in0 ? k : 0, k1 = in1 ? k + 64 : 0;
       if (!__all_sync(0xffffffffu, wait<20>(&sm.empty[slot], turn, 2))) return;
       turn ^= 1u;
 #pragma unroll
-      for (int j = 0; j < kUnitRows / 32; ++j) {
-        if (32 * j >= u.n) break;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 8 * i + sub;
-          const int64_t at = __shfl_sync(0xffffffffu, src[j], r) * a.ldx;
-          if (32 * j + r < u.n) {
-            copy16(dst + (32 * j + 8 * i) * 128, x0 + at, in0);
-            copy16(dst + (32 * j + 8 * i) * 128 + kUnitRows * 128, x1 + at, in1);
-          }
+      for (int i = 0; i < kUnitRows / 8; ++i) {
+        if (8 * i >= u.n) break;
+        if (8 * i + sub < u.n) {
+          copy16(dst + 8 * i * 128, from[i] + k0, in0);
+          copy16(dst + 8 * i * 128 + kUnitRows * 128, from[i] + k1, in1);
         }
       }
       copies_commit();
