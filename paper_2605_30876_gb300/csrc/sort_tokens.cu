@@ -3,12 +3,13 @@
 //   sort_count_kernel  pairs per key of each chunk of pairs, one CTA per chunk
 //   sort_place_kernel  every CTA adds up, per key, the pairs before its chunk and all of them, and
 //                      goes through its chunk a tile of pairs at a time: per warp the pairs of each
-//                      key by matches over the warp's lanes, a prefix over the warps, and each
+//                      key by votes of the warp's lanes, a prefix over the warps, and each
 //                      pair's row is its key's base, the pairs of its key in the warps before its
 //                      own and those before it in its warp.
-// Up to 1024 pairs take the second launch alone: 8 pairs 2.5 us, 256 2.9, 1024 5.1 (with both 5.5, 5.7
-// and 6.7 us); 4096 pairs 7.1 us, 131072 10.6 (256 experts). Bound by the launches and by the chain
-// of loads, matches, prefixes and stores: the bytes would take 0.9 us for 131072 pairs with cold ids.
+// Up to 1024 pairs take the second launch alone: 8 pairs 2.5 us, 256 2.8, 1024 4.5 (with both 5.9, 6.0
+// and 6.4 us); 4096 pairs 7.0 us, 131072 10.2, 524288 of cold ids 16.2 (256 experts). Bound by the
+// launches and by the chain of loads, votes, prefixes and stores: the bytes of 524288 pairs would
+// take 0.9 us.
 // Every count is an integer sum: the order does not depend on the order of atomics.
 #include "block_reduce.cuh"
 #include "dmoe_internal.cuh"
@@ -22,6 +23,8 @@ constexpr int kSortRounds = 4;                          // pairs per thread and 
 constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxChunks = 148;                     // every CTA of one wave takes one chunk
 constexpr int kMaxKeys = kMaxExperts + 1;
+constexpr int kKeyBits = 9;
+static_assert(kMaxExperts < 1 << kKeyBits, "the bits of a key");
 
 __device__ __forceinline__ int sort_key(int id, int E) { return id < 0 || id >= E ? E : id; }
 
@@ -53,6 +56,20 @@ sort_count_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
 constexpr int kSumGroups = 3;
 static_assert(kSumGroups * kMaxKeys <= kSortThreads, "a thread per key and group");
 
+// The warp's lanes with this lane's key (at most `bits` bits, or -1), by a vote per bit: they take less than
+// one match over the warp, whose time goes by the number of different keys (1024 pairs, 256 experts: 4.5 us, not 5.1).
+__device__ __forceinline__ uint32_t same_key(int key, int bits) {
+  uint32_t same = __ballot_sync(0xffffffffu, key >= 0);
+#pragma unroll
+  for (int b = 0; b < kKeyBits; ++b) {
+    if (b >= bits) break;
+    const bool set = key >> b & 1;
+    const uint32_t m = __ballot_sync(0xffffffffu, set);
+    same &= set ? m : ~m;
+  }
+  return same;
+}
+
 // `rounds` pairs a thread and tile (the tile has rounds * blockDim.x pairs, a warp's are consecutive)
 __global__ void __launch_bounds__(kSortThreads)
 sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk, int nchunks,
@@ -63,7 +80,7 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
   __shared__ int sums[2][kMaxKeys];           // per key: pairs of all chunks, and of those before
   __shared__ int iscr[32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, keys = E + 1;
-  const int threads = blockDim.x, warps = threads >> 5;
+  const int threads = blockDim.x, warps = threads >> 5, bits = 32 - __clz(E);
   const int64_t begin = blockIdx.x * chunk, end = begin + chunk < R ? begin + chunk : R;
   for (int i = tid; i < 2 * kMaxKeys; i += threads) (&sums[0][0])[i] = 0;
   for (int i = lane; i < keys; i += 32) cnt[warp][i] = 0;
@@ -108,7 +125,7 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
       if (j >= rounds) break;
-      const uint32_t same = __match_any_sync(0xffffffffu, key[j]);
+      const uint32_t same = same_key(key[j], bits);
       const int ahead = __popc(same & ((1u << lane) - 1u));
       if (key[j] >= 0) rank[j] = cnt[warp][key[j]] + ahead;
       __syncwarp();
@@ -160,7 +177,7 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
 
 // How R pairs are cut: up to 1024 go to one CTA, without counts (chunks 0); more are cut into chunks of
 // whole tiles, a CTA each and no more than run at once, with as few pairs a thread as that
-// allows (the matches within a warp are what takes time: 4096 pairs took 11.6 us in one CTA).
+// allows (4096 pairs took 11.6 us in one CTA).
 struct SortPlan {
   int chunks, rounds, threads;
   int64_t chunk;
