@@ -254,6 +254,26 @@ def test_groups_between_the_two_limits(n, N, K, gated):
 
 
 @pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("ydt", [BF16, torch.float32])
+@pytest.mark.parametrize("N,K,g", [(1, 256, 64), (33, 256, 128), (64, 512, 64), (65, 224, 32), (97, 1280, 32),
+                                   (130, 2048, 128), (200, 1472, 64)])
+def test_few_units(N, K, g, ydt, gated):
+    """Fewer units than CTAs: widths of part of a tile, sums that end inside a block, groups of one row to
+    several units."""
+    for sizes in ([1], [3, 0, 33], [16, 17, 15], [80]):
+        check_products(len(sizes), N, K, g, np.array(sizes), rows_from=7, k=3, ydt=ydt, gated=gated, gap=8)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 64, 65])
+@pytest.mark.parametrize("N", [4096, 4864, 4992, 9728, 9792])
+def test_about_as_many_units_as_ctas(rows, N, gated):
+    """On 152 SMs: one turn or two, units of 64 rows or 96, with pairs of CTAs and without."""
+    for K in (256, 384, 3328):
+        check_many_units(1, N, K, 64, np.array([rows]), gated, seed=rows)
+
+
+@pytest.mark.parametrize("gated", [False, True])
 def test_groups_with_their_own_experts(gated):
     ids = np.array([3, 3, -1, 0, 6, 2, 2 ** 31 - 1], np.int32)         # twice the same; three left out
     sizes = np.array([5, 2, 4, 0, 3, 40, 6])
