@@ -83,6 +83,7 @@ class MoELayerQ4:
     weights, with the SwiGLU intermediate and the rows per (token, slot) rounded to bf16.
 
     weights: as for MoELayer (the bf16 expert weights are not kept).
+    Its buffers and its workspace serve one forward at a time, a replayed graph's too.
     """
 
     def __init__(self, desc: LayerDesc, weights: Dict[str, Optional[torch.Tensor]],
