@@ -352,7 +352,7 @@ struct Q4Args {
   const void* scales[2];
   void* y;                     // [R, N]
   int64_t ldy;
-  bool y_fp32;
+  bool y_fp32, gated;
   int64_t R;
   int n_groups, n_experts;
 };

@@ -96,6 +96,7 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   a.y = y;
   a.ldy = ldy;
   a.y_fp32 = y_dtype == DMOE_FP32;
+  a.gated = weights.size() == 4;
   a.R = R;
   a.n_groups = n_groups;
   a.n_experts = desc->n_experts;
