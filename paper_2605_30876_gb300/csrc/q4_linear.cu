@@ -18,14 +18,14 @@
 // Few rows: the weights' bytes are the bound, and the instructions per code are close to it (64 pairs a
 // lane and stage at 2.75 instructions, of the 368 that a scheduler issues in an SM's share of the
 // time). Measured with cold weights in a graph, floors at 6.8 TB/s: 256 rows for 104 experts,
-// 512 x 2048, 20.8 us (62 MB, 9.2 us): issue slots 65 % busy, the ALUs 56 %, DRAM 45 %; one row
-// times 8192 x 8192 16.8 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
-// 59 us (36.6 us: 4.2 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
+// 512 x 2048, 21.0 us (62 MB, 9.2 us): issue slots 65 % busy, the ALUs 56 %, DRAM 45 %; one row
+// times 8192 x 8192 17.0 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
+// 60 us (36.6 us: 4.2 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
 // look-up of groups and rows and the first bytes' way from HBM are about half.
 // Many rows: a stage's values take 440 cycles, and with its MMAs 610 (not all of either overlaps); the
 // copies of x, 24 KB of every SM's from L2 in a stage of 96 rows, bring that to 830. 2048 rows times
-// 4096 x 4096 72.5 us (950 TFLOP/s), 2048 x 8 rows for 256 experts, gate and up of 2048 x 512,
-// 115 us (600 TFLOP/s; 64 rows an expert).
+// 4096 x 4096 74 us (930 TFLOP/s), 2048 x 8 rows for 256 experts, gate and up of 2048 x 512,
+// 116.5 us (590 TFLOP/s; 64 rows an expert).
 //
 // With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
 // CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
