@@ -18,7 +18,7 @@
 // Few rows: the weights' bytes are the bound, and the instructions per code are close to it (64 pairs a
 // lane and stage at 2.75 instructions, of the 368 that a scheduler issues in an SM's share of the
 // time). Measured with cold weights in a graph, floors at 6.8 TB/s: 256 rows for 104 experts,
-// 512 x 2048, 21.0 us (62 MB, 9.2 us): issue slots 65 % busy, the ALUs 56 %, DRAM 45 %; one row
+// 512 x 2048, 21.0 us (62 MB, 9.2 us): issue slots 58 % busy, the ALUs 44 %, DRAM 34 %; one row
 // times 8192 x 8192 17.0 us (5.3 us); 2048 rows for 220 of 256 experts, gate and up of 2048 x 512,
 // 60 us (36.6 us: 4.2 TB/s). Of the time for one token's eight experts (10.6 us) the launch, the
 // look-up of groups and rows and the first bytes' way from HBM are about half.
