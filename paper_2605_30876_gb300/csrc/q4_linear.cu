@@ -29,8 +29,8 @@
 //
 // With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
 // CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
-// its own. One row times 8192 x K, alone and in pairs: K = 2048 8.4 and 8.5 us, 4096 12.1 and 10.5,
-// 8192 19.4 and 14.4; the pairs' launch, barriers and exchange take 2 us. (Also 0.5 to 1 us where
+// its own. 64 rows times 8192 x K, alone and in pairs: K = 2048 13.1 and 13.6 us, 4096 18.7 and
+// 17.1, 8192 29.5 and 23.6; the pairs' launch, barriers and exchange take 2 us. (Also 0.5 to 1 us where
 // they share nothing.) So pairs are for kPairStages stages and more, and fewer tiles than CTAs.
 // Every wait has a limit of one second. One that runs out is recorded (dmoe_q4_device_error) and ends
 // its role; the others' waits run out after it, and the CTA gives its tensor memory back.
