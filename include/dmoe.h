@@ -85,9 +85,10 @@ typedef struct {
 } dmoe_layer_desc;
 
 /* Bytes of device workspace needed by every call below for this shape (host only; no
- * CUDA call). One workspace sized for the desc serves all calls on that desc. A workspace
- * must be zero-filled once before its first use (dmoe_workspace_init); every call leaves it
- * reusable. */
+ * CUDA call). One workspace sized for the desc serves all calls on that desc, and one sized for
+ * the largest of several descs serves the calls on all of them. A workspace must be zero-filled
+ * once before its first use (dmoe_workspace_init); every call leaves it reusable, for calls with
+ * any desc: what has to be zero between calls is in its first 4352 bytes for every desc. */
 dmoe_status dmoe_workspace_size(const dmoe_layer_desc* desc, size_t* bytes /* host */);
 
 /* Zero-fills a workspace (asynchronously, on `stream`) and forgets on the host that a workspace
@@ -220,7 +221,7 @@ dmoe_status dmoe_set_profile_events(int32_t kernel, void* ev_begin, void* ev_end
  * results are the same.
  *  - The call allocates nothing and frees nothing (no cudaMalloc/cudaFree, no allocating
  *    library routine). The scratch it needs is the leading part of the workspace layout,
- *    each region rounded up to 256 bytes: the fault record and the stage counters (1.3 KB),
+ *    each region rounded up to 256 bytes: the fault record and the counters (4.5 KB),
  *    the partial logits (T*E fp32, times the router's split of d when d is not a multiple
  *    of 256), the scores and the masked scores (T*E fp32 each) and the top-k candidates
  *    (T * ceil(E/32) * k_mask * 8 bytes, k_mask = block_top_k or k). With E = 256 and

@@ -123,8 +123,10 @@ Workspace plan_workspace(const dmoe_layer_desc& d) {
     off = align_up(off + (bytes == 0 ? 1 : bytes), 256);
     return o;
   };
+  const bool dec = experts_decode_ok((int)T, (int)dm, (int)I, (int)Is);
   w.err = take(sizeof(DevErrRecord));
-  w.tickets = take(sizeof(int32_t) * kRouteTickets);
+  w.tickets = kWsTickets;
+  off = kWsZeroEnd;
   w.n_unique = take(sizeof(int32_t));
   w.logits_part = take(sizeof(float) * (w.router_splits == 0 ? 1 : w.router_splits) * T * E);
   w.probs = take(sizeof(float) * T * E);
@@ -139,16 +141,13 @@ Workspace plan_workspace(const dmoe_layer_desc& d) {
   w.xperm = take(2 * T * k * dm);
   w.h = take(2 * T * k * I);
   w.hs = take(2 * T * Is);
-  w.h_ready = take(sizeof(int32_t) * experts_ready_counters((int)T, (int)E, w.n_max));
+  w.h_ready = dec ? kWsReady
+                  : take(sizeof(int32_t) * experts_ready_counters((int)T, (int)E, w.n_max));
   w.yslot = take(sizeof(float) * T * k * dm);
   w.yshared = take(sizeof(float) * T * dm);
-  const bool dec = experts_decode_ok((int)T, (int)dm, (int)I, (int)Is);
   w.hdense = take(dec ? 2 * (E + 1) * (size_t)((T + 15) / 16 * 16) * (I > Is ? I : Is) : 0);
-  w.spec = take(dec || d.mode == DMOE_ROUTE_BLOCK
-                    ? sizeof(uint32_t) * d.n_blocks *
-                          (dec && kSpecMaskWords > spec_words((int)k) ? kSpecMaskWords
-                                                                      : spec_words((int)k))
-                    : 0);
+  w.spec = dec ? kWsSpec
+               : take(d.mode == DMOE_ROUTE_BLOCK ? sizeof(uint32_t) * d.n_blocks * spec_words((int)k) : 0);
   const size_t nchunks = (T + 31) / 32;
   w.disp_bits = take(sizeof(uint32_t) * nchunks * E);
   w.w_parts_bytes = tc ? router_tc_parts_bytes((int)dm, (int)E) : 0;

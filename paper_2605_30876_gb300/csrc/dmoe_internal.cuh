@@ -38,7 +38,7 @@ enum DevWhere : int32_t {
   kAtRouter = 1, kAtBlockRoute = 2, kAtDispatch = 3, kAtGateUp = 4, kAtDown = 5,
   kAtCombine = 6, kAtGather = 7, kAtSort = 8, kAtQ4 = 9,
 };
-constexpr int kRouteTickets = 256;
+constexpr int kRouteTickets = 32;
 constexpr int kRouteClusterCtas = 8;   // CTAs per cluster of the decode-size routing launch
 struct DevErrRecord {
   int32_t code;
@@ -57,6 +57,15 @@ __device__ __forceinline__ void record_error(DevErrRecord* rec, int code, int wh
 // ---------------------------------------------------------------------------------------
 // workspace layout (byte offsets from the workspace base; every region 256-B aligned)
 // ---------------------------------------------------------------------------------------
+// What has to be zero when a call begins (every call leaves it so) lies at the same place for every
+// shape, and no call writes anything else there: calls with different shapes share a workspace.
+// Behind it a call may find anything.
+constexpr size_t kWsTickets = 256;                                          // behind the fault record
+constexpr size_t kWsReady = kWsTickets + sizeof(int32_t) * kRouteTickets;   // decode size: h_ready
+constexpr size_t kWsSpec = 1536;                                            // decode size: spec
+constexpr size_t kWsZeroEnd = 4352;
+static_assert(sizeof(DevErrRecord) <= kWsTickets && kWsReady % 128 == 0 &&
+              kWsReady + sizeof(int32_t) * (kMaxExperts + 2) <= kWsSpec, "no overlap");
 struct Workspace {
   size_t err;          // DevErrRecord
   size_t tickets;      // int32 [kRouteTickets]: stage counters of the routing launch (zero between calls)
@@ -75,7 +84,8 @@ struct Workspace {
   size_t xperm;        // bf16 [T*k, d]   x gathered in dispatch order
   size_t h;            // bf16 [T*k, I]   SwiGLU intermediate of the routed experts
   size_t hs;           // bf16 [T, I_s]   shared-expert intermediate
-  size_t h_ready;      // int32 [(E+1) * token tiles]: published gate/up tiles
+  size_t h_ready;      // int32 [(E+1) * token tiles]: published gate/up tiles. Decode size: zero
+                       // between calls; else cleared by the call before their use, as spec is
   size_t yslot;        // [T*k, d] expert outputs per (token, slot): fp32 (decode-size path)
                        // or bf16 (general path); sized for fp32
   size_t yshared;      // [T, d], the same element type
@@ -305,7 +315,10 @@ cudaError_t launch_combine(const ExpertArgs& a, cudaStream_t s, int32_t* zero = 
 __host__ __device__ inline int spec_words(int k) { return (k + 2) / 3; }
 // words per block of a published coreset mask: 24 member bits and a marker byte each
 constexpr int kSpecMaskWords = (kMaxExperts + 23) / 24;
-// Decode-sized forwards (T <= 64): one persistent launch over gate/up and down tiles of
+constexpr int kDecodeTokens = 64;
+static_assert(kWsSpec + sizeof(uint32_t) * kDecodeTokens * kSpecMaskWords <= kWsZeroEnd &&
+              kSpecMaskWords >= (kMaxTopK + 2) / 3, "coresets of as many blocks as tokens");
+// Decode-sized forwards (T <= kDecodeTokens): one persistent launch over gate/up and down tiles of
 // every group, all tokens at once (no gather), then the combine.
 bool experts_decode_ok(int T, int d, int I, int Is);
 cudaError_t launch_experts_decode(const ExpertArgs& a, cudaStream_t s);

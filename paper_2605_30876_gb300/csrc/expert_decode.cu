@@ -53,7 +53,7 @@ constexpr int kMaxKBG = 4;                      // K boxes per gate/up stage (hg
 constexpr int kMaxStagesD = 5;
 constexpr int kGateRows = 8;                    // rows of W_gate, then of W_up, in an A tile
 constexpr uint64_t kTimeoutNs = 1000000000ull;  // 1 s
-constexpr int kMaxTok = 64;                     // tokens of a decode-sized forward
+constexpr int kMaxTok = kDecodeTokens;          // tokens of a decode-sized forward
 
 // Debug builds (-DDMOE_TRACE): per-CTA timeline of the first unit of each kind,
 // g_dtrace[cta * 32 + slot] (globaltimer ns): 0 entry, 1 unit list known, 2 gate/up first
