@@ -323,7 +323,8 @@ static_assert(kWsSpec + sizeof(uint32_t) * kDecodeTokens * kSpecMaskWords <= kWs
 bool experts_decode_ok(int T, int d, int I, int Is);
 cudaError_t launch_experts_decode(const ExpertArgs& a, cudaStream_t s);
 
-// Tokens sorted by expert (sort_tokens.cu): the workspace is the fault record and the chunks' counts.
+// Tokens sorted by expert (sort_tokens.cu): the workspace is the fault record and, behind kWsZeroEnd,
+// the chunks' counts.
 size_t sort_workspace_bytes(int64_t R, int E);
 cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,
                                int32_t* rows, int32_t* pos, void* ws, cudaStream_t s);

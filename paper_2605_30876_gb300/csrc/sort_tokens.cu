@@ -22,15 +22,19 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortRounds = 4;                          // pairs per thread and tile, at most
 constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxChunks = 148;                     // every CTA of one wave takes one chunk
+// A chunk of at most 60 K pairs has counts of 16 bits; larger ones have 32, and a few chunks less.
+constexpr int64_t kNarrowPairs = (int64_t)kSortMaxChunks * 60 * kSortThreads;
+constexpr int kWideChunks = 144;
 constexpr int kMaxKeys = kMaxExperts + 1;
 constexpr int kKeyBits = 9;
 static_assert(kMaxExperts < 1 << kKeyBits, "the bits of a key");
 
 __device__ __forceinline__ int sort_key(int id, int E) { return id < 0 || id >= E ? E : id; }
 
+template <typename Count>
 __global__ void __launch_bounds__(kSortThreads)
 sort_count_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk,
-                  int32_t* __restrict__ counts) {
+                  Count* __restrict__ counts) {
   __shared__ int cnt[kMaxKeys];
   const int tid = threadIdx.x;
   pdl_wait();
@@ -48,7 +52,7 @@ sort_count_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
       if (i0 + j * kSortThreads < end) atomicAdd(&cnt[sort_key(id[j], E)], 1);
   }
   __syncthreads();
-  if (tid <= E) counts[(size_t)blockIdx.x * (E + 1) + tid] = cnt[tid];
+  if (tid <= E) counts[(size_t)blockIdx.x * (E + 1) + tid] = (Count)cnt[tid];
 }
 
 // A key's counts over the chunks: [0] all of them, [1] those before this CTA's. Three groups of threads
@@ -71,9 +75,10 @@ __device__ __forceinline__ uint32_t same_key(int key, int bits) {
 }
 
 // `rounds` pairs a thread and tile (the tile has rounds * blockDim.x pairs, a warp's are consecutive)
+template <typename Count>
 __global__ void __launch_bounds__(kSortThreads)
 sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chunk, int nchunks,
-                  int rounds, const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+                  int rounds, const Count* __restrict__ counts, int32_t* __restrict__ offsets,
                   int32_t* __restrict__ rows, int32_t* __restrict__ pos, DevErrRecord* err) {
   __shared__ int cnt[kSortWarps][kMaxKeys];   // per warp and key: pairs, then the first row
   __shared__ int base[kMaxKeys];              // per key: the next tile's first row
@@ -180,10 +185,12 @@ sort_place_kernel(const int32_t* __restrict__ ids, int64_t R, int E, int64_t chu
 // allows (4096 pairs took 11.6 us in one CTA).
 struct SortPlan {
   int chunks, rounds, threads;
+  bool wide;   // counts of 32 bits
   int64_t chunk;
 };
 SortPlan sort_plan(int64_t R, int E) {
   SortPlan p;
+  p.wide = R > kNarrowPairs;
   if (R <= kSortThreads) {
     p.chunks = 0;
     p.rounds = 1;
@@ -192,7 +199,8 @@ SortPlan sort_plan(int64_t R, int E) {
     return p;
   }
   const int64_t pieces = (R + kSortThreads - 1) / kSortThreads;
-  const int64_t per = (pieces + kSortMaxChunks - 1) / kSortMaxChunks;   // of a thread's pairs, per chunk
+  const int most = p.wide ? kWideChunks : kSortMaxChunks;
+  const int64_t per = (pieces + most - 1) / most;   // of a thread's pairs, per chunk
   p.rounds = per < kSortRounds ? (int)per : kSortRounds;
   p.threads = kSortThreads;
   p.chunk = (per + p.rounds - 1) / p.rounds * p.rounds * kSortThreads;
@@ -200,31 +208,40 @@ SortPlan sort_plan(int64_t R, int E) {
   return p;
 }
 
-constexpr size_t kSortCounts = 256;   // offset of the counts: behind the fault record
+// The counts lie behind what other calls on the workspace need at zero.
+constexpr size_t kSortCounts = kWsZeroEnd;
+
+template <typename Count>
+cudaError_t launch(const SortPlan& p, int64_t R, int E, const int32_t* ids, int32_t* offsets,
+                   int32_t* rows, int32_t* pos, void* ws, cudaStream_t s) {
+  DevErrRecord* err = static_cast<DevErrRecord*>(ws);
+  Count* counts = p.chunks > 0 ? reinterpret_cast<Count*>(static_cast<uint8_t*>(ws) + kSortCounts)
+                               : nullptr;
+  cudaError_t e = cudaSuccess;
+  if (p.chunks > 0)
+    e = launch_ex(sort_count_kernel<Count>, dim3(p.chunks), dim3(kSortThreads), 0, s, true, ids, R, E,
+                  p.chunk, counts);
+  if (e == cudaSuccess)
+    e = launch_ex(sort_place_kernel<Count>, dim3(p.chunks > 0 ? p.chunks : 1), dim3(p.threads), 0, s,
+                  true, ids, R, E, p.chunk, p.chunks, p.rounds, static_cast<const Count*>(counts),
+                  offsets, rows, pos, err);
+  if (e != cudaSuccess) return e;
+  return cudaGetLastError();
+}
 
 }  // namespace
 
 size_t sort_workspace_bytes(int64_t R, int E) {
-  return kSortCounts + sizeof(int32_t) * (size_t)sort_plan(R, E).chunks * (E + 1);
+  const SortPlan p = sort_plan(R, E);
+  if (p.chunks == 0) return kWsTickets;   // the fault record's 256 bytes
+  return kSortCounts + (p.wide ? sizeof(int32_t) : sizeof(uint16_t)) * (size_t)p.chunks * (E + 1);
 }
 
 cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,
                                int32_t* rows, int32_t* pos, void* ws, cudaStream_t s) {
   const SortPlan p = sort_plan(R, E);
-  DevErrRecord* err = static_cast<DevErrRecord*>(ws);
-  int32_t* counts = p.chunks > 0
-                        ? reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + kSortCounts)
-                        : nullptr;
-  cudaError_t e = cudaSuccess;
-  if (p.chunks > 0)
-    e = launch_ex(sort_count_kernel, dim3(p.chunks), dim3(kSortThreads), 0, s, true, ids, R, E,
-                  p.chunk, counts);
-  if (e == cudaSuccess)
-    e = launch_ex(sort_place_kernel, dim3(p.chunks > 0 ? p.chunks : 1), dim3(p.threads), 0, s, true,
-                  ids, R, E, p.chunk, p.chunks, p.rounds, static_cast<const int32_t*>(counts),
-                  offsets, rows, pos, err);
-  if (e != cudaSuccess) return e;
-  return cudaGetLastError();
+  return p.wide ? launch<int32_t>(p, R, E, ids, offsets, rows, pos, ws, s)
+                : launch<uint16_t>(p, R, E, ids, offsets, rows, pos, ws, s);
 }
 
 }  // namespace dmoe
