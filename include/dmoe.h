@@ -276,7 +276,7 @@ dmoe_status dmoe_no_alloc_scratch(void** device_ptr, size_t* bytes);
 typedef enum { DMOE_BF16 = 0, DMOE_FP16 = 1, DMOE_FP32 = 2 } dmoe_dtype;
 
 /* Bytes of the workspace of dmoe_sort_tokens (host only). 1 <= k <= 16, 1 <= E <= 256, T >= 0,
- * T * k <= 2^30. */
+ * T * k <= 2^30. They grow with T, k and E: a workspace for the largest batch serves smaller ones. */
 dmoe_status dmoe_sort_workspace_size(int64_t T, int32_t k, int32_t E, size_t* bytes /* host */);
 
 /* Tokens sorted by expert, for any number of tokens and with slots that have no expert (the

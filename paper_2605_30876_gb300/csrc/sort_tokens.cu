@@ -210,6 +210,7 @@ SortPlan sort_plan(int64_t R, int E) {
 
 // The counts lie behind what other calls on the workspace need at zero.
 constexpr size_t kSortCounts = kWsZeroEnd;
+static_assert(2 * kWideChunks >= kSortMaxChunks, "the workspace does not shrink where counts widen");
 
 template <typename Count>
 cudaError_t launch(const SortPlan& p, int64_t R, int E, const int32_t* ids, int32_t* offsets,
@@ -231,10 +232,14 @@ cudaError_t launch(const SortPlan& p, int64_t R, int E, const int32_t* ids, int3
 
 }  // namespace
 
+// Of as many chunks as any sort of at most R pairs has (the chunks of R itself may be fewer): a
+// workspace for R pairs is large enough for fewer.
 size_t sort_workspace_bytes(int64_t R, int E) {
-  const SortPlan p = sort_plan(R, E);
-  if (p.chunks == 0) return kWsTickets;   // the fault record's 256 bytes
-  return kSortCounts + (p.wide ? sizeof(int32_t) : sizeof(uint16_t)) * (size_t)p.chunks * (E + 1);
+  if (R <= kSortThreads) return kWsTickets;   // the fault record's 256 bytes
+  if (R > kNarrowPairs) return kSortCounts + sizeof(int32_t) * kWideChunks * (E + 1);
+  const int64_t pieces = (R + kSortThreads - 1) / kSortThreads;
+  const int64_t chunks = pieces < kSortMaxChunks ? pieces : kSortMaxChunks;
+  return kSortCounts + sizeof(uint16_t) * (size_t)chunks * (E + 1);
 }
 
 cudaError_t launch_sort_tokens(int64_t R, int E, const int32_t* ids, int32_t* offsets,

@@ -128,3 +128,9 @@ def test_sorts_of_chunks_around_16_bits(most):
     want = torch.cat([at[-5:-4], at[:R // 2], at[R // 2 + 1:-5], at[-4:], at[:1] - 1])
     assert torch.equal(rows, want)
     assert int(pos[R // 2]) == -R and torch.equal(pos[rows[:-1].long()], at[:-1])
+
+
+def test_smaller_sorts_on_the_largest_ones_workspace():
+    ws = P.dm().alloc_sort_workspace(65536, 8, 256)
+    for T, k, E in [(65536, 8, 256), (18944, 8, 256), (18945, 8, 256), (300, 5, 7), (2000, 16, 256), (1, 1, 1)]:
+        sort(T, k, E, ws)

@@ -258,3 +258,29 @@ def test_oracle_q4_error_is_at_most_half_a_step():
         exact = torch.from_numpy(v).to(torch.bfloat16).double().numpy()
         assert (exact == v).all()
         assert (np.frexp(s)[0] * 32 % 1 == 0).all()
+
+
+# ---------------------------------------------------------------- one workspace for sorts of many sizes
+
+def test_sort_workspace_never_shrinks(dm):
+    """By the pairs, over every step in which they are cut into chunks, and by the experts."""
+    for E in (1, 64, 256):
+        last = 0
+        around = {n * p * 1024 + i for n in (144, 148) for p in range(1, 70) for i in (-1024, 0, 1, 1024)}
+        for R in sorted({0, 1, 1024, 1025, 2 ** 30} | around | {int(1.07 ** i) for i in range(300)}):
+            size = dm.dmoe_sort_workspace_size(R, 1, E)
+            assert size >= last, R
+            last = size
+    for R in (1, 1025, 151552, 151553, 524288, 2 ** 27):
+        sizes = [dm.dmoe_sort_workspace_size(R, 8, E) for E in range(1, 257)]
+        assert sizes == sorted(sizes)
+
+
+def test_sort_of_a_smaller_batch_is_taken(dm, lib):
+    """The workspace of 65536 x 8 pairs is not refused for 18944 x 8 (148 chunks, where the larger has 128):
+    the call gets past the check of its size, to the launch, which has no device here."""
+    if torch.cuda.is_available():
+        pytest.skip("would run on addresses that are not there")
+    n = dm.dmoe_sort_workspace_size(65536, 8, 256)
+    for T in (18944, 18945, 1000, 8):
+        assert lib.dmoe_sort_tokens(T, 8, 256, *[P(FAKE)] * 5, n, None) == 4
