@@ -3,6 +3,7 @@
 MoELayerQ4 the same layer's experts in 4 bits."""
 from __future__ import annotations
 
+import contextlib
 from typing import Dict, Optional
 
 import torch
@@ -10,6 +11,24 @@ import torch
 from . import (DMOE_ROUTE_BLOCK, LayerDesc, alloc_q4, alloc_workspace, dmoe_combine_rows,
                dmoe_dispatch, dmoe_layer_forward, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_size,
                dmoe_q4_swiglu, dmoe_router, dmoe_router_prepare, make_desc, make_q4_desc)
+
+_AS_IT_IS = contextlib.nullcontext()
+
+
+def _indexed(device) -> torch.device:
+    """The device with its number: "cuda" is the one that is current now, whichever is later."""
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        return torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
+def _on(device: torch.device):
+    """Makes a layer's device the current one, on which the router's and the dispatch's calls run."""
+    if device.type != "cuda" or device.index == torch.cuda.current_device():
+        return _AS_IT_IS
+    return torch.cuda.device(device)
+
 
 WEIGHT_KEYS = ("w_r", "bias", "w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
 
@@ -26,7 +45,7 @@ class MoELayer:
                  device="cuda", workspace: Optional[torch.Tensor] = None):
         self.desc = desc
         self.w = {k: weights.get(k) for k in WEIGHT_KEYS}
-        self.device = torch.device(device)
+        self.device = _indexed(device)
         T, k, E, d = desc.T, desc.top_k, desc.n_experts, desc.d_model
         self.ws = workspace if workspace is not None else alloc_workspace(desc, self.device)
         self.y = torch.empty((T, d), dtype=torch.bfloat16, device=self.device)
@@ -39,7 +58,8 @@ class MoELayer:
         self.prepare()
 
     def prepare(self, stream=None) -> None:
-        dmoe_router_prepare(self.desc, self.w["w_r"], self.ws, stream=stream)
+        with _on(self.device):
+            dmoe_router_prepare(self.desc, self.w["w_r"], self.ws, stream=stream)
 
     @classmethod
     def from_shape(cls, shape, weights, device="cuda", workspace=None) -> "MoELayer":
@@ -52,10 +72,11 @@ class MoELayer:
     def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         out = self.y if y is None else y
         w = self.w
-        dmoe_layer_forward(self.desc, x, w["w_r"], w["bias"], w["w_gate"], w["w_up"], w["w_down"],
-                           w["ws_gate"], w["ws_up"], w["ws_down"], out, self.topk_idx,
-                           self.topk_gate, self.n_unique, self.unique_ids, workspace=self.ws,
-                           stream=stream)
+        with _on(self.device):
+            dmoe_layer_forward(self.desc, x, w["w_r"], w["bias"], w["w_gate"], w["w_up"], w["w_down"],
+                               w["ws_gate"], w["ws_up"], w["ws_down"], out, self.topk_idx,
+                               self.topk_gate, self.n_unique, self.unique_ids, workspace=self.ws,
+                               stream=stream)
         return out
 
 
@@ -82,14 +103,18 @@ class MoELayerQ4:
     experts and the rows are those of MoELayer, the experts' outputs those of the quantised
     weights, with the SwiGLU intermediate and the rows per (token, slot) rounded to bf16.
 
-    weights: as for MoELayer (the bf16 expert weights are not kept).
+    weights: as for MoELayer, on `device` (the bf16 expert weights are not kept). The layer runs on that
+    device, on its current stream or the one given, whichever device is current.
     Its buffers and its workspace serve one forward at a time, a replayed graph's too.
     """
 
     def __init__(self, desc: LayerDesc, weights: Dict[str, Optional[torch.Tensor]],
                  device="cuda", workspace: Optional[torch.Tensor] = None, group: int = 64):
         self.desc = desc
-        self.device = torch.device(device)
+        self.device = _indexed(device)
+        for n, t in [*((n, weights.get(n)) for n in WEIGHT_KEYS), ("workspace", workspace)]:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{n}: on {t.device}, the layer on {self.device}")
         T, k, E, d, I = desc.T, desc.top_k, desc.n_experts, desc.d_model, desc.d_ff
         Is = desc.d_ff_shared
         self.w_r, self.bias = weights["w_r"], weights.get("bias")
@@ -124,7 +149,8 @@ class MoELayerQ4:
         self.prepare()
 
     def prepare(self, stream=None) -> None:
-        dmoe_router_prepare(self.desc, self.w_r, self.ws, stream=stream)
+        with _on(self.device):
+            dmoe_router_prepare(self.desc, self.w_r, self.ws, stream=stream)
 
     @classmethod
     def from_shape(cls, shape, weights, device="cuda", workspace=None, group=64) -> "MoELayerQ4":
@@ -135,7 +161,13 @@ class MoELayerQ4:
         return cls(desc, weights, device, workspace, group)
 
     def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        out, k = self.y if y is None else y, self.desc.top_k
+        out = self.y if y is None else y
+        with _on(self.device):
+            self._forward(x, out, stream)
+        return out
+
+    def _forward(self, x, out, stream) -> None:
+        k = self.desc.top_k
         dmoe_router(self.desc, x, self.w_r, self.bias, self.topk_idx, self.topk_gate,
                     workspace=self.ws, stream=stream)
         dmoe_dispatch(self.desc, self.topk_idx, self.n_unique, self.unique_ids, self.offsets,
@@ -152,4 +184,3 @@ class MoELayerQ4:
             dmoe_q4_linear(d.desc, self.hs, None, d.codes, d.scales, self.y_shared, stream=stream)
         dmoe_combine_rows(self.ys[:self.desc.T * k], self.pos, self.topk_gate, self.y_shared, out,
                           stream=stream)
-        return out
