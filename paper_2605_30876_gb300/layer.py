@@ -80,21 +80,32 @@ class MoELayer:
         return out
 
 
+def _in_stream(stream, device):
+    """What torch allocates and copies in it is on the given stream, too (None: the current one)."""
+    if stream is None:
+        return _AS_IT_IS
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
+
+
 class Q4Weight:
     """Matrices in 4 bits with group scales: codes and scales of `desc`, quantised from bf16 [n_experts,
-    n_out, n_in]. `more` ([n_out, n_in], a shared expert's) is one more expert behind them."""
+    n_out, n_in]. `more` ([n_out, n_in], a shared expert's) is one more expert behind them. With a
+    stream the weights are read on it, and codes and scales are its allocations."""
 
     def __init__(self, w: torch.Tensor, group: int = 64, more: Optional[torch.Tensor] = None,
                  stream=None):
         E, n_out, n_in = w.shape
         self.desc = make_q4_desc(E + (more is not None), n_out, n_in, group)
-        self.codes, self.scales = alloc_q4(self.desc, w.device)
         first = make_q4_desc(E, n_out, n_in, group)
         nc, ns = dmoe_q4_size(first)
-        dmoe_q4_quantize(first, w.contiguous(), self.codes[:nc], self.scales[:ns], stream=stream)
-        if more is not None:
-            dmoe_q4_quantize(make_q4_desc(1, n_out, n_in, group), more.contiguous(), self.codes[nc:],
-                             self.scales[ns:], stream=stream)
+        with _in_stream(stream, w.device):
+            self.codes, self.scales = alloc_q4(self.desc, w.device)
+            dmoe_q4_quantize(first, w.contiguous(), self.codes[:nc], self.scales[:ns])
+            if more is not None:
+                dmoe_q4_quantize(make_q4_desc(1, n_out, n_in, group), more.contiguous(),
+                                 self.codes[nc:], self.scales[ns:])
 
 
 class MoELayerQ4:
