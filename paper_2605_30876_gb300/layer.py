@@ -173,6 +173,11 @@ class MoELayerQ4:
 
     def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         out = self.y if y is None else y
+        # (the router goes by the desc's sizes, the other calls by the tensors')
+        for n, t in (("x", x), ("y", out)):
+            if t.shape != self.y.shape or t.device != self.y.device:
+                raise ValueError(f"{n}: expected {tuple(self.y.shape)} on {self.y.device}, "
+                                 f"got {tuple(t.shape)} on {t.device}")
         with _on(self.device):
             self._forward(x, out, stream)
         return out

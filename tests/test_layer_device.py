@@ -1,7 +1,5 @@
 """Resident layers on a device that is not the current one, without a GPU: every call of the library that
 goes to the current device's stream finds the layer's device current."""
-import types
-
 import pytest
 import torch
 
@@ -39,7 +37,7 @@ def test_a_layer_runs_on_its_own_device(calls, kind, shared):
     shape = TINY.with_(d_ff_shared=shared)
     layer = getattr(L, kind).from_shape(shape, layer_inputs(shape, seed=0, device="cpu"), device="cpu")
     del calls[:]
-    x = types.SimpleNamespace(shape=(shape.T, shape.d_model), device=torch.device("cuda", 1))
+    x = torch.zeros(shape.T, shape.d_model, dtype=torch.bfloat16)
     for index in (1, 0):
         layer.device = torch.device("cuda", index)
         layer.prepare()
@@ -66,3 +64,19 @@ def test_weights_elsewhere_are_refused(calls):
     with pytest.raises(ValueError, match="workspace"):
         L.MoELayerQ4.from_shape(TINY, weights, device="cpu", workspace=torch.empty(1, device="meta"))
     assert calls == []
+
+
+def test_other_shapes_are_refused_before_any_call(calls):
+    """Fewer tokens than the layer's (the router would read behind them), an output of half the rows (its
+    slots would be taken for twice as many), another width, another device."""
+    layer = L.MoELayerQ4.from_shape(TINY, layer_inputs(TINY, seed=0, device="cpu"), device="cpu")
+    del calls[:]
+    T, d = TINY.T, TINY.d_model
+    good = torch.zeros(T, d, dtype=torch.bfloat16)
+    for bad in (good[:-1], good[: T // 2], good[:, :-8], good[None], good.to("meta"), torch.cat([good, good])):
+        with pytest.raises(ValueError, match="x: expected"):
+            layer.forward(bad)
+        with pytest.raises(ValueError, match="y: expected"):
+            layer.forward(good, bad)
+    assert calls == []
+    assert layer.forward(good, good.clone()) is not None and len(calls) >= 5
