@@ -363,9 +363,18 @@ def _launch(fn, device, stream, *args) -> None:
 
 def _slots(tokens, pos, name="pos") -> int:
     k, rest = divmod(pos.numel(), tokens) if tokens > 0 else (1, pos.numel())
-    if rest or k < 1:
-        raise ValueError(f"{name}: {pos.numel()} entries are no k slots for each of {tokens} tokens")
+    if rest or k < 1 or (pos.dim() == 2 and pos.shape[0] != tokens):
+        raise ValueError(f"{name}: {pos.numel()} entries {tuple(pos.shape)} are no k slots for "
+                         f"each of {tokens} tokens")
     return k
+
+
+def _gates(t, name, tokens, k, device) -> Optional[int]:
+    """Device pointer of fp32 gates [T, k] (None -> NULL). Their shape says how the R slots are cut: it has
+    to agree with the other tensors' tokens."""
+    if isinstance(t, _Tensor) and t.dim() == 2 and t.shape[0] != tokens:
+        raise ValueError(f"{name}: expected shape {(tokens, k)}, got {tuple(t.shape)}")
+    return _vector(t, name, tokens * k, torch.float32, device)
 
 
 def _row_dtype(t, name) -> int:
@@ -436,7 +445,7 @@ def dmoe_combine_rows(ys, pos, gates, add, y, stream=None) -> None:
     po, ldo = _matrix(y, "y", T, d, ys.dtype, dev)
     _launch(_lib.dmoe_combine_rows, dev, stream, dt, T, k, d, pi, ldi,
             _vector(pos, "pos", R, torch.int32, dev),
-            _vector(gates, "gates", R, torch.float32, dev), pa, lda, po, ldo)
+            _gates(gates, "gates", T, k, dev), pa, lda, po, ldo)
 
 
 def dmoe_combine_rows_backward(dy, ys, pos, gates, dys, dgates, stream=None) -> None:
@@ -449,10 +458,9 @@ def dmoe_combine_rows_backward(dy, ys, pos, gates, dys, dgates, stream=None) -> 
     pd, ldd = _matrix(dy, "dy", T, d, dy.dtype, dev)
     py, ldy = (None, 0) if ys is None else _matrix(ys, "ys", R, d, dy.dtype, dev)
     po, ldo = (None, 0) if dys is None else _matrix(dys, "dys", R, d, dy.dtype, dev)
-    f32 = torch.float32
     _launch(_lib.dmoe_combine_rows_backward, dev, stream, dt, T, k, d, pd, ldd, py, ldy,
-            _vector(pos, "pos", R, torch.int32, dev), _vector(gates, "gates", R, f32, dev), po, ldo,
-            _vector(dgates, "dgates", R, f32, dev))
+            _vector(pos, "pos", R, torch.int32, dev), _gates(gates, "gates", T, k, dev), po, ldo,
+            _gates(dgates, "dgates", T, k, dev))
 
 
 def dmoe_q4_size(desc: Q4Desc) -> Tuple[int, int]:

@@ -284,3 +284,24 @@ def test_sort_of_a_smaller_batch_is_taken(dm, lib):
     n = dm.dmoe_sort_workspace_size(65536, 8, 256)
     for T in (18944, 18945, 1000, 8):
         assert lib.dmoe_sort_tokens(T, 8, 256, *[P(FAKE)] * 5, n, None) == 4
+
+
+def test_binding_refuses_slots_cut_another_way(dm):
+    """Gates or positions [T, k] beside rows of another number of tokens, which divides the slots as well."""
+    T, k, d = 4, 2, 8
+    bf = lambda n: torch.zeros(n, d, dtype=torch.bfloat16, device="meta")
+    pos, gates = torch.zeros(T * k, dtype=torch.int32), torch.zeros(T, k)
+
+    def refusal(f, *a):
+        with pytest.raises(ValueError) as ei:
+            f(*a)
+        return str(ei.value)
+    for n in (2, 8):
+        assert refusal(dm._gates, gates, "gates", n, T * k // n, 0).startswith("gates: expected shape")
+        two = pos.view(T, k)
+        assert "slots" in refusal(dm.dmoe_gather_rows, bf(n), two, bf(8))
+        assert "slots" in refusal(dm.dmoe_gather_rows_backward, bf(8), two, bf(n))
+        assert "slots" in refusal(dm.dmoe_combine_rows, bf(8), two, None, None, bf(n))
+        assert "slots" in refusal(dm.dmoe_combine_rows_backward, bf(n), None, two, None, bf(8), None)
+    assert "device" in refusal(dm._gates, gates, "gates", T, k, 0)      # the right split, on the host
+    assert dm._slots(T, pos.view(T, k)) == k and dm._slots(T, pos) == k and dm._gates(None, "g", T, k, 0) is None
