@@ -18,7 +18,7 @@
  *  - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream). All
  *    work is enqueued asynchronously on it, in order; calls on one workspace must not
  *    overlap on the GPU.
- *  - Outputs are fully overwritten (no need to zero them).
+ *  - Outputs are fully overwritten (no need to zero them), unless a call says otherwise.
  *  - Argument errors are detected on the host before anything is launched and return
  *    DMOE_ERR_INVALID_ARG / DMOE_ERR_UNSUPPORTED / DMOE_ERR_WORKSPACE; launch failures
  *    return DMOE_ERR_CUDA (dmoe_last_error_message() has the CUDA text). Faults detected
@@ -271,6 +271,9 @@ dmoe_status dmoe_no_alloc_scratch(void** device_ptr, size_t* bytes);
  *    leaves gaps between keep what is in the gaps.
  *  - `pos` entries outside [-R, R) and `rows` entries outside [0, T * k) are not followed: they
  *    count as slots without an expert, and as rows of zeros.
+ *  - `pos` as from dmoe_sort_tokens, or from dmoe_dispatch without a fault, names every row once
+ *    (as r or ~r). With another one, rows of xs and dys that no entry names are not written, and
+ *    one that several name gets each of its elements from one of them.
  * ------------------------------------------------------------------------------------- */
 
 typedef enum { DMOE_BF16 = 0, DMOE_FP16 = 1, DMOE_FP32 = 2 } dmoe_dtype;

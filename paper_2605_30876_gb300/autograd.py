@@ -9,7 +9,9 @@ _backward calls). Between the two a program puts its own expert products:
 
 Rows of slots without an expert are zeros in xs, are not read from ys, and get no gradient. The
 gradients can be taken once (there is no second derivative). `pos` is int32 and must not change
-between forward and backward.
+between forward and backward. It has to name every row once, as dmoe_sort_tokens writes it (and
+dmoe_dispatch, unless it records a fault): the kernels write the rows that it names, so that others of
+xs, and of the gradient by ys, would hold what the memory held.
 """
 from __future__ import annotations
 

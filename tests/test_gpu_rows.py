@@ -328,3 +328,29 @@ def test_offsets_past_32_bits():
     far_t.copy_(dy)
     m.dmoe_combine_rows_backward(far_t, far_r, pos, gates, far_o, far_gates)
     assert torch.equal(far_o, near) and torch.equal(far_gates, dgates)
+
+
+@pytest.mark.parametrize("d", [64, 33])
+def test_rows_that_no_position_names_are_not_written(d):
+    """Entries that are not followed, and two that name one row (with the same token's values)."""
+    m = P.dm()
+    T, k = 9, 4
+    x, _ = rows_of(T, d, torch.bfloat16, 0)
+    pos = setup(T, k, 0)
+    pos[::5] = T * k
+    pos[2] = pos[1]
+    pos[7] = ~pos[7]                                       # named, by a slot without an expert
+    pd = torch.from_numpy(pos).cuda()
+    named = np.zeros(T * k, bool)
+    want = np.full((T * k, d), 5.0)
+    for i, p in enumerate(pos):
+        if p < T * k:
+            named[p if p >= 0 else ~p] = True
+            want[p if p >= 0 else ~p] = f64(x)[i // k] if p >= 0 else 0.0
+    assert not named.all()
+    xs = torch.full((T * k, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    m.dmoe_gather_rows(x, pd, xs)
+    assert np.array_equal(f64(xs), want)
+    xs.fill_(5.0)
+    m.dmoe_combine_rows_backward(x, None, pd, None, xs, None)
+    assert np.array_equal(f64(xs), want)
