@@ -403,6 +403,13 @@ dmoe_status dmoe_q4_swiglu(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups
  * and clears it. Returns and fills `info` (host, 4 int32, or NULL) as dmoe_get_device_error does. */
 dmoe_status dmoe_q4_device_error(void* stream, int32_t* info);
 
+/* Diagnostic, as dmoe_set_debug_hold, for the two calls above: while `hold` is nonzero, their launches
+ * (of any host thread; captured ones keep it) wait for an arrival that never comes. Their bounded waits
+ * run out after 1 s; they record DMOE_ERR_TIMEOUT and unwind (no trap), and their outputs are
+ * unspecified. dmoe_q4_device_error, when it reads such a fault, clears the hold with it; a hold of 0
+ * clears it too. Host only. DMOE_ERR_INVALID_ARG for a negative hold. */
+dmoe_status dmoe_q4_set_debug_hold(int32_t hold);
+
 /* Synchronises `stream`, then reads and clears the fault code the kernels recorded in
  * `workspace`. Returns DMOE_OK if none, DMOE_ERR_TIMEOUT for a bounded wait that ran out,
  * DMOE_ERR_DEVICE for any other recorded fault, DMOE_ERR_CUDA if the sync failed.

@@ -136,6 +136,7 @@ def _load() -> ctypes.CDLL:
             "dmoe_q4_quantize": [Q, P, P, P, P],
             "dmoe_q4_dequantize": [Q, P, P, P, P],
             "dmoe_q4_device_error": [P, ctypes.POINTER(i32)],
+            "dmoe_q4_set_debug_hold": [i32],
             "dmoe_q4_linear": products + [P] * 2 + [P, i64, i32, P],
             "dmoe_q4_swiglu": products + [P] * 4 + [P, i64, i32, P]}.items():
         fn = getattr(lib, name)
@@ -546,6 +547,12 @@ def dmoe_q4_device_error(stream=None) -> Tuple[int, Tuple[int, int, int]]:
     info = (ctypes.c_int32 * 4)()
     st = _lib.dmoe_q4_device_error(_stream(stream), info)
     return st, (info[0], info[1], info[2])
+
+
+def dmoe_q4_set_debug_hold(hold: int) -> None:
+    """Diagnostic: makes the 4-bit products' bounded waits run out while `hold` is nonzero (see
+    include/dmoe.h); cleared by dmoe_q4_device_error."""
+    _check(_lib.dmoe_q4_set_debug_hold(int(hold)), "dmoe_q4_set_debug_hold")
 
 
 KERNELS = {"router": 0, "dispatch": 1, "gather": 2, "experts": 3, "combine": 4}

@@ -369,6 +369,7 @@ struct Q4Args {
   bool y_fp32, gated;
   int64_t R;
   int n_groups, n_experts;
+  int hold;                    // 0, or 1: the waits run out (dmoe_q4_set_debug_hold)
 };
 cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_t s);
 // the products' fault record in the current device's memory

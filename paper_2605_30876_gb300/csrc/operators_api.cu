@@ -10,6 +10,8 @@ namespace {
 constexpr int64_t kMaxPairs = 1 << 30;
 constexpr int kMaxRowWidth = 1 << 20;
 
+std::atomic<int32_t> g_q4_hold{0};   // dmoe_q4_set_debug_hold
+
 dmoe_status status_of(cudaError_t e) {
   if (e == cudaSuccess) return DMOE_OK;
   set_last_error(e);
@@ -100,6 +102,7 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   a.R = R;
   a.n_groups = n_groups;
   a.n_experts = desc->n_experts;
+  a.hold = g_q4_hold.load(std::memory_order_relaxed) != 0 ? 1 : 0;
   return status_of(launch_q4_linear(a, *desc, static_cast<cudaStream_t>(stream)));
 }
 
@@ -257,10 +260,19 @@ dmoe_status dmoe_q4_swiglu(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups
                 {gate_codes, gate_scales, up_codes, up_scales}, y, ldy, y_dtype, stream);
 }
 
+dmoe_status dmoe_q4_set_debug_hold(int32_t hold) {
+  if (hold < 0) return DMOE_ERR_INVALID_ARG;
+  g_q4_hold.store(hold);
+  return DMOE_OK;
+}
+
 dmoe_status dmoe_q4_device_error(void* stream, int32_t* info) {
   void* record = nullptr;
   const cudaError_t e = q4_fault_address(&record);
-  return e != cudaSuccess ? status_of(e) : dmoe_get_device_error(record, stream, info);
+  if (e != cudaSuccess) return status_of(e);
+  const dmoe_status st = dmoe_get_device_error(record, stream, info);
+  if (st == DMOE_ERR_TIMEOUT) g_q4_hold.store(0);
+  return st;
 }
 
 }  // extern "C"

@@ -643,7 +643,8 @@ q4_kernel(const __grid_constant__ Q4Args a, const __grid_constant__ Q4Shape s, c
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
-      ptx::mbar_init(&sm.full[i], 4 + 2);   // the set's warps and the loading ones
+      // the set's warps and the loading ones (and with dmoe_q4_set_debug_hold one that never comes)
+      ptx::mbar_init(&sm.full[i], 4 + 2 + a.hold);
       ptx::mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {

@@ -305,3 +305,8 @@ def test_binding_refuses_slots_cut_another_way(dm):
         assert "slots" in refusal(dm.dmoe_combine_rows_backward, bf(n), None, two, None, bf(8), None)
     assert "device" in refusal(dm._gates, gates, "gates", T, k, 0)      # the right split, on the host
     assert dm._slots(T, pos.view(T, k)) == k and dm._slots(T, pos) == k and dm._gates(None, "g", T, k, 0) is None
+
+
+def test_q4_hold_refusal(dm, lib):
+    assert lib.dmoe_q4_set_debug_hold(-1) == 1
+    dm.dmoe_q4_set_debug_hold(0)
