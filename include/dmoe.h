@@ -303,7 +303,7 @@ dmoe_status dmoe_sort_tokens(int64_t T, int32_t k, int32_t E, const int32_t* top
  * without an expert.
  *   x   [T, d] of dtype, row stride ldx    pos  int32 [R], as from dmoe_sort_tokens or
  *   xs  [R, d] out, row stride ldxs             dmoe_dispatch
- * 1 <= k <= 16, d >= 1, T * k <= 2^30. */
+ * 1 <= k <= 16, 1 <= d <= 2^20, T * k <= 2^30, here and in the three calls below. */
 dmoe_status dmoe_gather_rows(int32_t dtype, int64_t T, int32_t k, int32_t d, const void* x,
                              int64_t ldx, const int32_t* pos, void* xs, int64_t ldxs,
                              void* stream);
@@ -381,8 +381,11 @@ dmoe_status dmoe_q4_dequantize(const dmoe_q4_desc* desc, const void* codes, cons
  *              [0, n_experts) are left out
  *   y          [R, n_out] out, bf16 or fp32 (y_dtype), row stride ldy. Rows that are in no group
  *              (from offsets[n_groups] on, the slots without an expert) are not written
- * 0 <= R <= 2^30; 1 <= n_groups <= 512; (R / 64 + 1) * ceil(n_out / 64) * n_groups < 2^31; offsets
- * outside [0, R] are cut to it. */
+ * 0 <= R <= 2^30; 1 <= k <= 16; ldx < 2^39; 1 <= n_groups <= 512;
+ * (R / 64 + 1) * ceil(n_out / 64) * n_groups < 2^31; offsets outside [0, R] are cut to it. Groups do
+ * not overlap: an element of a row that two have is either's.
+ * A row's sum is added up in one, two or four parts, which follow from the sizes of all groups of the
+ * call: with other rows beside it a row may have other last bits. The same call gives the same bits. */
 dmoe_status dmoe_q4_linear(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const void* x,
                            int64_t ldx, int64_t T_x, const int32_t* rows, int32_t k,
                            const int32_t* offsets, const int32_t* expert_ids,

@@ -29,9 +29,15 @@
 //
 // With long sums the CTAs run in pairs (clusters of two). Where there are at most half as many units as
 // CTAs, a pair shares a unit, half of the stages each, and the first CTA adds the second one's sums to
-// its own. 64 rows times 8192 x K, alone and in pairs: K = 2048 13.1 and 13.6 us, 4096 18.7 and
-// 17.1, 8192 29.5 and 23.6; the pairs' launch, barriers and exchange take 2 us. (Also 0.5 to 1 us where
-// they share nothing.) So pairs are for kPairStages stages and more, and fewer tiles than CTAs.
+// its own. Alone and in pairs, us, cold weights in a graph:
+//   outputs x K     8192 x 2048   x 2944       x 4096       x 8192       2048 x 2048   x 2944
+//   1 row            9.6  9.9   11.2 11.1   13.2 12.6   20.3 16.0        8.8  8.8   10.4  9.6
+//   64 rows         12.2 12.7   15.0 14.5   17.8 16.5   28.0 22.0       11.7 11.5   14.2 12.9
+//   96 rows         12.2 14.7   14.6 16.8   17.1 18.8   26.4 25.2       11.4 10.9   13.7 12.1
+// The pairs' launch, barriers and exchange take 1 to 2 us (0.5 to 1 where they share nothing), the
+// exchange more with more rows. So pairs are for kPairStages stages and more, and at most half as many
+// tiles as SMs; that gives away 0.8 to 1.6 us with few tiles just below it, and 1.7 with 96 rows
+// and 64 tiles above it.
 // Every wait has a limit of one second. One that runs out is recorded (dmoe_q4_device_error) and ends
 // its role; the others' waits run out after it, and the CTA gives its tensor memory back.
 #include "q4.cuh"
@@ -52,7 +58,8 @@ constexpr int kUnitRows = 96, kSmallUnitRows = 64;
 // and two loading warps', and one pair of barriers serves both operands: an issuing warp's waits
 // and commits take as long as the MMAs of few rows (100 to 150 cycles each). There are two issuing
 // warps for the same reason, with the even and the odd stages of a unit and sums of their own,
-// which the epilogue adds (even plus odd whichever warp has which: the same sums at any place).
+// which the epilogue adds (even plus odd whichever warp has which: the same sums wherever a unit is;
+// units of the other limit, of one issuing warp, and shared ones have other partial sums).
 constexpr int kSlots = 4;
 constexpr int kCodeSlots = 3;              // blocks of codes per warp, one of them in use
 constexpr int kAcc0 = kSlots * 64;         // first column of the sums
@@ -118,8 +125,9 @@ __device__ __forceinline__ bool share_units(int units, int ctas, bool paired) {
 }
 // The limit of a launch, from the units that there are with either (of `rows` rows and tiles in all): a
 // stage of n rows takes about as long as (100 + n) / 0.44 ns, so the limit is the one whose turns
-// (halves, in pairs) times that are less. (256 rows times 8192 x 8192, two turns with either: 51 us
-// with 64 and 55 with 96. 2048 rows times 4096 x 4096, seven and five turns: 86 and 74.)
+// (halves, in pairs) times that are less. (The two constants are fitted to these: 256 rows times 8192 x
+// 8192, two turns with either, 51 us with 64 and 55 with 96; 2048 rows times 4096 x 4096, seven and
+// five turns, 86 and 74.)
 __device__ __forceinline__ float unit_cost(float rows, int units, int ctas, bool paired) {
   const uint32_t halves = share_units(units, ctas, paired) ? 1u : 2u * ((uint32_t)(units - 1) / (uint32_t)ctas + 1u);
   return (float)halves * (100.f + __fdividef(rows, (float)units));

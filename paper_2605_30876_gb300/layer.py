@@ -116,7 +116,8 @@ class MoELayerQ4:
 
     weights: as for MoELayer, on `device` (the bf16 expert weights are not kept). The layer runs on that
     device, on its current stream or the one given, whichever device is current.
-    Its buffers and its workspace serve one forward at a time, a replayed graph's too.
+    Its buffers and its workspace serve one forward at a time, a replayed graph's too. A token's last bits
+    may differ with other tokens beside it (dmoe_q4_linear).
     """
 
     def __init__(self, desc: LayerDesc, weights: Dict[str, Optional[torch.Tensor]],
