@@ -173,15 +173,19 @@ class MoELayerQ4:
         return cls(desc, weights, device, workspace, group)
 
     def forward(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        out = self.y if y is None else y
         # (the router goes by the desc's sizes, the other calls by the tensors')
-        for n, t in (("x", x), ("y", out)):
-            if t.shape != self.y.shape or t.device != self.y.device:
-                raise ValueError(f"{n}: expected {tuple(self.y.shape)} on {self.y.device}, "
-                                 f"got {tuple(t.shape)} on {t.device}")
+        self._check(x, "x")
+        if y is not None:
+            self._check(y, "y")
+        out = self.y if y is None else y
         with _on(self.device):
             self._forward(x, out, stream)
         return out
+
+    def _check(self, t, name) -> None:
+        if t.shape != self.y.shape or t.device != self.y.device:
+            raise ValueError(f"{name}: expected {tuple(self.y.shape)} on {self.y.device}, "
+                             f"got {tuple(t.shape)} on {t.device}")
 
     def _forward(self, x, out, stream) -> None:
         k = self.desc.top_k
