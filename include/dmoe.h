@@ -413,6 +413,66 @@ dmoe_status dmoe_q4_device_error(void* stream, int32_t* info);
  * clears it too. Host only. DMOE_ERR_INVALID_ARG for a negative hold. */
 dmoe_status dmoe_q4_set_debug_hold(int32_t hold);
 
+/* The experts' gated feed-forward block on sorted rows, for serving and training. The weights are
+ * bf16 or fp16, laid out as dmoe_moe_forward's; dtype is that of all tensors but the offsets.
+ * Limits: 1 <= n_experts <= 512; d_model and d_ff multiples of 8, at most 16384; 0 <= R <= 2^30;
+ * 1 <= n_groups <= 512; (R / 256 + 1, or 2 if R < 256) * ceil(max(d_model, d_ff) / 128) * n_groups
+ * < 2^31. Every base is 16-byte aligned and every row stride a multiple of 8. */
+typedef struct {
+  int32_t dtype;          /* DMOE_BF16 or DMOE_FP16 */
+  int32_t n_experts;
+  int32_t d_model;        /* d */
+  int32_t d_ff;           /* I */
+} dmoe_expert_desc;
+
+/* Row r of group u has expert e = expert_ids[u] (or u), and
+ *   g[r] = w_gate[e] x[r],  u[r] = w_up[e] x[r],  h[r] = silu(g[r]) * u[r],  y[r] = w_down[e] h[r]
+ * with fp32 sums; g, u, h and y are rounded once each (h from the unrounded g and u). One group of one
+ * expert is a dense block.
+ *   x          [R, d], row stride ldx
+ *   offsets    int32 [n_groups + 1]: group u has rows offsets[u] .. offsets[u+1]; values outside
+ *              [0, R] are cut to it. NULL: one group of all rows (n_groups = 1)
+ *   expert_ids int32 [n_groups], or NULL (group u is expert u, n_groups <= n_experts). With
+ *              dmoe_dispatch's offsets: its unique_ids. A group whose id is outside
+ *              [0, n_experts) is left out; an id may stand in several groups
+ *   w_gate, w_up  [E, I, d];  w_down  [E, d, I]
+ *   pre        [R, 2, I] out: g and u, for the backward pass; or NULL
+ *   h          [R, I] out: also the second product's input, so it is always needed
+ *   y          [R, d] out, row stride ldy
+ *   zero_rest  nonzero: rows of y that are in no group become zeros; 0: they are not written
+ * Rows of pre and h that are in no group are not written. Groups do not overlap: an element of a
+ * row that two have is either's. A row's values do not depend on the call's other rows as long as
+ * their number is the same side of the sizes at which the library changes its kernel. */
+dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_groups,
+                            const void* x, int64_t ldx, const int32_t* offsets,
+                            const int32_t* expert_ids, const void* w_gate, const void* w_up,
+                            const void* w_down, void* pre, void* h, void* y, int64_t ldy,
+                            int32_t zero_rest, void* stream);
+
+/* Its gradients, by x and by the weights, for groups that are the experts in turn (offsets
+ * [n_experts + 1], as from dmoe_sort_tokens; NULL for one expert of all rows):
+ *   dh = w_down^T dy,  s = sigmoid(g),  dg = dh u s (1 + g (1 - s)),  du = dh g s
+ *   dx = w_gate^T dg + w_up^T du,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T h
+ * with fp32 sums over an expert's rows; dg, du and the results are rounded once each.
+ *   dy         [R, d], row stride lddy;  x as above (read for dw_gate and dw_up only)
+ *   pre, h     as dmoe_expert_ffn wrote them (h is read for dw_down only)
+ *   dpre       [R, 2, I] out: dg and du (scratch; not needed for dw_down alone)
+ *   dx         [R, d] out (row stride lddx), or NULL
+ *   dw_gate, dw_up  [E, I, d] out, or NULL for both;  dw_down  [E, d, I] out, or NULL. Experts
+ *              without rows get zeros. One output at least is wanted
+ *   zero_rest  as above, for the rows of dx */
+dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, const void* dy,
+                                     int64_t lddy, const void* x, int64_t ldx,
+                                     const int32_t* offsets, const void* w_gate, const void* w_up,
+                                     const void* w_down, const void* pre, const void* h, void* dpre,
+                                     void* dx, int64_t lddx, void* dw_gate, void* dw_up,
+                                     void* dw_down, int32_t zero_rest, void* stream);
+
+/* The fault record of the two calls above on the current device, and the diagnostic that makes
+ * their bounded waits run out: as dmoe_q4_device_error and dmoe_q4_set_debug_hold. */
+dmoe_status dmoe_expert_device_error(void* stream, int32_t* info);
+dmoe_status dmoe_expert_set_debug_hold(int32_t hold);
+
 /* Synchronises `stream`, then reads and clears the fault code the kernels recorded in
  * `workspace`. Returns DMOE_OK if none, DMOE_ERR_TIMEOUT for a bounded wait that ran out,
  * DMOE_ERR_DEVICE for any other recorded fault, DMOE_ERR_CUDA if the sync failed.

@@ -25,6 +25,7 @@ __all__ = [
     "Q4Desc", "make_q4_desc", "dmoe_q4_size", "alloc_q4", "dmoe_q4_quantize",
     "dmoe_q4_dequantize", "dmoe_q4_linear", "dmoe_q4_swiglu",
     "dmoe_q4_device_error",
+    "ExpertDesc", "dmoe_expert_ffn", "dmoe_expert_ffn_backward", "dmoe_expert_device_error",
 ]
 
 DMOE_ROUTE_TOKEN = 0
@@ -68,6 +69,12 @@ class Q4Desc(ctypes.Structure):
 
 def make_q4_desc(n_experts, n_out, n_in, group=64) -> Q4Desc:
     return Q4Desc(n_experts, n_out, n_in, group)
+
+
+class ExpertDesc(ctypes.Structure):
+    """dmoe_expert_desc (include/dmoe.h)."""
+    _fields_ = [("dtype", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+                ("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32)]
 
 
 class DmoeError(RuntimeError):
@@ -125,6 +132,7 @@ def _load() -> ctypes.CDLL:
     Q = ctypes.POINTER(Q4Desc)
     sizes = ctypes.POINTER(size)
     products = [Q, i64, i32, P, i64, i64, P, i32, P, P]
+    X = ctypes.POINTER(ExpertDesc)
     for name, args in {
             "dmoe_sort_workspace_size": [i64, i32, i32, sizes],
             "dmoe_sort_tokens": [i64, i32, i32, P, P, P, P, P, size, P],
@@ -137,6 +145,10 @@ def _load() -> ctypes.CDLL:
             "dmoe_q4_dequantize": [Q, P, P, P, P],
             "dmoe_q4_device_error": [P, ctypes.POINTER(i32)],
             "dmoe_q4_set_debug_hold": [i32],
+            "dmoe_expert_ffn": [X, i64, i32, P, i64, P, P] + [P] * 5 + [P, i64, i32, P],
+            "dmoe_expert_ffn_backward": [X, i64, P, i64, P, i64] + [P] * 8 + [i64] + [P] * 3 + [i32, P],
+            "dmoe_expert_device_error": [P, ctypes.POINTER(i32)],
+            "dmoe_expert_set_debug_hold": [i32],
             "dmoe_q4_linear": products + [P] * 2 + [P, i64, i32, P],
             "dmoe_q4_swiglu": products + [P] * 4 + [P, i64, i32, P]}.items():
         fn = getattr(lib, name)
@@ -553,6 +565,83 @@ def dmoe_q4_set_debug_hold(hold: int) -> None:
     """Diagnostic: makes the 4-bit products' bounded waits run out while `hold` is nonzero (see
     include/dmoe.h); cleared by dmoe_q4_device_error."""
     _check(_lib.dmoe_q4_set_debug_hold(int(hold)), "dmoe_q4_set_debug_hold")
+
+
+def _experts(x, w_gate, w_up, w_down, name="x"):
+    """(desc, R, device, pointers of the three weights) of a feed-forward block's tensors."""
+    for n, t in ((name, x), ("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
+        if not isinstance(t, _Tensor) or t.dim() != (2 if t is x else 3):
+            raise TypeError(f"{n}: expected a {2 if n == name else 3}-D tensor")
+    dt, dev = x.dtype, x.get_device()
+    if dt is not torch.bfloat16 and dt is not torch.float16:
+        raise TypeError(f"{name}: expected bf16 or fp16, got {dt}")
+    E, I, d = w_gate.shape
+    if w_up.shape != w_gate.shape or w_down.shape != (E, d, I):
+        raise ValueError(f"expected w_gate and w_up [E, I, d] and w_down [E, d, I], got "
+                         f"{tuple(w_gate.shape)}, {tuple(w_up.shape)} and {tuple(w_down.shape)}")
+    n = E * I * d
+    return (ExpertDesc(_DTYPE_IDS[dt], E, d, I), x.shape[0], dev, _vector(w_gate, "w_gate", n, dt, dev),
+            _vector(w_up, "w_up", n, dt, dev), _vector(w_down, "w_down", n, dt, dev))
+
+
+def _offsets(offsets, dev):
+    """(groups, device pointer)."""
+    if offsets is None:
+        return 1, None
+    n = offsets.numel() - 1 if isinstance(offsets, _Tensor) else 0
+    if n < 1:
+        raise TypeError("offsets: expected an int32 tensor [groups + 1]")
+    return n, _vector(offsets, "offsets", n + 1, torch.int32, dev)
+
+
+def dmoe_expert_ffn(x, offsets, w_gate, w_up, w_down, h, y, pre=None, expert_ids=None, zero_rest=False,
+                    stream=None) -> None:
+    """y[r] = w_down[e] (silu(w_gate[e] x[r]) * (w_up[e] x[r])) for the rows of every group of offsets
+    (None: one group of all rows). h [R, I] and, for the gradients, pre [R, 2, I] are written, too."""
+    desc, R, dev, wg, wu, wd = _experts(x, w_gate, w_up, w_down)
+    d, I, dt = desc.d_model, desc.d_ff, x.dtype
+    px, ldx = _matrix(x, "x", R, d, dt, dev)
+    py, ldy = _matrix(y, "y", R, d, dt, dev)
+    if h is None:
+        raise TypeError("h: expected a tensor [R, I]")
+    n, po = _offsets(offsets, dev)
+    _launch(_lib.dmoe_expert_ffn, dev, stream, ctypes.byref(desc), R, n, px, ldx, po,
+            _vector(expert_ids, "expert_ids", n, torch.int32, dev), wg, wu, wd,
+            _vector(pre, "pre", 2 * R * I, dt, dev), _vector(h, "h", R * I, dt, dev), py, ldy,
+            1 if zero_rest else 0)
+
+
+def dmoe_expert_ffn_backward(dy, x, offsets, w_gate, w_up, w_down, pre, h, dpre, dx, dw_gate, dw_up,
+                             dw_down, zero_rest=False, stream=None) -> None:
+    """dmoe_expert_ffn's gradients by x and by the weights (any of dx, dw_gate with dw_up, and dw_down may
+    be None); group u is expert u. dpre [R, 2, I] is scratch."""
+    desc, R, dev, wg, wu, wd = _experts(dy, w_gate, w_up, w_down, "dy")
+    E, d, I, dt = desc.n_experts, desc.d_model, desc.d_ff, dy.dtype
+    n, po = _offsets(offsets, dev)
+    if n != E:
+        raise ValueError(f"offsets: expected {E + 1} entries, got {n + 1}")
+    pdy, lddy = _matrix(dy, "dy", R, d, dt, dev)
+    px, ldx = (None, 0) if x is None else _matrix(x, "x", R, d, dt, dev)
+    pdx, lddx = (None, 0) if dx is None else _matrix(dx, "dx", R, d, dt, dev)
+    _launch(_lib.dmoe_expert_ffn_backward, dev, stream, ctypes.byref(desc), R, pdy, lddy, px, ldx, po,
+            wg, wu, wd, _vector(pre, "pre", 2 * R * I, dt, dev), _vector(h, "h", R * I, dt, dev),
+            _vector(dpre, "dpre", 2 * R * I, dt, dev), pdx, lddx,
+            _vector(dw_gate, "dw_gate", E * I * d, dt, dev), _vector(dw_up, "dw_up", E * I * d, dt, dev),
+            _vector(dw_down, "dw_down", E * I * d, dt, dev), 1 if zero_rest else 0)
+
+
+def dmoe_expert_device_error(stream=None) -> Tuple[int, Tuple[int, int, int]]:
+    """Synchronises the stream; returns (status, (code, where, value)) of the fault record of the
+    feed-forward block's calls on the current device and clears it."""
+    info = (ctypes.c_int32 * 4)()
+    st = _lib.dmoe_expert_device_error(_stream(stream), info)
+    return st, (info[0], info[1], info[2])
+
+
+def dmoe_expert_set_debug_hold(hold: int) -> None:
+    """Diagnostic: makes the feed-forward block's bounded waits run out while `hold` is nonzero;
+    cleared by dmoe_expert_device_error."""
+    _check(_lib.dmoe_expert_set_debug_hold(int(hold)), "dmoe_expert_set_debug_hold")
 
 
 KERNELS = {"router": 0, "dispatch": 1, "gather": 2, "experts": 3, "combine": 4}

@@ -20,6 +20,7 @@ constexpr int kMaxTopK = 16;
 constexpr int kMaxTokens = 4096;
 constexpr int kMaxDModel = 16384;
 constexpr int kMaxFF = 8192;
+constexpr int kMaxFfnExperts = 512;   // of the feed-forward block on sorted rows
 constexpr int kTileM = 128;        // MMA M (weight rows per tile)
 constexpr int kTileK = 64;         // K elements per pipeline stage (128 B of bf16)
 constexpr int kMaxPersistentCtas = 320;
@@ -36,7 +37,7 @@ enum DevErr : int32_t {
 };
 enum DevWhere : int32_t {
   kAtRouter = 1, kAtBlockRoute = 2, kAtDispatch = 3, kAtGateUp = 4, kAtDown = 5,
-  kAtCombine = 6, kAtGather = 7, kAtSort = 8, kAtQ4 = 9,
+  kAtCombine = 6, kAtGather = 7, kAtSort = 8, kAtQ4 = 9, kAtFfn = 10,
 };
 constexpr int kRouteTickets = 32;
 constexpr int kRouteClusterCtas = 8;   // CTAs per cluster of the decode-size routing launch
@@ -374,6 +375,35 @@ struct Q4Args {
 cudaError_t launch_q4_linear(const Q4Args& a, const dmoe_q4_desc& d, cudaStream_t s);
 // the products' fault record in the current device's memory
 cudaError_t q4_fault_address(void** p);
+
+// The experts' feed-forward block on sorted rows and its gradients (ffn_products.cu). Rows and
+// weights are bf16 or fp16; strides in elements.
+struct FfnArgs {
+  int dtype;                   // DMOE_BF16 or DMOE_FP16
+  int n_experts, d, I;
+  int64_t R;
+  int n_groups;
+  const int32_t* offsets;      // [n_groups + 1] or null (one group of all rows)
+  const int32_t* expert_ids;   // [n_groups] or null (group u is expert u)
+  const void* x;               // [R, d]
+  int64_t ldx;
+  const void* w_gate; const void* w_up; const void* w_down;   // [E, I, d] x 2, [E, d, I]
+  void* pre;                   // [R, 2, I] gate and up products, or null
+  void* h;                     // [R, I]
+  void* y;                     // [R, d]
+  int64_t ldy;
+  const void* dy;              // [R, d]
+  int64_t lddy;
+  void* dpre;                  // [R, 2, I] their gradients
+  void* dx;                    // [R, d] or null
+  int64_t lddx;
+  void* dw_gate; void* dw_up; void* dw_down;   // or null
+  bool zero_rest;              // rows in no group: zeros in y (dx), not left as they are
+  int hold;                    // 0, or 1: the waits run out (dmoe_expert_set_debug_hold)
+};
+cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s);
+cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s);
+cudaError_t ffn_fault_address(void** p);
 
 // profiling events (dmoe_set_profile_events), per host thread
 void prof_begin(int kernel, cudaStream_t s);

@@ -1,0 +1,910 @@
+// The gated feed-forward block of the experts on rows sorted by expert, and its gradients:
+//   g = Wg x, u = Wu x, h = silu(g) * u, y = Wd h
+//   dh = Wd^T dy, dg = dh u s (1 + g (1 - s)), du = dh g s   (s = sigmoid(g))
+//   dx = Wg^T dg + Wu^T du, dWg = dg^T x, dWu = du^T x, dWd = dy^T h
+// Five products, one kernel form of each (kMode):
+//   kUp    D[i, r]  = Wg x, Wu x      epilogue: SwiGLU -> h (and g, u for the gradients)
+//   kDown  D[c, r]  = Wd h            epilogue: y
+//   kGradH D[i, r]  = Wd^T dy         epilogue: dg, du from g, u (dh stays in tensor memory, fp32)
+//   kGradX D[c, r]  = Wg^T dg + Wu^T du, one sum over both
+//   kGradW D[n, c]  = out^T in        over the rows of an expert
+// In the first four the weights are the MMA's M operand and the rows of a group its N: a group of
+// few rows wastes no tensor work on the other side and its weights stream once. Wd and Wg / Wu are
+// read as they lie, along the reduction (kUp, kDown: K-major) or across it (kGradH, kGradX:
+// MN-major, the tensor cores' transposed operand); so are both operands of kGradW. Nothing is
+// transposed in memory.
+//
+// Two CTAs of neighbouring SMs (a cluster) share an MMA of M = 256 (cta_group::2): each holds 128 of
+// the M rows and half of the N columns. A persistent pair per two SMs takes units (group, 256 rows
+// of M, up to 256 columns of N) in turn; they are found on the device from the offsets, so that no
+// call waits for the host. Warp 0 issues the TMA loads, warp 1 of the first CTA the MMAs, warps 2-9
+// run the epilogue from one of two accumulators in tensor memory while the other fills, warp 10
+// decodes units ahead, warp 11 (kGradW) clears what a stage holds behind an expert's last row: the
+// rows there are another expert's, and 0 * inf would not be 0.
+// Sums are fp32 throughout. g, u, dg, du and h are rounded to the rows' type between products: they
+// are the next product's operands, and the tensor cores take 16 bits.
+// Waits are bounded (1 s), record a timeout and unwind.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "dmoe_internal.cuh"
+#include "silu.cuh"
+#include "sm100_ptx.cuh"
+
+namespace dmoe {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kPlanWarp = 10;
+constexpr int kFixWarp = 11;
+constexpr int kCluster = 2;
+constexpr int kTileABytes = 128 * 128;      // 128 rows (or 2 x 64 columns) x 64 of K
+constexpr int kMaxStages = 8;
+constexpr int kQueue = 4;
+constexpr int kLevels = 4;                  // heights of the boxes of rows
+constexpr int kMaxGroups = kMaxFfnExperts;
+constexpr int kNMax = 256;
+constexpr uint64_t kWaitNs = 1000000000ull;
+
+enum Mode { kUp, kDown, kGradH, kGradX, kGradW };
+
+__device__ DevErrRecord ffn_fault;
+
+struct Maps {
+  CUtensorMap a[2];         // weights [E][rows][cols], or (kGradW) the output side's rows
+  CUtensorMap b[kLevels];   // rows [R][parts][K] in boxes of level_rows
+  CUtensorMap out[2];       // kGradW: the gradients
+};
+
+struct Params {
+  const int32_t* offsets;
+  const int32_t* expert_ids;
+  int n_groups, n_experts;
+  int64_t R;
+  int n_max;                // columns of a unit, at most (kGradW: of N)
+  int M;                    // valid rows of D: I or d
+  int K;                    // length of a part's reduction
+  int N;                    // kGradW: width of the gradient's rows
+  int parts;                // kGradX: sums over gate and up; kGradW: outputs (gate, up)
+  int m_tiles, n_tiles;     // n_tiles: kGradW
+  int level_rows[kLevels];
+  int stages;
+  void* out;                // h, y, dpre or dx
+  int64_t ldo;
+  void* pre;                // kUp: written (or null); kGradH: read
+  int I;
+  int hold;
+};
+
+// kSub steps of K = 64 make a stage of the ring: a commit costs the issuing thread about as much
+// as two MMAs, so most stages hold eight MMAs. An expert's rows are few, and an end inside a
+// stage costs loads: kGradW takes four.
+template <int kMode> constexpr int sub_steps() { return kMode == kGradW ? 1 : 2; }
+template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
+template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
+template <int kMode> constexpr int epi_bytes() {
+  return kMode == kGradW ? kEpiWarps * 4096 : kMode == kUp ? kEpiWarps * 2048 : 0;
+}
+
+template <bool kHalf>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (kHalf) {
+    const __half2 b = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+  } else {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+  }
+}
+template <bool kHalf>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (kHalf) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
+}
+
+// A thread holds eight columns' values of one row of D, its neighbour (lane xor 1) those of the next
+// row. Afterwards it holds both rows (the lower first, as one word) of four columns: the even lane
+// columns 0-3, the odd lane 4-7.
+template <bool kHalf>
+__device__ __forceinline__ void pair_up(const float (&v)[8], uint32_t (&w)[4]) {
+  uint32_t pk[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) pk[i] = pack2<kHalf>(v[2 * i], v[2 * i + 1]);
+  const bool odd = threadIdx.x & 1;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t mine = odd ? pk[2 + i] : pk[i];
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? pk[i] : pk[2 + i], 1);
+    const uint32_t lo = odd ? other : mine, hi = odd ? mine : other;
+    w[2 * i] = __byte_perm(lo, hi, 0x5410);
+    w[2 * i + 1] = __byte_perm(lo, hi, 0x7632);
+  }
+}
+
+// AND over the epilogue's 256 threads (named barrier 1)
+__device__ __forceinline__ bool epilogue_all(bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 1, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)v)
+      : "memory");
+  return r != 0;
+}
+
+__host__ __device__ inline int round_up(int v, int to) { return (v + to - 1) / to * to; }
+
+// rows of group g, cut to [0, R]
+__device__ __forceinline__ void group_rows(const Params& p, int g, int64_t* row0, int* count) {
+  int64_t lo = 0, hi = p.R;
+  if (p.offsets != nullptr) {
+    lo = __ldg(p.offsets + g);
+    hi = __ldg(p.offsets + g + 1);
+    lo = lo < 0 ? 0 : lo > p.R ? p.R : lo;
+    hi = hi < 0 ? 0 : hi > p.R ? p.R : hi;
+  }
+  *row0 = lo;
+  *count = hi > lo ? (int)(hi - lo) : 0;
+}
+__device__ __forceinline__ int group_expert(const Params& p, int g) {
+  const int e = p.expert_ids != nullptr ? __ldg(p.expert_ids + g) : g;
+  return e >= 0 && e < p.n_experts ? e : -1;
+}
+
+struct Unit {
+  int row, rows, e;   // first row and their number (kGradW: of the sum); e < 0: the end
+  int part, m, n;     // n: kGradW
+};
+
+template <int kMode, bool kHalf>
+__global__ void __launch_bounds__(kThreads, 1)
+ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
+  constexpr int kSub = sub_steps<kMode>();
+  constexpr bool kAmn = a_mn<kMode>(), kBmn = b_mn<kMode>();
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
+  const uint32_t b_sub = (uint32_t)p.level_rows[0] * 128u;   // bytes of one K = 64 step of B
+  const uint32_t stage_bytes = kSub * (kTileABytes + b_sub);
+  uint8_t* s_epi = smem + (uint32_t)p.stages * stage_bytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_epi + epi_bytes<kMode>());
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* ready = empty + kMaxStages;      // kGradW: full, and cleared behind the last row
+  uint64_t* acc_full = ready + kMaxStages;
+  uint64_t* acc_empty = acc_full + 2;
+  uint64_t* drain = acc_empty + 2;
+  uint64_t* held = drain + 1;
+  uint64_t* d_full = held + 1;
+  uint64_t* d_empty = d_full + kQueue;
+  int* s_unit = reinterpret_cast<int*>(d_empty + kQueue);   // [kQueue][4]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_unit + 4 * kQueue);
+  volatile int* s_abort = reinterpret_cast<int*>(s_tmem + 1);
+  int* s_first = reinterpret_cast<int*>(s_tmem + 2);        // [kMaxGroups + 1] units before a group
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)ptx::cluster_ctarank();
+  const int cl = (int)blockIdx.x / kCluster, ncl = (int)gridDim.x / kCluster;
+
+  if (tid == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+      ptx::mbar_init(&ready[s], kCluster);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(&acc_full[a], 1);
+      ptx::mbar_init(&acc_empty[a], kCluster * kEpiWarps);
+    }
+    ptx::mbar_init(drain, 1);
+    ptx::mbar_init(held, 1);
+    for (int i = 0; i < kQueue; ++i) {
+      ptx::mbar_init(&d_full[i], 1);
+      // the producer, the epilogue's warps, and the MMAs' (first CTA) and the clearing warp
+      ptx::mbar_init(&d_empty[i], 1 + kEpiWarps + (rank == 0 ? 1 : 0) + (kMode == kGradW ? 1 : 0));
+    }
+    ptx::fence_mbarrier_init();
+    *s_abort = 0;
+    ptx::prefetch_tensormap(&tm.a[0]);
+    ptx::prefetch_tensormap(&tm.b[0]);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc2(s_tmem, 512);
+    ptx::tmem_relinquish2();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_arrive();   // the barriers of both CTAs are set up
+  ptx::cluster_wait();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *s_tmem;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  auto wait_for = [&](auto try_wait, int value) -> bool {
+    if (try_wait()) return true;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    for (uint32_t i = 1;; ++i) {
+      if (try_wait()) return true;
+      if ((i & 63u) == 0u) {
+        if (*s_abort) return false;
+        if (ptx::globaltimer_ns() - t0 > kWaitNs) {
+          record_error(&ffn_fault, kErrTimeout, kAtFfn, value);
+          *s_abort = 1;
+          return false;
+        }
+      }
+    }
+  };
+  auto wait = [&](uint64_t* bar, uint32_t parity, int value) -> bool {
+    return wait_for([&] { return ptx::mbar_try_wait(bar, parity); }, value);
+  };
+  // The pair's i-th unit for a thread, or (warp_wide) a warp. A wait that failed gives an end.
+  auto unit_at = [&](int i, bool warp_wide) -> Unit {
+    const int q = i % kQueue;
+    bool got = wait(&d_full[q], (uint32_t)(i / kQueue) & 1u, i);
+    if (warp_wide) got = __all_sync(0xffffffffu, got);
+    Unit un{0, 0, -1, 0, 0, 0};
+    if (got) {
+      const int4 v = *reinterpret_cast<const int4*>(s_unit + 4 * q);
+      un.row = v.x;
+      un.rows = v.y;
+      un.e = v.z;
+      un.part = v.w >> 16;
+      un.m = (v.w >> 8) & 0xff;
+      un.n = v.w & 0xff;
+    }
+    if (warp_wide) __syncwarp();
+    if (got && (!warp_wide || lane == 0)) ptx::mbar_arrive(&d_empty[q]);
+    return un;
+  };
+  // columns of D: N of the unit's MMAs, a multiple of 32; half of them are each CTA's
+  auto columns = [&](const Unit& un) -> int {
+    if (kMode == kGradW) return min(round_up(p.N - un.n * kNMax, 32), kNMax);
+    return round_up(un.rows, 32);
+  };
+  auto k_steps = [&](const Unit& un) -> int {
+    if (kMode == kGradW) return (un.rows + 63) / 64;
+    return p.parts * ((p.K + 63) / 64);
+  };
+
+  if (warp == 0) {
+    // ================= TMA producer: this CTA's rows of A and its half of B's
+    if (lane == 0) {
+      const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_normal();
+      const uint32_t full0 = ptx::peer_smem(full, 0);
+      const int per_part = (p.K + 63) / 64;
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = 0; ok; ++i) {
+        const Unit un = unit_at(i, false);
+        if (un.e < 0) break;
+        const int steps = k_steps(un), half = columns(un) / 2;
+        const int m0 = kMode == kUp ? un.m * 128 + rank * 64 : un.m * 256 + rank * 128;
+        int lv = 0, rows = p.level_rows[0];   // the lowest box of rows that holds the half
+#pragma unroll
+        for (int l = 1; l < kLevels; ++l)
+          if (p.level_rows[l] >= half) { lv = l; rows = p.level_rows[l]; }
+        const int b_boxes = (half + 63) / 64;   // kGradW
+        const uint32_t sub_bytes = kTileABytes + (kMode == kGradW ? (uint32_t)b_boxes * 8192u
+                                                                  : (uint32_t)rows * 128u);
+        const int b_row = un.row + rank * half;
+        for (int c = 0; c < steps; c += kSub) {
+          if (!wait(&empty[stage], phase ^ 1u, i)) {
+            ok = false;
+            break;
+          }
+          const int n_sub = min(kSub, steps - c);
+          uint8_t* a = smem + (uint32_t)stage * stage_bytes;
+          uint8_t* b = a + kSub * kTileABytes;
+          const uint32_t bar = full0 + 8u * (uint32_t)stage;
+          if (kMode == kGradW) {
+            ptx::mbar_arrive_expect_tx(&full[stage], sub_bytes);
+            const int r = un.row + c * 64;
+            for (int j = 0; j < 2; ++j)
+              ptx::tma_load_3d(a + j * 8192, &tm.a[0], &full[stage], m0 + 64 * j, un.part, r, again);
+            for (int j = 0; j < b_boxes; ++j)
+              ptx::tma_load_3d(b + j * 8192, &tm.b[0], &full[stage],
+                               un.n * kNMax + rank * half + 64 * j, 0, r, again);
+          } else {
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], kCluster * n_sub * sub_bytes);
+            for (int s = 0; s < n_sub; ++s) {
+              const int part = (c + s) / per_part, k0 = (c + s - part * per_part) * 64;
+              uint8_t* as = a + s * kTileABytes;
+              if (kMode == kUp) {          // 64 rows of Wg, then 64 of Wu
+                ptx::tma_load_3d_pair(as, &tm.a[0], bar, k0, m0, un.e, once);
+                ptx::tma_load_3d_pair(as + 8192, &tm.a[1], bar, k0, m0, un.e, once);
+              } else if (kMode == kDown) {
+                ptx::tma_load_3d_pair(as, &tm.a[0], bar, k0, m0, un.e, once);
+              } else {                     // 64 rows of K, 2 x 64 columns
+                ptx::tma_load_3d_pair(as, &tm.a[part], bar, m0, k0, un.e, once);
+                ptx::tma_load_3d_pair(as + 8192, &tm.a[part], bar, m0 + 64, k0, un.e, once);
+              }
+              ptx::tma_load_3d_pair(b + s * b_sub, &tm.b[lv], bar, k0, part, b_row, again);
+            }
+          }
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      // the issuer's last commit arrives in this CTA, too
+      wait(drain, 0, -1);
+    }
+  } else if (warp == kPlanWarp) {
+    // ================= units: counted per group, then decoded ahead of their use
+    int carry = 0;
+    for (int base = 0; base < p.n_groups; base += 32) {
+      const int g = base + lane;
+      int n = 0;
+      if (g < p.n_groups && group_expert(p, g) >= 0) {
+        int64_t row0;
+        int cnt;
+        group_rows(p, g, &row0, &cnt);
+        n = kMode == kGradW ? p.parts * p.m_tiles * p.n_tiles
+                            : (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
+      }
+      int sum = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+      }
+      if (g < p.n_groups) s_first[g + 1] = carry + sum;
+      carry += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) s_first[0] = 0;
+    __syncwarp();
+    if (lane == 0) {
+      const int units = carry;
+      for (int i = 0;; ++i) {
+        const int u = cl + i * ncl;
+        int4 v = make_int4(0, 0, -1, 0);
+        if (u < units) {
+          int lo = 0, hi = p.n_groups - 1;
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (s_first[mid] <= u) lo = mid; else hi = mid - 1;
+          }
+          int64_t row0;
+          int cnt;
+          group_rows(p, lo, &row0, &cnt);
+          const int local = u - s_first[lo];
+          if (kMode == kGradW) {
+            const int n = local % p.n_tiles, mp = local / p.n_tiles;
+            v = make_int4((int)row0, cnt, lo, (mp / p.m_tiles) << 16 | (mp % p.m_tiles) << 8 | n);
+          } else {
+            // the tiles of a group next to one another share its weights; they are of one size
+            const int nt = (cnt + p.n_max - 1) / p.n_max;
+            const int m = local / nt, n = local - m * nt;
+            const int tile = round_up((cnt + nt - 1) / nt, 32);
+            v = make_int4((int)row0 + n * tile, min(tile, cnt - n * tile), group_expert(p, lo), m << 8);
+          }
+        }
+        const int q = i % kQueue;
+        if (i >= kQueue && !wait(&d_empty[q], ((uint32_t)(i / kQueue) & 1u) ^ 1u, i)) break;
+        *reinterpret_cast<int4*>(s_unit + 4 * q) = v;
+        ptx::mbar_arrive(&d_full[q]);
+        if (v.z < 0) break;
+      }
+    }
+  } else if (warp == 1) {
+    // ================= MMA issuer: the first CTA's, for both
+    if (rank == 0 && lane == 0) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = p.hold == 0 || wait(held, 0, -2);
+      for (int i = 0; ok; ++i) {
+        const Unit un = unit_at(i, false);
+        if (un.e < 0) break;
+        const int steps = k_steps(un), n = columns(un);
+        if (steps == 0) continue;
+        const uint32_t idesc = ptx::idesc_16bit(256, (uint32_t)n, !kHalf, kAmn, kBmn);
+        const int per_part = (p.K + 63) / 64;
+        const uint32_t d0 = tmem_base + (uint32_t)acc * kNMax;
+        ok = wait(&acc_empty[acc], acc_phase ^ 1u, i);
+        ptx::tc_fence_after();
+        for (int c = 0; ok && c < steps; c += kSub) {
+          if (kMode == kGradW)
+            ok = wait_for([&] { return ptx::mbar_try_wait_cluster(&ready[stage], phase); }, i);
+          else
+            ok = wait(&full[stage], phase, i);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint32_t a = ptx::smem_addr(smem) + (uint32_t)stage * stage_bytes;
+          const uint32_t b = a + kSub * kTileABytes;
+#pragma unroll
+          for (int s = 0; s < kSub; ++s) {
+            if (c + s >= steps) break;
+            const int left = kMode == kGradW ? un.rows - c * 64
+                                             : p.K - (c + s) % per_part * 64;
+            const int kk_end = min(4, (left + 15) / 16);
+            for (int kk = 0; kk < kk_end; ++kk) {
+              const uint32_t as = a + s * kTileABytes, bs = b + s * b_sub;
+              ptx::mma_bf16_pair(
+                  d0, kAmn ? ptx::sdesc_mn_sw128(as + kk * 2048, 8192) : ptx::sdesc_k_sw128(as + kk * 32),
+                  kBmn ? ptx::sdesc_mn_sw128(bs + kk * 2048, 8192) : ptx::sdesc_k_sw128(bs + kk * 32),
+                  idesc, (c > 0 || s > 0 || kk > 0) ? 1u : 0u);
+            }
+          }
+          ptx::mma_commit_pair(&empty[stage]);
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        ptx::mma_commit_pair(&acc_full[acc]);
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+      // no MMA is running when tensor memory is released
+      ptx::mma_commit_pair(drain);
+      const uint64_t t0 = ptx::globaltimer_ns();
+      while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer_ns() - t0 < kWaitNs) {
+      }
+    }
+  } else if (warp == kFixWarp) {
+    // ================= kGradW: zeros in the last stage's rows of K behind the group's last row, up
+    // to the 16 of its last MMA, in both operands of this CTA
+    if (kMode == kGradW) {
+      const uint32_t ready0 = ptx::peer_smem(ready, 0);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = 0; ok; ++i) {
+        const Unit un = unit_at(i, true);
+        if (un.e < 0) break;
+        const int steps = k_steps(un), blocks = 2 + (columns(un) / 2 + 63) / 64;
+        for (int c = 0; c < steps; ++c) {
+          ok = __all_sync(0xffffffffu, wait(&full[stage], phase, i));
+          if (!ok) break;
+          const int left = un.rows - c * 64, end = round_up(min(left, 64), 16);
+          if (left < end) {
+            // (a row of K is 128 bytes of each block of 64 columns; the swizzle stays within it)
+            uint8_t* a = smem + (uint32_t)stage * stage_bytes;
+            const int per_block = (end - left) * 8;
+            for (int j = lane; j < blocks * per_block; j += 32) {
+              const int blk = j / per_block, o = j - blk * per_block;
+              *reinterpret_cast<uint4*>(a + blk * 8192 + left * 128 + o * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+          }
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(ready0 + 8u * (uint32_t)stage);
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else {
+    // ================= epilogue: warps 2-9, TMEM lanes 32 * (warp % 4) ..; two groups of four
+    // warps take alternate slices of the columns
+    const int q = warp & 3, cg = (warp - 2) >> 2, odd = lane & 1;
+    const uint32_t lane_off = (uint32_t)(q * 32) << 16;
+    const uint32_t acc_empty0 = ptx::peer_smem(acc_empty, 0);
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int i = 0;; ++i) {
+      const Unit un = unit_at(i, true);
+      const bool sums = kMode != kGradW || un.rows > 0;
+      // (a warp whose wait failed leaves with the others)
+      if (!epilogue_all(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
+      ptx::tc_fence_after();
+      const uint32_t tbase = tmem_base + lane_off + (uint32_t)acc * kNMax;
+      const int nvalid = un.rows;
+      if constexpr (kMode == kUp) {
+        // TMEM lanes 0-63: g of 64 i, lanes 64-127: u of the same. Of 16 columns the warps of g
+        // keep the first eight and give the others to the warps of u, through shared memory.
+        const bool is_gate = q < 2;
+        const int ii = un.m * 128 + rank * 64 + (q & 1) * 32 + lane, ie = ii & ~1;
+        float4* box = reinterpret_cast<float4*>(s_epi) + (cg * 2 + (q & 1)) * 256;
+        const int bar_id = 2 + cg * 2 + (q & 1);
+        uint16_t* h = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.I + ie;
+        uint16_t* pre = static_cast<uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
+        int flip = 0;
+        for (int c0 = 16 * cg; c0 < nvalid; c0 += 32, flip ^= 1) {
+          float v[16];
+          ptx::tmem_ld16(tbase + c0, v);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+          // [flip][from gate / from up][two float4][lane]
+          float4* give = box + flip * 128 + (is_gate ? 0 : 64) + lane;
+          const float4* take = box + flip * 128 + (is_gate ? 64 : 0) + lane;
+          give[0] = is_gate ? make_float4(v[8], v[9], v[10], v[11]) : make_float4(v[0], v[1], v[2], v[3]);
+          give[32] = is_gate ? make_float4(v[12], v[13], v[14], v[15]) : make_float4(v[4], v[5], v[6], v[7]);
+          ptx::named_bar_sync(bar_id, 64);
+          const float4 o0 = take[0], o1 = take[32];
+          const float o[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
+          float g[8], u[8], hv[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            g[j] = is_gate ? v[j] : o[j];
+            u[j] = is_gate ? o[j] : v[8 + j];
+            hv[j] = g[j];
+          }
+          silu_all(hv);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) hv[j] *= u[j];
+          uint32_t wh[4], wg[4], wu[4];
+          pair_up<kHalf>(hv, wh);
+          if (p.pre != nullptr) {
+            pair_up<kHalf>(g, wg);
+            pair_up<kHalf>(u, wu);
+          }
+          const int t0 = c0 + (is_gate ? 0 : 8) + 4 * odd;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (t0 + j < nvalid && ie < p.I) {
+              *reinterpret_cast<uint32_t*>(h + (int64_t)(t0 + j) * p.I) = wh[j];
+              if (p.pre != nullptr) {
+                uint16_t* to = pre + (int64_t)(t0 + j) * 2 * p.I;
+                *reinterpret_cast<uint32_t*>(to) = wg[j];
+                *reinterpret_cast<uint32_t*>(to + p.I) = wu[j];
+              }
+            }
+        }
+        // (the last slice's words are read before the next unit's first are written: a slice of the
+        // other half, or this barrier, lies between)
+        ptx::named_bar_sync(bar_id, 64);
+      } else if constexpr (kMode == kGradH) {
+        const int ii = un.m * 256 + rank * 128 + q * 32 + lane, ie = ii & ~1;
+        const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
+        uint16_t* dpre = static_cast<uint16_t*>(p.out) + (int64_t)un.row * 2 * p.I + ie;
+        for (int c0 = 16 * cg; c0 < nvalid; c0 += 32) {
+          uint32_t gw[8], uw[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = c0 + 8 * (j >> 2) + 4 * odd + (j & 3);
+            const bool in = t < nvalid && ie < p.I;
+            const uint16_t* from = pre + (int64_t)t * 2 * p.I;
+            gw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from)) : 0u;
+            uw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from + p.I)) : 0u;
+          }
+          float v[16];
+          ptx::tmem_ld16(tbase + c0, v);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int at = 8 * (j >> 2) + (j & 3);
+            const float other = __shfl_xor_sync(0xffffffffu, odd ? v[at] : v[at + 4], 1);
+            const float dh[2] = {odd ? other : v[at], odd ? v[at + 4] : other};
+            const float2 g2 = unpack2<kHalf>(gw[j]), u2 = unpack2<kHalf>(uw[j]);
+            const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
+            float dg[2], du[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              const float s = __fdividef(1.f, 1.f + __expf(-g[b]));
+              dg[b] = dh[b] * u[b] * s * (1.f + g[b] * (1.f - s));
+              du[b] = dh[b] * g[b] * s;
+            }
+            const int t = c0 + at + 4 * odd;
+            if (t < nvalid && ie < p.I) {
+              uint16_t* to = dpre + (int64_t)t * 2 * p.I;
+              *reinterpret_cast<uint32_t*>(to) = pack2<kHalf>(dg[0], dg[1]);
+              *reinterpret_cast<uint32_t*>(to + p.I) = pack2<kHalf>(du[0], du[1]);
+            }
+          }
+        }
+      } else if constexpr (kMode == kGradW) {
+        // 64 columns of this warp's 32 rows at a time: through shared memory (128-byte swizzle), one
+        // bulk store each. What lies outside of the matrix is cut by its map.
+        const int row = un.m * 256 + rank * 128 + q * 32;
+        uint8_t* mine = s_epi + (warp - 2) * 4096;
+        const int n = columns(un);
+        const CUtensorMap* out = un.part == 0 ? &tm.out[0] : &tm.out[1];
+        for (int c0 = 64 * cg; c0 < n; c0 += 128) {
+          float v[2][32];
+          if (sums) {
+            ptx::tmem_ld32(tbase + c0, v[0]);
+            ptx::tmem_ld32(tbase + c0 + 32, v[1]);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) asm volatile("" : "+f"(v[0][j]), "+f"(v[1][j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[0][j] = v[1][j] = 0.f;
+          }
+          if (lane == 0) ptx::bulk_commit_wait_read();   // the store before has read its words
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float* f = &v[j >> 2][8 * (j & 3)];
+            *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) * 16)) =
+                make_uint4(pack2<kHalf>(f[0], f[1]), pack2<kHalf>(f[2], f[3]),
+                           pack2<kHalf>(f[4], f[5]), pack2<kHalf>(f[6], f[7]));
+          }
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && row < p.M && un.n * kNMax + c0 < p.N)
+            ptx::tma_store_3d(out, mine, un.n * kNMax + c0, row, un.e);
+        }
+      } else {
+        const int c = un.m * 256 + rank * 128 + q * 32 + lane, ce = c & ~1;
+        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.ldo + ce;
+        if (un.m * 256 + rank * 128 + q * 32 < p.M) {   // (the same for the warp)
+          for (int c0 = 16 * cg; c0 < nvalid; c0 += 32) {
+            float v[16];
+            ptx::tmem_ld16(tbase + c0, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              float a[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) a[j] = v[8 * s + j];
+              uint32_t w[4];
+              pair_up<kHalf>(a, w);
+              const int t0 = c0 + 8 * s + 4 * odd;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (t0 + j < nvalid && ce < p.M)
+                  *reinterpret_cast<uint32_t*>(out + (int64_t)(t0 + j) * p.ldo) = w[j];
+            }
+          }
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (sums) {
+        if (lane == 0) ptx::mbar_arrive_pair(acc_empty0 + 8u * (uint32_t)acc);
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+    }
+    if (kMode == kGradW && lane == 0) ptx::bulk_commit_wait_all();
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  // neither CTA leaves while the other may still signal its barriers or read its tiles
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+  if (warp == 1) {
+    __syncwarp();
+    ptx::tmem_dealloc2(tmem_base, 512);
+  }
+  // After a wait that failed, copies into this CTA's shared memory may not have been waited for: it
+  // stays until they have long landed.
+  if (*s_abort) {
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (ptx::globaltimer_ns() - t0 < kWaitNs / 10) __nanosleep(1000);
+  }
+}
+
+// Zeros in the rows of y [R, width] that are in no group: a CTA takes a run of rows.
+constexpr int kZeroRows = 64;
+__global__ void __launch_bounds__(256)
+zero_rest_kernel(const Params p, uint16_t* y, int64_t ldy, int width) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ uint8_t in_group[kZeroRows];
+  const int64_t r0 = (int64_t)blockIdx.x * kZeroRows;
+  if (threadIdx.x < kZeroRows) in_group[threadIdx.x] = 0;
+  __syncthreads();
+  for (int g = threadIdx.x; g < p.n_groups; g += blockDim.x) {
+    int64_t lo;
+    int cnt;
+    group_rows(p, g, &lo, &cnt);
+    if (cnt == 0 || lo >= r0 + kZeroRows || lo + cnt <= r0 || group_expert(p, g) < 0) continue;
+    const int64_t end = lo + cnt < r0 + kZeroRows ? lo + cnt : r0 + kZeroRows;
+    for (int64_t r = lo > r0 ? lo : r0; r < end; ++r) in_group[r - r0] = 1;
+  }
+  __syncthreads();
+  for (int j = threadIdx.x >> 5; j < kZeroRows && r0 + j < p.R; j += blockDim.x >> 5) {
+    if (in_group[j]) continue;
+    uint16_t* row = y + (r0 + j) * ldy;
+    for (int c = 2 * (threadIdx.x & 31); c < width; c += 64)
+      *reinterpret_cast<uint32_t*>(row + c) = 0u;
+  }
+}
+
+// ------------------------------------------------------------------ host side
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(ptr);
+  });
+  return fn;
+}
+
+// [n2][n1][n0] of 16-bit elements with strides in elements, in boxes of 64 x b1 x b2
+bool make_map(CUtensorMap* m, bool half, const void* base, uint64_t n0, uint64_t n1, uint64_t n2,
+              uint64_t ld1, uint64_t ld2, uint32_t b1, uint32_t b2) {
+  EncodeTiledFn enc = encode_fn();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[3] = {n0, n1, n2};
+  const cuuint64_t strides[2] = {ld1 * 2, ld2 * 2};
+  const cuuint32_t box[3] = {64, b1, b2};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+             const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Rows {          // [R][parts][K], rows ld apart
+  const void* p;
+  int64_t ld;
+  int parts, K;
+};
+
+cudaError_t smem_limit(int* limit) {
+  static std::atomic<int> known[32];
+  int dev = 0, v = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  v = dev < 32 ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    e = cudaDeviceGetAttribute(&v, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+    if (e == cudaSuccess && dev < 32) known[dev].store(v, std::memory_order_relaxed);
+  }
+  *limit = v;
+  return e;
+}
+
+template <int kMode, bool kHalf>
+cudaError_t raise_limit(int limit) {
+  static std::atomic<uint32_t> done;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint32_t bit = dev < 32 ? 1u << dev : 0u;
+  if (e != cudaSuccess || (done.load(std::memory_order_relaxed) & bit) != 0u) return e;
+  e = cudaFuncSetAttribute(ffn_products_kernel<kMode, kHalf>,
+                           cudaFuncAttributeMaxDynamicSharedMemorySize, limit);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+Params base_params(const FfnArgs& a) {
+  Params p{};
+  p.offsets = a.offsets;
+  p.expert_ids = a.expert_ids;
+  p.n_groups = a.n_groups;
+  p.n_experts = a.n_experts;
+  p.R = a.R;
+  p.I = a.I;
+  p.parts = 1;
+  p.hold = a.hold;
+  return p;
+}
+
+// behind the ring: the epilogue's words, barriers, units, alignment
+size_t fixed_smem(int epi) {
+  return 1024 + epi + 8 * (3 * kMaxStages + 6 + 2 * kQueue) + 16 * kQueue + 8 +
+         4 * (kMaxGroups + 1);
+}
+
+// The rest of the launch: stages, grid. `units`: at most so many.
+template <int kMode, bool kHalf>
+cudaError_t launch(Maps& m, Params& p, int64_t units, cudaStream_t s) {
+  int limit = 0;
+  cudaError_t e = smem_limit(&limit);
+  if (e == cudaSuccess) e = raise_limit<kMode, kHalf>(limit);
+  if (e != cudaSuccess) return e;
+  const size_t fixed = fixed_smem(epi_bytes<kMode>());
+  const size_t stage = (size_t)sub_steps<kMode>() * (kTileABytes + (size_t)p.level_rows[0] * 128);
+  p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)limit - fixed) / stage);
+  if (p.stages < 2) return cudaErrorInvalidConfiguration;
+  const int pairs = (int)std::min<int64_t>(device_sm_count() / kCluster, std::max<int64_t>(units, 1));
+  return launch_cluster(ffn_products_kernel<kMode, kHalf>, dim3(pairs * kCluster), dim3(kThreads),
+                        fixed + p.stages * stage, s, kCluster, true, m, p);
+}
+
+// A product of weights with the groups' rows (all but kGradW).
+template <int kMode, bool kHalf>
+cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const Rows& b, void* out,
+                         int64_t ldo, cudaStream_t s) {
+  Params p = base_params(a);
+  Maps m{};
+  p.parts = b.parts;
+  p.K = b.K;
+  p.M = kMode == kUp || kMode == kGradH ? a.I : a.d;
+  const int per_m = kMode == kUp ? 128 : 256;
+  p.m_tiles = (p.M + per_m - 1) / per_m;
+  p.out = out;
+  p.ldo = ldo;
+  p.pre = kMode == kUp || kMode == kGradH ? a.pre : nullptr;
+  p.n_max = (int)std::min<int64_t>(kNMax, (a.R + 31) / 32 * 32);
+  // w: as it lies, [E][rows][cols]; its rows are M (kUp, kDown) or K
+  const uint64_t rows = a_mn<kMode>() ? p.K : p.M, cols = a_mn<kMode>() ? p.M : p.K;
+  bool ok = true;
+  for (int i = 0; i < 2; ++i) {
+    const void* w = i == 0 ? w0 : w1;
+    if (w != nullptr)
+      ok = ok && make_map(&m.a[i], kHalf, w, cols, rows, a.n_experts, cols, rows * cols,
+                          kMode == kDown ? 128 : 64, 1);
+  }
+  int level = 0;
+  for (int h = p.n_max / 2; level < kLevels; ++level) {
+    p.level_rows[level] = h;
+    if (level == 0 || h < p.level_rows[level - 1])
+      ok = ok && make_map(&m.b[level], kHalf, b.p, b.K, b.parts, a.R, b.K, b.ld, 1, h);
+    else
+      p.level_rows[level] = 0;   // (not taken)
+    h = std::max(16, (h / 2 + 15) / 16 * 16);
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  const int64_t units = (a.R / p.n_max + std::min<int64_t>(a.n_groups, a.R)) * p.m_tiles;
+  return launch<kMode, kHalf>(m, p, units, s);
+}
+
+// Gradients of weights [E][M][N] x parts: sums over the groups' rows of out [R][parts][M] and in [R][N].
+template <bool kHalf>
+cudaError_t weights_product(const FfnArgs& a, const Rows& out, const Rows& in, void* dw0, void* dw1,
+                            cudaStream_t s) {
+  Params p = base_params(a);
+  Maps m{};
+  p.M = out.K;
+  p.N = in.K;
+  p.parts = out.parts;
+  p.m_tiles = (p.M + 255) / 256;
+  p.n_tiles = (p.N + kNMax - 1) / kNMax;
+  p.level_rows[0] = 128;     // (a half of B: 64 rows of K of 128 columns)
+  bool ok = make_map(&m.a[0], kHalf, out.p, out.K, out.parts, a.R, out.K, out.ld, 1, 64) &&
+            make_map(&m.b[0], kHalf, in.p, in.K, 1, a.R, in.K, in.ld, 1, 64);
+  for (int i = 0; i < p.parts; ++i)
+    ok = ok && make_map(&m.out[i], kHalf, i == 0 ? dw0 : dw1, p.N, p.M, a.n_experts, p.N,
+                        (uint64_t)p.M * p.N, 32, 1);
+  if (!ok) return cudaErrorInvalidValue;
+  return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.parts * p.m_tiles * p.n_tiles, s);
+}
+
+cudaError_t zero_rest(const FfnArgs& a, void* y, int64_t ldy, cudaStream_t s) {
+  return launch_ex(zero_rest_kernel, dim3((unsigned)((a.R + kZeroRows - 1) / kZeroRows)), dim3(256), 0,
+                   s, true, base_params(a), static_cast<uint16_t*>(y), ldy, a.d);
+}
+
+template <bool kHalf>
+cudaError_t forward(const FfnArgs& a, cudaStream_t s) {
+  cudaError_t e = rows_product<kUp, kHalf>(a, a.w_gate, a.w_up, {a.x, a.ldx, 1, a.d}, a.h, a.I, s);
+  if (e == cudaSuccess)
+    e = rows_product<kDown, kHalf>(a, a.w_down, nullptr, {a.h, a.I, 1, a.I}, a.y, a.ldy, s);
+  if (e == cudaSuccess && a.zero_rest) e = zero_rest(a, a.y, a.ldy, s);
+  return e;
+}
+
+template <bool kHalf>
+cudaError_t backward(const FfnArgs& a, cudaStream_t s) {
+  const Rows x{a.x, a.ldx, 1, a.d}, dy{a.dy, a.lddy, 1, a.d}, h{a.h, a.I, 1, a.I};
+  const Rows dpre{a.dpre, 2 * a.I, 2, a.I};
+  cudaError_t e = cudaSuccess;
+  if (a.dx != nullptr || a.dw_gate != nullptr)
+    e = rows_product<kGradH, kHalf>(a, a.w_down, nullptr, dy, a.dpre, 2 * a.I, s);
+  if (e == cudaSuccess && a.dx != nullptr) {
+    e = rows_product<kGradX, kHalf>(a, a.w_gate, a.w_up, dpre, a.dx, a.lddx, s);
+    if (e == cudaSuccess && a.zero_rest) e = zero_rest(a, a.dx, a.lddx, s);
+  }
+  if (e == cudaSuccess && a.dw_gate != nullptr)
+    e = weights_product<kHalf>(a, dpre, x, a.dw_gate, a.dw_up, s);
+  if (e == cudaSuccess && a.dw_down != nullptr)
+    e = weights_product<kHalf>(a, dy, h, a.dw_down, nullptr, s);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s) {
+  return a.dtype == DMOE_FP16 ? forward<true>(a, s) : forward<false>(a, s);
+}
+cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s) {
+  return a.dtype == DMOE_FP16 ? backward<true>(a, s) : backward<false>(a, s);
+}
+cudaError_t ffn_fault_address(void** p) { return cudaGetSymbolAddress(p, ffn_fault); }
+
+}  // namespace dmoe

@@ -1,5 +1,7 @@
 // C-ABI entry points of the calls that do a layer by its parts: argument checks and launches.
 // Nothing here allocates device memory or synchronises.
+#include <algorithm>
+
 #include "dmoe_internal.cuh"
 #include "q4.cuh"
 
@@ -10,7 +12,8 @@ namespace {
 constexpr int64_t kMaxPairs = 1 << 30;
 constexpr int kMaxRowWidth = 1 << 20;
 
-std::atomic<int32_t> g_q4_hold{0};   // dmoe_q4_set_debug_hold
+std::atomic<int32_t> g_q4_hold{0};       // dmoe_q4_set_debug_hold
+std::atomic<int32_t> g_expert_hold{0};   // dmoe_expert_set_debug_hold
 
 dmoe_status status_of(cudaError_t e) {
   if (e == cudaSuccess) return DMOE_OK;
@@ -104,6 +107,42 @@ dmoe_status run_q4(const dmoe_q4_desc* desc, int64_t R, int32_t n_groups, const 
   a.n_experts = desc->n_experts;
   a.hold = g_q4_hold.load(std::memory_order_relaxed) != 0 ? 1 : 0;
   return status_of(launch_q4_linear(a, *desc, static_cast<cudaStream_t>(stream)));
+}
+
+dmoe_status check_expert(const dmoe_expert_desc* d, int64_t R, int64_t n_groups) {
+  if (d == nullptr || R < 0 || n_groups <= 0 || d->n_experts <= 0 || d->d_model <= 0 ||
+      d->d_ff <= 0 || (d->dtype != DMOE_BF16 && d->dtype != DMOE_FP16))
+    return DMOE_ERR_INVALID_ARG;
+  // rows and matrices are read in boxes of 16 bytes; a unit's place is packed in 8 bits each
+  if (d->d_model % 8 != 0 || d->d_ff % 8 != 0 || d->d_model > kMaxDModel || d->d_ff > kMaxDModel ||
+      d->n_experts > kMaxFfnExperts || n_groups > kMaxFfnExperts || R > kMaxPairs)
+    return DMOE_ERR_UNSUPPORTED;
+  // units (up to 256 rows x 128 features of a group) are counted in 32 bits, whatever offsets hold
+  const int64_t tiles = (std::max(d->d_model, d->d_ff) + 127) / 128;
+  if ((R / 32 < 8 ? 2 : R / 256 + 1) * tiles * n_groups > INT32_MAX) return DMOE_ERR_UNSUPPORTED;
+  return DMOE_OK;
+}
+
+// a matrix whose rows are read or written 16 bytes at a time
+bool matrix16(const void* p, int64_t ld, int32_t d) {
+  return given16(p) && ld >= d && ld % 8 == 0 && ld < (int64_t)1 << 38;
+}
+
+FfnArgs expert_args(const dmoe_expert_desc* d, int64_t R, int32_t n_groups, const int32_t* offsets,
+                    const void* w_gate, const void* w_up, const void* w_down) {
+  FfnArgs a{};
+  a.dtype = d->dtype;
+  a.n_experts = d->n_experts;
+  a.d = d->d_model;
+  a.I = d->d_ff;
+  a.R = R;
+  a.n_groups = n_groups;
+  a.offsets = offsets;
+  a.w_gate = w_gate;
+  a.w_up = w_up;
+  a.w_down = w_down;
+  a.hold = g_expert_hold.load(std::memory_order_relaxed) != 0 ? 1 : 0;
+  return a;
 }
 
 }  // namespace
@@ -273,6 +312,97 @@ dmoe_status dmoe_q4_device_error(void* stream, int32_t* info) {
   const dmoe_status st = dmoe_get_device_error(record, stream, info);
   if (st == DMOE_ERR_TIMEOUT) g_q4_hold.store(0);
   return st;
+}
+
+dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_groups,
+                            const void* x, int64_t ldx, const int32_t* offsets,
+                            const int32_t* expert_ids, const void* w_gate, const void* w_up,
+                            const void* w_down, void* pre, void* h, void* y, int64_t ldy,
+                            int32_t zero_rest, void* stream) {
+  const dmoe_status st = check_expert(desc, R, n_groups);
+  if (st != DMOE_OK) return st;
+  if ((offsets == nullptr && n_groups != 1) ||
+      (expert_ids == nullptr && n_groups > desc->n_experts))
+    return DMOE_ERR_INVALID_ARG;
+  if (R == 0) return DMOE_OK;
+  if (!matrix16(x, ldx, desc->d_model) || !matrix16(y, ldy, desc->d_model) || !given16(h) ||
+      !null_or16(pre) || !given16(w_gate) || !given16(w_up) || !given16(w_down) ||
+      !null_or16(offsets) || !null_or16(expert_ids) || y == x || h == x || h == y ||
+      (pre != nullptr && (pre == x || pre == h || pre == y)))
+    return DMOE_ERR_INVALID_ARG;
+  FfnArgs a = expert_args(desc, R, n_groups, offsets, w_gate, w_up, w_down);
+  a.expert_ids = expert_ids;
+  a.x = x;
+  a.ldx = ldx;
+  a.pre = pre;
+  a.h = h;
+  a.y = y;
+  a.ldy = ldy;
+  a.zero_rest = zero_rest != 0;
+  return status_of(launch_expert_ffn(a, static_cast<cudaStream_t>(stream)));
+}
+
+dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, const void* dy,
+                                     int64_t lddy, const void* x, int64_t ldx,
+                                     const int32_t* offsets, const void* w_gate, const void* w_up,
+                                     const void* w_down, const void* pre, const void* h, void* dpre,
+                                     void* dx, int64_t lddx, void* dw_gate, void* dw_up,
+                                     void* dw_down, int32_t zero_rest, void* stream) {
+  const int32_t n_groups = desc != nullptr ? desc->n_experts : 0;
+  const dmoe_status st = check_expert(desc, R, n_groups);
+  if (st != DMOE_OK) return st;
+  const bool inner = dx != nullptr || dw_gate != nullptr;
+  if ((offsets == nullptr && n_groups != 1) || (!inner && dw_down == nullptr) ||
+      (dw_gate == nullptr) != (dw_up == nullptr) || !null_or16(dw_gate) || !null_or16(dw_up) ||
+      !null_or16(dw_down) || (dw_gate != nullptr && dw_gate == dw_up))
+    return DMOE_ERR_INVALID_ARG;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (R == 0) {   // no rows: the weights' gradients are zeros
+    const size_t bytes = (size_t)2 * desc->n_experts * desc->d_model * desc->d_ff;
+    for (void* dw : {dw_gate, dw_up, dw_down})
+      if (dw != nullptr) {
+        const cudaError_t e = cudaMemsetAsync(dw, 0, bytes, s);
+        if (e != cudaSuccess) return status_of(e);
+      }
+    return DMOE_OK;
+  }
+  if (!matrix16(dy, lddy, desc->d_model) || !null_or16(offsets) ||
+      (inner && (!given16(w_down) || !given16(pre) || !given16(dpre) || pre == dpre)) ||
+      (dx != nullptr && (!matrix16(dx, lddx, desc->d_model) || !given16(w_gate) ||
+                         !given16(w_up) || dx == dy || dx == x)) ||
+      (dw_gate != nullptr && !matrix16(x, ldx, desc->d_model)) ||
+      (dw_down != nullptr && !given16(h)))
+    return DMOE_ERR_INVALID_ARG;
+  FfnArgs a = expert_args(desc, R, n_groups, offsets, w_gate, w_up, w_down);
+  a.dy = dy;
+  a.lddy = lddy;
+  a.x = x;
+  a.ldx = ldx;
+  a.pre = const_cast<void*>(pre);
+  a.h = const_cast<void*>(h);
+  a.dpre = dpre;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dw_gate = dw_gate;
+  a.dw_up = dw_up;
+  a.dw_down = dw_down;
+  a.zero_rest = zero_rest != 0;
+  return status_of(launch_expert_ffn_backward(a, s));
+}
+
+dmoe_status dmoe_expert_device_error(void* stream, int32_t* info) {
+  void* record = nullptr;
+  const cudaError_t e = ffn_fault_address(&record);
+  if (e != cudaSuccess) return status_of(e);
+  const dmoe_status st = dmoe_get_device_error(record, stream, info);
+  if (st == DMOE_ERR_TIMEOUT) g_expert_hold.store(0);
+  return st;
+}
+
+dmoe_status dmoe_expert_set_debug_hold(int32_t hold) {
+  if (hold < 0) return DMOE_ERR_INVALID_ARG;
+  g_expert_hold.store(hold);
+  return DMOE_OK;
 }
 
 }  // extern "C"

@@ -429,6 +429,26 @@ __host__ __device__ constexpr uint32_t idesc_bf16(uint32_t M, uint32_t N) {
          | ((M >> 4) << 24);   // M / 16
 }
 
+// The same for an operand whose reduction dimension is the slow one (MN-major): 128-B rows of 64
+// elements of M (or N), one row per k, in groups of 8 rows (1 KB, swizzled within). `lbo` bytes from
+// one block of 64 elements to the next, 1 KB from one group of 8 k to the next. Advancing K by 16
+// adds 2 KB to the start.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lbo) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+// Instruction descriptor, kind::f16: both operands bf16 or both fp16, each K-major or MN-major.
+__host__ __device__ constexpr uint32_t idesc_16bit(uint32_t M, uint32_t N, bool bf16, bool a_mn,
+                                                   bool b_mn) {
+  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_mn ? 1u << 15 : 0u) |
+         (b_mn ? 1u << 16 : 0u) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+
 // ------------------------------------------------------------------ epilogue helpers
 // A thread holds eight tokens' values of one row; the row of lane xor 1 is its neighbour. After
 // the swap it holds two neighbouring rows (the lower one first) of four tokens: the even
