@@ -473,6 +473,59 @@ dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, co
 dmoe_status dmoe_expert_device_error(void* stream, int32_t* info);
 dmoe_status dmoe_expert_set_debug_hold(int32_t hold);
 
+/* The norms before and after a block with its gate and its residual, in one pass over the rows:
+ *   p[t] = y[t] * ry[t] * w_post                       (w_post NULL: p = y)
+ *   r[t] = scale * x[t] + gate[t / gate_tokens] * p[t] (gate NULL: ones)
+ *   n[t] = r[t] * rr[t] * w_pre                        (w_pre NULL: there is no n)
+ *   ry = 1 / sqrt(mean(y^2) + eps),  rr = 1 / sqrt(mean(r^2) + eps)  over the row's d elements
+ * in fp32, r and n rounded once each (n from the unrounded r). y is a block's output, x the residual
+ * stream, n the next block's input; without y it is the norm before a first block alone.
+ * Limits: 1 <= d <= 16384, 0 <= T <= 2^30, eps >= 0. */
+typedef struct {
+  int32_t dtype;          /* dmoe_dtype of all rows and of the gate */
+  int32_t d;
+  int64_t T;              /* tokens */
+  int64_t gate_tokens;    /* tokens that share a row of the gate: 1 (one each), a block's, a
+                             sequence's, T or more (one for all); 0 where there is no gate */
+  float scale;            /* of the residual */
+  float eps;
+} dmoe_norm_desc;
+
+/*   x      [T, d], row stride ldx       y     [T, d] (ldy), or NULL (then w_post and gate are, too)
+ *   w_post, w_pre  fp32 [d], or NULL    gate  [ceil(T / gate_tokens), d] (ldgate), or NULL
+ *   r      [T, d] out (ldr), or NULL if n is wanted alone; may be x itself (with its stride)
+ *   n      [T, d] out (ldn) where w_pre is given, else NULL; may be y itself (with its stride)
+ *   stats  fp32 [2, T] out: ry and rr (1 where there is no such norm), for the backward pass; or
+ *          NULL */
+dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y,
+                               int64_t ldy, const float* w_post, const void* gate, int64_t ldgate,
+                               const float* w_pre, void* r, int64_t ldr, void* n, int64_t ldn,
+                               float* stats, void* stream);
+
+/* Bytes of the workspace of dmoe_norm_residual_backward (host only). They grow with T and d, and a
+ * workspace for a desc with a gate serves one without. It needs no preparation, and nothing in it
+ * has to last from call to call. */
+dmoe_status dmoe_norm_workspace_size(const dmoe_norm_desc* desc, size_t* bytes /* host */);
+
+/* The gradients by x, y, the gate and the weights, from those by r (dr) and by n (dn), either of
+ * which may be NULL for zeros (dn is, where w_pre is). r is computed again from x and y, so these
+ * have to be as they were.
+ *   x, y, w_post, gate, w_pre  as above;  stats  as written there
+ *   dr, dn     [T, d], row strides lddr, lddn
+ *   dx, dy     [T, d] out (lddx, lddy);  dgate  out, of the gate's shape (lddgate): sums over the
+ *              tokens of a gate row, in fp32, rounded once
+ *   dw_post, dw_pre  fp32 [d] out: sums over all tokens
+ *              Any of the five may be NULL, but not all; none overlaps an input
+ *   workspace  16-byte aligned; NULL is allowed for dx and dy alone
+ * Sums over tokens are taken in an order that follows from the sizes: the same call gives the same
+ * bits. */
+dmoe_status dmoe_norm_residual_backward(
+    const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y, int64_t ldy,
+    const float* w_post, const void* gate, int64_t ldgate, const float* w_pre, const float* stats,
+    const void* dr, int64_t lddr, const void* dn, int64_t lddn, void* dx, int64_t lddx, void* dy,
+    int64_t lddy, void* dgate, int64_t lddgate, float* dw_post, float* dw_pre, void* workspace,
+    size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`, then reads and clears the fault code the kernels recorded in
  * `workspace`. Returns DMOE_OK if none, DMOE_ERR_TIMEOUT for a bounded wait that ran out,
  * DMOE_ERR_DEVICE for any other recorded fault, DMOE_ERR_CUDA if the sync failed.

@@ -26,6 +26,8 @@ __all__ = [
     "dmoe_q4_dequantize", "dmoe_q4_linear", "dmoe_q4_swiglu",
     "dmoe_q4_device_error",
     "ExpertDesc", "dmoe_expert_ffn", "dmoe_expert_ffn_backward", "dmoe_expert_device_error",
+    "NormDesc", "dmoe_norm_residual", "dmoe_norm_workspace_size", "alloc_norm_workspace",
+    "dmoe_norm_residual_backward",
 ]
 
 DMOE_ROUTE_TOKEN = 0
@@ -75,6 +77,12 @@ class ExpertDesc(ctypes.Structure):
     """dmoe_expert_desc (include/dmoe.h)."""
     _fields_ = [("dtype", ctypes.c_int32), ("n_experts", ctypes.c_int32),
                 ("d_model", ctypes.c_int32), ("d_ff", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    """dmoe_norm_desc (include/dmoe.h)."""
+    _fields_ = [("dtype", ctypes.c_int32), ("d", ctypes.c_int32), ("T", ctypes.c_int64),
+                ("gate_tokens", ctypes.c_int64), ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 class DmoeError(RuntimeError):
@@ -133,6 +141,7 @@ def _load() -> ctypes.CDLL:
     sizes = ctypes.POINTER(size)
     products = [Q, i64, i32, P, i64, i64, P, i32, P, P]
     X = ctypes.POINTER(ExpertDesc)
+    N = ctypes.POINTER(NormDesc)
     for name, args in {
             "dmoe_sort_workspace_size": [i64, i32, i32, sizes],
             "dmoe_sort_tokens": [i64, i32, i32, P, P, P, P, P, size, P],
@@ -149,6 +158,10 @@ def _load() -> ctypes.CDLL:
             "dmoe_expert_ffn_backward": [X, i64, P, i64, P, i64] + [P] * 8 + [i64] + [P] * 3 + [i32, P],
             "dmoe_expert_device_error": [P, ctypes.POINTER(i32)],
             "dmoe_expert_set_debug_hold": [i32],
+            "dmoe_norm_residual": [N] + [P, i64] * 2 + [P, P, i64, P] + [P, i64] * 2 + [P, P],
+            "dmoe_norm_workspace_size": [N, sizes],
+            "dmoe_norm_residual_backward": [N] + [P, i64] * 2 + [P, P, i64, P, P] + [P, i64] * 5 +
+                                           [P, P, P, size, P],
             "dmoe_q4_linear": products + [P] * 2 + [P, i64, i32, P],
             "dmoe_q4_swiglu": products + [P] * 4 + [P, i64, i32, P]}.items():
         fn = getattr(lib, name)
@@ -642,6 +655,63 @@ def dmoe_expert_set_debug_hold(hold: int) -> None:
     """Diagnostic: makes the feed-forward block's bounded waits run out while `hold` is nonzero;
     cleared by dmoe_expert_device_error."""
     _check(_lib.dmoe_expert_set_debug_hold(int(hold)), "dmoe_expert_set_debug_hold")
+
+
+def _norm_args(x, y, w_post, gate, w_pre, scale, eps, gate_tokens):
+    """(desc, device, arguments of what both directions read, None where there is nothing)."""
+    dt = _row_dtype(x, "x")
+    T, d = x.shape
+    dev, t = x.get_device(), x.dtype
+    G = 0 if gate is None else int(gate_tokens) or 1
+    px, ldx = _matrix(x, "x", T, d, t, dev)
+    py, ldy = (None, 0) if y is None else _matrix(y, "y", T, d, t, dev)
+    pg, ldg = (None, 0) if gate is None else _matrix(gate, "gate", -(-T // G) if G > 0 else 0, d, t, dev)
+    return (NormDesc(dt, d, T, G, scale, eps), dev,
+            (px, ldx, py, ldy, _vector(w_post, "w_post", d, torch.float32, dev), pg, ldg,
+             _vector(w_pre, "w_pre", d, torch.float32, dev)))
+
+
+def dmoe_norm_residual(x, y, w_post, gate, w_pre, r, n, stats=None, scale=1.0, eps=1e-6, gate_tokens=0,
+                       stream=None) -> None:
+    """r = scale * x + gate * norm(y) * w_post, n = norm(r) * w_pre. y, w_post, gate, w_pre (with n) and r
+    may be None; gate [ceil(T / gate_tokens), d]: row t // gate_tokens holds for token t."""
+    desc, dev, args = _norm_args(x, y, w_post, gate, w_pre, scale, eps, gate_tokens)
+    T, d, t = desc.T, desc.d, x.dtype
+    pr, ldr = (None, 0) if r is None else _matrix(r, "r", T, d, t, dev)
+    pn, ldn = (None, 0) if n is None else _matrix(n, "n", T, d, t, dev)
+    _launch(_lib.dmoe_norm_residual, dev, stream, ctypes.byref(desc), *args, pr, ldr, pn, ldn,
+            _vector(stats, "stats", 2 * T, torch.float32, dev))
+
+
+def dmoe_norm_workspace_size(T: int, d: int, gate_tokens: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    desc = NormDesc(0, d, T, gate_tokens, 1.0, 0.0)
+    _check(_lib.dmoe_norm_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "dmoe_norm_workspace_size")
+    return n.value
+
+
+def alloc_norm_workspace(T: int, d: int, gate_tokens: int = 0, device="cuda") -> torch.Tensor:
+    """A workspace for dmoe_norm_residual_backward of these sizes."""
+    return torch.empty(dmoe_norm_workspace_size(T, d, gate_tokens), dtype=torch.uint8, device=device)
+
+
+def dmoe_norm_residual_backward(x, y, w_post, gate, w_pre, stats, dr, dn, dx, dy, dgate, dw_post, dw_pre,
+                                scale=1.0, gate_tokens=0, workspace=None, stream=None) -> None:
+    """dmoe_norm_residual's gradients by x, y, gate and the weights (any may be None) from those by r and
+    by n (either may be None)."""
+    desc, dev, args = _norm_args(x, y, w_post, gate, w_pre, scale, 0.0, gate_tokens)
+    T, d, t = desc.T, desc.d, x.dtype
+    more = []
+    for name, m, rows in (("dr", dr, T), ("dn", dn, T), ("dx", dx, T), ("dy", dy, T),
+                          ("dgate", dgate, 0 if gate is None else gate.shape[0])):
+        more += (None, 0) if m is None else _matrix(m, name, rows, d, t, dev)
+    f32 = torch.float32
+    ws = (None, 0)
+    if workspace is not None:
+        ws = (_vector(workspace, "workspace", workspace.numel(), torch.uint8, dev), workspace.numel())
+    _launch(_lib.dmoe_norm_residual_backward, dev, stream, ctypes.byref(desc), *args,
+            _vector(stats, "stats", 2 * T, f32, dev), *more, _vector(dw_post, "dw_post", d, f32, dev),
+            _vector(dw_pre, "dw_pre", d, f32, dev), *ws)
 
 
 KERNELS = {"router": 0, "dispatch": 1, "gather": 2, "experts": 3, "combine": 4}

@@ -405,6 +405,30 @@ cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s);
 cudaError_t ffn_fault_address(void** p);
 
+// The norms around a block with its gate and residual (norm_rows.cu). Strides in elements.
+struct NormArgs {
+  int dtype;
+  int64_t T;
+  int d, gate_tokens;          // gate_tokens 0: no gate
+  float scale, eps;
+  const void *x, *y, *gate;
+  int64_t ldx, ldy, ldgate;
+  const float *w_post, *w_pre;   // [d] or null
+  void *r, *n;                 // forward
+  int64_t ldr, ldn;
+  float* stats;                // [2, T]: 1 / rms of y and of r
+  const void *dr, *dn;         // backward
+  int64_t lddr, lddn;
+  void *dx, *dy, *dgate;
+  int64_t lddx, lddy, lddgate;
+  float *dw_post, *dw_pre;
+  float* workspace;
+};
+constexpr int kNormCtas = 304;   // of the backward launch, at most (two per SM)
+size_t norm_workspace_bytes(int64_t T, int d, int gate_tokens);
+cudaError_t launch_norm_residual(const NormArgs& a, cudaStream_t s);
+cudaError_t launch_norm_residual_backward(const NormArgs& a, cudaStream_t s);
+
 // profiling events (dmoe_set_profile_events), per host thread
 void prof_begin(int kernel, cudaStream_t s);
 void prof_end(int kernel, cudaStream_t s);

@@ -145,6 +145,40 @@ FfnArgs expert_args(const dmoe_expert_desc* d, int64_t R, int32_t n_groups, cons
   return a;
 }
 
+dmoe_status check_norm(const dmoe_norm_desc* d) {
+  if (d == nullptr || d->dtype < DMOE_BF16 || d->dtype > DMOE_FP32 || d->d <= 0 || d->T < 0 ||
+      d->gate_tokens < 0 || !(d->eps >= 0.f))
+    return DMOE_ERR_INVALID_ARG;
+  return d->d > kMaxDModel || d->T > kMaxPairs ? DMOE_ERR_UNSUPPORTED : DMOE_OK;
+}
+
+// what both directions read: x; y, its weight and its gate, or none of the three
+bool norm_inputs(const dmoe_norm_desc* d, const void* x, int64_t ldx, const void* y, int64_t ldy,
+                 const float* w_post, const void* gate, int64_t ldgate, const float* w_pre,
+                 NormArgs* a) {
+  if (!matrix(x, ldx, d->dtype, d->d) || (y != nullptr && !matrix(y, ldy, d->dtype, d->d)) ||
+      (y == nullptr && (w_post != nullptr || gate != nullptr)) || !null_or16(w_post) ||
+      !null_or16(w_pre) ||
+      (gate != nullptr && (!matrix(gate, ldgate, d->dtype, d->d) || d->gate_tokens == 0)))
+    return false;
+  *a = NormArgs{};
+  a->dtype = d->dtype;
+  a->T = d->T;
+  a->d = d->d;
+  a->gate_tokens = gate != nullptr ? (int)std::min<int64_t>(d->gate_tokens, d->T) : 0;
+  a->scale = d->scale;
+  a->eps = d->eps;
+  a->x = x;
+  a->ldx = ldx;
+  a->y = y;
+  a->ldy = ldy;
+  a->gate = gate;
+  a->ldgate = ldgate;
+  a->w_post = w_post;
+  a->w_pre = w_pre;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -403,6 +437,96 @@ dmoe_status dmoe_expert_set_debug_hold(int32_t hold) {
   if (hold < 0) return DMOE_ERR_INVALID_ARG;
   g_expert_hold.store(hold);
   return DMOE_OK;
+}
+
+dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y,
+                               int64_t ldy, const float* w_post, const void* gate, int64_t ldgate,
+                               const float* w_pre, void* r, int64_t ldr, void* n, int64_t ldn,
+                               float* stats, void* stream) {
+  const dmoe_status st = check_norm(desc);
+  if (st != DMOE_OK || desc->T == 0) return st;
+  const int dt = desc->dtype, d = desc->d;
+  NormArgs a;
+  if (!norm_inputs(desc, x, ldx, y, ldy, w_post, gate, ldgate, w_pre, &a) ||
+      (w_pre == nullptr) != (n == nullptr) || (r == nullptr && n == nullptr) ||
+      (r != nullptr && !matrix(r, ldr, dt, d)) || (n != nullptr && !matrix(n, ldn, dt, d)) ||
+      !null_or16(stats) || (r != nullptr && (r == n || r == y || r == gate)) ||
+      (n != nullptr && (n == x || n == gate)) || (r == x && ldr != ldx) ||
+      (n != nullptr && n == y && ldn != ldy))
+    return DMOE_ERR_INVALID_ARG;
+  a.r = r;
+  a.ldr = ldr;
+  a.n = n;
+  a.ldn = ldn;
+  a.stats = stats;
+  return status_of(launch_norm_residual(a, static_cast<cudaStream_t>(stream)));
+}
+
+dmoe_status dmoe_norm_workspace_size(const dmoe_norm_desc* desc, size_t* bytes) {
+  if (bytes == nullptr) return DMOE_ERR_INVALID_ARG;
+  const dmoe_status st = check_norm(desc);
+  if (st != DMOE_OK) return st;
+  *bytes = norm_workspace_bytes(desc->T, desc->d, desc->gate_tokens > 0 ? 1 : 0);
+  return DMOE_OK;
+}
+
+dmoe_status dmoe_norm_residual_backward(
+    const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y, int64_t ldy,
+    const float* w_post, const void* gate, int64_t ldgate, const float* w_pre, const float* stats,
+    const void* dr, int64_t lddr, const void* dn, int64_t lddn, void* dx, int64_t lddx, void* dy,
+    int64_t lddy, void* dgate, int64_t lddgate, float* dw_post, float* dw_pre, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  const dmoe_status st = check_norm(desc);
+  if (st != DMOE_OK) return st;
+  const int dt = desc->dtype, d = desc->d;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((dx == nullptr && dy == nullptr && dgate == nullptr && dw_post == nullptr && dw_pre == nullptr) ||
+      !null_or16(dw_post) || !null_or16(dw_pre) || (dw_post != nullptr && dw_post == dw_pre))
+    return DMOE_ERR_INVALID_ARG;
+  if (desc->T == 0) {   // no tokens: the weights' gradients are zeros
+    for (float* dw : {dw_post, dw_pre})
+      if (dw != nullptr) {
+        const cudaError_t e = cudaMemsetAsync(dw, 0, sizeof(float) * d, s);
+        if (e != cudaSuccess) return status_of(e);
+      }
+    return DMOE_OK;
+  }
+  NormArgs a;
+  if (!norm_inputs(desc, x, ldx, y, ldy, w_post, gate, ldgate, w_pre, &a) || !given16(stats) ||
+      (dr == nullptr && dn == nullptr) || (dr != nullptr && !matrix(dr, lddr, dt, d)) ||
+      (dn != nullptr && (!matrix(dn, lddn, dt, d) || w_pre == nullptr)) ||
+      (dx != nullptr && !matrix(dx, lddx, dt, d)) ||
+      (dy != nullptr && (!matrix(dy, lddy, dt, d) || y == nullptr)) ||
+      (dgate != nullptr && (!matrix(dgate, lddgate, dt, d) || gate == nullptr)) ||
+      (dw_post != nullptr && w_post == nullptr) || (dw_pre != nullptr && w_pre == nullptr))
+    return DMOE_ERR_INVALID_ARG;
+  void* const outs[] = {dx, dy, dgate};
+  for (int i = 0; i < 3; ++i)
+    if (outs[i] != nullptr) {
+      for (const void* in : {x, y, gate, dr, dn})
+        if (outs[i] == in) return DMOE_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (outs[i] == outs[j]) return DMOE_ERR_INVALID_ARG;
+    }
+  if (dw_post != nullptr || dw_pre != nullptr || (dgate != nullptr && a.gate_tokens > 1)) {
+    if (workspace == nullptr || !aligned(workspace, 16)) return DMOE_ERR_INVALID_ARG;
+    if (workspace_bytes < norm_workspace_bytes(desc->T, d, a.gate_tokens)) return DMOE_ERR_WORKSPACE;
+  }
+  a.stats = const_cast<float*>(stats);
+  a.dr = dr;
+  a.lddr = lddr;
+  a.dn = dn;
+  a.lddn = lddn;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.dgate = dgate;
+  a.lddgate = lddgate;
+  a.dw_post = dw_post;
+  a.dw_pre = dw_pre;
+  a.workspace = static_cast<float*>(workspace);
+  return status_of(launch_norm_residual_backward(a, s));
 }
 
 }  // extern "C"

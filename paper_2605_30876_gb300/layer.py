@@ -1,6 +1,6 @@
 """Resident MoE layers: device weights, workspace and output buffers around the library's calls
 (argument marshalling only; the forwards run in libdmoe's kernels). MoELayer holds bf16 weights,
-MoELayerQ4 the same layer's experts in 4 bits."""
+MoELayerQ4 the same layer's experts in 4 bits, MoEBlock a layer with the norms around it."""
 from __future__ import annotations
 
 import contextlib
@@ -9,7 +9,7 @@ from typing import Dict, Optional
 import torch
 
 from . import (DMOE_ROUTE_BLOCK, LayerDesc, alloc_q4, alloc_workspace, dmoe_combine_rows,
-               dmoe_dispatch, dmoe_layer_forward, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_size,
+               dmoe_dispatch, dmoe_layer_forward, dmoe_norm_residual, dmoe_q4_linear, dmoe_q4_quantize, dmoe_q4_size,
                dmoe_q4_swiglu, dmoe_router, dmoe_router_prepare, make_desc, make_q4_desc)
 
 _AS_IT_IS = contextlib.nullcontext()
@@ -205,3 +205,39 @@ class MoELayerQ4:
             dmoe_q4_linear(d.desc, self.hs, None, d.codes, d.scales, self.y_shared, stream=stream)
         dmoe_combine_rows(self.ys[:self.desc.T * k], self.pos, self.topk_gate, self.y_shared, out,
                           stream=stream)
+
+
+class MoEBlock:
+    """A MoE layer (MoELayer or MoELayerQ4) in its residual stream, for serving: from the residual r and
+    the layer's input n to the next residual and the next block's input,
+
+        y = layer(n),  r' = scale * r + gate * norm(y) * w_post,  n' = norm(r') * w_pre
+
+    in the layer's launches and one more. w_post (None: y is not normed) and w_pre (None: there is no
+    n') are fp32 [d]. Its buffers serve one forward at a time, as the layer's do.
+    """
+
+    def __init__(self, layer, w_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+                 scale: float = 1.0, eps: float = 1e-6):
+        self.layer, self.w_post, self.w_pre, self.scale, self.eps = layer, w_post, w_pre, scale, eps
+        self.r = torch.empty_like(layer.y)
+        self.n = torch.empty_like(layer.y) if w_pre is not None else None
+
+    def enter(self, r: torch.Tensor, w_pre: torch.Tensor, n: Optional[torch.Tensor] = None, stream=None):
+        """The norm before the first block: n = norm(r) * w_pre (into a tensor of its own, or `n`)."""
+        n = torch.empty_like(r) if n is None else n
+        with _in_stream(stream, r.device):
+            dmoe_norm_residual(r, None, None, None, w_pre, None, n, eps=self.eps, stream=stream)
+        return n
+
+    def forward(self, r: torch.Tensor, n: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                gate_tokens: int = 0, r_out: Optional[torch.Tensor] = None,
+                n_out: Optional[torch.Tensor] = None, stream=None):
+        """(r', n'), in the block's buffers unless r_out (which may be r) or n_out are given. gate:
+        [ceil(T / gate_tokens), d], or None."""
+        y = self.layer.forward(n, stream=stream)
+        r_out = self.r if r_out is None else r_out
+        n_out = n_out if n_out is not None or self.w_pre is None else self.n
+        dmoe_norm_residual(r, y, self.w_post, gate, self.w_pre, r_out, n_out, scale=self.scale,
+                           eps=self.eps, gate_tokens=gate_tokens, stream=stream)
+        return r_out, n_out

@@ -58,8 +58,9 @@ def forward(x, offsets, w_gate, w_up, w_down, ids=None):
     return out
 
 
-def backward(dy, x, offsets, w_gate, w_up, w_down, pre, h):
-    """The same of dpre (gate, up), dx and the three weights' gradients, from pre and h as given."""
+def backward(dy, x, offsets, w_gate, w_up, w_down, pre, h, off=None):
+    """The same of dpre (gate, up), dx and the three weights' gradients, from pre and h as given; off: how
+    far the kernel's g, u and h may be from those, rows by rows."""
     dt, (R, d), (E, I) = x.dtype, x.shape, w_gate.shape[:2]
     nan = lambda n: torch.full((R, n), float("nan"), dtype=torch.float64, device=x.device)
     out = {n: (nan(k), nan(k)) for n, k in (("dg", I), ("du", I), ("dx", d))}
@@ -80,6 +81,11 @@ def backward(dy, x, offsets, w_gate, w_up, w_down, pre, h):
         dg, du = dh * fg, dh * fu
         edg = edh * (fg.abs() + FN * part) + FN * dh.abs() * part
         edu = edh * fu.abs() * (1 + FN) + FN * du.abs()
+        eh = torch.zeros_like(H)
+        if off is not None:      # |s'| = |(silu)'| <= 1.1, |silu''| <= 0.5
+            og, ou, eh = (o[lo:hi] for o in off)
+            edg = edg + (dh.abs() + edh) * (1.1 * ou + 0.5 * og * (u.abs() + ou))
+            edu = edu + (dh.abs() + edh) * 1.1 * og
         rdg, rdu = edg + rounding(dg.abs() + edg, dt), edu + rounding(du.abs() + edu, dt)
         dx = dg @ G + du @ U
         size = (dg.abs() + rdg) @ G.abs() + (du.abs() + rdu) @ U.abs()
@@ -87,10 +93,12 @@ def backward(dy, x, offsets, w_gate, w_up, w_down, pre, h):
         for name, v, b in (("dg", dg, edg), ("du", du, edu), ("dx", dx, edx)):
             out[name][0][lo:hi] = v
             out[name][1][lo:hi] = b + rounding(v.abs() + b, dt)
-        for name, a, ea, b in (("dw_gate", dg, rdg, X), ("dw_up", du, rdu, X),
-                               ("dw_down", DY, torch.zeros_like(DY), H)):
+        none, zero = torch.zeros_like(X), torch.zeros_like(DY)
+        for name, a, ea, b, eb in (("dw_gate", dg, rdg, X, none), ("dw_up", du, rdu, X, none),
+                                   ("dw_down", DY, zero, H, eh)):
             v = a.t() @ b
-            err = ea.t() @ b.abs() + acc(n) * ((a.abs() + ea).t() @ b.abs())
+            size = (a.abs() + ea).t() @ (b.abs() + eb)
+            err = ea.t() @ (b.abs() + eb) + a.abs().t() @ eb + acc(n) * size
             out[name][0][e] = v
             out[name][1][e] = err + rounding(v.abs() + err, dt)
     return out

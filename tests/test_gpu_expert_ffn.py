@@ -108,3 +108,171 @@ def test_backward(shape, dtype):
     pre, h, _ = run_forward(c)
     check_backward(c, pre, h, run_backward(c, pre, h))
     check_backward(c, pre, h, run_backward(c, pre, h, zero_rest=True, stride=8), zero_rest=True)
+
+
+def test_expert_ids():
+    """Groups in any order, an expert in two groups, ids that are no expert's."""
+    c = case(torch.bfloat16, 6, 136, 72, [20, 5, 0, 40, 33, 2], 4)
+    ids = torch.tensor([5, 0, 3, 5, -1, 6], dtype=torch.int32, device="cuda")
+    check_forward(c, run_forward(c, ids), ids)
+    check_forward(c, run_forward(c, ids, zero_rest=True), ids, zero_rest=True)
+    # more groups than experts
+    few = dict(c, w_gate=c["w_gate"][:2].contiguous(), w_up=c["w_up"][:2].contiguous(),
+               w_down=c["w_down"][:2].contiguous())
+    ids = torch.tensor([1, 0, 0, 1, 0, 1], dtype=torch.int32, device="cuda")
+    check_forward(few, run_forward(few, ids), ids)
+
+
+def test_one_expert_of_all_rows():
+    c = case(torch.float16, 1, 200, 104, [71], 0)
+    want = run_forward(c)
+    dense = dict(c, offsets=None)
+    for a, b in zip(run_forward(dense), want):
+        assert torch.equal(a, b)
+    got, same = run_backward(dense, *want[:2]), run_backward(c, *want[:2])
+    assert all(torch.equal(got[n], same[n]) for n in got)
+
+
+@pytest.mark.parametrize("offsets", [[-7, 10, 30, 99], [0, 30, 10, 50], [50, 50, 60, 7], [3, 3, 20, 41]])
+def test_offsets_that_are_cut(offsets):
+    c = case(torch.bfloat16, 3, 72, 72, [10, 20, 20], 0)
+    c["offsets"] = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    got = run_forward(c)
+    if offsets != [0, 30, 10, 50]:         # (two groups share rows there: either's values)
+        check_forward(c, got)
+        check_backward(c, *got[:2], run_backward(c, *got[:2]))
+    else:
+        run_backward(c, *got[:2])
+        assert dm.dmoe_expert_device_error()[0] == 0
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_other_experts_rows_and_weights_stay_out(bad):
+    """Rows of other groups, rows of none and other experts' weights do not reach a group's results."""
+    c = case(torch.bfloat16, 3, 136, 72, [21, 35, 70], 10)
+    pre, h, y = run_forward(c)
+    want = run_backward(c, pre, h)
+    for where in ("rows", "weights"):
+        b = {k: v.clone() for k, v in c.items()}
+        if where == "rows":
+            b["x"][21:56] = bad
+            b["dy"][21:56] = bad
+            b["x"][126:] = bad
+            b["dy"][126:] = bad
+        else:
+            for n in ("w_gate", "w_up", "w_down"):
+                b[n][1] = bad
+        pre2, h2, y2 = run_forward(b)
+        keep = torch.ones(136, dtype=torch.bool, device="cuda")
+        keep[21:56] = False
+        for a, z in ((pre, pre2), (h, h2), (y, y2)):
+            assert torch.equal(a[keep], z[keep])
+        got = run_backward(b, pre2, h2)
+        assert torch.equal(got["dx"][keep], want["dx"][keep])
+        for n in ("dw_gate", "dw_up", "dw_down"):
+            assert torch.equal(got[n][[0, 2]], want[n][[0, 2]])
+
+
+@pytest.mark.parametrize("skip", [("dx",), ("dw_gate", "dw_up"), ("dw_down",), ("dx", "dw_gate", "dw_up", "dpre"),
+                                  ("dw_gate", "dw_up", "dw_down")])
+def test_some_of_the_gradients(skip):
+    c = case(torch.bfloat16, 2, 72, 136, [40, 13], 0)
+    pre, h, _ = run_forward(c)
+    whole, got = run_backward(c, pre, h), run_backward(c, pre, h, skip=skip)
+    assert all(got[n] is None or torch.equal(got[n], whole[n]) for n in got)
+
+
+def test_no_rows():
+    c = case(torch.bfloat16, 2, 72, 136, [0, 0], 0)
+    pre, h, y = run_forward(c)
+    got = run_backward(c, pre, h)
+    assert y.shape == (0, 72) and all((got[n] == 0).all() for n in ("dw_gate", "dw_up", "dw_down"))
+    c = case(torch.bfloat16, 2, 72, 136, [0, 0], 5)            # rows, but none of an expert
+    pre, h, y = run_forward(c, zero_rest=True)
+    got = run_backward(c, pre, h, zero_rest=True)
+    assert (y == 0).all() and (h == 7).all() and all((v == 0).all() for n, v in got.items() if n != "dpre")
+
+
+def test_rows_and_offsets_beyond_32_bits():
+    """Elements of h, pre and x further than 2^31 from their bases."""
+    d, I, R = 1096, 520, 2100000
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda *s, size=1.0: torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(0, size, generator=gen)
+    x, w = new(R, d), (new(2, I, d, size=0.03), new(2, I, d, size=0.03), new(2, d, I, size=0.04))
+    offsets = torch.tensor([0, R - 300, R], dtype=torch.int32, device="cuda")
+    pre, h, y = (torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in ((R, 2, I), (R, I), (R, d)))
+    dm.dmoe_expert_ffn(x, offsets, *w, h, y, pre=pre)
+    last = slice(R - 300, R)
+    c = dict(x=x[last], offsets=torch.tensor([0, 0, 300], dtype=torch.int32, device="cuda"), w_gate=w[0],
+             w_up=w[1], w_down=w[2], dy=x[:300])
+    check_forward(c, (pre[last], h[last], y[last]))
+    dpre, dx = torch.empty_like(pre), torch.empty_like(x)
+    dw = [torch.empty_like(t) for t in w]
+    dy = y
+    dy[last] = x[:300]
+    dm.dmoe_expert_ffn_backward(dy, x, offsets, *w, pre, h, dpre, dx, *dw)
+    want = O.backward(dy[last], x[last], [0, 0, 300], *w, pre[last], h[last])
+    O.check("dx", dx[last], want["dx"])
+    O.check("dg", dpre[last, 0], want["dg"])
+    for n, v in zip(("dw_gate", "dw_up", "dw_down"), dw):
+        O.check(n, v[1], (want[n][0][1], want[n][1][1]))
+
+
+def test_same_call_same_bits_on_any_stream():
+    c = case(torch.bfloat16, 5, 264, 136, [33, 0, 260, 7, 100], 3)
+    want = run_forward(c)
+    grads = run_backward(c, *want[:2])
+    torch.cuda.synchronize()
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        a = run_forward(c)
+    with torch.cuda.stream(other):
+        b = run_forward(c)
+        more = run_backward(c, *want[:2])
+    torch.cuda.synchronize()
+    d = run_forward(c, stream=side)
+    torch.cuda.synchronize()
+    for got in (a, b, d):
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert all(torch.equal(more[n], grads[n]) for n in grads)
+
+
+def test_captured_and_replayed():
+    c = case(torch.float16, 3, 264, 136, [33, 70, 7], 3)
+    R, d, I = 113, 264, 136
+    new = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")
+    pre, h, y, dpre, dx = new(R, 2, I), new(R, I), new(R, d), new(R, 2, I), new(R, d)
+    dw = [torch.zeros_like(t) for t in weights(c)]
+
+    def both():
+        dm.dmoe_expert_ffn(c["x"], c["offsets"], *weights(c), h, y, pre=pre, zero_rest=True)
+        dm.dmoe_expert_ffn_backward(c["dy"], c["x"], c["offsets"], *weights(c), pre, h, dpre, dx, *dw,
+                                    zero_rest=True)
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    c["x"].mul_(-0.5)
+    c["offsets"].copy_(torch.tensor([0, 50, 50, 110], dtype=torch.int32))
+    both()
+    want = [t.clone() for t in (pre[:110], h[:110], y, dpre[:110], dx, *dw)]
+    for t in (pre, h, y, dpre, dx, *dw):
+        t.zero_()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((pre[:110], h[:110], y, dpre[:110], dx, *dw), want))
+
+
+def test_waits_that_run_out_are_recorded():
+    c = case(torch.bfloat16, 2, 264, 136, [33, 70], 0)
+    pre, h, y = run_forward(c)
+    torch.cuda.synchronize()
+    dm.dmoe_expert_set_debug_hold(1)
+    run_forward(c)
+    status, (code, where, _) = dm.dmoe_expert_device_error()
+    assert status == 6 and code == 1 and where == 10
+    assert dm.dmoe_expert_device_error()[0] == 0      # read and cleared, and the hold with it
+    check_forward(c, run_forward(c))
+    check_backward(c, pre, h, run_backward(c, pre, h))
