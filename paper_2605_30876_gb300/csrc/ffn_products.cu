@@ -19,8 +19,9 @@
 // of M, up to 256 columns of N) in turn; they are found on the device from the offsets, so that no
 // call waits for the host. Warp 0 issues the TMA loads, warp 1 of the first CTA the MMAs, warps 2-9
 // run the epilogue from one of two accumulators in tensor memory while the other fills, warp 10
-// decodes units ahead, warp 11 (kGradW) clears what a stage holds behind an expert's last row: the
-// rows there are another expert's, and 0 * inf would not be 0.
+// decodes units ahead. Warp 11: in kGradW it clears what a stage holds behind an expert's last row (the
+// rows there are another expert's, and 0 * inf would not be 0); in kDown and kGradX it writes the
+// zeros of rows in no group, where they are wanted.
 // Sums are fp32 throughout. g, u, dg, du and h are rounded to the rows' type between products: they
 // are the next product's operands, and the tensor cores take 16 bits.
 // Waits are bounded (1 s), record a timeout and unwind.
@@ -77,12 +78,14 @@ struct Params {
   void* pre;                // kUp: written (or null); kGradH: read
   int I;
   int hold;
+  int zero_rest;            // kDown, kGradX
 };
 
-// kSub steps of K = 64 make a stage of the ring: a commit costs the issuing thread about as much
-// as two MMAs, so most stages hold eight MMAs. An expert's rows are few, and an end inside a
-// stage costs loads: kGradW takes four.
+// A commit costs the issuing thread about as much as two MMAs, so slots of the ring are given back
+// after eight MMAs: a stage is two steps of K = 64. An expert's rows are few, and an end inside a
+// stage costs loads: kGradW's stages are one step, given back two at a time.
 template <int kMode> constexpr int sub_steps() { return kMode == kGradW ? 1 : 2; }
+template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1; }
 template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
 template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
 template <int kMode> constexpr int epi_bytes() {
@@ -165,7 +168,7 @@ struct Unit {
 template <int kMode, bool kHalf>
 __global__ void __launch_bounds__(kThreads, 1)
 ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
-  constexpr int kSub = sub_steps<kMode>();
+  constexpr int kSub = sub_steps<kMode>(), kPer = per_commit<kMode>();
   constexpr bool kAmn = a_mn<kMode>(), kBmn = b_mn<kMode>();
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -174,8 +177,8 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   uint8_t* s_epi = smem + (uint32_t)p.stages * stage_bytes;
   uint64_t* full = reinterpret_cast<uint64_t*>(s_epi + epi_bytes<kMode>());
   uint64_t* empty = full + kMaxStages;
-  uint64_t* ready = empty + kMaxStages;      // kGradW: full, and cleared behind the last row
-  uint64_t* acc_full = ready + kMaxStages;
+  uint64_t* tail = empty + kMaxStages;       // kGradW: this CTA's part of a group's last stage
+  uint64_t* acc_full = tail + kMaxStages;
   uint64_t* acc_empty = acc_full + 2;
   uint64_t* drain = acc_empty + 2;
   uint64_t* held = drain + 1;
@@ -192,9 +195,11 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
 
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
-      ptx::mbar_init(&full[s], 1);
+      // kGradW: the first CTA's producer, and for each CTA the producer, or the clearing warp of a
+      // group's last stage
+      ptx::mbar_init(&full[s], kMode == kGradW ? 1 + kCluster : 1);
       ptx::mbar_init(&empty[s], 1);
-      ptx::mbar_init(&ready[s], kCluster);
+      ptx::mbar_init(&tail[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&acc_full[a], 1);
@@ -277,7 +282,6 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     if (lane == 0) {
       const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_normal();
       const uint32_t full0 = ptx::peer_smem(full, 0);
-      const int per_part = (p.K + 63) / 64;
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -285,6 +289,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const Unit un = unit_at(i, false);
         if (un.e < 0) break;
         const int steps = k_steps(un), half = columns(un) / 2;
+        int part = 0, k0 = 0;                   // of the next step
         const int m0 = kMode == kUp ? un.m * 128 + rank * 64 : un.m * 256 + rank * 128;
         int lv = 0, rows = p.level_rows[0];   // the lowest box of rows that holds the half
 #pragma unroll
@@ -295,7 +300,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
                                                                   : (uint32_t)rows * 128u);
         const int b_row = un.row + rank * half;
         for (int c = 0; c < steps; c += kSub) {
-          if (!wait(&empty[stage], phase ^ 1u, i)) {
+          if (stage % kPer == 0 && !wait(&empty[stage / kPer], phase ^ 1u, i)) {
             ok = false;
             break;
           }
@@ -304,17 +309,22 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           uint8_t* b = a + kSub * kTileABytes;
           const uint32_t bar = full0 + 8u * (uint32_t)stage;
           if (kMode == kGradW) {
-            ptx::mbar_arrive_expect_tx(&full[stage], sub_bytes);
+            // the last stage, if it is to be cleared, completes on this CTA's own barrier, and the
+            // clearing warp arrives for this CTA
             const int r = un.row + c * 64;
+            const bool ends = (un.rows & 15) != 0 && c == steps - 1;
+            const uint32_t to = ends ? ptx::peer_smem(&tail[stage], rank) : bar;
+            if (ends) ptx::mbar_arrive_expect_tx(&tail[stage], sub_bytes);
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], ends ? 0 : kCluster * sub_bytes);
+            if (!ends) ptx::mbar_arrive_pair(bar);
             for (int j = 0; j < 2; ++j)
-              ptx::tma_load_3d(a + j * 8192, &tm.a[0], &full[stage], m0 + 64 * j, un.part, r, again);
+              ptx::tma_load_3d_pair(a + j * 8192, &tm.a[0], to, m0 + 64 * j, un.part, r, again);
             for (int j = 0; j < b_boxes; ++j)
-              ptx::tma_load_3d(b + j * 8192, &tm.b[0], &full[stage],
-                               un.n * kNMax + rank * half + 64 * j, 0, r, again);
+              ptx::tma_load_3d_pair(b + j * 8192, &tm.b[0], to, un.n * kNMax + rank * half + 64 * j, 0, r,
+                                    again);
           } else {
             if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], kCluster * n_sub * sub_bytes);
             for (int s = 0; s < n_sub; ++s) {
-              const int part = (c + s) / per_part, k0 = (c + s - part * per_part) * 64;
               uint8_t* as = a + s * kTileABytes;
               if (kMode == kUp) {          // 64 rows of Wg, then 64 of Wu
                 ptx::tma_load_3d_pair(as, &tm.a[0], bar, k0, m0, un.e, once);
@@ -326,6 +336,8 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
                 ptx::tma_load_3d_pair(as + 8192, &tm.a[part], bar, m0 + 64, k0, un.e, once);
               }
               ptx::tma_load_3d_pair(b + s * b_sub, &tm.b[lv], bar, k0, part, b_row, again);
+              k0 += 64;
+              if (k0 >= p.K) { k0 = 0; ++part; }
             }
           }
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -336,28 +348,31 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     }
   } else if (warp == kPlanWarp) {
     // ================= units: counted per group, then decoded ahead of their use
-    int carry = 0;
-    for (int base = 0; base < p.n_groups; base += 32) {
-      const int g = base + lane;
-      int n = 0;
-      if (g < p.n_groups && group_expert(p, g) >= 0) {
-        int64_t row0;
-        int cnt;
-        group_rows(p, g, &row0, &cnt);
-        n = kMode == kGradW ? p.parts * p.m_tiles * p.n_tiles
-                            : (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
-      }
-      int sum = n;
+    const int per_group = p.parts * p.m_tiles * p.n_tiles;   // kGradW
+    int carry = p.n_groups * per_group;
+    if (kMode != kGradW) {
+      carry = 0;
+      for (int base = 0; base < p.n_groups; base += 32) {
+        const int g = base + lane;
+        int n = 0;
+        if (g < p.n_groups && group_expert(p, g) >= 0) {
+          int64_t row0;
+          int cnt;
+          group_rows(p, g, &row0, &cnt);
+          n = (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
+        }
+        int sum = n;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += v;
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += v;
+        }
+        if (g < p.n_groups) s_first[g + 1] = carry + sum;
+        carry += __shfl_sync(0xffffffffu, sum, 31);
       }
-      if (g < p.n_groups) s_first[g + 1] = carry + sum;
-      carry += __shfl_sync(0xffffffffu, sum, 31);
+      if (lane == 0) s_first[0] = 0;
+      __syncwarp();
     }
-    if (lane == 0) s_first[0] = 0;
-    __syncwarp();
     if (lane == 0) {
       const int units = carry;
       for (int i = 0;; ++i) {
@@ -365,6 +380,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         int4 v = make_int4(0, 0, -1, 0);
         if (u < units) {
           int lo = 0, hi = p.n_groups - 1;
+          if (kMode == kGradW) lo = hi = u / per_group;
           while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (s_first[mid] <= u) lo = mid; else hi = mid - 1;
@@ -372,7 +388,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           int64_t row0;
           int cnt;
           group_rows(p, lo, &row0, &cnt);
-          const int local = u - s_first[lo];
+          const int local = u - (kMode == kGradW ? lo * per_group : s_first[lo]);
           if (kMode == kGradW) {
             const int n = local % p.n_tiles, mp = local / p.n_tiles;
             v = make_int4((int)row0, cnt, lo, (mp / p.m_tiles) << 16 | (mp % p.m_tiles) << 8 | n);
@@ -396,6 +412,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     if (rank == 0 && lane == 0) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
+      const uint32_t ring = ptx::smem_addr(smem);
+      bool in = false;        // the next stage was seen full: tested while MMAs are queued, as the
+                              // pipe takes one or two ahead and this thread's pauses are its own
       bool ok = p.hold == 0 || wait(held, 0, -2);
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, false);
@@ -403,35 +422,41 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const int steps = k_steps(un), n = columns(un);
         if (steps == 0) continue;
         const uint32_t idesc = ptx::idesc_16bit(256, (uint32_t)n, !kHalf, kAmn, kBmn);
-        const int per_part = (p.K + 63) / 64;
         const uint32_t d0 = tmem_base + (uint32_t)acc * kNMax;
+        const int K = kMode == kGradW ? un.rows : p.K;
         ok = wait(&acc_empty[acc], acc_phase ^ 1u, i);
         ptx::tc_fence_after();
+        int left = K;                           // of the part's sum
         for (int c = 0; ok && c < steps; c += kSub) {
-          if (kMode == kGradW)
-            ok = wait_for([&] { return ptx::mbar_try_wait_cluster(&ready[stage], phase); }, i);
-          else
-            ok = wait(&full[stage], phase, i);
+          ok = in || wait(&full[stage], phase, i);
           if (!ok) break;
+          // (the clearing warps' words, those of the other CTA as well)
+          if (kMode == kGradW && left < 64 && (left & 15) != 0)
+            asm volatile("fence.acq_rel.cluster;" ::: "memory");
           ptx::tc_fence_after();
-          const uint32_t a = ptx::smem_addr(smem) + (uint32_t)stage * stage_bytes;
-          const uint32_t b = a + kSub * kTileABytes;
+          const uint32_t a = ring + (uint32_t)stage * stage_bytes, b = a + kSub * kTileABytes;
+          const bool last = stage % kPer == kPer - 1;
+          uint64_t* const done = &empty[stage / kPer];
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
 #pragma unroll
           for (int s = 0; s < kSub; ++s) {
             if (c + s >= steps) break;
-            const int left = kMode == kGradW ? un.rows - c * 64
-                                             : p.K - (c + s) % per_part * 64;
-            const int kk_end = min(4, (left + 15) / 16);
-            for (int kk = 0; kk < kk_end; ++kk) {
-              const uint32_t as = a + s * kTileABytes, bs = b + s * b_sub;
+            const uint32_t as = a + s * kTileABytes, bs = b + s * b_sub;
+            auto mma = [&](int kk) {
               ptx::mma_bf16_pair(
                   d0, kAmn ? ptx::sdesc_mn_sw128(as + kk * 2048, 8192) : ptx::sdesc_k_sw128(as + kk * 32),
                   kBmn ? ptx::sdesc_mn_sw128(bs + kk * 2048, 8192) : ptx::sdesc_k_sw128(bs + kk * 32),
                   idesc, (c > 0 || s > 0 || kk > 0) ? 1u : 0u);
-            }
+            };
+            mma(0);
+            if (left > 16) mma(1);
+            if (s == kSub - 1 || c + s + 1 == steps) in = ptx::mbar_test_wait(&full[stage], phase);
+            if (left > 32) mma(2);
+            if (left > 48) mma(3);
+            left -= 64;
+            if (left <= 0) left = K;
           }
-          ptx::mma_commit_pair(&empty[stage]);
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          if (last) ptx::mma_commit_pair(done);
         }
         if (!ok) break;
         ptx::mma_commit_pair(&acc_full[acc]);
@@ -445,34 +470,54 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       }
     }
   } else if (warp == kFixWarp) {
-    // ================= kGradW: zeros in the last stage's rows of K behind the group's last row, up
-    // to the 16 of its last MMA, in both operands of this CTA
-    if (kMode == kGradW) {
-      const uint32_t ready0 = ptx::peer_smem(ready, 0);
+    if constexpr (kMode == kGradW) {
+      // ================= zeros in the rows of K behind the group's last row, up to the 16 of its last
+      // MMA, in both operands of this CTA (a row of K is 128 bytes of each block of 64 columns; the
+      // swizzle stays within it)
+      const uint32_t full0 = ptx::peer_smem(full, 0);
       int stage = 0;
-      uint32_t phase = 0;
+      uint32_t phases = 0;      // of tail, a bit each
       bool ok = true;
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, true);
         if (un.e < 0) break;
         const int steps = k_steps(un), blocks = 2 + (columns(un) / 2 + 63) / 64;
-        for (int c = 0; c < steps; ++c) {
-          ok = __all_sync(0xffffffffu, wait(&full[stage], phase, i));
-          if (!ok) break;
-          const int left = un.rows - c * 64, end = round_up(min(left, 64), 16);
-          if (left < end) {
-            // (a row of K is 128 bytes of each block of 64 columns; the swizzle stays within it)
-            uint8_t* a = smem + (uint32_t)stage * stage_bytes;
-            const int per_block = (end - left) * 8;
-            for (int j = lane; j < blocks * per_block; j += 32) {
-              const int blk = j / per_block, o = j - blk * per_block;
-              *reinterpret_cast<uint4*>(a + blk * 8192 + left * 128 + o * 16) = make_uint4(0, 0, 0, 0);
-            }
-            asm volatile("fence.proxy.async;" ::: "memory");
-          }
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive_cluster(ready0 + 8u * (uint32_t)stage);
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        const int at = (stage + steps - 1) % p.stages;
+        stage = (stage + steps) % p.stages;
+        if ((un.rows & 15) == 0) continue;
+        ok = __all_sync(0xffffffffu, wait(&tail[at], (phases >> at) & 1u, i));
+        if (!ok) break;
+        phases ^= 1u << at;
+        const int from = un.rows & 63, per_block = (16 - (from & 15)) * 8;
+        uint8_t* a = smem + (uint32_t)at * stage_bytes + from * 128;
+        for (int j = lane; j < blocks * per_block; j += 32) {
+          const int blk = j / per_block, o = j - blk * per_block;
+          *reinterpret_cast<uint4*>(a + blk * 8192 + o * 16) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(full0 + 8u * (uint32_t)at);
+      }
+    } else if ((kMode == kDown || kMode == kGradX) && p.zero_rest) {
+      // ================= zeros in the rows in no group, 64 rows at a time
+      uint16_t* out = static_cast<uint16_t*>(p.out);
+      for (int64_t r0 = (int64_t)blockIdx.x * 64; r0 < p.R; r0 += (int64_t)gridDim.x * 64) {
+        uint64_t owned = 0;
+        for (int g = lane; g < p.n_groups; g += 32) {
+          int64_t lo;
+          int cnt;
+          group_rows(p, g, &lo, &cnt);
+          const int64_t hi = lo + cnt;
+          if (cnt == 0 || lo >= r0 + 64 || hi <= r0 || group_expert(p, g) < 0) continue;
+          const int b = lo > r0 ? (int)(lo - r0) : 0, e = hi < r0 + 64 ? (int)(hi - r0) : 64;
+          owned |= (~0ull >> (64 - (e - b))) << b;
+        }
+        owned = (uint64_t)__reduce_or_sync(0xffffffffu, (uint32_t)(owned >> 32)) << 32 |
+                __reduce_or_sync(0xffffffffu, (uint32_t)owned);
+        for (int j = 0; j < 64 && r0 + j < p.R; ++j) {
+          if (owned >> j & 1) continue;
+          uint4* row = reinterpret_cast<uint4*>(out + (r0 + j) * p.ldo);
+          for (int c = lane; c < p.M / 8; c += 32) row[c] = make_uint4(0, 0, 0, 0);
         }
       }
     }
@@ -676,33 +721,6 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   }
 }
 
-// Zeros in the rows of y [R, width] that are in no group: a CTA takes a run of rows.
-constexpr int kZeroRows = 64;
-__global__ void __launch_bounds__(256)
-zero_rest_kernel(const Params p, uint16_t* y, int64_t ldy, int width) {
-  pdl_wait();
-  pdl_launch_dependents();
-  __shared__ uint8_t in_group[kZeroRows];
-  const int64_t r0 = (int64_t)blockIdx.x * kZeroRows;
-  if (threadIdx.x < kZeroRows) in_group[threadIdx.x] = 0;
-  __syncthreads();
-  for (int g = threadIdx.x; g < p.n_groups; g += blockDim.x) {
-    int64_t lo;
-    int cnt;
-    group_rows(p, g, &lo, &cnt);
-    if (cnt == 0 || lo >= r0 + kZeroRows || lo + cnt <= r0 || group_expert(p, g) < 0) continue;
-    const int64_t end = lo + cnt < r0 + kZeroRows ? lo + cnt : r0 + kZeroRows;
-    for (int64_t r = lo > r0 ? lo : r0; r < end; ++r) in_group[r - r0] = 1;
-  }
-  __syncthreads();
-  for (int j = threadIdx.x >> 5; j < kZeroRows && r0 + j < p.R; j += blockDim.x >> 5) {
-    if (in_group[j]) continue;
-    uint16_t* row = y + (r0 + j) * ldy;
-    for (int c = 2 * (threadIdx.x & 31); c < width; c += 64)
-      *reinterpret_cast<uint32_t*>(row + c) = 0u;
-  }
-}
-
 // ------------------------------------------------------------------ host side
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -788,13 +806,15 @@ Params base_params(const FfnArgs& a) {
   p.I = a.I;
   p.parts = 1;
   p.hold = a.hold;
+  p.zero_rest = a.zero_rest ? 1 : 0;
   return p;
 }
 
 // behind the ring: the epilogue's words, barriers, units, alignment
-size_t fixed_smem(int epi) {
-  return 1024 + epi + 8 * (3 * kMaxStages + 6 + 2 * kQueue) + 16 * kQueue + 8 +
-         4 * (kMaxGroups + 1);
+template <int kMode>
+constexpr size_t fixed_smem() {
+  return 1024 + epi_bytes<kMode>() + 8 * (3 * kMaxStages + 6 + 2 * kQueue) + 16 * kQueue + 8 +
+         (kMode == kGradW ? 0 : 4 * (kMaxGroups + 1));
 }
 
 // The rest of the launch: stages, grid. `units`: at most so many.
@@ -804,9 +824,10 @@ cudaError_t launch(Maps& m, Params& p, int64_t units, cudaStream_t s) {
   cudaError_t e = smem_limit(&limit);
   if (e == cudaSuccess) e = raise_limit<kMode, kHalf>(limit);
   if (e != cudaSuccess) return e;
-  const size_t fixed = fixed_smem(epi_bytes<kMode>());
+  constexpr size_t fixed = fixed_smem<kMode>();
   const size_t stage = (size_t)sub_steps<kMode>() * (kTileABytes + (size_t)p.level_rows[0] * 128);
   p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)limit - fixed) / stage);
+  p.stages -= p.stages % per_commit<kMode>();
   if (p.stages < 2) return cudaErrorInvalidConfiguration;
   const int pairs = (int)std::min<int64_t>(device_sm_count() / kCluster, std::max<int64_t>(units, 1));
   return launch_cluster(ffn_products_kernel<kMode, kHalf>, dim3(pairs * kCluster), dim3(kThreads),
@@ -872,17 +893,11 @@ cudaError_t weights_product(const FfnArgs& a, const Rows& out, const Rows& in, v
   return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.parts * p.m_tiles * p.n_tiles, s);
 }
 
-cudaError_t zero_rest(const FfnArgs& a, void* y, int64_t ldy, cudaStream_t s) {
-  return launch_ex(zero_rest_kernel, dim3((unsigned)((a.R + kZeroRows - 1) / kZeroRows)), dim3(256), 0,
-                   s, true, base_params(a), static_cast<uint16_t*>(y), ldy, a.d);
-}
-
 template <bool kHalf>
 cudaError_t forward(const FfnArgs& a, cudaStream_t s) {
   cudaError_t e = rows_product<kUp, kHalf>(a, a.w_gate, a.w_up, {a.x, a.ldx, 1, a.d}, a.h, a.I, s);
   if (e == cudaSuccess)
     e = rows_product<kDown, kHalf>(a, a.w_down, nullptr, {a.h, a.I, 1, a.I}, a.y, a.ldy, s);
-  if (e == cudaSuccess && a.zero_rest) e = zero_rest(a, a.y, a.ldy, s);
   return e;
 }
 
@@ -893,10 +908,8 @@ cudaError_t backward(const FfnArgs& a, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (a.dx != nullptr || a.dw_gate != nullptr)
     e = rows_product<kGradH, kHalf>(a, a.w_down, nullptr, dy, a.dpre, 2 * a.I, s);
-  if (e == cudaSuccess && a.dx != nullptr) {
+  if (e == cudaSuccess && a.dx != nullptr)
     e = rows_product<kGradX, kHalf>(a, a.w_gate, a.w_up, dpre, a.dx, a.lddx, s);
-    if (e == cudaSuccess && a.zero_rest) e = zero_rest(a, a.dx, a.lddx, s);
-  }
   if (e == cudaSuccess && a.dw_gate != nullptr)
     e = weights_product<kHalf>(a, dpre, x, a.dw_gate, a.dw_up, s);
   if (e == cudaSuccess && a.dw_down != nullptr)
