@@ -480,7 +480,7 @@ dmoe_status dmoe_expert_set_debug_hold(int32_t hold);
  *   ry = 1 / sqrt(mean(y^2) + eps),  rr = 1 / sqrt(mean(r^2) + eps)  over the row's d elements
  * in fp32, r and n rounded once each (n from the unrounded r). y is a block's output, x the residual
  * stream, n the next block's input; without y it is the norm before a first block alone.
- * Limits: 1 <= d <= 16384, 0 <= T <= 2^30, eps >= 0. */
+ * Limits: 1 <= d <= 16384, 0 <= T <= 2^30, eps >= 0; row strides below 2^30. */
 typedef struct {
   int32_t dtype;          /* dmoe_dtype of all rows and of the gate */
   int32_t d;

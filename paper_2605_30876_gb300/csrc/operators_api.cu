@@ -152,6 +152,13 @@ dmoe_status check_norm(const dmoe_norm_desc* d) {
   return d->d > kMaxDModel || d->T > kMaxPairs ? DMOE_ERR_UNSUPPORTED : DMOE_OK;
 }
 
+// a row's place is computed from 32-bit numbers of tokens and bytes
+bool strides_fit(std::initializer_list<int64_t> lds) {
+  for (int64_t ld : lds)
+    if (ld >= (int64_t)1 << 30) return false;
+  return true;
+}
+
 // what both directions read: x; y, its weight and its gate, or none of the three
 bool norm_inputs(const dmoe_norm_desc* d, const void* x, int64_t ldx, const void* y, int64_t ldy,
                  const float* w_post, const void* gate, int64_t ldgate, const float* w_pre,
@@ -454,6 +461,8 @@ dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_
       (n != nullptr && (n == x || n == gate)) || (r == x && ldr != ldx) ||
       (n != nullptr && n == y && ldn != ldy))
     return DMOE_ERR_INVALID_ARG;
+  if (!strides_fit({ldx, y != nullptr ? ldy : 0, r != nullptr ? ldr : 0, n != nullptr ? ldn : 0}))
+    return DMOE_ERR_UNSUPPORTED;
   a.r = r;
   a.ldr = ldr;
   a.n = n;
@@ -512,6 +521,9 @@ dmoe_status dmoe_norm_residual_backward(
     if (workspace == nullptr || !aligned(workspace, 16)) return DMOE_ERR_INVALID_ARG;
     if (workspace_bytes < norm_workspace_bytes(desc->T, d, a.gate_tokens)) return DMOE_ERR_WORKSPACE;
   }
+  if (!strides_fit({ldx, y != nullptr ? ldy : 0, dr != nullptr ? lddr : 0, dn != nullptr ? lddn : 0,
+                    dx != nullptr ? lddx : 0, dy != nullptr ? lddy : 0}))
+    return DMOE_ERR_UNSUPPORTED;
   a.stats = const_cast<float*>(stats);
   a.dr = dr;
   a.lddr = lddr;

@@ -176,6 +176,7 @@ def test_norm_refusals(dm):
     x, y, g = (at(k, NORM) for k in ("x", "y", "gate"))
     assert norm(dm, r=y) == 1 and norm(dm, n=x) == 1 and norm(dm, r=g) == 1 and norm(dm, n=g) == 1
     assert norm(dm, n=at("r", NORM)) == 1
+    assert norm(dm, ld=dict(x=2 ** 30)) == 2 and norm_backward(dm, ld=dict(dx=2 ** 30)) == 2
     assert norm(dm, r=x, ld=dict(x=72)) == 1 and norm(dm, n=y, ld=dict(n=72)) == 1
 
 
