@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <cstdlib>
 
 #include "dmoe_internal.cuh"
 #include "silu.cuh"
@@ -86,6 +87,9 @@ struct Params {
 // stage costs loads: kGradW's stages are one step, given back two at a time.
 template <int kMode> constexpr int sub_steps() { return kMode == kGradW ? 1 : 2; }
 template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1; }
+// The launch before is one of the same call: it was released once what that call was given was there,
+// and nothing of it but the rows of B is waited for. The weights are on their way before that.
+template <int kMode> constexpr bool early() { return kMode == kDown || kMode == kGradX; }
 template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
 template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
 template <int kMode> constexpr int epi_bytes() {
@@ -187,7 +191,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   int* s_unit = reinterpret_cast<int*>(d_empty + kQueue);   // [kQueue][4]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_unit + 4 * kQueue);
   volatile int* s_abort = reinterpret_cast<int*>(s_tmem + 1);
-  int* s_first = reinterpret_cast<int*>(s_tmem + 2);        // [kMaxGroups + 1] units before a group
+  // (not kGradW) [kMaxGroups + 1] units before a group, and its first row and rows
+  int* s_first = reinterpret_cast<int*>(s_tmem + 2);
+  int2* s_rows = reinterpret_cast<int2*>(s_first + kMaxGroups + 2);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)ptx::cluster_ctarank();
@@ -227,8 +233,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   ptx::cluster_wait();
   ptx::tc_fence_after();
   const uint32_t tmem_base = *s_tmem;
-  pdl_wait();
-  pdl_launch_dependents();
+  if (!early<kMode>()) {
+    pdl_wait();
+    pdl_launch_dependents();
+  }
 
   auto wait_for = [&](auto try_wait, int value) -> bool {
     if (try_wait()) return true;
@@ -299,8 +307,38 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const uint32_t sub_bytes = kTileABytes + (kMode == kGradW ? (uint32_t)b_boxes * 8192u
                                                                   : (uint32_t)rows * 128u);
         const int b_row = un.row + rank * half;
+        // a step's weights
+        auto load_a = [&](uint8_t* as, uint32_t bar, int part_, int k) {
+          if (kMode == kUp) {          // 64 rows of Wg, then 64 of Wu
+            ptx::tma_load_3d_pair(as, &tm.a[0], bar, k, m0, un.e, once);
+            ptx::tma_load_3d_pair(as + 8192, &tm.a[1], bar, k, m0, un.e, once);
+          } else if (kMode == kDown) {
+            ptx::tma_load_3d_pair(as, &tm.a[0], bar, k, m0, un.e, once);
+          } else {                     // 64 rows of K, 2 x 64 columns
+            ptx::tma_load_3d_pair(as, &tm.a[part_], bar, m0, k, un.e, once);
+            ptx::tma_load_3d_pair(as + 8192, &tm.a[part_], bar, m0 + 64, k, un.e, once);
+          }
+        };
+        int ahead = 0;                 // stages whose weights were asked for before the wait
+        if (early<kMode>() && i == 0) {
+          int part_ = 0, k = 0;
+          for (int c = 0; c < steps && ahead < p.stages; c += kSub, ++ahead) {
+            const uint32_t bar = full0 + 8u * (uint32_t)ahead;
+            const int n_sub = min(kSub, steps - c);
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[ahead], kCluster * n_sub * sub_bytes);
+            for (int s = 0; s < n_sub; ++s) {
+              load_a(smem + (uint32_t)ahead * stage_bytes + s * kTileABytes, bar, part_, k);
+              k += 64;
+              if (k >= p.K) { k = 0; ++part_; }
+            }
+          }
+          pdl_wait();
+          pdl_launch_dependents();
+        }
         for (int c = 0; c < steps; c += kSub) {
-          if (stage % kPer == 0 && !wait(&empty[stage / kPer], phase ^ 1u, i)) {
+          const bool a_there = ahead > 0;
+          if (a_there) --ahead;
+          if (stage % kPer == 0 && !a_there && !wait(&empty[stage / kPer], phase ^ 1u, i)) {
             ok = false;
             break;
           }
@@ -323,18 +361,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
               ptx::tma_load_3d_pair(b + j * 8192, &tm.b[0], to, un.n * kNMax + rank * half + 64 * j, 0, r,
                                     again);
           } else {
-            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], kCluster * n_sub * sub_bytes);
+            if (rank == 0 && !a_there)
+              ptx::mbar_arrive_expect_tx(&full[stage], kCluster * n_sub * sub_bytes);
             for (int s = 0; s < n_sub; ++s) {
-              uint8_t* as = a + s * kTileABytes;
-              if (kMode == kUp) {          // 64 rows of Wg, then 64 of Wu
-                ptx::tma_load_3d_pair(as, &tm.a[0], bar, k0, m0, un.e, once);
-                ptx::tma_load_3d_pair(as + 8192, &tm.a[1], bar, k0, m0, un.e, once);
-              } else if (kMode == kDown) {
-                ptx::tma_load_3d_pair(as, &tm.a[0], bar, k0, m0, un.e, once);
-              } else {                     // 64 rows of K, 2 x 64 columns
-                ptx::tma_load_3d_pair(as, &tm.a[part], bar, m0, k0, un.e, once);
-                ptx::tma_load_3d_pair(as + 8192, &tm.a[part], bar, m0 + 64, k0, un.e, once);
-              }
+              if (!a_there) load_a(a + s * kTileABytes, bar, part, k0);
               ptx::tma_load_3d_pair(b + s * b_sub, &tm.b[lv], bar, k0, part, b_row, again);
               k0 += 64;
               if (k0 >= p.K) { k0 = 0; ++part; }
@@ -343,61 +373,72 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
+      if (early<kMode>()) pdl_wait();   // (a pair without units ends no earlier than the launch before)
       // the issuer's last commit arrives in this CTA, too
       wait(drain, 0, -1);
     }
   } else if (warp == kPlanWarp) {
     // ================= units: counted per group, then decoded ahead of their use
     const int per_group = p.parts * p.m_tiles * p.n_tiles;   // kGradW
-    int carry = p.n_groups * per_group;
+    int units = p.n_groups * per_group;
     if (kMode != kGradW) {
-      carry = 0;
-      for (int base = 0; base < p.n_groups; base += 32) {
-        const int g = base + lane;
-        int n = 0;
-        if (g < p.n_groups && group_expert(p, g) >= 0) {
-          int64_t row0;
-          int cnt;
-          group_rows(p, g, &row0, &cnt);
-          n = (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
-        }
-        int sum = n;
+      // a lane counts 16 groups in a row (their offsets are all asked for at once)
+      constexpr int kOwn = kMaxGroups / 32;
+      int own[kOwn], sum = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, sum, o);
-          if (lane >= o) sum += v;
+      for (int j = 0; j < kOwn; ++j) {
+        const int g = lane * kOwn + j;
+        int64_t row0 = 0;
+        int cnt = 0;
+        if (g < p.n_groups) {
+          group_rows(p, g, &row0, &cnt);
+          if (group_expert(p, g) < 0) cnt = 0;
+          s_rows[g] = make_int2((int)row0, cnt);
         }
-        if (g < p.n_groups) s_first[g + 1] = carry + sum;
-        carry += __shfl_sync(0xffffffffu, sum, 31);
+        own[j] = (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
+        sum += own[j];
       }
-      if (lane == 0) s_first[0] = 0;
+      int before = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += v;
+      }
+      units = __shfl_sync(0xffffffffu, before, 31);
+      before -= sum;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) {
+        s_first[lane * kOwn + j] = before;
+        before += own[j];
+      }
       __syncwarp();
     }
     if (lane == 0) {
-      const int units = carry;
+      int64_t row_ahead = 0;         // kGradW: the rows of the unit after this one, on their way
+      int cnt_ahead = 0;
+      if (kMode == kGradW && cl < units) group_rows(p, cl / per_group, &row_ahead, &cnt_ahead);
       for (int i = 0;; ++i) {
         const int u = cl + i * ncl;
         int4 v = make_int4(0, 0, -1, 0);
         if (u < units) {
-          int lo = 0, hi = p.n_groups - 1;
-          if (kMode == kGradW) lo = hi = u / per_group;
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (s_first[mid] <= u) lo = mid; else hi = mid - 1;
-          }
-          int64_t row0;
-          int cnt;
-          group_rows(p, lo, &row0, &cnt);
-          const int local = u - (kMode == kGradW ? lo * per_group : s_first[lo]);
           if (kMode == kGradW) {
+            const int g = u / per_group, local = u - g * per_group;
             const int n = local % p.n_tiles, mp = local / p.n_tiles;
-            v = make_int4((int)row0, cnt, lo, (mp / p.m_tiles) << 16 | (mp % p.m_tiles) << 8 | n);
+            v = make_int4((int)row_ahead, cnt_ahead, g, (mp / p.m_tiles) << 16 | (mp % p.m_tiles) << 8 | n);
+            if (u + ncl < units) group_rows(p, (u + ncl) / per_group, &row_ahead, &cnt_ahead);
           } else {
+            int lo = 0, hi = p.n_groups - 1;
+            while (lo < hi) {
+              const int mid = (lo + hi + 1) >> 1;
+              if (s_first[mid] <= u) lo = mid; else hi = mid - 1;
+            }
+            const int row0 = s_rows[lo].x, cnt = s_rows[lo].y, local = u - s_first[lo];
             // the tiles of a group next to one another share its weights; they are of one size
             const int nt = (cnt + p.n_max - 1) / p.n_max;
             const int m = local / nt, n = local - m * nt;
             const int tile = round_up((cnt + nt - 1) / nt, 32);
-            v = make_int4((int)row0 + n * tile, min(tile, cnt - n * tile), group_expert(p, lo), m << 8);
+            v = make_int4(row0 + n * tile, min(tile, cnt - n * tile),
+                          p.expert_ids != nullptr ? group_expert(p, lo) : lo, m << 8);
           }
         }
         const int q = i % kQueue;
@@ -814,7 +855,7 @@ Params base_params(const FfnArgs& a) {
 template <int kMode>
 constexpr size_t fixed_smem() {
   return 1024 + epi_bytes<kMode>() + 8 * (3 * kMaxStages + 6 + 2 * kQueue) + 16 * kQueue + 8 +
-         (kMode == kGradW ? 0 : 4 * (kMaxGroups + 1));
+         (kMode == kGradW ? 0 : 4 * (kMaxGroups + 2) + 8 * kMaxGroups);
 }
 
 // The rest of the launch: stages, grid. `units`: at most so many.
@@ -920,6 +961,8 @@ cudaError_t backward(const FfnArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s) {
+  static const int few = getenv("FEW") ? atoi(getenv("FEW")) : kFewRows;
+  if (a.R <= few) return launch_expert_ffn_few(a, s);
   return a.dtype == DMOE_FP16 ? forward<true>(a, s) : forward<false>(a, s);
 }
 cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s) {

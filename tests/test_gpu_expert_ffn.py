@@ -19,6 +19,10 @@ SHAPES = [
     (3, 264, 136, [300, 1, 513], 70),
     (1, 512, 256, [777], 0),
     (9, 136, 200, [0, 0, 31, 32, 0, 1, 0, 48, 0], 5),
+    # the same ends in calls of more rows
+    (4, 72, 40, [1, 0, 2, 700], 1),
+    (6, 256, 128, [15, 16, 17, 33, 600, 0], 0),
+    (7, 1000, 344, [0, 64, 65, 127, 0, 31, 300], 9),
 ]
 DTYPES = [torch.bfloat16, torch.float16]
 
@@ -266,7 +270,7 @@ def test_captured_and_replayed():
 
 
 def test_waits_that_run_out_are_recorded():
-    c = case(torch.bfloat16, 2, 264, 136, [33, 70], 0)
+    c = case(torch.bfloat16, 2, 264, 136, [433, 270], 0)     # (the form for few rows has no waits)
     pre, h, y = run_forward(c)
     torch.cuda.synchronize()
     dm.dmoe_expert_set_debug_hold(1)
