@@ -402,8 +402,8 @@ struct FfnArgs {
   int hold;                    // 0, or 1: the waits run out (dmoe_expert_set_debug_hold)
 };
 cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s);
-// the same for few rows (ffn_few.cu), which launch_expert_ffn takes by their number
-constexpr int kFewRows = 256;
+// the same for few rows (ffn_few.cu), which launch_expert_ffn takes where they are few enough
+bool expert_ffn_few_ok(const FfnArgs& a);
 cudaError_t launch_expert_ffn_few(const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s);
 cudaError_t ffn_fault_address(void** p);

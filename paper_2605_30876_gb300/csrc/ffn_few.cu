@@ -3,7 +3,9 @@
 // small CTAs; mma.sync.m16n8k16 with 16 rows of weights as A and eight token rows as B, both straight
 // from global memory into the fragments. A lane's fragment takes pairs of k from four places; any
 // order of k gives the same sum as long as A and B agree, so a lane takes eight neighbours (16 bytes)
-// of a 32-long piece of K for two MMAs.
+// of a 32-long piece of K for two MMAs. (tcgen05 has nothing to win here: the weights' bytes are the bound,
+// and its launches, with tensor memory and barriers to set up and 64 SMs at work, took 27 us where
+// these take 14, for one token's eight experts of 2048 x 512; the floor is 7.4.)
 // The eight warps of a CTA share the sum over K (kKS ways) or the rows (8 / kKS ways); the parts meet in
 // shared memory and are added in the order of the warps. The second launch has its first weights on
 // their way before it waits for the first one's h.
@@ -16,8 +18,6 @@
 namespace dmoe {
 namespace {
 
-constexpr int kFewThreads = 256;
-constexpr int kFewWarps = kFewThreads / 32;
 
 struct FewParams {
   const int32_t* offsets;
@@ -72,18 +72,28 @@ __device__ __forceinline__ int few_expert(const FewParams& p, int g) {
 }
 
 // kUp: a 16-row tile is eight rows of gate and the same eight of up, so that a lane holds both of an
-// element. kMT tiles a warp, kNT times eight token rows at once, kSteps pieces of K in flight.
-template <bool kUp, bool kHalf, int kMT, int kNT, int kKS, int kSteps>
-__global__ void __launch_bounds__(kFewThreads, kMT == 1 ? 3 : 2)
+// element. A unit is kMT tiles a warp and up to 32 token rows of a group.
+// - Up to eight token rows (single tokens, a batch routed token by token): a warp's part of them lies in
+//   shared memory, in a place of its own, and weights are read kAhead pieces of K (32 each) ahead, into
+//   the next unit, too: 256 experts of one row each come at 0.99 of the copy rate.
+// - More of them (a block of tokens through its experts): the registers hold the sums of 32, and two
+//   pieces of K are read at a time, token rows too (from L2, with the warps of the other rows).
+constexpr int kFewCols = 32;
+constexpr int few_pitch(int per) { return per * 64 + 16; }   // bytes of a row's part, off by a bank group
+template <bool kUp, bool kHalf, int kMT, int kKS>
+__global__ void __launch_bounds__(256, 2)
 ffn_few_kernel(const FewParams p) {
-  constexpr int kMW = kFewWarps / kKS;          // warps side by side in M
+  constexpr int kWarps = 8, kNT = kFewCols / 8, kAhead = kMT == 1 ? 8 : 4;
+  constexpr int kMW = kWarps / kKS;             // warps side by side in M
   constexpr int kTile = kUp ? 8 : 16;           // rows of M in a tile
   constexpr int kRows = kMW * kMT * kTile;      // ... of a CTA
-  constexpr int kCols = kNT * 8;
+  constexpr int kCols = kFewCols;
   constexpr int kMaxG = kMaxFfnExperts;
-  extern __shared__ float4 s_acc[];             // [warp][tile][n tile][lane]
-  __shared__ int s_first[kMaxG + 1];            // row chunks before a group
-  __shared__ int s_sum[kFewWarps];
+  extern __shared__ float4 smem[];
+  float4* s_acc = smem;                         // [warp][tile][n tile][lane]
+  uint8_t* s_rows = reinterpret_cast<uint8_t*>(smem + kWarps * kMT * kNT * 32);   // [warp][row][part]
+  __shared__ int s_first[2][kMaxG];             // chunks of rows before a group: groups of up to eight
+  __shared__ int2 s_sum[kWarps];                // rows, and the others
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int ks = warp % kKS, mw = warp / kKS, g8 = lane >> 2, q = lane & 3;
   // (the second launch: the offsets were there before the first one released it)
@@ -92,139 +102,112 @@ ffn_few_kernel(const FewParams p) {
     pdl_launch_dependents();
   }
 
-  // chunks of up to kCols rows of every group, counted
-  int mine[2] = {0, 0};
+  constexpr int kOwn = kMaxG / (kWarps * 32);
+  int2 mine[kOwn], sum = make_int2(0, 0);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int g = 2 * tid + j;
+  for (int j = 0; j < kOwn; ++j) {
+    const int g = kOwn * tid + j;
     int row0;
-    if (g < p.n_groups && few_expert(p, g) >= 0) mine[j] = (few_rows(p, g, &row0) + kCols - 1) / kCols;
+    const int cnt = g < p.n_groups && few_expert(p, g) >= 0 ? few_rows(p, g, &row0) : 0;
+    mine[j] = make_int2(cnt > 0 && cnt <= 8 ? 1 : 0, cnt > 8 ? (cnt + kCols - 1) / kCols : 0);
+    sum.x += mine[j].x;
+    sum.y += mine[j].y;
   }
-  int sum = mine[0] + mine[1];
+  const int2 own = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += v;
+    const int x = __shfl_up_sync(0xffffffffu, sum.x, o), y = __shfl_up_sync(0xffffffffu, sum.y, o);
+    if (lane >= o) {
+      sum.x += x;
+      sum.y += y;
+    }
   }
   if (lane == 31) s_sum[warp] = sum;
   __syncthreads();
-  int before = sum - mine[0] - mine[1], chunks = 0;
+  int2 before = make_int2(sum.x - own.x, sum.y - own.y), chunks = make_int2(0, 0);
 #pragma unroll
-  for (int w = 0; w < kFewWarps; ++w) {
-    if (w < warp) before += s_sum[w];
-    chunks += s_sum[w];
+  for (int w = 0; w < kWarps; ++w) {
+    const int2 v = s_sum[w];
+    if (w < warp) {
+      before.x += v.x;
+      before.y += v.y;
+    }
+    chunks.x += v.x;
+    chunks.y += v.y;
   }
-  s_first[2 * tid] = before;
-  s_first[2 * tid + 1] = before + mine[0];
-  if (tid == 0) s_first[kMaxG] = chunks;
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    s_first[0][kOwn * tid + j] = before.x;
+    s_first[1][kOwn * tid + j] = before.y;
+    before.x += mine[j].x;
+    before.y += mine[j].y;
+  }
   __syncthreads();
 
   const int m_units = (p.M + kRows - 1) / kRows, steps = (p.K + 31) / 32;
-  const int per = (steps + kKS - 1) / kKS, k_begin = ks * per, k_end = min(steps, k_begin + per);
-  bool waited = kUp;
-  for (int u = blockIdx.x; u < chunks * m_units; u += gridDim.x) {
-    const int chunk = u / m_units, m0 = (u - chunk * m_units) * kRows + mw * kMT * kTile;
+  const int per = (steps + kKS - 1) / kKS, k_begin = min(ks * per, steps), k_steps = min(steps, k_begin + per) - k_begin;
+
+  struct At {
+    const uint4* w[2];       // this lane's first rows of weights, at the warp's first piece of K
+    uint32_t there;          // bits: rows that exist
+    int row0, rows, m0;
+  };
+  auto locate = [&](int u, int kind) -> At {
+    At at;
+    const int chunk = u / m_units;
+    at.m0 = (u - chunk * m_units) * kRows + mw * kMT * kTile;
     int lo = 0, hi = kMaxG - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (s_first[mid] <= chunk) lo = mid; else hi = mid - 1;
+      if (s_first[kind][mid] <= chunk) lo = mid; else hi = mid - 1;
     }
-    int row0;
-    const int cnt = few_rows(p, lo, &row0), e = few_expert(p, lo);
-    const int at = (chunk - s_first[lo]) * kCols, rows = min(kCols, cnt - at);
-    row0 += at;
-    // this lane's rows of weights: g8 and g8 + 8 of every tile
-    const uint4* wr[kMT][2];
-    bool there[kMT][2];
+    const int cnt = few_rows(p, lo, &at.row0), skip = (chunk - s_first[kind][lo]) * kCols;
+    const int64_t e = few_expert(p, lo);
+    at.rows = min(kCols, cnt - skip);
+    at.row0 += skip;
+    at.there = 0;
 #pragma unroll
-    for (int m = 0; m < kMT; ++m)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = m0 + m * kTile + g8 + (kUp ? 0 : 8 * j);
-        there[m][j] = r < p.M;
-        wr[m][j] = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.w[kUp ? j : 0]) +
-                                                  ((int64_t)e * p.M + (r < p.M ? r : 0)) * p.K) + q;
-      }
-    const uint4* br[kNT];
-#pragma unroll
-    for (int n = 0; n < kNT; ++n) {
-      const int r = min(n * 8 + g8, rows - 1);     // (past the last row: its columns are not used)
-      br[n] = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.b) + (int64_t)(row0 + r) * p.ldb) + q;
-    }
-    float acc[kMT][kNT][4];
-#pragma unroll
-    for (int m = 0; m < kMT; ++m)
-#pragma unroll
-      for (int n = 0; n < kNT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[m][n][j] = 0.f;
-    for (int k = k_begin; k < k_end; k += kSteps) {
-      uint4 a[kSteps][kMT][2], b[kSteps][kNT];
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const bool in = k + s < k_end && (k + s) * 32 + q * 8 < p.K;
-#pragma unroll
-        for (int m = 0; m < kMT; ++m)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            a[s][m][j] = in && there[m][j] ? __ldcs(wr[m][j] + (k + s) * 4) : make_uint4(0, 0, 0, 0);
-      }
-      if (!waited) {            // the first launch's h
-        pdl_wait();
-        pdl_launch_dependents();
-        waited = true;
-      }
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const bool in = k + s < k_end && (k + s) * 32 + q * 8 < p.K;
-#pragma unroll
-        for (int n = 0; n < kNT; ++n)
-          b[s][n] = in && n * 8 < rows ? *(br[n] + (k + s) * 4) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-          if (n > 0 && n * 8 >= rows) break;
-#pragma unroll
-          for (int m = 0; m < kMT; ++m) {
-            const uint4 &x = a[s][m][0], &y = a[s][m][1];
-            mma_16816<kHalf>(acc[m][n], x.x, y.x, x.y, y.y, b[s][n].x, b[s][n].y);
-            mma_16816<kHalf>(acc[m][n], x.z, y.z, x.w, y.w, b[s][n].z, b[s][n].w);
-          }
-        }
-    }
-    // the warps' parts of the sum meet
-    if (kKS > 1) {
-      __syncthreads();          // (the unit before has been read)
+    for (int j = 0; j < 2; ++j) {
+      const int r = at.m0 + g8 + (kUp ? 0 : 8 * j);
 #pragma unroll
       for (int m = 0; m < kMT; ++m)
-#pragma unroll
-        for (int n = 0; n < kNT; ++n)
-          s_acc[((warp * kMT + m) * kNT + n) * 32 + lane] =
-              make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
-      __syncthreads();
+        if (r + m * kTile < p.M) at.there |= 1u << (2 * m + j);
+      at.w[j] = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.w[kUp ? j : 0]) +
+                                               (e * p.M + min(r, p.M - 1)) * p.K) + k_begin * 4 + q;
     }
-    // (tile, n tile) pairs of this warp's rows go round the warps that share them
+    return at;
+  };
+  const int tile_stride = kTile * p.K / 8;      // 16-byte words from a tile's rows to the next one's
+  auto load_weights = [&](const At& at, int k, uint4 (&a)[kMT][2]) {
+    const bool in = k < k_steps && (k_begin + k) * 32 + q * 8 < p.K;
 #pragma unroll
-    for (int i = 0; i < (kMT * kNT + kKS - 1) / kKS; ++i) {
-      const int t = i * kKS + ks, m = t / kNT, n = t % kNT;
-      if (t >= kMT * kNT || n * 8 >= rows) continue;
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        a[m][j] = in && (at.there >> (2 * m + j) & 1u) ? __ldcs(at.w[j] + m * tile_stride + k * 4)
+                                                       : make_uint4(0, 0, 0, 0);
+  };
+  // a warp's sums of tile m, columns 8 n .. 8 n + 7
+  auto sums_at = [&](int w, int m, int n) -> float4* { return s_acc + ((w * kMT + m) * kNT + n) * 32 + lane; };
+  // all of them are there: (tile, n tile) pairs of this warp's rows go round the warps that share them
+  auto finish = [&](const At& now, int n_tiles) {
+    for (int t = ks; t < kMT * n_tiles; t += kKS) {
+      const int m = t % kMT, n = t / kMT;
       float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < kKS; ++k) {
-        const float4 f = s_acc[(((mw * kKS + k) * kMT + m) * kNT + n) * 32 + lane];
+        const float4 f = *sums_at(mw * kKS + k, m, n);
         v[0] += f.x;
         v[1] += f.y;
         v[2] += f.z;
         v[3] += f.w;
       }
       // rows g8 and g8 + 8 of the tile, columns (token rows) 2 q and 2 q + 1
-      const int r = m0 + m * kTile + g8, c = n * 8 + 2 * q;
+      const int r = now.m0 + m * kTile + g8, c = n * 8 + 2 * q;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        if (c + j >= rows) continue;
-        const int64_t row = row0 + c + j;
+        if (c + j >= now.rows) continue;
+        const int64_t row = now.row0 + c + j;
         if constexpr (kUp) {
           if (r < p.M) {
             store_16<kHalf>(p.out, row * p.ldo + r, v[j] / (1.f + __expf(-v[j])) * v[2 + j]);
@@ -239,9 +222,135 @@ ffn_few_kernel(const FewParams p) {
         }
       }
     }
+  };
+
+  // ---------------- groups of up to eight rows
+  const int narrow = chunks.x * m_units, wide = chunks.y * m_units;
+  {
+    const int pitch = few_pitch(per);
+    uint8_t* const my_rows = s_rows + warp * 8 * pitch;
+    // the warp's part of the token rows: 16-byte words, four lanes to a piece of K
+    auto fetch_rows = [&](const At& at) {
+      const int words = k_steps * 4, all = words * at.rows;
+      for (int i = lane; i < all; i += 32) {
+        const int r = i / words, c = i - r * words;
+        const bool in = k_begin * 32 + c * 8 < p.K;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(my_rows + r * pitch + c * 16);
+        const uint16_t* from = static_cast<const uint16_t*>(p.b) + (int64_t)(at.row0 + r) * p.ldb +
+                               (in ? k_begin * 32 + c * 8 : 0);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0)
+                     : "memory");
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    uint4 ring[kAhead][kMT][2];
+    int u = blockIdx.x;
+    At at;
+    if (u < narrow) {
+      at = locate(u, 0);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) load_weights(at, s, ring[s]);
+    }
+    if (!kUp) {              // the first launch's h
+      pdl_wait();
+      pdl_launch_dependents();
+    }
+    if (u < narrow) fetch_rows(at);
+    while (u < narrow) {
+      const At now = at;
+      float acc[kMT][4];
+#pragma unroll
+      for (int m = 0; m < kMT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][j] = 0.f;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      // (past the last row: what the place held; its columns are not used)
+      const uint8_t* from = my_rows + g8 * pitch + q * 16;
+      for (int k0 = 0; k0 < k_steps; k0 += kAhead) {
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) {
+          if (k0 + s >= k_steps) break;
+          const uint4 b = *reinterpret_cast<const uint4*>(from + (k0 + s) * 64);
+#pragma unroll
+          for (int m = 0; m < kMT; ++m) {
+            const uint4 &x = ring[s][m][0], &y = ring[s][m][1];
+            mma_16816<kHalf>(acc[m], x.x, y.x, x.y, y.y, b.x, b.y);
+            mma_16816<kHalf>(acc[m], x.z, y.z, x.w, y.w, b.z, b.w);
+          }
+          load_weights(now, k0 + s + kAhead, ring[s]);
+        }
+      }
+      // the next unit's weights and rows are on their way while this one's sums meet
+      u += gridDim.x;
+      if (u < narrow) {
+        at = locate(u, 0);
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) load_weights(at, s, ring[s]);
+        __syncwarp();
+        fetch_rows(at);
+      }
+#pragma unroll
+      for (int m = 0; m < kMT; ++m)
+        *sums_at(warp, m, 0) = make_float4(acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
+      __syncthreads();
+      finish(now, 1);
+      __syncthreads();       // the sums have been read
+    }
+  }
+  // ---------------- groups of more, 32 rows at a time (the CTAs that had fewer units begin)
+  for (int u = (int)((blockIdx.x + gridDim.x - narrow % gridDim.x) % gridDim.x); u < wide; u += gridDim.x) {
+    const At now = locate(u, 1);
+    const uint4* br[kNT];
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      const int r = min(n * 8 + g8, now.rows - 1);     // (as above)
+      br[n] = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.b) + (int64_t)(now.row0 + r) * p.ldb) +
+              k_begin * 4 + q;
+    }
+    float acc[kMT][kNT][4];
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+      for (int n = 0; n < kNT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][n][j] = 0.f;
+    for (int k = 0; k < k_steps; k += 2) {
+      uint4 a[2][kMT][2], b[2][kNT];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) load_weights(now, k + s, a[s]);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bool in = k + s < k_steps && (k_begin + k + s) * 32 + q * 8 < p.K;
+#pragma unroll
+        for (int n = 0; n < kNT; ++n)
+          b[s][n] = in && n * 8 < now.rows ? *(br[n] + (k + s) * 4) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+          if (n * 8 >= now.rows) break;
+#pragma unroll
+          for (int m = 0; m < kMT; ++m) {
+            const uint4 &x = a[s][m][0], &y = a[s][m][1];
+            mma_16816<kHalf>(acc[m][n], x.x, y.x, x.y, y.y, b[s][n].x, b[s][n].y);
+            mma_16816<kHalf>(acc[m][n], x.z, y.z, x.w, y.w, b[s][n].z, b[s][n].w);
+          }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+      for (int n = 0; n < kNT; ++n)
+        if (n * 8 < now.rows)
+          *sums_at(warp, m, n) = make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+    __syncthreads();
+    finish(now, (now.rows + 7) / 8);
+    __syncthreads();
   }
   if (!kUp && p.zero_rest) {    // rows in no group, a warp each
-    for (int r = blockIdx.x * kFewWarps + warp; r < p.R; r += gridDim.x * kFewWarps) {
+    for (int r = blockIdx.x * kWarps + warp; r < p.R; r += gridDim.x * kWarps) {
       bool owned = false;
       for (int g = lane; g < p.n_groups; g += 32) {
         int row0;
@@ -253,17 +362,47 @@ ffn_few_kernel(const FewParams p) {
       for (int c = lane; c < p.M / 8; c += 32) row[c] = make_uint4(0, 0, 0, 0);
     }
   }
-  if (!waited) pdl_wait();      // (a CTA without units: nothing behind this launch starts before the first)
 }
 
-template <bool kUp, bool kHalf, int kMT, int kNT, int kKS, int kSteps>
+constexpr size_t few_smem(int tiles, int per) {
+  return sizeof(float4) * 8 * tiles * kFewCols / 8 * 32 + (size_t)8 * 8 * few_pitch(per);
+}
+
+template <bool kUp, bool kHalf, int kMT, int kKS>
+cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
+  constexpr int rows = 8 / kKS * kMT * (kUp ? 8 : 16);
+  const int64_t units = (int64_t)std::min(p.R, p.n_groups + p.R / kFewCols) * ((p.M + rows - 1) / rows);
+  const int ctas = (int)std::min<int64_t>(units, 152 * 2);
+  const int per = ((p.K + 31) / 32 + kKS - 1) / kKS;
+  const size_t smem = few_smem(kMT, per);
+  auto* kernel = ffn_few_kernel<kUp, kHalf, kMT, kKS>;
+  static std::atomic<uint32_t> done;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint32_t bit = dev < 32 ? 1u << dev : 0u;
+  if (e == cudaSuccess && (done.load(std::memory_order_relaxed) & bit) == 0u) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return e;
+  return launch_ex(kernel, dim3(ctas), dim3(256), smem, s, true, p);
+}
+
+// Units of a tile a warp where those of two would not fill two CTAs per SM (with as many groups as there
+// can be); the second launch's sums are cut eight ways, not four, where they are long.
+template <bool kUp, bool kHalf>
 cudaError_t launch_few(const FewParams& p, cudaStream_t s) {
-  constexpr int rows = kFewWarps / kKS * kMT * (kUp ? 8 : 16);
-  const int64_t units = (int64_t)std::min(p.R, p.n_groups + p.R / (kNT * 8)) * ((p.M + rows - 1) / rows);
-  const int ctas = (int)std::min<int64_t>(units, 152 * (kMT == 1 ? 3 : 2));
-  const size_t smem = sizeof(float4) * kFewWarps * kMT * kNT * 32;
-  return launch_ex(ffn_few_kernel<kUp, kHalf, kMT, kNT, kKS, kSteps>, dim3(ctas), dim3(kFewThreads), smem, s,
-                   true, p);
+  const int groups = std::min(p.R, p.n_groups);
+  if (kUp) {
+    if ((int64_t)groups * (p.M / 16) < 304) return launch_form<kUp, kHalf, 1, 8>(p, s);
+    return launch_form<kUp, kHalf, 2, 8>(p, s);
+  }
+  if (p.K > 512) {
+    if ((int64_t)groups * (p.M / 32) < 304) return launch_form<kUp, kHalf, 1, 8>(p, s);
+    return launch_form<kUp, kHalf, 2, 8>(p, s);
+  }
+  if ((int64_t)groups * (p.M / 64) < 304) return launch_form<kUp, kHalf, 1, 4>(p, s);
+  return launch_form<kUp, kHalf, 2, 4>(p, s);
 }
 
 template <bool kHalf>
@@ -283,7 +422,7 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
   p.out = a.h;
   p.ldo = a.I;
   p.pre = a.pre;
-  cudaError_t e = a.R <= 8 ? launch_few<true, kHalf, 1, 1, 8, 8>(p, s) : launch_few<true, kHalf, 2, 4, 8, 2>(p, s);
+  const cudaError_t e = launch_few<true, kHalf>(p, s);
   if (e != cudaSuccess) return e;
   p.M = a.d;
   p.K = a.I;
@@ -295,10 +434,18 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
   p.ldo = a.ldy;
   p.pre = nullptr;
   p.zero_rest = a.zero_rest ? 1 : 0;
-  return a.R <= 8 ? launch_few<false, kHalf, 1, 1, 2, 8>(p, s) : launch_few<false, kHalf, 2, 4, 4, 2>(p, s);
+  return launch_few<false, kHalf>(p, s);
 }
 
 }  // namespace
+
+// Which of the two forms a call takes. The number of experts in use is not known to the host; what counts is
+// how many rows there are and how large the weights are, as a group's come once for 32 rows.
+bool expert_ffn_few_ok(const FfnArgs& a) {
+  const int most = std::max(a.d, a.I);
+  return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 26)) &&
+         few_smem(2, (most / 32 + 8) / 8 + 1) <= 112 * 1024;
+}
 
 cudaError_t launch_expert_ffn_few(const FfnArgs& a, cudaStream_t s) {
   return a.dtype == DMOE_FP16 ? few<true>(a, s) : few<false>(a, s);

@@ -29,7 +29,6 @@
 
 #include <algorithm>
 #include <mutex>
-#include <cstdlib>
 
 #include "dmoe_internal.cuh"
 #include "silu.cuh"
@@ -55,10 +54,14 @@ enum Mode { kUp, kDown, kGradH, kGradX, kGradW };
 
 __device__ DevErrRecord ffn_fault;
 
+// A box costs the SM's copy engine about 100 cycles besides its rows, and with six boxes of 2 to 8 KB for
+// 128 of K a stage took 0.5 us whatever its MMAs took: whole stages come in as few boxes as can be, through
+// maps in which 64 neighbours of the fast dimension are one of their own (`whole`). What is cut by the
+// end of a matrix comes in boxes of 64 (`cut`), filled up with zeros.
 struct Maps {
-  CUtensorMap a[2];         // weights [E][rows][cols], or (kGradW) the output side's rows
-  CUtensorMap b[kLevels];   // rows [R][parts][K] in boxes of level_rows
-  CUtensorMap out[2];       // kGradW: the gradients
+  CUtensorMap a[2], a_cut[2];             // weights, or (kGradW) the output side's rows
+  CUtensorMap b[kLevels], b_cut[kLevels]; // rows in boxes of level_rows
+  CUtensorMap out[2];                     // kGradW: the gradients
 };
 
 struct Params {
@@ -220,8 +223,8 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     }
     ptx::fence_mbarrier_init();
     *s_abort = 0;
-    ptx::prefetch_tensormap(&tm.a[0]);
-    ptx::prefetch_tensormap(&tm.b[0]);
+    if (kAmn ? p.M >= 128 : p.K >= 128) ptx::prefetch_tensormap(&tm.a[0]);
+    if (kBmn ? p.N >= 128 : p.K >= 128) ptx::prefetch_tensormap(&tm.b[0]);
   }
   if (warp == 1) {
     ptx::tmem_alloc2(s_tmem, 512);
@@ -280,9 +283,19 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     if (kMode == kGradW) return min(round_up(p.N - un.n * kNMax, 32), kNMax);
     return round_up(un.rows, 32);
   };
-  auto k_steps = [&](const Unit& un) -> int {
+  // stages of a unit: 64 rows (kGradW), or 128 of K of each part
+  auto stages_of = [&](const Unit& un) -> int {
     if (kMode == kGradW) return (un.rows + 63) / 64;
-    return p.parts * ((p.K + 63) / 64);
+    return p.parts * ((p.K + 127) / 128);
+  };
+  // the lowest box of rows that holds a CTA's half of the columns
+  auto level_of = [&](int half, int* rows) -> int {
+    int lv = 0;
+    *rows = p.level_rows[0];
+#pragma unroll
+    for (int l = 1; l < kLevels; ++l)
+      if (p.level_rows[l] >= half) { lv = l; *rows = p.level_rows[l]; }
+    return lv;
   };
 
   if (warp == 0) {
@@ -296,79 +309,100 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, false);
         if (un.e < 0) break;
-        const int steps = k_steps(un), half = columns(un) / 2;
-        int part = 0, k0 = 0;                   // of the next step
+        const int stages = stages_of(un), half = columns(un) / 2;
         const int m0 = kMode == kUp ? un.m * 128 + rank * 64 : un.m * 256 + rank * 128;
-        int lv = 0, rows = p.level_rows[0];   // the lowest box of rows that holds the half
-#pragma unroll
-        for (int l = 1; l < kLevels; ++l)
-          if (p.level_rows[l] >= half) { lv = l; rows = p.level_rows[l]; }
-        const int b_boxes = (half + 63) / 64;   // kGradW
-        const uint32_t sub_bytes = kTileABytes + (kMode == kGradW ? (uint32_t)b_boxes * 8192u
-                                                                  : (uint32_t)rows * 128u);
+        int rows;
+        const int lv = level_of(half, &rows);
         const int b_row = un.row + rank * half;
-        // a step's weights
-        auto load_a = [&](uint8_t* as, uint32_t bar, int part_, int k) {
-          if (kMode == kUp) {          // 64 rows of Wg, then 64 of Wu
-            ptx::tma_load_3d_pair(as, &tm.a[0], bar, k, m0, un.e, once);
-            ptx::tma_load_3d_pair(as + 8192, &tm.a[1], bar, k, m0, un.e, once);
-          } else if (kMode == kDown) {
-            ptx::tma_load_3d_pair(as, &tm.a[0], bar, k, m0, un.e, once);
-          } else {                     // 64 rows of K, 2 x 64 columns
-            ptx::tma_load_3d_pair(as, &tm.a[part_], bar, m0, k, un.e, once);
-            ptx::tma_load_3d_pair(as + 8192, &tm.a[part_], bar, m0 + 64, k, un.e, once);
+        // a stage's weights: 128 of K from k on
+        auto load_a = [&](uint8_t* a, uint32_t bar, int part, int k) {
+          if constexpr (kMode == kUp || kMode == kDown) {
+            // K-major. Whole: eight rows over both 64 of K, then the next eight
+            const int row8 = (un.e * p.M + m0) >> 3;
+            if (k + 128 <= p.K) {
+              ptx::tma_load_4d_pair(a, &tm.a[0], bar, 0, 0, k >> 6, row8, once);
+              if (kMode == kUp) ptx::tma_load_4d_pair(a + kTileABytes, &tm.a[1], bar, 0, 0, k >> 6, row8, once);
+            } else {
+              for (int s = 0; s < 2 && k + 64 * s < p.K; ++s) {
+                uint8_t* as = a + s * kTileABytes;
+                ptx::tma_load_3d_pair(as, &tm.a_cut[0], bar, k + 64 * s, m0, un.e, once);
+                if (kMode == kUp) ptx::tma_load_3d_pair(as + 8192, &tm.a_cut[1], bar, k + 64 * s, m0, un.e, once);
+              }
+            }
+          } else {
+            // MN-major: 128 rows of K of 64 columns, then of the next 64
+            if (m0 + 128 <= p.M) {
+              ptx::tma_load_4d_pair(a, &tm.a[part], bar, 0, k, m0 >> 6, un.e, once);
+            } else {
+              ptx::tma_load_3d_pair(a, &tm.a_cut[part], bar, m0, k, un.e, once);
+              ptx::tma_load_3d_pair(a + kTileABytes, &tm.a_cut[part], bar, m0 + 64, k, un.e, once);
+            }
           }
+        };
+        auto stage_tx = [&](int k) -> uint32_t {
+          const uint32_t subs = k + 64 < p.K ? 2 : 1;
+          return subs * (uint32_t)rows * 128u + (kAmn ? 2u : subs) * kTileABytes;
+        };
+        int part = 0, k0 = 0;
+        auto next = [&](int& part_, int& k) {
+          k += 128;
+          if (k >= p.K) { k = 0; ++part_; }
         };
         int ahead = 0;                 // stages whose weights were asked for before the wait
         if (early<kMode>() && i == 0) {
           int part_ = 0, k = 0;
-          for (int c = 0; c < steps && ahead < p.stages; c += kSub, ++ahead) {
-            const uint32_t bar = full0 + 8u * (uint32_t)ahead;
-            const int n_sub = min(kSub, steps - c);
-            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[ahead], kCluster * n_sub * sub_bytes);
-            for (int s = 0; s < n_sub; ++s) {
-              load_a(smem + (uint32_t)ahead * stage_bytes + s * kTileABytes, bar, part_, k);
-              k += 64;
-              if (k >= p.K) { k = 0; ++part_; }
-            }
+          for (; ahead < stages && ahead < p.stages; ++ahead, next(part_, k)) {
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[ahead], kCluster * stage_tx(k));
+            load_a(smem + (uint32_t)ahead * stage_bytes, full0 + 8u * (uint32_t)ahead, part_, k);
           }
           pdl_wait();
           pdl_launch_dependents();
         }
-        for (int c = 0; c < steps; c += kSub) {
+        for (int c = 0; c < stages; ++c) {
           const bool a_there = ahead > 0;
           if (a_there) --ahead;
           if (stage % kPer == 0 && !a_there && !wait(&empty[stage / kPer], phase ^ 1u, i)) {
             ok = false;
             break;
           }
-          const int n_sub = min(kSub, steps - c);
           uint8_t* a = smem + (uint32_t)stage * stage_bytes;
           uint8_t* b = a + kSub * kTileABytes;
           const uint32_t bar = full0 + 8u * (uint32_t)stage;
-          if (kMode == kGradW) {
+          if constexpr (kMode == kGradW) {
             // the last stage, if it is to be cleared, completes on this CTA's own barrier, and the
             // clearing warp arrives for this CTA
-            const int r = un.row + c * 64;
-            const bool ends = (un.rows & 15) != 0 && c == steps - 1;
+            const int r = un.row + c * 64, n0 = un.n * kNMax + rank * half;
+            const int b_boxes = (half + 63) / 64;
+            const uint32_t bytes = kTileABytes + (uint32_t)b_boxes * 8192u;
+            const bool ends = (un.rows & 15) != 0 && c == stages - 1;
             const uint32_t to = ends ? ptx::peer_smem(&tail[stage], rank) : bar;
-            if (ends) ptx::mbar_arrive_expect_tx(&tail[stage], sub_bytes);
-            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], ends ? 0 : kCluster * sub_bytes);
+            if (ends) ptx::mbar_arrive_expect_tx(&tail[stage], bytes);
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], ends ? 0 : kCluster * bytes);
             if (!ends) ptx::mbar_arrive_pair(bar);
-            for (int j = 0; j < 2; ++j)
-              ptx::tma_load_3d_pair(a + j * 8192, &tm.a[0], to, m0 + 64 * j, un.part, r, again);
-            for (int j = 0; j < b_boxes; ++j)
-              ptx::tma_load_3d_pair(b + j * 8192, &tm.b[0], to, un.n * kNMax + rank * half + 64 * j, 0, r,
-                                    again);
-          } else {
-            if (rank == 0 && !a_there)
-              ptx::mbar_arrive_expect_tx(&full[stage], kCluster * n_sub * sub_bytes);
-            for (int s = 0; s < n_sub; ++s) {
-              if (!a_there) load_a(a + s * kTileABytes, bar, part, k0);
-              ptx::tma_load_3d_pair(b + s * b_sub, &tm.b[lv], bar, k0, part, b_row, again);
-              k0 += 64;
-              if (k0 >= p.K) { k0 = 0; ++part; }
+            if (m0 + 128 <= p.M) {
+              ptx::tma_load_4d_pair(a, &tm.a[0], to, 0, r, m0 >> 6, un.part, again);
+            } else {
+              for (int j = 0; j < 2; ++j)
+                ptx::tma_load_3d_pair(a + j * 8192, &tm.a_cut[0], to, m0 + 64 * j, un.part, r, again);
             }
+            if (half == 128 && n0 + 128 <= p.N) {
+              ptx::tma_load_4d_pair(b, &tm.b[0], to, 0, r, n0 >> 6, 0, again);
+            } else {
+              for (int j = 0; j < b_boxes; ++j)
+                ptx::tma_load_3d_pair(b + j * 8192, &tm.b_cut[0], to, n0 + 64 * j, 0, r, again);
+            }
+          } else {
+            if (!a_there) {
+              if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], kCluster * stage_tx(k0));
+              load_a(a, bar, part, k0);
+            }
+            if (k0 + 128 <= p.K) {
+              ptx::tma_load_4d_pair(b, &tm.b[lv], bar, 0, b_row, k0 >> 6, part, again);
+            } else {
+              for (int s = 0; s < 2 && k0 + 64 * s < p.K; ++s)
+                ptx::tma_load_3d_pair(b + s * rows * 128, &tm.b_cut[lv], bar, k0 + 64 * s, part, b_row, again);
+            }
+            next(part, k0);
           }
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
@@ -460,15 +494,17 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, false);
         if (un.e < 0) break;
-        const int steps = k_steps(un), n = columns(un);
-        if (steps == 0) continue;
+        const int stages = stages_of(un), n = columns(un);
+        if (stages == 0) continue;
         const uint32_t idesc = ptx::idesc_16bit(256, (uint32_t)n, !kHalf, kAmn, kBmn);
         const uint32_t d0 = tmem_base + (uint32_t)acc * kNMax;
         const int K = kMode == kGradW ? un.rows : p.K;
+        int rows;
+        level_of(n / 2, &rows);
         ok = wait(&acc_empty[acc], acc_phase ^ 1u, i);
         ptx::tc_fence_after();
         int left = K;                           // of the part's sum
-        for (int c = 0; ok && c < steps; c += kSub) {
+        for (int c = 0; ok && c < stages; ++c) {
           ok = in || wait(&full[stage], phase, i);
           if (!ok) break;
           // (the clearing warps' words, those of the other CTA as well)
@@ -479,24 +515,27 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           const bool last = stage % kPer == kPer - 1;
           uint64_t* const done = &empty[stage / kPer];
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          const bool whole = left >= 128;       // (kUp, kDown: how the weights lie)
 #pragma unroll
           for (int s = 0; s < kSub; ++s) {
-            if (c + s >= steps) break;
-            const uint32_t as = a + s * kTileABytes, bs = b + s * b_sub;
+            if (s > 0 && left <= 64 * s) break;
+            const uint32_t as = a + (kMode == kGradW ? 0u : kAmn ? s * 8192u : s * (whole ? 1024u : kTileABytes));
+            const uint32_t bs = b + s * (uint32_t)rows * 128u;
+            const int l = left - 64 * s;
             auto mma = [&](int kk) {
-              ptx::mma_bf16_pair(
-                  d0, kAmn ? ptx::sdesc_mn_sw128(as + kk * 2048, 8192) : ptx::sdesc_k_sw128(as + kk * 32),
-                  kBmn ? ptx::sdesc_mn_sw128(bs + kk * 2048, 8192) : ptx::sdesc_k_sw128(bs + kk * 32),
-                  idesc, (c > 0 || s > 0 || kk > 0) ? 1u : 0u);
+              const uint64_t ad = kAmn ? ptx::sdesc_mn_sw128(as + kk * 2048, kMode == kGradW ? 8192 : 16384)
+                                       : ptx::sdesc_k_sw128(as + kk * 32, whole ? 2048u : 1024u);
+              const uint64_t bd = kBmn ? ptx::sdesc_mn_sw128(bs + kk * 2048, 8192) : ptx::sdesc_k_sw128(bs + kk * 32);
+              ptx::mma_bf16_pair(d0, ad, bd, idesc, (c > 0 || s > 0 || kk > 0) ? 1u : 0u);
             };
             mma(0);
-            if (left > 16) mma(1);
-            if (s == kSub - 1 || c + s + 1 == steps) in = ptx::mbar_test_wait(&full[stage], phase);
-            if (left > 32) mma(2);
-            if (left > 48) mma(3);
-            left -= 64;
-            if (left <= 0) left = K;
+            if (l > 16) mma(1);
+            if (s == 0) in = ptx::mbar_test_wait(&full[stage], phase);
+            if (l > 32) mma(2);
+            if (l > 48) mma(3);
           }
+          left -= 64 * kSub;
+          if (left <= 0) left = K;
           if (last) ptx::mma_commit_pair(done);
         }
         if (!ok) break;
@@ -522,9 +561,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, true);
         if (un.e < 0) break;
-        const int steps = k_steps(un), blocks = 2 + (columns(un) / 2 + 63) / 64;
-        const int at = (stage + steps - 1) % p.stages;
-        stage = (stage + steps) % p.stages;
+        const int stages = stages_of(un), blocks = 2 + (columns(un) / 2 + 63) / 64;
+        const int at = (stage + stages - 1) % p.stages;
+        stage = (stage + stages) % p.stages;
         if ((un.rows & 15) == 0) continue;
         ok = __all_sync(0xffffffffu, wait(&tail[at], (phases >> at) & 1u, i));
         if (!ok) break;
@@ -782,19 +821,22 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// [n2][n1][n0] of 16-bit elements with strides in elements, in boxes of 64 x b1 x b2
-bool make_map(CUtensorMap* m, bool half, const void* base, uint64_t n0, uint64_t n1, uint64_t n2,
-              uint64_t ld1, uint64_t ld2, uint32_t b1, uint32_t b2) {
+// A map of 16-bit elements with n.size() dimensions (the fastest first), strides in elements from the second
+// on, in boxes of 64 x box.
+bool make_map(CUtensorMap* m, bool half, const void* base, std::initializer_list<uint64_t> n,
+              std::initializer_list<uint64_t> ld, std::initializer_list<uint32_t> box) {
   EncodeTiledFn enc = encode_fn();
   if (enc == nullptr) return false;
-  const cuuint64_t dims[3] = {n0, n1, n2};
-  const cuuint64_t strides[2] = {ld1 * 2, ld2 * 2};
-  const cuuint32_t box[3] = {64, b1, b2};
-  const cuuint32_t estr[3] = {1, 1, 1};
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t b[4] = {64, 1, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  std::copy(n.begin(), n.end(), dims);
+  std::transform(ld.begin(), ld.end(), strides, [](uint64_t v) { return 2 * v; });
+  std::copy(box.begin(), box.end(), b + 1);
   auto encode = [&] {
-    return enc(m, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-               const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    return enc(m, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+               (cuuint32_t)n.size(), const_cast<void*>(base), dims, strides, b, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
   if (encode()) return true;
@@ -890,22 +932,33 @@ cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const
   p.ldo = ldo;
   p.pre = kMode == kUp || kMode == kGradH ? a.pre : nullptr;
   p.n_max = (int)std::min<int64_t>(kNMax, (a.R + 31) / 32 * 32);
-  // w: as it lies, [E][rows][cols]; its rows are M (kUp, kDown) or K
-  const uint64_t rows = a_mn<kMode>() ? p.K : p.M, cols = a_mn<kMode>() ? p.M : p.K;
+  // (only the maps that are used: each costs the host time)
+  const uint64_t M = p.M, K = p.K, E = a.n_experts, R = a.R, parts = p.parts, ld = b.ld;
+  const bool whole = p.K >= 128, cut = p.K % 128 != 0;
   bool ok = true;
   for (int i = 0; i < 2; ++i) {
     const void* w = i == 0 ? w0 : w1;
-    if (w != nullptr)
-      ok = ok && make_map(&m.a[i], kHalf, w, cols, rows, a.n_experts, cols, rows * cols,
-                          kMode == kDown ? 128 : 64, 1);
+    if (w == nullptr) continue;
+    if (a_mn<kMode>()) {       // w [E][K][M]
+      if (M >= 128)
+        ok = ok && make_map(&m.a[i], kHalf, w, {64, K, M / 64, E}, {M, 64, K * M}, {128, 2, 1});
+      if (M % 256 != 0)
+        ok = ok && make_map(&m.a_cut[i], kHalf, w, {M, K, E}, {M, K * M}, {128, 1});
+    } else {                   // w [E][M][K]
+      const uint32_t rows = kMode == kDown ? 128 : 64;
+      if (whole)
+        ok = ok && make_map(&m.a[i], kHalf, w, {64, 8, K / 64, E * M / 8}, {K, 64, 8 * K}, {8, 2, rows / 8});
+      if (cut) ok = ok && make_map(&m.a_cut[i], kHalf, w, {K, M, E}, {K, M * K}, {rows, 1});
+    }
   }
   int level = 0;
   for (int h = p.n_max / 2; level < kLevels; ++level) {
-    p.level_rows[level] = h;
-    if (level == 0 || h < p.level_rows[level - 1])
-      ok = ok && make_map(&m.b[level], kHalf, b.p, b.K, b.parts, a.R, b.K, b.ld, 1, h);
-    else
-      p.level_rows[level] = 0;   // (not taken)
+    if (level == 0 || h < p.level_rows[level - 1]) {
+      p.level_rows[level] = h;
+      if (whole)
+        ok = ok && make_map(&m.b[level], kHalf, b.p, {64, R, K / 64, parts}, {ld, 64, K}, {(uint32_t)h, 2, 1});
+      if (cut) ok = ok && make_map(&m.b_cut[level], kHalf, b.p, {K, parts, R}, {K, ld}, {1, (uint32_t)h});
+    }
     h = std::max(16, (h / 2 + 15) / 16 * 16);
   }
   if (!ok) return cudaErrorInvalidValue;
@@ -925,11 +978,14 @@ cudaError_t weights_product(const FfnArgs& a, const Rows& out, const Rows& in, v
   p.m_tiles = (p.M + 255) / 256;
   p.n_tiles = (p.N + kNMax - 1) / kNMax;
   p.level_rows[0] = 128;     // (a half of B: 64 rows of K of 128 columns)
-  bool ok = make_map(&m.a[0], kHalf, out.p, out.K, out.parts, a.R, out.K, out.ld, 1, 64) &&
-            make_map(&m.b[0], kHalf, in.p, in.K, 1, a.R, in.K, in.ld, 1, 64);
+  const uint64_t M = p.M, N = p.N, R = a.R, parts = p.parts, lda = out.ld, ldb = in.ld;
+  bool ok = true;
+  if (M >= 128) ok = make_map(&m.a[0], kHalf, out.p, {64, R, M / 64, parts}, {lda, 64, M}, {64, 2, 1});
+  if (M % 256 != 0) ok = ok && make_map(&m.a_cut[0], kHalf, out.p, {M, parts, R}, {M, lda}, {1, 64});
+  if (N >= 128) ok = ok && make_map(&m.b[0], kHalf, in.p, {64, R, N / 64, 1}, {ldb, 64, N}, {64, 2, 1});
+  if (N % 256 != 0) ok = ok && make_map(&m.b_cut[0], kHalf, in.p, {N, 1, R}, {N, ldb}, {1, 64});
   for (int i = 0; i < p.parts; ++i)
-    ok = ok && make_map(&m.out[i], kHalf, i == 0 ? dw0 : dw1, p.N, p.M, a.n_experts, p.N,
-                        (uint64_t)p.M * p.N, 32, 1);
+    ok = ok && make_map(&m.out[i], kHalf, i == 0 ? dw0 : dw1, {N, M, (uint64_t)a.n_experts}, {N, M * N}, {32, 1});
   if (!ok) return cudaErrorInvalidValue;
   return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.parts * p.m_tiles * p.n_tiles, s);
 }
@@ -961,8 +1017,7 @@ cudaError_t backward(const FfnArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_expert_ffn(const FfnArgs& a, cudaStream_t s) {
-  static const int few = getenv("FEW") ? atoi(getenv("FEW")) : kFewRows;
-  if (a.R <= few) return launch_expert_ffn_few(a, s);
+  if (expert_ffn_few_ok(a)) return launch_expert_ffn_few(a, s);
   return a.dtype == DMOE_FP16 ? forward<true>(a, s) : forward<false>(a, s);
 }
 cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s) {

@@ -23,6 +23,11 @@ SHAPES = [
     (4, 72, 40, [1, 0, 2, 700], 1),
     (6, 256, 128, [15, 16, 17, 33, 600, 0], 0),
     (7, 1000, 344, [0, 64, 65, 127, 0, 31, 300], 9),
+    # whole tiles, and widths a little off 64, 128 and 256
+    (2, 256, 384, [257, 300], 0),
+    (2, 248, 136, [300, 290], 0),
+    (2, 120, 504, [520, 10], 2),
+    (1, 192, 320, [600], 0),
 ]
 DTYPES = [torch.bfloat16, torch.float16]
 
