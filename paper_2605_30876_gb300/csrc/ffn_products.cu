@@ -508,8 +508,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           ok = in || wait(&full[stage], phase, i);
           if (!ok) break;
           // (the clearing warps' words, those of the other CTA as well)
-          if (kMode == kGradW && left < 64 && (left & 15) != 0)
-            asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          if (kMode == kGradW && left < 64 && (left & 15) != 0) ptx::fence_acquire_cluster_smem();
           ptx::tc_fence_after();
           const uint32_t a = ring + (uint32_t)stage * stage_bytes, b = a + kSub * kTileABytes;
           const bool last = stage % kPer == kPer - 1;
@@ -554,6 +553,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       // ================= zeros in the rows of K behind the group's last row, up to the 16 of its last
       // MMA, in both operands of this CTA (a row of K is 128 bytes of each block of 64 columns; the
       // swizzle stays within it)
+      // (Fences that also order global memory cost a microsecond a group: the gradient of 256 experts'
+      // 2048 x 512 from 230 rows each took 190 us with them, 141 without, as from 240 rows, which need
+      // no clearing.)
       const uint32_t full0 = ptx::peer_smem(full, 0);
       int stage = 0;
       uint32_t phases = 0;      // of tail, a bit each
@@ -567,16 +569,16 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         if ((un.rows & 15) == 0) continue;
         ok = __all_sync(0xffffffffu, wait(&tail[at], (phases >> at) & 1u, i));
         if (!ok) break;
-        phases ^= 1u << at;
         const int from = un.rows & 63, per_block = (16 - (from & 15)) * 8;
         uint8_t* a = smem + (uint32_t)at * stage_bytes + from * 128;
         for (int j = lane; j < blocks * per_block; j += 32) {
           const int blk = j / per_block, o = j - blk * per_block;
           *reinterpret_cast<uint4*>(a + blk * 8192 + o * 16) = make_uint4(0, 0, 0, 0);
         }
-        asm volatile("fence.proxy.async;" ::: "memory");
+        ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_cluster(full0 + 8u * (uint32_t)at);
+        if (lane == 0) ptx::mbar_arrive_cluster_smem(full0 + 8u * (uint32_t)at);
+        phases ^= 1u << at;
       }
     } else if ((kMode == kDown || kMode == kGradX) && p.zero_rest) {
       // ================= zeros in the rows in no group, 64 rows at a time

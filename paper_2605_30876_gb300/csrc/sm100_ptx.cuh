@@ -246,6 +246,17 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t pa
       : "memory");
   return ok != 0;
 }
+// The pair of the same for shared memory alone: what this thread has written to its own CTA's shared memory
+// (and what it knows of) before the arrival is there for a thread of the cluster that has seen the
+// phase complete and then calls fence_acquire_cluster_smem. (mbar_arrive_cluster also waits until
+// the CTA's global stores are visible.)
+__device__ __forceinline__ void mbar_arrive_cluster_smem(uint32_t bar_cluster) {
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+}
+__device__ __forceinline__ void fence_acquire_cluster_smem() {
+  asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
+}
 __device__ __forceinline__ void st_cluster_f32(uint32_t addr_cluster, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr_cluster), "f"(v) : "memory");
 }
