@@ -37,10 +37,6 @@
 namespace dmoe {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kEpiWarps = 8;
-constexpr int kPlanWarp = 10;
-constexpr int kFixWarp = 11;
 constexpr int kCluster = 2;
 constexpr int kTileABytes = 128 * 128;      // 128 rows (or 2 x 64 columns) x 64 of K
 constexpr int kMaxStages = 8;
@@ -93,10 +89,15 @@ template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1
 // The launch before is one of the same call: it was released once what that call was given was there,
 // and nothing of it but the rows of B is waited for. The weights are on their way before that.
 template <int kMode> constexpr bool early() { return kMode == kDown || kMode == kGradX; }
+// Warps of the epilogue: sixteen take half as long as eight with a launch's last tile (a small training step of 6186 rows
+// 143 us with eight, 133 with sixteen), but kGradW's
+// words in shared memory would take the place of stages.
+template <int kMode> constexpr int epi_warps() { return kMode == kGradW ? 8 : 16; }
+template <int kMode> constexpr int threads() { return (4 + epi_warps<kMode>()) * 32; }
 template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
 template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
 template <int kMode> constexpr int epi_bytes() {
-  return kMode == kGradW ? kEpiWarps * 4096 : kMode == kUp ? kEpiWarps * 2048 : 0;
+  return epi_warps<kMode>() * (kMode == kGradW ? 4096 : kMode == kUp ? 1024 : 0);
 }
 
 template <bool kHalf>
@@ -134,16 +135,17 @@ __device__ __forceinline__ void pair_up(const float (&v)[8], uint32_t (&w)[4]) {
   }
 }
 
-// AND over the epilogue's 256 threads (named barrier 1)
+// AND over the epilogue's threads (named barrier 1)
+template <int kThreads>
 __device__ __forceinline__ bool epilogue_all(bool v) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.and.pred q, 1, 256, p;\n\t"
+      "bar.red.and.pred q, 1, %2, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)v)
+      : "r"((uint32_t)v), "n"(kThreads)
       : "memory");
   return r != 0;
 }
@@ -173,9 +175,11 @@ struct Unit {
 };
 
 template <int kMode, bool kHalf>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads<kMode>(), 1)
 ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   constexpr int kSub = sub_steps<kMode>(), kPer = per_commit<kMode>();
+  constexpr int kEpiWarps = epi_warps<kMode>(), kPlanWarp = 2 + kEpiWarps, kFixWarp = 3 + kEpiWarps;
+  constexpr int kStep = kEpiWarps * 4;       // columns that the groups of four warps take at once, 16 each
   constexpr bool kAmn = a_mn<kMode>(), kBmn = b_mn<kMode>();
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -604,7 +608,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       }
     }
   } else {
-    // ================= epilogue: warps 2-9, TMEM lanes 32 * (warp % 4) ..; two groups of four
+    // ================= epilogue: warps from 2 on, TMEM lanes 32 * (warp % 4) ..; groups of four
     // warps take alternate slices of the columns
     const int q = warp & 3, cg = (warp - 2) >> 2, odd = lane & 1;
     const uint32_t lane_off = (uint32_t)(q * 32) << 16;
@@ -615,7 +619,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       const Unit un = unit_at(i, true);
       const bool sums = kMode != kGradW || un.rows > 0;
       // (a warp whose wait failed leaves with the others)
-      if (!epilogue_all(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
+      if (!epilogue_all<kEpiWarps * 32>(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
       ptx::tc_fence_after();
       const uint32_t tbase = tmem_base + lane_off + (uint32_t)acc * kNMax;
       const int nvalid = un.rows;
@@ -624,24 +628,24 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         // keep the first eight and give the others to the warps of u, through shared memory.
         const bool is_gate = q < 2;
         const int ii = un.m * 128 + rank * 64 + (q & 1) * 32 + lane, ie = ii & ~1;
-        float4* box = reinterpret_cast<float4*>(s_epi) + (cg * 2 + (q & 1)) * 256;
+        float4* box = reinterpret_cast<float4*>(s_epi) + (cg * 2 + (q & 1)) * 128;
         const int bar_id = 2 + cg * 2 + (q & 1);
         uint16_t* h = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.I + ie;
         uint16_t* pre = static_cast<uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
-        int flip = 0;
-        for (int c0 = 16 * cg; c0 < nvalid; c0 += 32, flip ^= 1) {
+        for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
           float v[16];
           ptx::tmem_ld16(tbase + c0, v);
           ptx::tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
-          // [flip][from gate / from up][two float4][lane]
-          float4* give = box + flip * 128 + (is_gate ? 0 : 64) + lane;
-          const float4* take = box + flip * 128 + (is_gate ? 64 : 0) + lane;
+          // [from gate / from up][two float4][lane]
+          float4* give = box + (is_gate ? 0 : 64) + lane;
+          const float4* take = box + (is_gate ? 64 : 0) + lane;
           give[0] = is_gate ? make_float4(v[8], v[9], v[10], v[11]) : make_float4(v[0], v[1], v[2], v[3]);
           give[32] = is_gate ? make_float4(v[12], v[13], v[14], v[15]) : make_float4(v[4], v[5], v[6], v[7]);
           ptx::named_bar_sync(bar_id, 64);
           const float4 o0 = take[0], o1 = take[32];
+          ptx::named_bar_sync(bar_id, 64);       // (the words have been read)
           const float o[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
           float g[8], u[8], hv[8];
 #pragma unroll
@@ -671,14 +675,11 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
               }
             }
         }
-        // (the last slice's words are read before the next unit's first are written: a slice of the
-        // other half, or this barrier, lies between)
-        ptx::named_bar_sync(bar_id, 64);
       } else if constexpr (kMode == kGradH) {
         const int ii = un.m * 256 + rank * 128 + q * 32 + lane, ie = ii & ~1;
         const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
         uint16_t* dpre = static_cast<uint16_t*>(p.out) + (int64_t)un.row * 2 * p.I + ie;
-        for (int c0 = 16 * cg; c0 < nvalid; c0 += 32) {
+        for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
           uint32_t gw[8], uw[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -752,7 +753,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const int c = un.m * 256 + rank * 128 + q * 32 + lane, ce = c & ~1;
         uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.ldo + ce;
         if (un.m * 256 + rank * 128 + q * 32 < p.M) {   // (the same for the warp)
-          for (int c0 = 16 * cg; c0 < nvalid; c0 += 32) {
+          for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
             float v[16];
             ptx::tmem_ld16(tbase + c0, v);
             ptx::tmem_ld_wait();
@@ -915,7 +916,7 @@ cudaError_t launch(Maps& m, Params& p, int64_t units, cudaStream_t s) {
   p.stages -= p.stages % per_commit<kMode>();
   if (p.stages < 2) return cudaErrorInvalidConfiguration;
   const int pairs = (int)std::min<int64_t>(device_sm_count() / kCluster, std::max<int64_t>(units, 1));
-  return launch_cluster(ffn_products_kernel<kMode, kHalf>, dim3(pairs * kCluster), dim3(kThreads),
+  return launch_cluster(ffn_products_kernel<kMode, kHalf>, dim3(pairs * kCluster), dim3(threads<kMode>()),
                         fixed + p.stages * stage, s, kCluster, true, m, p);
 }
 
