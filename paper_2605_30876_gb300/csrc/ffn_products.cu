@@ -57,7 +57,7 @@ __device__ DevErrRecord ffn_fault;
 struct Maps {
   CUtensorMap a[2], a_cut[2];             // weights, or (kGradW) the output side's rows
   CUtensorMap b[kLevels], b_cut[kLevels]; // rows in boxes of level_rows
-  CUtensorMap out[2];                     // kGradW: the gradients
+  CUtensorMap out[3];                     // kGradW: the gradients
 };
 
 struct Params {
@@ -68,9 +68,12 @@ struct Params {
   int n_max;                // columns of a unit, at most (kGradW: of N)
   int M;                    // valid rows of D: I or d
   int K;                    // length of a part's reduction
-  int N;                    // kGradW: width of the gradient's rows
-  int parts;                // kGradX: sums over gate and up; kGradW: outputs (gate, up)
-  int m_tiles, n_tiles;     // n_tiles: kGradW
+  int parts;                // kGradX: sums over gate and up
+  int m_tiles;
+  // kGradW: the gradients of gate and up, M x N each, then that of down (either may be missing), in tiles
+  int M_down, N, N_down;
+  int n_tiles, m_tiles_down, n_tiles_down;
+  int up_units, per_group;  // of a group: of gate and up together, and all
   int level_rows[kLevels];
   int stages;
   void* out;                // h, y, dpre or dx
@@ -171,7 +174,7 @@ __device__ __forceinline__ int group_expert(const Params& p, int g) {
 
 struct Unit {
   int row, rows, e;   // first row and their number (kGradW: of the sum); e < 0: the end
-  int part, m, n;     // n: kGradW
+  int part, m, n;     // kGradW: gate, up or down; column tile
 };
 
 template <int kMode, bool kHalf>
@@ -227,8 +230,8 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     }
     ptx::fence_mbarrier_init();
     *s_abort = 0;
-    if (kAmn ? p.M >= 128 : p.K >= 128) ptx::prefetch_tensormap(&tm.a[0]);
-    if (kBmn ? p.N >= 128 : p.K >= 128) ptx::prefetch_tensormap(&tm.b[0]);
+    if (kMode != kGradW && (kAmn ? p.M : p.K) >= 128) ptx::prefetch_tensormap(&tm.a[0]);
+    if (kMode != kGradW && p.K >= 128) ptx::prefetch_tensormap(&tm.b[0]);
   }
   if (warp == 1) {
     ptx::tmem_alloc2(s_tmem, 512);
@@ -283,8 +286,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     return un;
   };
   // columns of D: N of the unit's MMAs, a multiple of 32; half of them are each CTA's
+  auto rows_m = [&](const Unit& un) -> int { return kMode == kGradW && un.part == 2 ? p.M_down : p.M; };
+  auto cols_n = [&](const Unit& un) -> int { return un.part == 2 ? p.N_down : p.N; };   // kGradW
   auto columns = [&](const Unit& un) -> int {
-    if (kMode == kGradW) return min(round_up(p.N - un.n * kNMax, 32), kNMax);
+    if (kMode == kGradW) return min(round_up(cols_n(un) - un.n * kNMax, 32), kNMax);
     return round_up(un.rows, 32);
   };
   // stages of a unit: 64 rows (kGradW), or 128 of K of each part
@@ -383,17 +388,18 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             if (ends) ptx::mbar_arrive_expect_tx(&tail[stage], bytes);
             if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], ends ? 0 : kCluster * bytes);
             if (!ends) ptx::mbar_arrive_pair(bar);
-            if (m0 + 128 <= p.M) {
-              ptx::tma_load_4d_pair(a, &tm.a[0], to, 0, r, m0 >> 6, un.part, again);
+            const int job = un.part >> 1, part = un.part & 1;   // (down: part 0 of its own rows)
+            if (m0 + 128 <= rows_m(un)) {
+              ptx::tma_load_4d_pair(a, &tm.a[job], to, 0, r, m0 >> 6, part, again);
             } else {
               for (int j = 0; j < 2; ++j)
-                ptx::tma_load_3d_pair(a + j * 8192, &tm.a_cut[0], to, m0 + 64 * j, un.part, r, again);
+                ptx::tma_load_3d_pair(a + j * 8192, &tm.a_cut[job], to, m0 + 64 * j, part, r, again);
             }
-            if (half == 128 && n0 + 128 <= p.N) {
-              ptx::tma_load_4d_pair(b, &tm.b[0], to, 0, r, n0 >> 6, 0, again);
+            if (half == 128 && n0 + 128 <= cols_n(un)) {
+              ptx::tma_load_4d_pair(b, &tm.b[job], to, 0, r, n0 >> 6, 0, again);
             } else {
               for (int j = 0; j < b_boxes; ++j)
-                ptx::tma_load_3d_pair(b + j * 8192, &tm.b_cut[0], to, n0 + 64 * j, 0, r, again);
+                ptx::tma_load_3d_pair(b + j * 8192, &tm.b_cut[job], to, n0 + 64 * j, 0, r, again);
             }
           } else {
             if (!a_there) {
@@ -417,8 +423,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     }
   } else if (warp == kPlanWarp) {
     // ================= units: counted per group, then decoded ahead of their use
-    const int per_group = p.parts * p.m_tiles * p.n_tiles;   // kGradW
+    const int per_group = p.per_group;   // kGradW
     int units = p.n_groups * per_group;
+    // (n_max is kNMax, or no less than the call's rows)
+    auto tiles_of = [&](int cnt) -> int { return p.n_max == kNMax ? (cnt + kNMax - 1) / kNMax : cnt > 0 ? 1 : 0; };
     if (kMode != kGradW) {
       // a lane counts 16 groups in a row (their offsets are all asked for at once)
       constexpr int kOwn = kMaxGroups / 32;
@@ -433,7 +441,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           if (group_expert(p, g) < 0) cnt = 0;
           s_rows[g] = make_int2((int)row0, cnt);
         }
-        own[j] = (cnt + p.n_max - 1) / p.n_max * p.m_tiles;
+        own[j] = tiles_of(cnt) * p.m_tiles;
         sum += own[j];
       }
       int before = sum;
@@ -461,8 +469,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         if (u < units) {
           if (kMode == kGradW) {
             const int g = u / per_group, local = u - g * per_group;
-            const int n = local % p.n_tiles, mp = local / p.n_tiles;
-            v = make_int4((int)row_ahead, cnt_ahead, g, (mp / p.m_tiles) << 16 | (mp % p.m_tiles) << 8 | n);
+            const bool down = local >= p.up_units;
+            const int in_job = down ? local - p.up_units : local, nt = down ? p.n_tiles_down : p.n_tiles;
+            const int mt = down ? p.m_tiles_down : p.m_tiles, n = in_job % nt, mp = in_job / nt;
+            v = make_int4((int)row_ahead, cnt_ahead, g, (down ? 2 : mp / mt) << 16 | (mp % mt) << 8 | n);
             if (u + ncl < units) group_rows(p, (u + ncl) / per_group, &row_ahead, &cnt_ahead);
           } else {
             int lo = 0, hi = p.n_groups - 1;
@@ -472,7 +482,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             }
             const int row0 = s_rows[lo].x, cnt = s_rows[lo].y, local = u - s_first[lo];
             // the tiles of a group next to one another share its weights; they are of one size
-            const int nt = (cnt + p.n_max - 1) / p.n_max;
+            const int nt = tiles_of(cnt);
             const int m = local / nt, n = local - m * nt;
             const int tile = round_up((cnt + nt - 1) / nt, 32);
             v = make_int4(row0 + n * tile, min(tile, cnt - n * tile),
@@ -722,7 +732,8 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const int row = un.m * 256 + rank * 128 + q * 32;
         uint8_t* mine = s_epi + (warp - 2) * 4096;
         const int n = columns(un);
-        const CUtensorMap* out = un.part == 0 ? &tm.out[0] : &tm.out[1];
+        const CUtensorMap* out = &tm.out[un.part];
+        const int M = rows_m(un), N = cols_n(un);
         for (int c0 = 64 * cg; c0 < n; c0 += 128) {
           float v[2][32];
           if (sums) {
@@ -746,7 +757,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           }
           ptx::fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0 && row < p.M && un.n * kNMax + c0 < p.N)
+          if (lane == 0 && row < M && un.n * kNMax + c0 < N)
             ptx::tma_store_3d(out, mine, un.n * kNMax + c0, row, un.e);
         }
       } else {
@@ -969,28 +980,44 @@ cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const
   return launch<kMode, kHalf>(m, p, units, s);
 }
 
-// Gradients of weights [E][M][N] x parts: sums over the groups' rows of out [R][parts][M] and in [R][N].
+// Gradients of weights: sums over the groups' rows of out [R][parts][M] and in [R][N].
 template <bool kHalf>
-cudaError_t weights_product(const FfnArgs& a, const Rows& out, const Rows& in, void* dw0, void* dw1,
-                            cudaStream_t s) {
+cudaError_t weights_products(const FfnArgs& a, const Rows& dpre, const Rows& x, const Rows& dy, const Rows& h,
+                             cudaStream_t s) {
   Params p = base_params(a);
   Maps m{};
-  p.M = out.K;
-  p.N = in.K;
-  p.parts = out.parts;
-  p.m_tiles = (p.M + 255) / 256;
-  p.n_tiles = (p.N + kNMax - 1) / kNMax;
   p.level_rows[0] = 128;     // (a half of B: 64 rows of K of 128 columns)
-  const uint64_t M = p.M, N = p.N, R = a.R, parts = p.parts, lda = out.ld, ldb = in.ld;
+  const bool up = a.dw_gate != nullptr, down = a.dw_down != nullptr;
   bool ok = true;
-  if (M >= 128) ok = make_map(&m.a[0], kHalf, out.p, {64, R, M / 64, parts}, {lda, 64, M}, {64, 2, 1});
-  if (M % 256 != 0) ok = ok && make_map(&m.a_cut[0], kHalf, out.p, {M, parts, R}, {M, lda}, {1, 64});
-  if (N >= 128) ok = ok && make_map(&m.b[0], kHalf, in.p, {64, R, N / 64, 1}, {ldb, 64, N}, {64, 2, 1});
-  if (N % 256 != 0) ok = ok && make_map(&m.b_cut[0], kHalf, in.p, {N, 1, R}, {N, ldb}, {1, 64});
-  for (int i = 0; i < p.parts; ++i)
-    ok = ok && make_map(&m.out[i], kHalf, i == 0 ? dw0 : dw1, {N, M, (uint64_t)a.n_experts}, {N, M * N}, {32, 1});
+  auto maps = [&](int job, const Rows& out, const Rows& in, std::initializer_list<void*> dws) {
+    const uint64_t M = out.K, N = in.K, R = a.R, parts = out.parts, lda = out.ld, ldb = in.ld;
+    if (M >= 128) ok = ok && make_map(&m.a[job], kHalf, out.p, {64, R, M / 64, parts}, {lda, 64, M}, {64, 2, 1});
+    if (M % 256 != 0) ok = ok && make_map(&m.a_cut[job], kHalf, out.p, {M, parts, R}, {M, lda}, {1, 64});
+    if (N >= 128) ok = ok && make_map(&m.b[job], kHalf, in.p, {64, R, N / 64, 1}, {ldb, 64, N}, {64, 2, 1});
+    if (N % 256 != 0) ok = ok && make_map(&m.b_cut[job], kHalf, in.p, {N, 1, R}, {N, ldb}, {1, 64});
+    int i = 2 * job;
+    for (void* dw : dws)
+      ok = ok && make_map(&m.out[i++], kHalf, dw, {N, M, (uint64_t)a.n_experts}, {N, M * N}, {32, 1});
+  };
+  if (up) {
+    maps(0, dpre, x, {a.dw_gate, a.dw_up});
+    p.M = a.I;
+    p.N = a.d;
+    p.m_tiles = (p.M + 255) / 256;
+    p.n_tiles = (p.N + kNMax - 1) / kNMax;
+    p.up_units = 2 * p.m_tiles * p.n_tiles;
+  }
+  p.per_group = p.up_units;
+  if (down) {
+    maps(1, dy, h, {a.dw_down});
+    p.M_down = a.d;
+    p.N_down = a.I;
+    p.m_tiles_down = (p.M_down + 255) / 256;
+    p.n_tiles_down = (p.N_down + kNMax - 1) / kNMax;
+    p.per_group += p.m_tiles_down * p.n_tiles_down;
+  }
   if (!ok) return cudaErrorInvalidValue;
-  return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.parts * p.m_tiles * p.n_tiles, s);
+  return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.per_group, s);
 }
 
 template <bool kHalf>
@@ -1010,10 +1037,8 @@ cudaError_t backward(const FfnArgs& a, cudaStream_t s) {
     e = rows_product<kGradH, kHalf>(a, a.w_down, nullptr, dy, a.dpre, 2 * a.I, s);
   if (e == cudaSuccess && a.dx != nullptr)
     e = rows_product<kGradX, kHalf>(a, a.w_gate, a.w_up, dpre, a.dx, a.lddx, s);
-  if (e == cudaSuccess && a.dw_gate != nullptr)
-    e = weights_product<kHalf>(a, dpre, x, a.dw_gate, a.dw_up, s);
-  if (e == cudaSuccess && a.dw_down != nullptr)
-    e = weights_product<kHalf>(a, dy, h, a.dw_down, nullptr, s);
+  if (e == cudaSuccess && (a.dw_gate != nullptr || a.dw_down != nullptr))
+    e = weights_products<kHalf>(a, dpre, x, dy, h, s);
   return e;
 }
 
