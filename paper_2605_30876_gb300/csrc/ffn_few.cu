@@ -51,6 +51,14 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// weights, read once: past L1
+__device__ __forceinline__ uint4 load_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
 template <bool kHalf>
 __device__ __forceinline__ void store_16(void* p, int64_t at, float v) {
   if constexpr (kHalf) static_cast<__half*>(p)[at] = __float2half_rn(v);
@@ -91,7 +99,8 @@ ffn_few_kernel(const FewParams p) {
   constexpr int kMaxG = kMaxFfnExperts;
   extern __shared__ float4 smem[];
   float4* s_acc = smem;                         // [warp][tile][n tile][lane]
-  uint8_t* s_rows = reinterpret_cast<uint8_t*>(smem + kWarps * kMT * kNT * 32);   // [warp][row][part]
+  const int acc_nt = p.R <= 8 ? 1 : kNT;
+  uint8_t* s_rows = reinterpret_cast<uint8_t*>(smem + kWarps * kMT * acc_nt * 32);   // [warp][row][part]
   __shared__ int s_first[2][kMaxG];             // chunks of rows before a group: groups of up to eight
   __shared__ int2 s_sum[kWarps];                // rows, and the others
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -184,11 +193,11 @@ ffn_few_kernel(const FewParams p) {
     for (int m = 0; m < kMT; ++m)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        a[m][j] = in && (at.there >> (2 * m + j) & 1u) ? __ldcs(at.w[j] + m * tile_stride + k * 4)
+        a[m][j] = in && (at.there >> (2 * m + j) & 1u) ? load_stream(at.w[j] + m * tile_stride + k * 4)
                                                        : make_uint4(0, 0, 0, 0);
   };
   // a warp's sums of tile m, columns 8 n .. 8 n + 7
-  auto sums_at = [&](int w, int m, int n) -> float4* { return s_acc + ((w * kMT + m) * kNT + n) * 32 + lane; };
+  auto sums_at = [&](int w, int m, int n) -> float4* { return s_acc + ((w * kMT + m) * acc_nt + n) * 32 + lane; };
   // all of them are there: (tile, n tile) pairs of this warp's rows go round the warps that share them
   auto finish = [&](const At& now, int n_tiles) {
     for (int t = ks; t < kMT * n_tiles; t += kKS) {
@@ -364,8 +373,11 @@ ffn_few_kernel(const FewParams p) {
   }
 }
 
-constexpr size_t few_smem(int tiles, int per) {
-  return sizeof(float4) * 8 * tiles * kFewCols / 8 * 32 + (size_t)8 * 8 * few_pitch(per);
+// What shared memory takes is missing from L1, through which the weights in flight come (two CTAs of 98 KB
+// each: 4 experts of 4096 x 2048, a row or two each, 60 us; of 75 KB: 38).
+constexpr size_t kFewSmem = 80 * 1024;
+constexpr size_t few_smem(int64_t R, int tiles, int per) {
+  return sizeof(float4) * 8 * tiles * (R <= 8 ? 1 : kFewCols / 8) * 32 + (size_t)8 * 8 * few_pitch(per);
 }
 
 template <bool kUp, bool kHalf, int kMT, int kKS>
@@ -374,14 +386,14 @@ cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
   const int64_t units = (int64_t)std::min(p.R, p.n_groups + p.R / kFewCols) * ((p.M + rows - 1) / rows);
   const int ctas = (int)std::min<int64_t>(units, 152 * 2);
   const int per = ((p.K + 31) / 32 + kKS - 1) / kKS;
-  const size_t smem = few_smem(kMT, per);
+  const size_t smem = few_smem(p.R, kMT, per);
   auto* kernel = ffn_few_kernel<kUp, kHalf, kMT, kKS>;
   static std::atomic<uint32_t> done;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   const uint32_t bit = dev < 32 ? 1u << dev : 0u;
   if (e == cudaSuccess && (done.load(std::memory_order_relaxed) & bit) == 0u) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
   }
   if (e != cudaSuccess) return e;
@@ -440,11 +452,18 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
 }  // namespace
 
 // Which of the two forms a call takes. The number of experts in use is not known to the host; what counts is
-// how many rows there are and how large the weights are, as a group's come once for 32 rows.
+// how many rows there are, how large the weights are (a group's come once for 32 rows), and that
+// shared memory leaves room in L1. Us in a graph, weights of several calls in turn, tcgen05 / this form:
+//   one expert of 2048 x 512: 8 rows 16.7 / 7.4, 128 rows 18.5 / 13.4, 256 rows 23.2 / 22.0
+//   of 4096 x 4096: 8 rows 37.8 / 27.9, 64 rows 39.0 / 64.5; of 512 x 512: 512 rows 16.0 / 16.6
+//   4 experts of 4096 x 2048: 8 rows 42 / 38, 16 rows 42 / 63 (room in L1)
+//   32 of 2048 x 512: 32 rows 43.2 / 43.3; 256 of them: 256 rows 243.6 / 242.7
+//   8 of 2048 x 512: 8 rows 25.5 / 14.3, 128 rows 25.4 / 16.7, 256 rows 25.4 / 18.9 if each has 32, but
+//   30.7 if they have 13 to 61 (two chunks for some, one for others)
 bool expert_ffn_few_ok(const FfnArgs& a) {
   const int most = std::max(a.d, a.I);
-  return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 26)) &&
-         few_smem(2, (most / 32 + 8) / 8 + 1) <= 112 * 1024;
+  return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 27)) &&
+         few_smem(a.R, 2, (most / 32 + 8) / 8 + 1) <= kFewSmem;
 }
 
 cudaError_t launch_expert_ffn_few(const FfnArgs& a, cudaStream_t s) {
