@@ -628,6 +628,22 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     for (int i = 0;; ++i) {
       const Unit un = unit_at(i, true);
       const bool sums = kMode != kGradW || un.rows > 0;
+      // kGradH: g and u of the next slice of columns, asked for before this one's sums are there (the
+      // backward pass of 59000 rows over 16 experts of 2048 x 1024 took 833 us when they were asked for in turn, 789 so)
+      const int he = (un.m * 256 + rank * 128 + q * 32 + lane) & ~1;
+      uint32_t gw[8], uw[8];
+      auto ask_pre = [&](int c0) {
+        const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + he;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = c0 + 8 * (j >> 2) + 4 * odd + (j & 3);
+          const bool in = t < un.rows && he < p.I;
+          const uint16_t* from = pre + (int64_t)t * 2 * p.I;
+          gw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from)) : 0u;
+          uw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from + p.I)) : 0u;
+        }
+      };
+      if (kMode == kGradH && un.e >= 0) ask_pre(16 * cg);
       // (a warp whose wait failed leaves with the others)
       if (!epilogue_all<kEpiWarps * 32>(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
       ptx::tc_fence_after();
@@ -686,19 +702,16 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             }
         }
       } else if constexpr (kMode == kGradH) {
-        const int ii = un.m * 256 + rank * 128 + q * 32 + lane, ie = ii & ~1;
-        const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
+        const int ie = he;
         uint16_t* dpre = static_cast<uint16_t*>(p.out) + (int64_t)un.row * 2 * p.I + ie;
         for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
-          uint32_t gw[8], uw[8];
+          uint32_t g_now[8], u_now[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int t = c0 + 8 * (j >> 2) + 4 * odd + (j & 3);
-            const bool in = t < nvalid && ie < p.I;
-            const uint16_t* from = pre + (int64_t)t * 2 * p.I;
-            gw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from)) : 0u;
-            uw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from + p.I)) : 0u;
+            g_now[j] = gw[j];
+            u_now[j] = uw[j];
           }
+          if (c0 + kStep < nvalid) ask_pre(c0 + kStep);
           float v[16];
           ptx::tmem_ld16(tbase + c0, v);
           ptx::tmem_ld_wait();
@@ -709,7 +722,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             const int at = 8 * (j >> 2) + (j & 3);
             const float other = __shfl_xor_sync(0xffffffffu, odd ? v[at] : v[at + 4], 1);
             const float dh[2] = {odd ? other : v[at], odd ? v[at + 4] : other};
-            const float2 g2 = unpack2<kHalf>(gw[j]), u2 = unpack2<kHalf>(uw[j]);
+            const float2 g2 = unpack2<kHalf>(g_now[j]), u2 = unpack2<kHalf>(u_now[j]);
             const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
             float dg[2], du[2];
 #pragma unroll
