@@ -22,7 +22,7 @@ LIB = os.path.join(PKG, "libdmoe.so")
 SOURCES = ["dmoe_api.cu", "router.cu", "route_cluster.cu", "dispatch.cu", "expert_ffn.cu",
            "expert_decode.cu", "router_no_alloc.cu", "router_logits_tc.cu", "operators_api.cu",
            "sort_tokens.cu", "rows.cu", "q4_weights.cu", "q4_linear.cu", "ffn_products.cu",
-           "ffn_few.cu", "norm_rows.cu"]
+           "ffn_few.cu", "norm_rows.cu", "norm_rows_backward.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
          "--expt-relaxed-constexpr", "-I", INCLUDE]
