@@ -440,6 +440,7 @@ typedef struct {
  *   h          [R, I] out: also the second product's input, so it is always needed
  *   y          [R, d] out, row stride ldy
  *   zero_rest  nonzero: rows of y that are in no group become zeros; 0: they are not written
+ * No output overlaps another one or an input.
  * Rows of pre and h that are in no group are not written. Groups do not overlap: an element of a
  * row that two have is either's. A row's values do not depend on the call's other rows as long as
  * their number is the same side of the sizes at which the library changes its kernel. */
@@ -460,7 +461,8 @@ dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_g
  *   dx         [R, d] out (row stride lddx), or NULL
  *   dw_gate, dw_up  [E, I, d] out, or NULL for both;  dw_down  [E, d, I] out, or NULL. Experts
  *              without rows get zeros. One output at least is wanted
- *   zero_rest  as above, for the rows of dx */
+ *   zero_rest  as above, for the rows of dx
+ * No output overlaps another one or an input. */
 dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, const void* dy,
                                      int64_t lddy, const void* x, int64_t ldx,
                                      const int32_t* offsets, const void* w_gate, const void* w_up,
@@ -496,7 +498,8 @@ typedef struct {
  *   r      [T, d] out (ldr), or NULL if n is wanted alone; may be x itself (with its stride)
  *   n      [T, d] out (ldn) where w_pre is given, else NULL; may be y itself (with its stride)
  *   stats  fp32 [2, T] out: ry and rr (1 where there is no such norm), for the backward pass; or
- *          NULL */
+ *          NULL
+ * No output overlaps another one or an input otherwise. */
 dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y,
                                int64_t ldy, const float* w_post, const void* gate, int64_t ldgate,
                                const float* w_pre, void* r, int64_t ldr, void* n, int64_t ldn,
@@ -515,7 +518,7 @@ dmoe_status dmoe_norm_workspace_size(const dmoe_norm_desc* desc, size_t* bytes /
  *   dx, dy     [T, d] out (lddx, lddy);  dgate  out, of the gate's shape (lddgate): sums over the
  *              tokens of a gate row, in fp32, rounded once
  *   dw_post, dw_pre  fp32 [d] out: sums over all tokens
- *              Any of the five may be NULL, but not all; none overlaps an input
+ *              Any of the five may be NULL, but not all; none overlaps an input or another one
  *   workspace  16-byte aligned; NULL is allowed for dx and dy alone
  * Sums over tokens are taken in an order that follows from the sizes: the same call gives the same
  * bits. */

@@ -205,6 +205,8 @@ def norm_residual(x: torch.Tensor, y: Optional[torch.Tensor] = None,
     tokens = x.shape[0]
     if gate is not None and gate.dim() == 1:
         gate = gate.unsqueeze(0)
+    if gate is not None and tokens == 0:
+        gate = gate[:0]                    # (its gradient is zeros)
     if gate is None:
         gate_tokens = 0
     elif gate_tokens is None:

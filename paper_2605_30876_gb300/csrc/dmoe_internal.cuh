@@ -408,7 +408,7 @@ cudaError_t launch_expert_ffn_few(const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_expert_ffn_backward(const FfnArgs& a, cudaStream_t s);
 cudaError_t ffn_fault_address(void** p);
 
-// The norms around a block with its gate and residual (norm_rows.cu). Strides in elements.
+// The norms around a block with its gate and residual (norm_rows.cu, norm_rows_backward.cu). Strides in elements.
 struct NormArgs {
   int dtype;
   int64_t T;

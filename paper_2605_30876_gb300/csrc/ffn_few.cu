@@ -3,9 +3,10 @@
 // small CTAs; mma.sync.m16n8k16 with 16 rows of weights as A and eight token rows as B, both straight
 // from global memory into the fragments. A lane's fragment takes pairs of k from four places; any
 // order of k gives the same sum as long as A and B agree, so a lane takes eight neighbours (16 bytes)
-// of a 32-long piece of K for two MMAs. (tcgen05 has nothing to win here: the weights' bytes are the bound,
-// and its launches, with tensor memory and barriers to set up and 64 SMs at work, took 27 us where
-// these take 14, for one token's eight experts of 2048 x 512; the floor is 7.4.)
+// of a 32-long piece of K for two MMAs. (tcgen05 has nothing to win here: the weights'
+// bytes are the bound, and its launches, with tensor memory and barriers to set up and 64 SMs at work,
+// take 25.5 us where these take 14.3, for one token's eight experts of 2048 x 512; 50 MB at the copy rate are
+// 7.4.)
 // The eight warps of a CTA share the sum over K (kKS ways) or the rows (8 / kKS ways); the parts meet in
 // shared memory and are added in the order of the warps. The second launch has its first weights on
 // their way before it waits for the first one's h.
@@ -17,7 +18,6 @@
 
 namespace dmoe {
 namespace {
-
 
 struct FewParams {
   const int32_t* offsets;

@@ -12,19 +12,28 @@
 // few rows wastes no tensor work on the other side and its weights stream once. Wd and Wg / Wu are
 // read as they lie, along the reduction (kUp, kDown: K-major) or across it (kGradH, kGradX:
 // MN-major, the tensor cores' transposed operand); so are both operands of kGradW. Nothing is
-// transposed in memory.
+// transposed in memory. kGradW's three gradients are one launch (a small training step takes 5 us less than
+// with two).
 //
 // Two CTAs of neighbouring SMs (a cluster) share an MMA of M = 256 (cta_group::2): each holds 128 of
 // the M rows and half of the N columns. A persistent pair per two SMs takes units (group, 256 rows
 // of M, up to 256 columns of N) in turn; they are found on the device from the offsets, so that no
-// call waits for the host. Warp 0 issues the TMA loads, warp 1 of the first CTA the MMAs, warps 2-9
-// run the epilogue from one of two accumulators in tensor memory while the other fills, warp 10
-// decodes units ahead. Warp 11: in kGradW it clears what a stage holds behind an expert's last row (the
-// rows there are another expert's, and 0 * inf would not be 0); in kDown and kGradX it writes the
-// zeros of rows in no group, where they are wanted.
+// call waits for the host. Warp 0 issues the TMA loads, warp 1 of the first CTA the MMAs; the warps from
+// 2 on (sixteen, in kGradW eight) run the epilogue from one of two accumulators in tensor memory while
+// the other fills; the one behind them decodes units ahead. The last warp: in kGradW it clears what a stage
+// holds behind an expert's last row (the rows there are another expert's, and 0 * inf would not be 0);
+// in kDown and kGradX it writes the zeros of rows in no group, where they are wanted.
 // Sums are fp32 throughout. g, u, dg, du and h are rounded to the rows' type between products: they
-// are the next product's operands, and the tensor cores take 16 bits.
+// are the next product's operands, and the tensor cores take 16 bits (two operands for each, high and low
+// part, would be twice the work). The weights' gradients of 59000 rows in bf16 are off by 0.0031 of
+// their size so, and by 0.0017 with g, u and h in fp32.
 // Waits are bounded (1 s), record a timeout and unwind.
+//
+// What bounds it, in bf16 with inputs larger than L2: 1024 rows for each of 64 experts of 2048 x 1024 take
+// 525 us forward (1.57 PFLOP/s, 0.83 of a large library product's rate) and 1083 backward (1.52): the
+// tensor pipe, epilogues at the ends. 230 rows each of 256 experts of 2048 x 512: 406 (5.8 TB/s) and
+// 794 us (5.4 TB/s): weights and rows from HBM, with MMAs of N < 256, which take 60 ns from N = 32 to 160,
+// close behind. Small calls: 5 us a launch before the first bytes and after the last.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -92,9 +101,9 @@ template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1
 // The launch before is one of the same call: it was released once what that call was given was there,
 // and nothing of it but the rows of B is waited for. The weights are on their way before that.
 template <int kMode> constexpr bool early() { return kMode == kDown || kMode == kGradX; }
-// Warps of the epilogue: sixteen take half as long as eight with a launch's last tile (a small training step of 6186 rows
-// 143 us with eight, 133 with sixteen), but kGradW's
-// words in shared memory would take the place of stages.
+// Warps of the epilogue: sixteen take half as long as eight with a launch's last tile (a small training
+// step of 6186 rows 143 us with eight, 133 with sixteen), but kGradW's words in shared memory would take
+// the place of stages.
 template <int kMode> constexpr int epi_warps() { return kMode == kGradW ? 8 : 16; }
 template <int kMode> constexpr int threads() { return (4 + epi_warps<kMode>()) * 32; }
 template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }

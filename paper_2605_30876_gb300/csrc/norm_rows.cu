@@ -1,4 +1,4 @@
-// The norms around a block, with its gate and its residual, in one pass, and the gradients:
+// The norms around a block, with its gate and its residual, in one pass:
 //   p = y * ry * w_post,  r = scale * x + gate * p,  n = r * rr * w_pre
 //   ry = 1 / sqrt(mean(y^2) + eps),  rr = 1 / sqrt(mean(r^2) + eps)
 // Both directions are bound by the bytes of their rows, each read once and written once. A row is held

@@ -395,7 +395,8 @@ dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, co
   const bool inner = dx != nullptr || dw_gate != nullptr;
   if ((offsets == nullptr && n_groups != 1) || (!inner && dw_down == nullptr) ||
       (dw_gate == nullptr) != (dw_up == nullptr) || !null_or16(dw_gate) || !null_or16(dw_up) ||
-      !null_or16(dw_down) || (dw_gate != nullptr && dw_gate == dw_up))
+      !null_or16(dw_down) ||
+      (dw_gate != nullptr && (dw_gate == dw_up || dw_gate == dw_down || dw_up == dw_down)))
     return DMOE_ERR_INVALID_ARG;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (R == 0) {   // no rows: the weights' gradients are zeros
@@ -408,7 +409,8 @@ dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, co
     return DMOE_OK;
   }
   if (!matrix16(dy, lddy, desc->d_model) || !null_or16(offsets) ||
-      (inner && (!given16(w_down) || !given16(pre) || !given16(dpre) || pre == dpre)) ||
+      (inner && (!given16(w_down) || !given16(pre) || !given16(dpre) || dpre == pre || dpre == h ||
+                 dpre == dy || dpre == x || dpre == dx)) ||
       (dx != nullptr && (!matrix16(dx, lddx, desc->d_model) || !given16(w_gate) ||
                          !given16(w_up) || dx == dy || dx == x)) ||
       (dw_gate != nullptr && !matrix16(x, ldx, desc->d_model)) ||

@@ -89,6 +89,13 @@ def test_expert_backward_refusals(dm):
     assert ffn_backward(dm, dx=at("dy", BACK)) == 1 and ffn_backward(dm, dx=at("x", BACK)) == 1
 
 
+def test_expert_outputs_that_overlap(dm):
+    for k in ("h", "dy", "x", "dx", "pre"):
+        assert ffn_backward(dm, dpre=at(k, BACK)) == 1, k
+    for a, b in (("dw_gate", "dw_up"), ("dw_gate", "dw_down"), ("dw_up", "dw_down")):
+        assert ffn_backward(dm, **{a: at(b, BACK)}) == 1, (a, b)
+
+
 def test_expert_hold(dm):
     assert dm._lib.dmoe_expert_set_debug_hold(-1) == 1
     assert dm._lib.dmoe_expert_set_debug_hold(0) == 0

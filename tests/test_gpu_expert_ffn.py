@@ -28,6 +28,17 @@ SHAPES = [
     (2, 248, 136, [300, 290], 0),
     (2, 120, 504, [520, 10], 2),
     (1, 192, 320, [600], 0),
+    # few rows: groups of up to eight and of more together, long sums, and either side of the sizes
+    # at which the kernels change
+    (8, 256, 264, [8, 9, 1, 33, 0, 64, 7, 32], 2),
+    (2, 4096, 2048, [5, 3], 0),
+    (2, 4096, 2048, [5, 4], 0),
+    (1, 8192, 64, [8], 0),
+    (12, 520, 136, [40] * 12, 32),
+    (12, 520, 136, [40] * 12, 33),
+    (3, 1024, 1024, [100, 4, 24], 0),
+    (3, 1024, 1024, [100, 4, 25], 0),
+    (40, 136, 1040, [3, 0, 1, 5] * 10, 0),
 ]
 DTYPES = [torch.bfloat16, torch.float16]
 
@@ -130,6 +141,29 @@ def test_expert_ids():
                w_down=c["w_down"][:2].contiguous())
     ids = torch.tensor([1, 0, 0, 1, 0, 1], dtype=torch.int32, device="cuda")
     check_forward(few, run_forward(few, ids), ids)
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+def test_as_many_groups_as_there_can_be(rows):
+    """512 groups of the same few experts; the call's rows are few and more than that."""
+    c = case(torch.bfloat16, 3, 72, 40, [0, 0, 0], 512 * rows)
+    c["offsets"] = torch.arange(513, dtype=torch.int32, device="cuda") * rows
+    ids = (torch.arange(512, device="cuda") * 7 % 4).to(torch.int32)     # (3 is no expert)
+    check_forward(c, run_forward(c, ids, zero_rest=True), ids, zero_rest=True)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("counts", [[5, 3, 0], [40, 9, 30]], ids=str)
+def test_few_rows_keep_to_themselves(counts, bad):
+    """A row's values are its own: other rows of its group, and rows of no group, may hold anything."""
+    c = case(torch.bfloat16, 3, 264, 136, counts, 2)
+    want = run_forward(c)
+    c["x"][1] = bad
+    c["x"][-2:] = bad
+    got = run_forward(c)
+    keep = torch.ones(sum(counts) + 2, dtype=torch.bool, device="cuda")
+    keep[1] = False
+    assert all(torch.equal(a[keep], b[keep]) for a, b in zip(got, want))
 
 
 def test_one_expert_of_all_rows():

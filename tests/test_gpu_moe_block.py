@@ -205,6 +205,56 @@ def test_a_block_in_training(dtype):
     assert dm.dmoe_expert_device_error()[0] == 0
 
 
+def test_no_tokens():
+    """The gradients of what all tokens share are zeros then."""
+    gen = generator(9)
+    w = [new(gen, 2, 40, 72), new(gen, 2, 40, 72), new(gen, 2, 72, 40)]
+    for gate in (new(gen, 72), new(gen, 0, 72), None):
+        x, y = leaves(new(gen, 0, 72), new(gen, 0, 72))
+        w_post, w_pre = (torch.ones(72, device="cuda", requires_grad=True) for _ in range(2))
+        ws = leaves(*w)
+        gate = None if gate is None else gate.requires_grad_()
+        idx, gates = torch.zeros((0, 2), dtype=torch.int32, device="cuda"), torch.zeros((0, 2), device="cuda")
+        r, n = norm_residual(x, moe_ffn(y, idx, gates, *ws), w_post, gate, w_pre)
+        (r.sum() + n.sum()).backward()
+        for t in (w_post, w_pre, gate, *ws):
+            assert t is None or (t.grad.shape == t.shape and (t.grad == 0).all())
+
+
+def test_a_captured_training_step():
+    """Forward and backward of a block in a graph, replayed on other values. (Gradients are asked for by
+    name: leaves that accumulate them keep the stream of their first use.)"""
+    gen = generator(10)
+    T, k, E, d, I = 150, 2, 4, 72, 40
+    idx, gates = routing(gen, T, k, E)
+    vec = lambda: 1 + new(gen, d, size=0.2, dtype=torch.float32)
+    args = leaves(new(gen, T, d), gates, vec(), vec(), new(gen, -(-T // 32), d),
+                  new(gen, E, I, d, size=0.1), new(gen, E, I, d, size=0.1), new(gen, E, d, I, size=0.1))
+    dr, dn = new(gen, T, d), new(gen, T, d)
+
+    def step():
+        x, gates, w_in, w_out, gate, *w = args
+        _, n = norm_residual(x, w_pre=w_in)
+        r, n = norm_residual(x, moe_ffn(n, idx, gates, *w), None, gate, w_out, gate_tokens=32)
+        return [r, n, *torch.autograd.grad([r, n], args, [dr, dn])]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    with torch.no_grad():
+        args[0].mul_(-0.5)
+        idx.copy_(idx.flip(0))
+    want = step()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_moe_ffn_is_its_parts():
     gen = generator(6)
     T, k, E, d, I = 60, 3, 5, 72, 40
