@@ -33,6 +33,8 @@ __all__ = ["gather_rows", "combine_rows", "expert_ffn", "moe_ffn", "norm_residua
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """The matrix with contiguous rows at least their width apart (an expanded gradient has none)."""
+    if t.numel() == 0:                     # (any strides count as contiguous)
+        return t.new_empty(t.shape)
     ok = t.shape[1] <= 1 or t.stride(1) == 1
     return t if ok and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]) else t.contiguous()
 

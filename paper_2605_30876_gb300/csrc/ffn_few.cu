@@ -380,13 +380,15 @@ constexpr size_t few_smem(int64_t R, int tiles, int per) {
   return sizeof(float4) * 8 * tiles * (R <= 8 ? 1 : kFewCols / 8) * 32 + (size_t)8 * 8 * few_pitch(per);
 }
 
+// pieces of K that are a warp's
+constexpr int few_per(int K, int ks) { return ((K + 31) / 32 + ks - 1) / ks; }
+
 template <bool kUp, bool kHalf, int kMT, int kKS>
 cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
   constexpr int rows = 8 / kKS * kMT * (kUp ? 8 : 16);
   const int64_t units = (int64_t)std::min(p.R, p.n_groups + p.R / kFewCols) * ((p.M + rows - 1) / rows);
   const int ctas = (int)std::min<int64_t>(units, 152 * 2);
-  const int per = ((p.K + 31) / 32 + kKS - 1) / kKS;
-  const size_t smem = few_smem(p.R, kMT, per);
+  const size_t smem = few_smem(p.R, kMT, few_per(p.K, kKS));
   auto* kernel = ffn_few_kernel<kUp, kHalf, kMT, kKS>;
   static std::atomic<uint32_t> done;
   int dev = 0;
@@ -400,21 +402,24 @@ cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
   return launch_ex(kernel, dim3(ctas), dim3(256), smem, s, true, p);
 }
 
+// Ways a sum over K is cut: a warp's part is a few pieces of 32.
+constexpr int few_ks(int K) { return K > 512 ? 8 : K > 256 ? 4 : 2; }
+
 // Units of a tile a warp where those of two would not fill two CTAs per SM (with as many groups as there
-// can be); the second launch's sums are cut eight ways, not four, where they are long.
+// can be).
+template <bool kUp, bool kHalf, int kKS>
+cudaError_t launch_cut(const FewParams& p, cudaStream_t s) {
+  constexpr int rows = 8 / kKS * 2 * (kUp ? 8 : 16);
+  if ((int64_t)std::min(p.R, p.n_groups) * (p.M / rows) < 304) return launch_form<kUp, kHalf, 1, kKS>(p, s);
+  return launch_form<kUp, kHalf, 2, kKS>(p, s);
+}
 template <bool kUp, bool kHalf>
 cudaError_t launch_few(const FewParams& p, cudaStream_t s) {
-  const int groups = std::min(p.R, p.n_groups);
-  if (kUp) {
-    if ((int64_t)groups * (p.M / 16) < 304) return launch_form<kUp, kHalf, 1, 8>(p, s);
-    return launch_form<kUp, kHalf, 2, 8>(p, s);
+  switch (few_ks(p.K)) {
+    case 8: return launch_cut<kUp, kHalf, 8>(p, s);
+    case 4: return launch_cut<kUp, kHalf, 4>(p, s);
+    default: return launch_cut<kUp, kHalf, 2>(p, s);
   }
-  if (p.K > 512) {
-    if ((int64_t)groups * (p.M / 32) < 304) return launch_form<kUp, kHalf, 1, 8>(p, s);
-    return launch_form<kUp, kHalf, 2, 8>(p, s);
-  }
-  if ((int64_t)groups * (p.M / 64) < 304) return launch_form<kUp, kHalf, 1, 4>(p, s);
-  return launch_form<kUp, kHalf, 2, 4>(p, s);
 }
 
 template <bool kHalf>
@@ -461,9 +466,8 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
 //   8 of 2048 x 512: 8 rows 25.5 / 14.3, 128 rows 25.4 / 16.7, 256 rows 25.4 / 18.9 if each has 32, but
 //   30.7 if they have 13 to 61 (two chunks for some, one for others)
 bool expert_ffn_few_ok(const FfnArgs& a) {
-  const int most = std::max(a.d, a.I);
-  return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 27)) &&
-         few_smem(a.R, 2, (most / 32 + 8) / 8 + 1) <= kFewSmem;
+  auto fits = [&](int K) { return few_smem(a.R, 2, few_per(K, few_ks(K))) <= kFewSmem; };
+  return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 27)) && fits(a.d) && fits(a.I);
 }
 
 cudaError_t launch_expert_ffn_few(const FfnArgs& a, cudaStream_t s) {

@@ -91,6 +91,7 @@ struct Params {
   int I;
   int hold;
   int zero_rest;            // kDown, kGradX
+  int after_x;              // kGradW: the launch before is kGradX's
 };
 
 // A commit costs the issuing thread about as much as two MMAs, so slots of the ring are given back
@@ -100,6 +101,8 @@ template <int kMode> constexpr int sub_steps() { return kMode == kGradW ? 1 : 2;
 template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1; }
 // The launch before is one of the same call: it was released once what that call was given was there,
 // and nothing of it but the rows of B is waited for. The weights are on their way before that.
+// kGradW behind kGradX waits only before it ends: kGradX writes nothing that it reads, and released it
+// when kGradH's results were there. Its units begin where kGradX's have run out.
 template <int kMode> constexpr bool early() { return kMode == kDown || kMode == kGradX; }
 // Warps of the epilogue: sixteen take half as long as eight with a launch's last tile (a small training
 // step of 6186 rows 143 us with eight, 133 with sixteen), but kGradW's words in shared memory would take
@@ -252,7 +255,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   ptx::cluster_wait();
   ptx::tc_fence_after();
   const uint32_t tmem_base = *s_tmem;
-  if (!early<kMode>()) {
+  if (!early<kMode>() && !(kMode == kGradW && p.after_x)) {
     pdl_wait();
     pdl_launch_dependents();
   }
@@ -427,6 +430,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         }
       }
       if (early<kMode>()) pdl_wait();   // (a pair without units ends no earlier than the launch before)
+      if (kMode == kGradW && p.after_x) {
+        pdl_wait();
+        pdl_launch_dependents();
+      }
       // the issuer's last commit arrives in this CTA, too
       wait(drain, 0, -1);
     }
@@ -1010,6 +1017,7 @@ cudaError_t weights_products(const FfnArgs& a, const Rows& dpre, const Rows& x, 
   Maps m{};
   p.level_rows[0] = 128;     // (a half of B: 64 rows of K of 128 columns)
   const bool up = a.dw_gate != nullptr, down = a.dw_down != nullptr;
+  p.after_x = a.dx != nullptr ? 1 : 0;
   bool ok = true;
   auto maps = [&](int job, const Rows& out, const Rows& in, std::initializer_list<void*> dws) {
     const uint64_t M = out.K, N = in.K, R = a.R, parts = out.parts, lda = out.ld, ldb = in.ld;
