@@ -442,8 +442,8 @@ typedef struct {
  *   zero_rest  nonzero: rows of y that are in no group become zeros; 0: they are not written
  * No output overlaps another one or an input.
  * Rows of pre and h that are in no group are not written. Groups do not overlap: an element of a
- * row that two have is either's. A row's values do not depend on the call's other rows as long as
- * their number is the same side of the sizes at which the library changes its kernel. */
+ * row that two have is either's. A row's values do not depend on what the call's other rows hold, nor
+ * on the groups they are in; R and n_groups choose the kernel, and with it the order of a row's sums. */
 dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_groups,
                             const void* x, int64_t ldx, const int32_t* offsets,
                             const int32_t* expert_ids, const void* w_gate, const void* w_up,

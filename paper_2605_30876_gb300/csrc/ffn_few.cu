@@ -380,14 +380,20 @@ constexpr size_t few_smem(int64_t R, int tiles, int per) {
   return sizeof(float4) * 8 * tiles * (R <= 8 ? 1 : kFewCols / 8) * 32 + (size_t)8 * 8 * few_pitch(per);
 }
 
-// pieces of K that are a warp's
+// Ways a sum over K is cut, at least, and the pieces of K that are a warp's then.
+constexpr int few_ks(int K) { return K > 1024 ? 8 : K > 512 ? 4 : K > 256 ? 2 : 1; }
 constexpr int few_per(int K, int ks) { return ((K + 31) / 32 + ks - 1) / ks; }
+
+// Units of a launch, at most
+template <bool kUp>
+int64_t few_units(const FewParams& p, int tiles, int ks) {
+  const int rows = 8 / ks * tiles * (kUp ? 8 : 16);
+  return (int64_t)std::min(p.R, p.n_groups + p.R / kFewCols) * ((p.M + rows - 1) / rows);
+}
 
 template <bool kUp, bool kHalf, int kMT, int kKS>
 cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
-  constexpr int rows = 8 / kKS * kMT * (kUp ? 8 : 16);
-  const int64_t units = (int64_t)std::min(p.R, p.n_groups + p.R / kFewCols) * ((p.M + rows - 1) / rows);
-  const int ctas = (int)std::min<int64_t>(units, 152 * 2);
+  const int ctas = (int)std::min<int64_t>(few_units<kUp>(p, kMT, kKS), 152 * 2);
   const size_t smem = few_smem(p.R, kMT, few_per(p.K, kKS));
   auto* kernel = ffn_few_kernel<kUp, kHalf, kMT, kKS>;
   static std::atomic<uint32_t> done;
@@ -402,23 +408,25 @@ cudaError_t launch_form(const FewParams& p, cudaStream_t s) {
   return launch_ex(kernel, dim3(ctas), dim3(256), smem, s, true, p);
 }
 
-// Ways a sum over K is cut: a warp's part is a few pieces of 32.
-constexpr int few_ks(int K) { return K > 512 ? 8 : K > 256 ? 4 : 2; }
-
-// Units of a tile a warp where those of two would not fill two CTAs per SM (with as many groups as there
-// can be).
+// The sums over K are cut into as many parts as leave a warp eight pieces of each, and into more where there are
+// fewer than 100 units for the SMs; a warp takes two tiles where that leaves two CTAs per SM their units.
+// Us in a graph: 191 experts of 168 x 1632, a row each, cut eight ways 140, four (or two) 77, once 66; eight of
+// 2048 x 512, down's sums of 512 cut four ways 15.1, two 14.2; one of 512 x 512 and 64 rows, two ways 11.3, eight
+// 7.7; of 64 such eight in use, up cut two ways (128 units) 7.1, four 8.2.
 template <bool kUp, bool kHalf, int kKS>
 cudaError_t launch_cut(const FewParams& p, cudaStream_t s) {
-  constexpr int rows = 8 / kKS * 2 * (kUp ? 8 : 16);
-  if ((int64_t)std::min(p.R, p.n_groups) * (p.M / rows) < 304) return launch_form<kUp, kHalf, 1, kKS>(p, s);
+  if (few_units<kUp>(p, 2, kKS) < 304) return launch_form<kUp, kHalf, 1, kKS>(p, s);
   return launch_form<kUp, kHalf, 2, kKS>(p, s);
 }
 template <bool kUp, bool kHalf>
 cudaError_t launch_few(const FewParams& p, cudaStream_t s) {
-  switch (few_ks(p.K)) {
+  int ks = few_ks(p.K);
+  while (ks < 8 && 32 * ks < p.K && few_units<kUp>(p, 1, ks) < 100) ks *= 2;
+  switch (ks) {
     case 8: return launch_cut<kUp, kHalf, 8>(p, s);
     case 4: return launch_cut<kUp, kHalf, 4>(p, s);
-    default: return launch_cut<kUp, kHalf, 2>(p, s);
+    case 2: return launch_cut<kUp, kHalf, 2>(p, s);
+    default: return launch_cut<kUp, kHalf, 1>(p, s);
   }
 }
 
@@ -459,12 +467,13 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
 // Which of the two forms a call takes. The number of experts in use is not known to the host; what counts is
 // how many rows there are, how large the weights are (a group's come once for 32 rows), and that
 // shared memory leaves room in L1. Us in a graph, weights of several calls in turn, tcgen05 / this form:
-//   one expert of 2048 x 512: 8 rows 16.7 / 7.4, 128 rows 18.5 / 13.4, 256 rows 23.2 / 22.0
-//   of 4096 x 4096: 8 rows 37.8 / 27.9, 64 rows 39.0 / 64.5; of 512 x 512: 512 rows 16.0 / 16.6
-//   4 experts of 4096 x 2048: 8 rows 42 / 38, 16 rows 42 / 63 (room in L1)
-//   32 of 2048 x 512: 32 rows 43.2 / 43.3; 256 of them: 256 rows 243.6 / 242.7
-//   8 of 2048 x 512: 8 rows 25.5 / 14.3, 128 rows 25.4 / 16.7, 256 rows 25.4 / 18.9 if each has 32, but
-//   30.7 if they have 13 to 61 (two chunks for some, one for others)
+//   one expert of 2048 x 512: 8 rows 18.0 / 7.5, 128 rows 21.6 / 15.4; of 4096 x 4096: 8 rows 38.7 / 28.3,
+//   64 rows 39.0 / 64.5; of 512 x 512: 512 rows 16.9 / 13.5
+//   4 experts of 4096 x 2048: 8 rows 44 / 39, 16 rows 42 / 63 (room in L1)
+//   8 of 2048 x 512: 8 rows 23.9 / 14.2, 64 rows 23.9 / 15.3, 256 rows 25.4 / 18.9 if each has 32, but 30.7 if
+//   they have 13 to 61 (two chunks for some, one for others)
+//   128 of 1024 x 512: 128 rows 70.3 / 71.7; 256 of 2048 x 512: 128 rows 128.9 / 131.6; 191 of 168 x 1632:
+//   191 rows 84.5 / 65.9; 75 of 72 x 2480: 75 rows 48.3 / 24.1
 bool expert_ffn_few_ok(const FfnArgs& a) {
   auto fits = [&](int K) { return few_smem(a.R, 2, few_per(K, few_ks(K))) <= kFewSmem; };
   return (a.R <= 8 || (a.R <= 512 && a.R * a.d * a.I <= (int64_t)1 << 27)) && fits(a.d) && fits(a.I);
