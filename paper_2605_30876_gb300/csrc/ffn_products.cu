@@ -441,8 +441,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     // ================= units: counted per group, then decoded ahead of their use
     const int per_group = p.per_group;   // kGradW
     int units = p.n_groups * per_group;
-    // (n_max is kNMax, or no less than the call's rows)
+    // (several groups: n_max is kNMax, or no less than the call's rows. A division by a variable for each
+    // of them would be half a microsecond)
     auto tiles_of = [&](int cnt) -> int { return p.n_max == kNMax ? (cnt + kNMax - 1) / kNMax : cnt > 0 ? 1 : 0; };
+    int one = 0;                     // tiles of rows of the only group
     if (kMode != kGradW) {
       // a lane counts 16 groups in a row (their offsets are all asked for at once)
       constexpr int kOwn = kMaxGroups / 32;
@@ -457,7 +459,12 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           if (group_expert(p, g) < 0) cnt = 0;
           s_rows[g] = make_int2((int)row0, cnt);
         }
-        own[j] = tiles_of(cnt) * p.m_tiles;
+        if (p.n_groups > 1) {
+          own[j] = tiles_of(cnt) * p.m_tiles;
+        } else {
+          if (j == 0) one = (cnt + p.n_max - 1) / p.n_max;
+          own[j] = j == 0 ? one * p.m_tiles : 0;
+        }
         sum += own[j];
       }
       int before = sum;
@@ -498,7 +505,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             }
             const int row0 = s_rows[lo].x, cnt = s_rows[lo].y, local = u - s_first[lo];
             // the tiles of a group next to one another share its weights; they are of one size
-            const int nt = tiles_of(cnt);
+            const int nt = p.n_groups > 1 ? tiles_of(cnt) : one;
             const int m = local / nt, n = local - m * nt;
             const int tile = round_up((cnt + nt - 1) / nt, 32);
             v = make_int4(row0 + n * tile, min(tile, cnt - n * tile),
@@ -975,6 +982,21 @@ cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const
   p.ldo = ldo;
   p.pre = kMode == kUp || kMode == kGradH ? a.pre : nullptr;
   p.n_max = (int)std::min<int64_t>(kNMax, (a.R + 31) / 32 * 32);
+  // One group: the columns of a unit for which the pairs' turns take the least, when an MMA of up to
+  // 160 columns takes as long as one of 160. (A dense block of 2031 rows, 2048 x 2744: gate and up in
+  // 22 x 8 units of 256 are three turns of 76 pairs, and so are 22 x 10 of 224. Its backward pass takes 120 us
+  // so, 127 with units of 256.)
+  if (a.n_groups == 1 && a.R > kNMax) {
+    const int pairs = device_sm_count() / kCluster;
+    int64_t best = INT64_MAX;
+    for (int n = kNMax; n >= 160; n -= 32) {
+      const int64_t turns = ((a.R + n - 1) / n * p.m_tiles + pairs - 1) / pairs, cost = turns * (n + 32);
+      if (cost < best) {
+        best = cost;
+        p.n_max = n;
+      }
+    }
+  }
   // (only the maps that are used: each costs the host time)
   const uint64_t M = p.M, K = p.K, E = a.n_experts, R = a.R, parts = p.parts, ld = b.ld;
   const bool whole = p.K >= 128, cut = p.K % 128 != 0;
