@@ -23,6 +23,9 @@
 // the other fills; the one behind them decodes units ahead. The last warp: in kGradW it clears what a stage
 // holds behind an expert's last row (the rows there are another expert's, and 0 * inf would not be 0);
 // in kDown and kGradX it writes the zeros of rows in no group, where they are wanted.
+// Where there are fewer units than half of the pairs, up to four pairs (a cluster) share a unit's sum (split):
+// each takes a part of the reduction and, at the end, a part of the columns, for which it reads the other
+// pairs' sums from their shared memory and adds them in the order of the pairs.
 // Sums are fp32 throughout. g, u, dg, du and h are rounded to the rows' type between products: they
 // are the next product's operands, and the tensor cores take 16 bits (two operands for each, high and low
 // part, would be twice the work). The weights' gradients of 59000 rows in bf16 are off by 0.0031 of
@@ -37,6 +40,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <climits>
 #include <mutex>
 
 #include "dmoe_internal.cuh"
@@ -92,6 +96,7 @@ struct Params {
   int hold;
   int zero_rest;            // kDown, kGradX
   int after_x;              // kGradW: the launch before is kGradX's
+  int split;                // pairs of a cluster, which share a unit (then the only one of theirs)
 };
 
 // A commit costs the issuing thread about as much as two MMAs, so slots of the ring are given back
@@ -189,7 +194,7 @@ struct Unit {
   int part, m, n;     // kGradW: gate, up or down; column tile
 };
 
-template <int kMode, bool kHalf>
+template <int kMode, bool kHalf, bool kSplit>
 __global__ void __launch_bounds__(threads<kMode>(), 1)
 ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   constexpr int kSub = sub_steps<kMode>(), kPer = per_commit<kMode>();
@@ -218,8 +223,15 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   int2* s_rows = reinterpret_cast<int2*>(s_first + kMaxGroups + 2);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)ptx::cluster_ctarank();
-  const int cl = (int)blockIdx.x / kCluster, ncl = (int)gridDim.x / kCluster;
+  const int pair = (int)ptx::cluster_ctarank() >> 1, rank = (int)ptx::cluster_ctarank() & 1, base = 2 * pair;
+  const int S = kSplit ? p.split : 1;
+  const int cl = S == 1 ? (int)blockIdx.x >> 1 : (int)blockIdx.x / (2 * S);
+  const int ncl = S == 1 ? (int)gridDim.x >> 1 : (int)gridDim.x / (2 * S);
+  // stages of a sum (not kGradW): all parts', or those of this pair
+  const int part_stages = (p.K + 127) / 128, all_stages = p.parts * part_stages;
+  const int stage0 = S == 1 ? 0 : all_stages * pair / S;
+  const int row_stages = S == 1 ? all_stages : all_stages * (pair + 1) / S - stage0;
+  int joined = 0;                        // the cluster's barrier within a shared sum was passed
 
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
@@ -307,7 +319,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   // stages of a unit: 64 rows (kGradW), or 128 of K of each part
   auto stages_of = [&](const Unit& un) -> int {
     if (kMode == kGradW) return (un.rows + 63) / 64;
-    return p.parts * ((p.K + 127) / 128);
+    return row_stages;
   };
   // the lowest box of rows that holds a CTA's half of the columns
   auto level_of = [&](int half, int* rows) -> int {
@@ -323,10 +335,11 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     // ================= TMA producer: this CTA's rows of A and its half of B's
     if (lane == 0) {
       const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_normal();
-      const uint32_t full0 = ptx::peer_smem(full, 0);
+      const uint32_t full0 = ptx::peer_smem(full, base);
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
+      const int part0 = stage0 >= part_stages ? 1 : 0, first_k = (stage0 - part0 * part_stages) * 128;
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, false);
         if (un.e < 0) break;
@@ -364,14 +377,14 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           const uint32_t subs = k + 64 < p.K ? 2 : 1;
           return subs * (uint32_t)rows * 128u + (kAmn ? 2u : subs) * kTileABytes;
         };
-        int part = 0, k0 = 0;
+        int part = part0, k0 = first_k;
         auto next = [&](int& part_, int& k) {
           k += 128;
           if (k >= p.K) { k = 0; ++part_; }
         };
         int ahead = 0;                 // stages whose weights were asked for before the wait
         if (early<kMode>() && i == 0) {
-          int part_ = 0, k = 0;
+          int part_ = part0, k = first_k;
           for (; ahead < stages && ahead < p.stages; ++ahead, next(part_, k)) {
             if (rank == 0) ptx::mbar_arrive_expect_tx(&full[ahead], kCluster * stage_tx(k));
             load_a(smem + (uint32_t)ahead * stage_bytes, full0 + 8u * (uint32_t)ahead, part_, k);
@@ -396,7 +409,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             const int b_boxes = (half + 63) / 64;
             const uint32_t bytes = kTileABytes + (uint32_t)b_boxes * 8192u;
             const bool ends = (un.rows & 15) != 0 && c == stages - 1;
-            const uint32_t to = ends ? ptx::peer_smem(&tail[stage], rank) : bar;
+            const uint32_t to = ends ? ptx::peer_smem(&tail[stage], base + rank) : bar;
             if (ends) ptx::mbar_arrive_expect_tx(&tail[stage], bytes);
             if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], ends ? 0 : kCluster * bytes);
             if (!ends) ptx::mbar_arrive_pair(bar);
@@ -495,7 +508,13 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             const bool down = local >= p.up_units;
             const int in_job = down ? local - p.up_units : local, nt = down ? p.n_tiles_down : p.n_tiles;
             const int mt = down ? p.m_tiles_down : p.m_tiles, n = in_job % nt, mp = in_job / nt;
-            v = make_int4((int)row_ahead, cnt_ahead, g, (down ? 2 : mp / mt) << 16 | (mp % mt) << 8 | n);
+            int skip = 0, cnt = cnt_ahead;
+            if (S > 1) {             // this pair's rows
+              const int per = round_up((cnt + S - 1) / S, 64);
+              skip = min(pair * per, cnt);
+              cnt = min(per, cnt - skip);
+            }
+            v = make_int4((int)row_ahead + skip, cnt, g, (down ? 2 : mp / mt) << 16 | (mp % mt) << 8 | n);
             if (u + ncl < units) group_rows(p, (u + ncl) / per_group, &row_ahead, &cnt_ahead);
           } else {
             int lo = 0, hi = p.n_groups - 1;
@@ -541,6 +560,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         ok = wait(&acc_empty[acc], acc_phase ^ 1u, i);
         ptx::tc_fence_after();
         int left = K;                           // of the part's sum
+        if (kMode != kGradW) left -= (stage0 >= part_stages ? stage0 - part_stages : stage0) * 128;
         for (int c = 0; ok && c < stages; ++c) {
           ok = in || wait(&full[stage], phase, i);
           if (!ok) break;
@@ -572,15 +592,15 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           }
           left -= 64 * kSub;
           if (left <= 0) left = K;
-          if (last) ptx::mma_commit_pair(done);
+          if (last) ptx::mma_commit_pair(done, base);
         }
         if (!ok) break;
-        ptx::mma_commit_pair(&acc_full[acc]);
+        ptx::mma_commit_pair(&acc_full[acc], base);
         acc ^= 1;
         if (acc == 0) acc_phase ^= 1u;
       }
       // no MMA is running when tensor memory is released
-      ptx::mma_commit_pair(drain);
+      ptx::mma_commit_pair(drain, base);
       const uint64_t t0 = ptx::globaltimer_ns();
       while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer_ns() - t0 < kWaitNs) {
       }
@@ -593,7 +613,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       // (Fences that also order global memory cost a microsecond a group: the gradient of 256 experts'
       // 2048 x 512 from 230 rows each took 190 us with them, 141 without, as from 240 rows, which need
       // no clearing.)
-      const uint32_t full0 = ptx::peer_smem(full, 0);
+      const uint32_t full0 = ptx::peer_smem(full, base);
       int stage = 0;
       uint32_t phases = 0;      // of tail, a bit each
       bool ok = true;
@@ -645,7 +665,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     // warps take alternate slices of the columns
     const int q = warp & 3, cg = (warp - 2) >> 2, odd = lane & 1;
     const uint32_t lane_off = (uint32_t)(q * 32) << 16;
-    const uint32_t acc_empty0 = ptx::peer_smem(acc_empty, 0);
+    const uint32_t acc_empty0 = ptx::peer_smem(acc_empty, base);
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int i = 0;; ++i) {
@@ -666,12 +686,71 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           uw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from + p.I)) : 0u;
         }
       };
-      if (kMode == kGradH && un.e >= 0) ask_pre(16 * cg);
+      if (kMode == kGradH && un.e >= 0 && S == 1) ask_pre(16 * cg);
       // (a warp whose wait failed leaves with the others)
       if (!epilogue_all<kEpiWarps * 32>(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
       ptx::tc_fence_after();
       const uint32_t tbase = tmem_base + lane_off + (uint32_t)acc * kNMax;
-      const int nvalid = un.rows;
+      // this pair's columns: all, or a part of them
+      int lo = 0, hi = kMode == kGradW ? columns(un) : un.rows, slice = 0;
+      if (S > 1) {
+        // The other pairs' columns, as [4 columns][row of D][4], in the place of the ring (its MMAs are done).
+        const int n = columns(un);
+        slice = round_up((n + S - 1) / S, kMode == kGradW ? 64 : 16);
+        for (int c0 = 16 * cg; c0 < n; c0 += kStep) {
+          if (c0 >= pair * slice && c0 < (pair + 1) * slice) continue;
+          float v[16];
+          if (sums) {
+            ptx::tmem_ld16(tbase + c0, v);
+            ptx::tmem_ld_wait();
+          }
+          float4* to = reinterpret_cast<float4*>(smem) + c0 / 4 * 128 + q * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            to[j * 128] = sums ? make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3])
+                               : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+        joined = 1;
+        lo = min(pair * slice, hi);
+        hi = min(lo + slice, hi);
+        if (kMode == kGradH) ask_pre(lo + 16 * cg);
+      }
+      const int nvalid = hi;
+      // 16 columns of the sum
+      auto sum16 = [&](int c0, float (&v)[16]) {
+        if (S == 1 || sums) {
+          ptx::tmem_ld16(tbase + c0, v);
+          ptx::tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+        if (S > 1) {
+          const float4* mine = reinterpret_cast<const float4*>(smem) + c0 / 4 * 128 + q * 32 + lane;
+          float t[16];
+          for (int s = 0; s < S; ++s) {
+            float4 f[4];
+            const uint32_t from = ptx::peer_smem(mine, 2 * s + rank);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              f[j] = s == pair ? make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3])
+                               : ptx::ld_cluster_f32x4(from + j * 2048);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              t[4 * j] = s == 0 ? f[j].x : t[4 * j] + f[j].x;
+              t[4 * j + 1] = s == 0 ? f[j].y : t[4 * j + 1] + f[j].y;
+              t[4 * j + 2] = s == 0 ? f[j].z : t[4 * j + 2] + f[j].z;
+              t[4 * j + 3] = s == 0 ? f[j].w : t[4 * j + 3] + f[j].w;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = t[j];
+        }
+      };
       if constexpr (kMode == kUp) {
         // TMEM lanes 0-63: g of 64 i, lanes 64-127: u of the same. Of 16 columns the warps of g
         // keep the first eight and give the others to the warps of u, through shared memory.
@@ -681,12 +760,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const int bar_id = 2 + cg * 2 + (q & 1);
         uint16_t* h = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.I + ie;
         uint16_t* pre = static_cast<uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
-        for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
+        for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
           float v[16];
-          ptx::tmem_ld16(tbase + c0, v);
-          ptx::tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+          sum16(c0, v);
           // [from gate / from up][two float4][lane]
           float4* give = box + (is_gate ? 0 : 64) + lane;
           const float4* take = box + (is_gate ? 64 : 0) + lane;
@@ -727,7 +803,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       } else if constexpr (kMode == kGradH) {
         const int ie = he;
         uint16_t* dpre = static_cast<uint16_t*>(p.out) + (int64_t)un.row * 2 * p.I + ie;
-        for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
+        for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
           uint32_t g_now[8], u_now[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -736,10 +812,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           }
           if (c0 + kStep < nvalid) ask_pre(c0 + kStep);
           float v[16];
-          ptx::tmem_ld16(tbase + c0, v);
-          ptx::tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+          sum16(c0, v);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int at = 8 * (j >> 2) + (j & 3);
@@ -767,12 +840,19 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         // bulk store each. What lies outside of the matrix is cut by its map.
         const int row = un.m * 256 + rank * 128 + q * 32;
         uint8_t* mine = s_epi + (warp - 2) * 4096;
-        const int n = columns(un);
         const CUtensorMap* out = &tm.out[un.part];
         const int M = rows_m(un), N = cols_n(un);
-        for (int c0 = 64 * cg; c0 < n; c0 += 128) {
+        for (int c0 = lo + 64 * cg; c0 < nvalid; c0 += 128) {
           float v[2][32];
-          if (sums) {
+          if (S > 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float t[16];
+              sum16(c0 + 16 * j, t);
+#pragma unroll
+              for (int i16 = 0; i16 < 16; ++i16) v[j >> 1][16 * (j & 1) + i16] = t[i16];
+            }
+          } else if (sums) {
             ptx::tmem_ld32(tbase + c0, v[0]);
             ptx::tmem_ld32(tbase + c0 + 32, v[1]);
             ptx::tmem_ld_wait();
@@ -800,12 +880,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         const int c = un.m * 256 + rank * 128 + q * 32 + lane, ce = c & ~1;
         uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.ldo + ce;
         if (un.m * 256 + rank * 128 + q * 32 < p.M) {   // (the same for the warp)
-          for (int c0 = 16 * cg; c0 < nvalid; c0 += kStep) {
+          for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
             float v[16];
-            ptx::tmem_ld16(tbase + c0, v);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+            sum16(c0, v);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               float a[8];
@@ -833,6 +910,12 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     if (kMode == kGradW && lane == 0) ptx::bulk_commit_wait_all();
   }
 
+  // (the barrier of a shared sum, for the warps that have no part in it, and where a wait failed)
+  __syncwarp();
+  if (S > 1 && joined == 0) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
@@ -916,14 +999,14 @@ cudaError_t smem_limit(int* limit) {
   return e;
 }
 
-template <int kMode, bool kHalf>
+template <int kMode, bool kHalf, bool kSplit>
 cudaError_t raise_limit(int limit) {
   static std::atomic<uint32_t> done;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   const uint32_t bit = dev < 32 ? 1u << dev : 0u;
   if (e != cudaSuccess || (done.load(std::memory_order_relaxed) & bit) != 0u) return e;
-  e = cudaFuncSetAttribute(ffn_products_kernel<kMode, kHalf>,
+  e = cudaFuncSetAttribute(ffn_products_kernel<kMode, kHalf, kSplit>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, limit);
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
   return e;
@@ -938,6 +1021,7 @@ Params base_params(const FfnArgs& a) {
   p.R = a.R;
   p.I = a.I;
   p.parts = 1;
+  p.split = 1;
   p.hold = a.hold;
   p.zero_rest = a.zero_rest ? 1 : 0;
   return p;
@@ -951,20 +1035,35 @@ constexpr size_t fixed_smem() {
 }
 
 // The rest of the launch: stages, grid. `units`: at most so many.
-template <int kMode, bool kHalf>
-cudaError_t launch(Maps& m, Params& p, int64_t units, cudaStream_t s) {
+template <int kMode, bool kHalf, bool kSplit>
+cudaError_t launch_form(Maps& m, Params& p, int64_t units, cudaStream_t s) {
   int limit = 0;
   cudaError_t e = smem_limit(&limit);
-  if (e == cudaSuccess) e = raise_limit<kMode, kHalf>(limit);
+  if (e == cudaSuccess) e = raise_limit<kMode, kHalf, kSplit>(limit);
   if (e != cudaSuccess) return e;
   constexpr size_t fixed = fixed_smem<kMode>();
   const size_t stage = (size_t)sub_steps<kMode>() * (kTileABytes + (size_t)p.level_rows[0] * 128);
   p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)limit - fixed) / stage);
   p.stages -= p.stages % per_commit<kMode>();
   if (p.stages < 2) return cudaErrorInvalidConfiguration;
-  const int pairs = (int)std::min<int64_t>(device_sm_count() / kCluster, std::max<int64_t>(units, 1));
-  return launch_cluster(ffn_products_kernel<kMode, kHalf>, dim3(pairs * kCluster), dim3(threads<kMode>()),
-                        fixed + p.stages * stage, s, kCluster, true, m, p);
+  const int cluster = kCluster * p.split;      // (a cluster has one unit at most where it is more than a pair)
+  const int most = p.split > 1 ? INT_MAX / cluster : device_sm_count() / kCluster;
+  const int clusters = (int)std::min<int64_t>(most, std::max<int64_t>(units, 1));
+  return launch_cluster(ffn_products_kernel<kMode, kHalf, kSplit>, dim3(clusters * cluster), dim3(threads<kMode>()),
+                        fixed + p.stages * stage, s, cluster, true, m, p);
+}
+template <int kMode, bool kHalf>
+cudaError_t launch(Maps& m, Params& p, int64_t units, cudaStream_t s) {
+  return p.split > 1 ? launch_form<kMode, kHalf, true>(m, p, units, s)
+                     : launch_form<kMode, kHalf, false>(m, p, units, s);
+}
+
+// Pairs that share a unit's sum of `stages` x 128: as many as there are for all units at once, with 512 of the sum
+// or more for each. (Larger clusters do not fill the machine: 36 of four CTAs are resident at most, 23 of six,
+// 15 of eight.) Us in a graph, a pair a unit / so: 64 rows of 4096 x 4096 forward 41 / 32, backward 85 / 60; 300 of
+// 8192 x 1024 52 / 33, 73 / 52; 50000 of 512 x 1024 backward 449 / 330; 1024 of 512 x 512 backward 25.9 / 24.6.
+int pairs_of_unit(int64_t units, int stages) {
+  return units <= 15 && stages >= 16 ? 4 : units <= 23 && stages >= 12 ? 3 : units <= 36 && stages >= 8 ? 2 : 1;
 }
 
 // A product of weights with the groups' rows (all but kGradW).
@@ -1027,7 +1126,9 @@ cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const
     h = std::max(16, (h / 2 + 15) / 16 * 16);
   }
   if (!ok) return cudaErrorInvalidValue;
-  const int64_t units = (a.R / p.n_max + std::min<int64_t>(a.n_groups, a.R)) * p.m_tiles;
+  const int64_t units = (a.n_groups == 1 ? (a.R + p.n_max - 1) / p.n_max
+                                         : a.R / p.n_max + std::min<int64_t>(a.n_groups, a.R)) * p.m_tiles;
+  p.split = pairs_of_unit(units, p.parts * ((p.K + 127) / 128));
   return launch<kMode, kHalf>(m, p, units, s);
 }
 
@@ -1069,7 +1170,9 @@ cudaError_t weights_products(const FfnArgs& a, const Rows& dpre, const Rows& x, 
     p.per_group += p.m_tiles_down * p.n_tiles_down;
   }
   if (!ok) return cudaErrorInvalidValue;
-  return launch<kGradW, kHalf>(m, p, (int64_t)a.n_groups * p.per_group, s);
+  const int64_t units = (int64_t)a.n_groups * p.per_group;
+  p.split = pairs_of_unit(units, (int)(a.R / a.n_groups / 128));
+  return launch<kGradW, kHalf>(m, p, units, s);
 }
 
 template <bool kHalf>

@@ -257,6 +257,14 @@ __device__ __forceinline__ void mbar_arrive_cluster_smem(uint32_t bar_cluster) {
 __device__ __forceinline__ void fence_acquire_cluster_smem() {
   asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
 }
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr_cluster) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr_cluster)
+               : "memory");
+  return v;
+}
 __device__ __forceinline__ void st_cluster_f32(uint32_t addr_cluster, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr_cluster), "f"(v) : "memory");
 }
@@ -327,11 +335,11 @@ __device__ __forceinline__ void mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
       : "memory");
 }
 // Arrive on `bar` of both CTAs once all pair MMAs issued by this thread have completed.
-__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar, uint32_t first_rank = 0) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
       "[%0], %1;" ::"r"(smem_addr(bar)),
-      "h"((unsigned short)3)
+      "h"((unsigned short)(3u << first_rank))
       : "memory");
 }
 // Allocation for pair MMAs: one warp of each CTA.

@@ -39,6 +39,15 @@ SHAPES = [
     (3, 1024, 1024, [100, 4, 24], 0),
     (3, 1024, 1024, [100, 4, 25], 0),
     (40, 136, 1040, [3, 0, 1, 5] * 10, 0),
+    # few units with long sums (several pairs share one): over the width, and over the rows, where some
+    # have none
+    (1, 1096, 1544, [100], 3),
+    (1, 4096, 64, [300], 0),
+    (1, 72, 4104, [290], 1),
+    (1, 264, 136, [2500], 5),
+    (3, 136, 72, [4000, 0, 50], 0),
+    (2, 136, 520, [3001, 3], 7),
+    (1, 8, 8, [3000], 0),
 ]
 DTYPES = [torch.bfloat16, torch.float16]
 
