@@ -5,7 +5,7 @@
 // order of k gives the same sum as long as A and B agree, so a lane takes eight neighbours (16 bytes)
 // of a 32-long piece of K for two MMAs. (tcgen05 has nothing to win here: the weights'
 // bytes are the bound, and its launches, with tensor memory and barriers to set up and 64 SMs at work,
-// take 25.5 us where these take 14.3, for one token's eight experts of 2048 x 512; 50 MB at the copy rate are
+// take 23.9 us where these take 14.2, for one token's eight experts of 2048 x 512; 50 MB at the copy rate are
 // 7.4.)
 // The eight warps of a CTA share the sum over K (kKS ways) or the rows (8 / kKS ways); the parts meet in
 // shared memory and are added in the order of the warps. The second launch has its first weights on
@@ -467,11 +467,11 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
 // Which of the two forms a call takes. The number of experts in use is not known to the host; what counts is
 // how many rows there are, how large the weights are (a group's come once for 32 rows), and that
 // shared memory leaves room in L1. Us in a graph, weights of several calls in turn, tcgen05 / this form:
-//   one expert of 2048 x 512: 8 rows 18.0 / 7.5, 128 rows 21.6 / 15.4; of 4096 x 4096: 8 rows 38.7 / 28.3,
-//   64 rows 39.0 / 64.5; of 512 x 512: 512 rows 16.9 / 13.5
-//   4 experts of 4096 x 2048: 8 rows 44 / 39, 16 rows 42 / 63 (room in L1)
-//   8 of 2048 x 512: 8 rows 23.9 / 14.2, 64 rows 23.9 / 15.3, 256 rows 25.4 / 18.9 if each has 32, but 30.7 if
-//   they have 13 to 61 (two chunks for some, one for others)
+//   one expert of 2048 x 512: 8 rows 14.8 / 7.4, 128 rows 17.5 / 15.3, 256 rows 21.4 / 20.6; of 4096 x 4096:
+//   8 rows 32.8 / 28.6; of 2048 x 2048: 32 rows 22.0 / 16.4; of 512 x 512: 512 rows 14.3 / 13.5
+//   4 experts of 4096 x 2048: 8 rows 43.8 / 39.4, 16 rows 42 / 63 (room in L1)
+//   8 of 2048 x 512: 8 rows 23.9 / 14.2, 64 rows 23.7 / 15.4, 256 rows 23.5 / 20.0 if each has 32, but 25.3 / 30.7
+//   if they have 13 to 61 (two chunks for some, one for others)
 //   128 of 1024 x 512: 128 rows 70.3 / 71.7; 256 of 2048 x 512: 128 rows 128.9 / 131.6; 191 of 168 x 1632:
 //   191 rows 84.5 / 65.9; 75 of 72 x 2480: 75 rows 48.3 / 24.1
 bool expert_ffn_few_ok(const FfnArgs& a) {
