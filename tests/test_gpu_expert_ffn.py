@@ -317,8 +317,10 @@ def test_captured_and_replayed():
     assert all(torch.equal(a, b) for a, b in zip((pre[:110], h[:110], y, dpre[:110], dx, *dw), want))
 
 
-def test_waits_that_run_out_are_recorded():
-    c = case(torch.bfloat16, 2, 264, 136, [433, 270], 0)     # (the form for few rows has no waits)
+# (the form for few rows has no waits; in the second shape several pairs of CTAs share a sum)
+@pytest.mark.parametrize("shape", [(2, 264, 136, [433, 270], 0), (1, 2048, 264, [400], 0)], ids=str)
+def test_waits_that_run_out_are_recorded(shape):
+    c = case(torch.bfloat16, *shape)
     pre, h, y = run_forward(c)
     torch.cuda.synchronize()
     dm.dmoe_expert_set_debug_hold(1)
