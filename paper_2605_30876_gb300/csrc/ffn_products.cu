@@ -116,8 +116,9 @@ template <int kMode> constexpr int epi_warps() { return kMode == kGradW ? 8 : 16
 template <int kMode> constexpr int threads() { return (4 + epi_warps<kMode>()) * 32; }
 template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
 template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
+constexpr int kPitch = 80;      // of a column's 32 rows of D in shared memory, off by a bank group
 template <int kMode> constexpr int epi_bytes() {
-  return epi_warps<kMode>() * (kMode == kGradW ? 4096 : kMode == kUp ? 1024 : 0);
+  return epi_warps<kMode>() * (kMode == kGradW ? 4096 : kMode == kUp ? 1024 : kMode == kGradH ? 0 : 16 * kPitch);
 }
 
 template <bool kHalf>
@@ -691,19 +692,25 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       if (!epilogue_all<kEpiWarps * 32>(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
       ptx::tc_fence_after();
       const uint32_t tbase = tmem_base + lane_off + (uint32_t)acc * kNMax;
+      // 16 columns: a lane's row, or (kDown, kGradX) as 8 x 8 blocks
+      auto load16 = [&](int c0, float (&v)[16]) {
+        if constexpr (kMode == kDown || kMode == kGradX) ptx::tmem_ld16_blocks(tbase + c0, v);
+        else ptx::tmem_ld16(tbase + c0, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
+      };
       // this pair's columns: all, or a part of them
       int lo = 0, hi = kMode == kGradW ? columns(un) : un.rows, slice = 0;
       if (S > 1) {
-        // The other pairs' columns, as [4 columns][row of D][4], in the place of the ring (its MMAs are done).
+        // The other pairs' columns, as [16 columns][4 of a lane's values][lane], in the place of the ring (its
+        // MMAs are done).
         const int n = columns(un);
         slice = round_up((n + S - 1) / S, kMode == kGradW ? 64 : 16);
         for (int c0 = 16 * cg; c0 < n; c0 += kStep) {
           if (c0 >= pair * slice && c0 < (pair + 1) * slice) continue;
           float v[16];
-          if (sums) {
-            ptx::tmem_ld16(tbase + c0, v);
-            ptx::tmem_ld_wait();
-          }
+          if (sums) load16(c0, v);
           float4* to = reinterpret_cast<float4*>(smem) + c0 / 4 * 128 + q * 32 + lane;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -721,14 +728,11 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       // 16 columns of the sum
       auto sum16 = [&](int c0, float (&v)[16]) {
         if (S == 1 || sums) {
-          ptx::tmem_ld16(tbase + c0, v);
-          ptx::tmem_ld_wait();
+          load16(c0, v);
         } else {
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = 0.f;
         }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) asm volatile("" : "+f"(v[j]));
         if (S > 1) {
           const float4* mine = reinterpret_cast<const float4*>(smem) + c0 / 4 * 128 + q * 32 + lane;
           float t[16];
@@ -877,24 +881,28 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             ptx::tma_store_3d(out, mine, un.n * kNMax + c0, row, un.e);
         }
       } else {
-        const int c = un.m * 256 + rank * 128 + q * 32 + lane, ce = c & ~1;
-        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.ldo + ce;
+        // Transposed by stmatrix: 16 columns' 64 bytes each, which four lanes store.
+        const int c = un.m * 256 + rank * 128 + q * 32 + 8 * (lane & 3);
+        uint8_t* mine = s_epi + (warp - 2) * 16 * kPitch;
+        const uint32_t put = ptx::smem_addr(mine) + (8 * (lane >> 4) + (lane & 7)) * kPitch + (lane & 8) * 2;
+        const uint4* take = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kPitch + (lane & 3) * 16);
+        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)(un.row + (lane >> 2)) * p.ldo + c;
         if (un.m * 256 + rank * 128 + q * 32 < p.M) {   // (the same for the warp)
           for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
             float v[16];
             sum16(c0, v);
+            __syncwarp();                               // (the words before have been read)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              ptx::stmatrix4_trans(put + 32 * h, pack2<kHalf>(v[8 * h], v[8 * h + 1]),
+                                   pack2<kHalf>(v[8 * h + 2], v[8 * h + 3]), pack2<kHalf>(v[8 * h + 4], v[8 * h + 5]),
+                                   pack2<kHalf>(v[8 * h + 6], v[8 * h + 7]));
+            __syncwarp();
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-              float a[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) a[j] = v[8 * s + j];
-              uint32_t w[4];
-              pair_up<kHalf>(a, w);
-              const int t0 = c0 + 8 * s + 4 * odd;
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (t0 + j < nvalid && ce < p.M)
-                  *reinterpret_cast<uint32_t*>(out + (int64_t)(t0 + j) * p.ldo) = w[j];
+              const uint4 w = take[s * 8 * kPitch / 16];
+              if (c0 + 8 * s + (lane >> 2) < nvalid && c < p.M)
+                *reinterpret_cast<uint4*>(out + (c0 + 8 * s) * p.ldo) = w;
             }
           }
         }

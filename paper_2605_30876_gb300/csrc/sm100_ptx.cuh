@@ -389,6 +389,26 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
 }
 // 32 TMEM lanes x 32-bit, 32 consecutive columns per thread (one wait covers it and any
 // other loads issued before the wait).
+// 16 columns of the warp's 32 lanes as 8 x 8 blocks: v[8 h + 4 c + 2 r + i] is of TMEM lane 16 h + 8 r + lane / 4 and
+// column 8 c + 2 (lane % 4) + i.
+__device__ __forceinline__ void tmem_ld16_blocks(uint32_t taddr, float (&v)[16]) {
+  uint32_t r[16];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[8 * h]), "=r"(r[8 * h + 1]), "=r"(r[8 * h + 2]), "=r"(r[8 * h + 3]),
+                   "=r"(r[8 * h + 4]), "=r"(r[8 * h + 5]), "=r"(r[8 * h + 6]), "=r"(r[8 * h + 7])
+                 : "r"(taddr + ((uint32_t)(16 * h) << 16)));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+// four 8 x 8 blocks of 16 bits (a lane's word: row lane / 4, columns 2 (lane % 4) and the next), transposed: lanes
+// 8 i .. 8 i + 7 give the places of block i's columns, 16 bytes each
+__device__ __forceinline__ void stmatrix4_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a),
+               "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
