@@ -334,7 +334,8 @@ __device__ __forceinline__ void mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Arrive on `bar` of both CTAs once all pair MMAs issued by this thread have completed.
+// Arrive on `bar` of both CTAs (of the pair whose first CTA has that rank) once all pair MMAs issued by this
+// thread have completed.
 __device__ __forceinline__ void mma_commit_pair(uint64_t* bar, uint32_t first_rank = 0) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
@@ -387,8 +388,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-// 32 TMEM lanes x 32-bit, 32 consecutive columns per thread (one wait covers it and any
-// other loads issued before the wait).
 // 16 columns of the warp's 32 lanes as 8 x 8 blocks: v[8 h + 4 c + 2 r + i] is of TMEM lane 16 h + 8 r + lane / 4 and
 // column 8 c + 2 (lane % 4) + i.
 __device__ __forceinline__ void tmem_ld16_blocks(uint32_t taddr, float (&v)[16]) {
@@ -409,6 +408,8 @@ __device__ __forceinline__ void stmatrix4_trans(uint32_t addr, uint32_t a, uint3
                "r"(b), "r"(c), "r"(d)
                : "memory");
 }
+// 32 TMEM lanes x 32-bit, 32 consecutive columns per thread (one wait covers it and any
+// other loads issued before the wait).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
