@@ -118,7 +118,7 @@ template <int kMode> constexpr bool a_mn() { return kMode >= kGradH; }
 template <int kMode> constexpr bool b_mn() { return kMode == kGradW; }
 constexpr int kPitch = 80;      // of a column's 32 rows of D in shared memory, off by a bank group
 template <int kMode> constexpr int epi_bytes() {
-  return epi_warps<kMode>() * (kMode == kGradW ? 4096 : kMode == kUp ? 1024 : kMode == kGradH ? 0 : 16 * kPitch);
+  return epi_warps<kMode>() * (kMode == kGradW ? 4096 : kMode == kUp ? 1024 + 8 * kPitch : 16 * kPitch);
 }
 
 template <bool kHalf>
@@ -135,25 +135,6 @@ template <bool kHalf>
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
   if constexpr (kHalf) return __half22float2(*reinterpret_cast<const __half2*>(&w));
   return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
-}
-
-// A thread holds eight columns' values of one row of D, its neighbour (lane xor 1) those of the next
-// row. Afterwards it holds both rows (the lower first, as one word) of four columns: the even lane
-// columns 0-3, the odd lane 4-7.
-template <bool kHalf>
-__device__ __forceinline__ void pair_up(const float (&v)[8], uint32_t (&w)[4]) {
-  uint32_t pk[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) pk[i] = pack2<kHalf>(v[2 * i], v[2 * i + 1]);
-  const bool odd = threadIdx.x & 1;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t mine = odd ? pk[2 + i] : pk[i];
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? pk[i] : pk[2 + i], 1);
-    const uint32_t lo = odd ? other : mine, hi = odd ? mine : other;
-    w[2 * i] = __byte_perm(lo, hi, 0x5410);
-    w[2 * i + 1] = __byte_perm(lo, hi, 0x7632);
-  }
 }
 
 // AND over the epilogue's threads (named barrier 1)
@@ -664,7 +645,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   } else {
     // ================= epilogue: warps from 2 on, TMEM lanes 32 * (warp % 4) ..; groups of four
     // warps take alternate slices of the columns
-    const int q = warp & 3, cg = (warp - 2) >> 2, odd = lane & 1;
+    const int q = warp & 3, cg = (warp - 2) >> 2;
     const uint32_t lane_off = (uint32_t)(q * 32) << 16;
     const uint32_t acc_empty0 = ptx::peer_smem(acc_empty, base);
     int acc = 0;
@@ -672,19 +653,25 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
     for (int i = 0;; ++i) {
       const Unit un = unit_at(i, true);
       const bool sums = kMode != kGradW || un.rows > 0;
+      // Rows of D become words of a token's row by stmatrix: 16 columns' (tokens') 64 bytes each in shared memory,
+      // which four lanes store, 16 bytes each.
+      const int feature = un.m * 256 + rank * 128 + q * 32 + 8 * (lane & 3);     // (not kUp)
+      uint8_t* mine = s_epi + (warp - 2) * 16 * kPitch;
+      const uint32_t blocks = ptx::smem_addr(mine) + (8 * (lane >> 4) + (lane & 7)) * kPitch + (lane & 8) * 2;
+      uint4* const words = reinterpret_cast<uint4*>(mine + (lane >> 2) * kPitch + (lane & 3) * 16);
+      constexpr int kEight = 8 * kPitch / 16;       // to the words eight tokens on
       // kGradH: g and u of the next slice of columns, asked for before this one's sums are there (the
-      // backward pass of 59000 rows over 16 experts of 2048 x 1024 took 833 us when they were asked for in turn, 789 so)
-      const int he = (un.m * 256 + rank * 128 + q * 32 + lane) & ~1;
-      uint32_t gw[8], uw[8];
+      // backward pass of 59000 rows over 256 experts of 2048 x 512 took 833 us when they were asked for in turn, 789 so)
+      uint4 gw[2], uw[2];
       auto ask_pre = [&](int c0) {
-        const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + he;
+        const uint16_t* pre = static_cast<const uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + feature;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = c0 + 8 * (j >> 2) + 4 * odd + (j & 3);
-          const bool in = t < un.rows && he < p.I;
+        for (int s = 0; s < 2; ++s) {
+          const int t = c0 + 8 * s + (lane >> 2);
+          const bool in = t < un.rows && feature < p.I;
           const uint16_t* from = pre + (int64_t)t * 2 * p.I;
-          gw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from)) : 0u;
-          uw[j] = in ? __ldg(reinterpret_cast<const uint32_t*>(from + p.I)) : 0u;
+          gw[s] = in ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
+          uw[s] = in ? __ldg(reinterpret_cast<const uint4*>(from + p.I)) : make_uint4(0, 0, 0, 0);
         }
       };
       if (kMode == kGradH && un.e >= 0 && S == 1) ask_pre(16 * cg);
@@ -692,9 +679,9 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       if (!epilogue_all<kEpiWarps * 32>(un.e >= 0 && (!sums || wait(&acc_full[acc], acc_phase, i)))) break;
       ptx::tc_fence_after();
       const uint32_t tbase = tmem_base + lane_off + (uint32_t)acc * kNMax;
-      // 16 columns: a lane's row, or (kDown, kGradX) as 8 x 8 blocks
+      // 16 columns as 8 x 8 blocks (kGradW: a lane's row)
       auto load16 = [&](int c0, float (&v)[16]) {
-        if constexpr (kMode == kDown || kMode == kGradX) ptx::tmem_ld16_blocks(tbase + c0, v);
+        if constexpr (kMode != kGradW) ptx::tmem_ld16_blocks(tbase + c0, v);
         else ptx::tmem_ld16(tbase + c0, v);
         ptx::tmem_ld_wait();
 #pragma unroll
@@ -759,19 +746,25 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         // TMEM lanes 0-63: g of 64 i, lanes 64-127: u of the same. Of 16 columns the warps of g
         // keep the first eight and give the others to the warps of u, through shared memory.
         const bool is_gate = q < 2;
-        const int ii = un.m * 128 + rank * 64 + (q & 1) * 32 + lane, ie = ii & ~1;
+        const int f = un.m * 128 + rank * 64 + (q & 1) * 32 + 8 * (lane & 3);
         float4* box = reinterpret_cast<float4*>(s_epi) + (cg * 2 + (q & 1)) * 128;
         const int bar_id = 2 + cg * 2 + (q & 1);
-        uint16_t* h = static_cast<uint16_t*>(p.out) + (int64_t)un.row * p.I + ie;
-        uint16_t* pre = static_cast<uint16_t*>(p.pre) + (int64_t)un.row * 2 * p.I + ie;
+        uint8_t* own = s_epi + kEpiWarps * 1024 + (warp - 2) * 8 * kPitch;
+        const uint32_t put = ptx::smem_addr(own) + (lane & 7) * kPitch + (lane >> 3) * 16;
+        const uint4* take_words = reinterpret_cast<const uint4*>(own + (lane >> 2) * kPitch + (lane & 3) * 16);
+        const int64_t row = un.row + (is_gate ? 0 : 8) + (lane >> 2);      // (and c0)
+        uint16_t* h = static_cast<uint16_t*>(p.out) + row * p.I + f;
+        uint16_t* pre = static_cast<uint16_t*>(p.pre) + row * 2 * p.I + f;
         for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
           float v[16];
           sum16(c0, v);
           // [from gate / from up][two float4][lane]
           float4* give = box + (is_gate ? 0 : 64) + lane;
           const float4* take = box + (is_gate ? 64 : 0) + lane;
-          give[0] = is_gate ? make_float4(v[8], v[9], v[10], v[11]) : make_float4(v[0], v[1], v[2], v[3]);
-          give[32] = is_gate ? make_float4(v[12], v[13], v[14], v[15]) : make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            give[32 * j] = is_gate ? make_float4(v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7])
+                                   : make_float4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
           ptx::named_bar_sync(bar_id, 64);
           const float4 o0 = take[0], o1 = take[32];
           ptx::named_bar_sync(bar_id, 64);       // (the words have been read)
@@ -779,65 +772,76 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
           float g[8], u[8], hv[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            g[j] = is_gate ? v[j] : o[j];
-            u[j] = is_gate ? o[j] : v[8 + j];
+            const int at = 8 * (j >> 2) + (j & 3);
+            g[j] = is_gate ? v[at] : o[j];
+            u[j] = is_gate ? o[j] : v[at + 4];
             hv[j] = g[j];
           }
           silu_all(hv);
 #pragma unroll
           for (int j = 0; j < 8; ++j) hv[j] *= u[j];
-          uint32_t wh[4], wg[4], wu[4];
-          pair_up<kHalf>(hv, wh);
+          const bool in = c0 + (is_gate ? 0 : 8) + (lane >> 2) < nvalid && f < p.I;
+          auto store = [&](const float (&w)[8], uint16_t* to) {
+            __syncwarp();                        // (the words before have been read)
+            ptx::stmatrix4_trans(put, pack2<kHalf>(w[0], w[1]), pack2<kHalf>(w[2], w[3]),
+                                 pack2<kHalf>(w[4], w[5]), pack2<kHalf>(w[6], w[7]));
+            __syncwarp();
+            const uint4 words8 = *take_words;
+            if (in) *reinterpret_cast<uint4*>(to) = words8;
+          };
+          store(hv, h + (int64_t)c0 * p.I);
           if (p.pre != nullptr) {
-            pair_up<kHalf>(g, wg);
-            pair_up<kHalf>(u, wu);
+            store(g, pre + (int64_t)c0 * 2 * p.I);
+            store(u, pre + (int64_t)c0 * 2 * p.I + p.I);
           }
-          const int t0 = c0 + (is_gate ? 0 : 8) + 4 * odd;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (t0 + j < nvalid && ie < p.I) {
-              *reinterpret_cast<uint32_t*>(h + (int64_t)(t0 + j) * p.I) = wh[j];
-              if (p.pre != nullptr) {
-                uint16_t* to = pre + (int64_t)(t0 + j) * 2 * p.I;
-                *reinterpret_cast<uint32_t*>(to) = wg[j];
-                *reinterpret_cast<uint32_t*>(to + p.I) = wu[j];
-              }
-            }
         }
       } else if constexpr (kMode == kGradH) {
-        const int ie = he;
-        uint16_t* dpre = static_cast<uint16_t*>(p.out) + (int64_t)un.row * 2 * p.I + ie;
+        uint16_t* dpre = static_cast<uint16_t*>(p.out) + ((int64_t)un.row + (lane >> 2)) * 2 * p.I + feature;
         for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
-          uint32_t g_now[8], u_now[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            g_now[j] = gw[j];
-            u_now[j] = uw[j];
-          }
+          uint32_t g2[2][4], u2[2][4];           // [h][2 c + r] of the blocks
+          auto spread = [&](const uint4 (&w)[2], uint32_t (&o)[2][4]) {
+            __syncwarp();                        // (the words before have been read)
+            words[0] = w[0];
+            words[kEight] = w[1];
+            __syncwarp();
+            ptx::ldmatrix4_trans(blocks, o[0]);
+            ptx::ldmatrix4_trans(blocks + 32, o[1]);
+          };
+          spread(gw, g2);
+          spread(uw, u2);
           if (c0 + kStep < nvalid) ask_pre(c0 + kStep);
           float v[16];
           sum16(c0, v);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int at = 8 * (j >> 2) + (j & 3);
-            const float other = __shfl_xor_sync(0xffffffffu, odd ? v[at] : v[at + 4], 1);
-            const float dh[2] = {odd ? other : v[at], odd ? v[at + 4] : other};
-            const float2 g2 = unpack2<kHalf>(g_now[j]), u2 = unpack2<kHalf>(u_now[j]);
-            const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
-            float dg[2], du[2];
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              const float s = __fdividef(1.f, 1.f + __expf(-g[b]));
-              dg[b] = dh[b] * u[b] * s * (1.f + g[b] * (1.f - s));
-              du[b] = dh[b] * g[b] * s;
+            for (int j = 0; j < 4; ++j) {
+              const float2 gj = unpack2<kHalf>(g2[h][j]), uj = unpack2<kHalf>(u2[h][j]);
+              const float g[2] = {gj.x, gj.y}, u[2] = {uj.x, uj.y};
+              float dg[2], du[2];
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
+                const float dh = v[8 * h + 2 * j + b], s = __fdividef(1.f, 1.f + __expf(-g[b]));
+                dg[b] = dh * u[b] * s * (1.f + g[b] * (1.f - s));
+                du[b] = dh * g[b] * s;
+              }
+              g2[h][j] = pack2<kHalf>(dg[0], dg[1]);
+              u2[h][j] = pack2<kHalf>(du[0], du[1]);
             }
-            const int t = c0 + at + 4 * odd;
-            if (t < nvalid && ie < p.I) {
-              uint16_t* to = dpre + (int64_t)t * 2 * p.I;
-              *reinterpret_cast<uint32_t*>(to) = pack2<kHalf>(dg[0], dg[1]);
-              *reinterpret_cast<uint32_t*>(to + p.I) = pack2<kHalf>(du[0], du[1]);
+          auto store = [&](const uint32_t (&w)[2][4], uint16_t* to) {
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) ptx::stmatrix4_trans(blocks + 32 * h, w[h][0], w[h][1], w[h][2], w[h][3]);
+            __syncwarp();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const uint4 word = words[s * kEight];
+              if (c0 + 8 * s + (lane >> 2) < nvalid && feature < p.I)
+                *reinterpret_cast<uint4*>(to + (int64_t)(c0 + 8 * s) * 2 * p.I) = word;
             }
-          }
+          };
+          store(g2, dpre);
+          store(u2, dpre + p.I);
         }
       } else if constexpr (kMode == kGradW) {
         // 64 columns of this warp's 32 rows at a time: through shared memory (128-byte swizzle), one
@@ -881,12 +885,7 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             ptx::tma_store_3d(out, mine, un.n * kNMax + c0, row, un.e);
         }
       } else {
-        // Transposed by stmatrix: 16 columns' 64 bytes each, which four lanes store.
-        const int c = un.m * 256 + rank * 128 + q * 32 + 8 * (lane & 3);
-        uint8_t* mine = s_epi + (warp - 2) * 16 * kPitch;
-        const uint32_t put = ptx::smem_addr(mine) + (8 * (lane >> 4) + (lane & 7)) * kPitch + (lane & 8) * 2;
-        const uint4* take = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kPitch + (lane & 3) * 16);
-        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)(un.row + (lane >> 2)) * p.ldo + c;
+        uint16_t* out = static_cast<uint16_t*>(p.out) + (int64_t)(un.row + (lane >> 2)) * p.ldo + feature;
         if (un.m * 256 + rank * 128 + q * 32 < p.M) {   // (the same for the warp)
           for (int c0 = lo + 16 * cg; c0 < nvalid; c0 += kStep) {
             float v[16];
@@ -894,14 +893,14 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
             __syncwarp();                               // (the words before have been read)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              ptx::stmatrix4_trans(put + 32 * h, pack2<kHalf>(v[8 * h], v[8 * h + 1]),
+              ptx::stmatrix4_trans(blocks + 32 * h, pack2<kHalf>(v[8 * h], v[8 * h + 1]),
                                    pack2<kHalf>(v[8 * h + 2], v[8 * h + 3]), pack2<kHalf>(v[8 * h + 4], v[8 * h + 5]),
                                    pack2<kHalf>(v[8 * h + 6], v[8 * h + 7]));
             __syncwarp();
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-              const uint4 w = take[s * 8 * kPitch / 16];
-              if (c0 + 8 * s + (lane >> 2) < nvalid && c < p.M)
+              const uint4 w = words[s * kEight];
+              if (c0 + 8 * s + (lane >> 2) < nvalid && feature < p.M)
                 *reinterpret_cast<uint4*>(out + (c0 + 8 * s) * p.ldo) = w;
             }
           }

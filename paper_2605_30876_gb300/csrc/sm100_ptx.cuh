@@ -408,6 +408,13 @@ __device__ __forceinline__ void stmatrix4_trans(uint32_t addr, uint32_t a, uint3
                "r"(b), "r"(c), "r"(d)
                : "memory");
 }
+// the same words back from those places
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&w)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(addr)
+               : "memory");
+}
 // 32 TMEM lanes x 32-bit, 32 consecutive columns per thread (one wait covers it and any
 // other loads issued before the wait).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
