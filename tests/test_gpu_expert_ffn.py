@@ -318,7 +318,7 @@ def test_captured_and_replayed():
 
 
 # (the form for few rows has no waits; in the second shape several pairs of CTAs share a sum)
-@pytest.mark.parametrize("shape", [(2, 264, 136, [433, 270], 0), (1, 2048, 264, [400], 0)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 264, 136, [433, 270], 0), (1, 2048, 264, [600], 0)], ids=str)
 def test_waits_that_run_out_are_recorded(shape):
     c = case(torch.bfloat16, *shape)
     pre, h, y = run_forward(c)
