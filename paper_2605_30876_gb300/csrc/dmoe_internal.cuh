@@ -427,7 +427,7 @@ struct NormArgs {
   float *dw_post, *dw_pre;
   float* workspace;
 };
-constexpr int kNormCtas = 304;   // of the backward launch, at most (two per SM)
+constexpr int kNormCtas = 456;   // of the backward launch, at most (three per SM)
 size_t norm_workspace_bytes(int64_t T, int d, int gate_tokens);
 cudaError_t launch_norm_residual(const NormArgs& a, cudaStream_t s);
 cudaError_t launch_norm_residual_backward(const NormArgs& a, cudaStream_t s);

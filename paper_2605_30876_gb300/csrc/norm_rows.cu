@@ -2,7 +2,7 @@
 //   p = y * ry * w_post,  r = scale * x + gate * p,  n = r * rr * w_pre
 //   ry = 1 / sqrt(mean(y^2) + eps),  rr = 1 / sqrt(mean(r^2) + eps)
 // Both directions are bound by the bytes of their rows, each read once and written once. A row is held
-// in registers by a group of threads (a power of two, so that a thread has a few pieces of 16 bytes);
+// in registers by a group of threads, a few pieces of 16 bytes each;
 // groups go on from row to row. The gradients: norm_rows_backward.cu.
 #include "norm_rows.cuh"
 
@@ -26,7 +26,7 @@ norm_kernel(const NormArgs a, int width, int depth, int run) {
   const int group = threadIdx.x / width, v0 = threadIdx.x % width, nv = a.d / P::n, G = a.gate_tokens;
   const int64_t me = (int64_t)blockIdx.x * (blockDim.x / width) + group;
   const int begin = (int)min(me * run, a.T), end = (int)min((me + 1) * run, a.T);
-  int flip = 0;
+  GroupSum<1> group_sum(scratch, width, group);
   const uint32_t ldx = (uint32_t)a.ldx, ldy = (uint32_t)a.ldy, ldr = (uint32_t)a.ldr, ldn = (uint32_t)a.ldn;
   Ahead<T, VB, kE, 2, kBlock, kFull> ahead(smem4 + 8, depth);
   auto rows_of = [&](int t, const T* (&rows)[2]) {
@@ -76,7 +76,7 @@ norm_kernel(const NormArgs a, int width, int depth, int run) {
 #pragma unroll
       for (int e = 0; e < kH; ++e) s2 = fma2(r[e], r[e], s2);
       float s[1] = {s2.lo() + s2.hi()};
-      group_sum(s, width, group, scratch, flip);
+      group_sum(s);
       ry = rstd_of(s[0], inv_d, a.eps);
       const F2 ry2(ry);
 #pragma unroll
@@ -98,7 +98,7 @@ norm_kernel(const NormArgs a, int width, int depth, int run) {
       F2 w[kHold ? 1 : kH];
       if constexpr (!kHold) load_vector<T, VB, kE, kFull>(w, a.w_pre, v0, width, n_in, 0.f);
       float s[1] = {s2.lo() + s2.hi()};
-      group_sum(s, width, group, scratch, flip);
+      group_sum(s);
       rr = rstd_of(s[0], inv_d, a.eps);
       const F2 rr2(rr);
 #pragma unroll
@@ -126,13 +126,15 @@ cudaError_t launch_norm_residual(const NormArgs& a, cudaStream_t s) {
       const int width = group_width(a.d, VB / (int)sizeof(T), kE);
       const bool full = VB == 16 && width >= 32 && width * kE == a.d && a.y != nullptr && a.r != nullptr &&
                         a.n != nullptr;
-      int block = kBlock;
+      int per_cta = std::max(1, kBlock / width);
+      const int per_sm = ctas_per_sm(kBlock, per_cta * width);
       // few rows: a CTA for each, as far as there are SMs
-      while (block > width && block > 32 && a.T * width / block < 152) block /= 2;
+      while (per_cta > 1 && per_cta * width > 32 && a.T / per_cta < 152) per_cta = (per_cta + 1) / 2;
+      const int block = per_cta * width;
       constexpr int row = Ahead<T, VB, kE, 2, kBlock, false>::kToken;
-      const int depth = tokens_ahead(kBlock, 128, row);
+      const int depth = tokens_ahead(per_sm, 128, row);
       int ctas = 0;
-      const int run = runs(a.T, block / width, kBlock > 256 ? 152 : 304, &ctas);
+      const int run = runs(a.T, per_cta, 152 * per_sm, &ctas);
       const size_t smem = 128 + (size_t)depth * row;
       static std::atomic<uint32_t> done[2];
       auto* kernel = full ? norm_kernel<T, VB, kE, kBlock, VB == 16> : norm_kernel<T, VB, kE, kBlock, false>;

@@ -239,36 +239,51 @@ __device__ __forceinline__ T* row_at(T* base, int t, uint32_t ld) {
   return reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + (uint64_t)(uint32_t)t * (ld * (uint32_t)sizeof(T)));
 }
 
-// Sums of K values over the `width` threads of a row's group (a power of two), the same in every
-// thread. Groups of more than a warp pass `scratch` (K floats per warp of the CTA, twice) and a
-// barrier of their own; `flip` changes from call to call, so that one barrier is enough.
+// Sums of K values over the `width` threads of a row's group (a power of two up to a warp, or whole warps),
+// the same in every thread. Groups of more than a warp use `scratch` (2 x 16 K floats) and a barrier of
+// their own; its halves alternate from call to call, so that one barrier is enough. A group has a power of
+// two of places there; those behind its warps stay zeros.
 template <int K>
-__device__ __forceinline__ void group_sum(float (&v)[K], int width, int group, float* scratch, int& flip) {
-  if (width >= 32) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-    if (width == 32) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = blockDim.x >> 5, per = width >> 5;
-    float* s = scratch + flip * nw * K;
-    flip ^= 1;
-    if (lane == 0)
-#pragma unroll
-      for (int k = 0; k < K; ++k) s[warp * K + k] = v[k];
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(width) : "memory");
-    const int from = group * per + (lane & (per - 1));
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = s[from * K + k];
-    for (int o = per >> 1; o > 0; o >>= 1)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-  } else {
-    for (int o = width >> 1; o > 0; o >>= 1)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+struct GroupSum {
+  float* put;
+  const float* take;
+  int width, barrier, first, half;
+  __device__ __forceinline__ GroupSum(float* scratch, int width_, int group)
+      : width(width_), barrier(group + 1), half(0) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = width >> 5;
+    const int places = per > 8 ? 16 : per > 4 ? 8 : per > 2 ? 4 : 2;
+    first = places >> 1;
+    put = scratch + (group * places + warp - group * per) * K;
+    take = scratch + (group * places + (lane & (places - 1))) * K;
+    if (width > 32 && places != per) {
+      for (int i = threadIdx.x; i < 32 * K; i += blockDim.x) scratch[i] = 0.f;
+      __syncthreads();
+    }
   }
-}
+  __device__ __forceinline__ void operator()(float (&v)[K]) {
+    if (width >= 32) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+      if (width == 32) return;
+      if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) put[half + k] = v[k];
+      asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(width) : "memory");
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = take[half + k];
+      half ^= 16 * K;
+      for (int o = first; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    } else {
+      for (int o = width >> 1; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
+  }
+};
 
 __device__ __forceinline__ float rstd_of(float sum, float inv_d, float eps) {
   return rsqrtf(fmaf(sum, inv_d, eps));
@@ -294,8 +309,8 @@ cudaError_t with_type(int dtype, int piece, F f) {
 int esize(int dtype) { return dtype == DMOE_FP32 ? 4 : 2; }
 
 // Bytes that every row can be read and written at a time: 16, 4 or 2. The smaller, the more instructions a
-// row takes: 16384 rows in bf16, forward and backward, of 2048 (16 bytes) 45 and 74 us, of 2050 (4) 102 and
-// 203, of 2049 (2) 221 and 500.
+// row takes: 16384 rows in bf16, cold, forward and backward, of 2048 (16 bytes) 53 and 81 us, of 2050 (4) 72
+// and 177, of 2049 (2) 154 and 474.
 int piece_of_rows(const NormArgs& a) {
   const uint64_t es = esize(a.dtype);
   uint64_t bits = a.d * es;
@@ -309,11 +324,12 @@ int piece_of_rows(const NormArgs& a) {
   return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
 
-// threads of a row's group: a power of two, 8 at least, so that each holds at most kE elements
+// Threads of a row's group, so that each holds at most kE elements: 8, 16 or 32, or whole warps. (Powers of two
+// alone leave up to half of the threads idle: 6553 rows of 5120 in bf16 took 70 us forward and 218 backward
+// so, 64 and 139 with whole warps; 26214 of 1280 61 and 122, 57 and 86.)
 int group_width(int d, int n, int kE) {
-  int w = 8;
-  while ((int64_t)w * kE < (d + n - 1) / n * n) w *= 2;
-  return w;
+  const int threads = ((d + n - 1) / n * n + kE - 1) / kE;
+  return threads <= 8 ? 8 : threads <= 16 ? 16 : (threads + 31) / 32 * 32;
 }
 
 // the largest shared memory that a CTA can have, once per device and kernel
@@ -330,11 +346,13 @@ cudaError_t raise_smem(F* kernel, std::atomic<uint32_t>& done) {
   return e;
 }
 
-// Tokens that the shared memory holds rows of: two CTAs of 256 threads an SM, or one of more.
-// `fixed`: what else a CTA needs.
-int tokens_ahead(int block, size_t fixed, int row) {
+// CTAs per SM: two of 256 threads, three of 160 or fewer, or one of more
+int ctas_per_sm(int most, int block) { return most > 256 ? 1 : block <= 160 ? 3 : 2; }
+
+// Tokens that the shared memory holds rows of, with that many CTAs per SM. `fixed`: what else a CTA needs.
+int tokens_ahead(int ctas, size_t fixed, int row) {
   if (row == 0) return 2;
-  const size_t room = (block > 256 ? 227 * 1024 : 113 * 1024) - fixed;
+  const size_t room = (ctas == 1 ? 227 : ctas == 2 ? 113 : 74) * 1024 - fixed;
   return (int)std::max<size_t>(2, std::min<size_t>(4, room / row));
 }
 

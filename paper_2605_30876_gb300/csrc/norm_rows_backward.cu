@@ -39,7 +39,7 @@ norm_backward_kernel(const NormArgs a, int width, int depth, int per) {
   const float inv_d = 1.f / (float)a.d;
   float* part_w = a.workspace + (size_t)blockIdx.x * 2 * a.d;
   float* part_g = a.workspace + (size_t)gridDim.x * 2 * a.d + (size_t)me * 2 * a.d;
-  int flip = 0;
+  GroupSum<3> group_sum(scratch, width, group);
   F2 A_[kR], post_[kR], pre_[kR], w_post_[kR], w_pre_[kR], gate_[kR];
   // [sum][element][thread] behind the reductions' words
   float4* sums = smem4 + 48 + threadIdx.x;
@@ -150,7 +150,7 @@ norm_backward_kernel(const NormArgs a, int width, int depth, int per) {
     }
     if (kFull || a.dw_pre != nullptr) update(2, [&](F2 v, int i) { return fma2(dn.get(i), rh[i], v); });
     float s[3] = {s0.lo() + s0.hi(), s1.lo() + s1.hi(), s2.lo() + s2.hi()};
-    group_sum(s, width, group, scratch, flip);
+    group_sum(s);
     const float m1 = s[0] * inv_d * rr_t;
     const float m2 = a.w_post != nullptr ? fmaf(-m1, s[2], s[1]) * inv_d : 0.f;
     const F2 less1(-m1), less2(-m2);
@@ -326,16 +326,17 @@ cudaError_t launch_norm_residual_backward(const NormArgs& a, cudaStream_t s) {
     constexpr int VB = decltype(w)::value;
     auto launch = [&](auto k, auto b) {
       constexpr int kE = decltype(k)::value, kBlock = decltype(b)::value;
-      const int width = group_width(a.d, VB / (int)sizeof(T), kE), per_cta = kBlock / width;
+      const int width = group_width(a.d, VB / (int)sizeof(T), kE), per_cta = std::max(1, kBlock / width);
+      const int block = per_cta * width, per_sm = ctas_per_sm(kBlock, block);
       const bool full = VB == 16 && width >= 32 && width * kE == a.d && a.y != nullptr && a.dr != nullptr &&
                         a.dn != nullptr && a.dx != nullptr && a.dy != nullptr && a.dw_pre != nullptr;
       int ctas = 0;
-      const int run = runs(a.T, per_cta, kBlock > 256 ? kNormCtas / 2 : kNormCtas, &ctas);
+      const int run = runs(a.T, per_cta, 152 * per_sm, &ctas);
       // the reductions' words (three sums a warp, twice), the sums of wide rows, the rows ahead (and
       // in their place the groups' sums together)
       constexpr int row = Ahead<T, VB, kE, 4, kBlock, false>::kToken;
       constexpr size_t fixed = 192 * sizeof(float) + (kE > 8 ? 3 * kE * kBlock * sizeof(float) : 0);
-      const int depth = tokens_ahead(kBlock, fixed, row);
+      const int depth = tokens_ahead(per_sm, fixed, row);
       const size_t smem =
           fixed + std::max<size_t>((size_t)depth * row, per_cta > 1 ? kE * kBlock * sizeof(float) : 0);
       auto* kernel = full ? norm_backward_kernel<T, VB, kE, kBlock, VB == 16>
@@ -346,7 +347,7 @@ cudaError_t launch_norm_residual_backward(const NormArgs& a, cudaStream_t s) {
         e = raise_smem(kernel, done[full ? 1 : 0]);
       }
       if (e == cudaSuccess)
-        e = launch_ex(kernel, dim3(ctas), dim3(kBlock), smem, s, true, a, width, depth, run);
+        e = launch_ex(kernel, dim3(ctas), dim3(block), smem, s, true, a, width, depth, run);
       const bool gates = a.dgate != nullptr && a.gate_tokens > 1;
       if (e != cudaSuccess || (a.dw_post == nullptr && a.dw_pre == nullptr && !gates)) return e;
       const int64_t rows = gates ? (a.T + a.gate_tokens - 1) / a.gate_tokens : 0;

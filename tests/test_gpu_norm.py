@@ -12,7 +12,9 @@ DTYPES = [torch.bfloat16, torch.float16, torch.float32]
 # a piece, gate rows that end inside a run, hold many runs, or are a token's
 SHAPES = [(1, 1, 0), (3, 7, 1), (5, 8, 2), (33, 64, 33), (700, 100, 7), (257, 129, 64), (40, 1001, 0),
           (611, 2048, 32), (613, 2050, 700), (90, 4096, 48), (311, 8192, 5), (9, 10001, 4), (7, 16384, 7),
-          (4000, 24, 1000), (20011, 16, 3)]
+          (4000, 24, 1000), (20011, 16, 3),
+          # rows of whole warps that are no power of two, several to a CTA and one
+          (900, 1280, 7), (1201, 768, 100), (700, 2560, 33), (333, 5120, 50), (411, 2056, 4), (600, 644, 9)]
 
 
 def rows(gen, n, d, dtype, size, pad=0):
