@@ -16,6 +16,10 @@ gradients can be taken once (there is no second derivative). `pos` is int32 and 
 between forward and backward. It has to name every row once, as dmoe_sort_tokens writes it (and
 dmoe_dispatch, unless it records a fault): the kernels write the rows that it names, so that others of
 xs, and of the gradient by ys, would hold what the memory held.
+
+A forward and backward pass captured into a CUDA graph asks for its gradients with torch.autograd.grad:
+leaves that accumulate them (backward()) keep the stream on which an eager pass first used them, and
+torch does not let a capture wait for that one.
 """
 from __future__ import annotations
 
