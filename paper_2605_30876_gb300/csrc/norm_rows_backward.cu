@@ -74,7 +74,8 @@ norm_backward_kernel(const NormArgs a, int width, int depth, int per) {
   Ahead<T, VB, kE, 4, kBlock, kFull> ahead(smem4 + 48 + (kShared ? 3 * kE / 4 * kBlock : 0), depth);
   const uint32_t ldx = (uint32_t)a.ldx, ldy = (uint32_t)a.ldy, lddr = (uint32_t)a.lddr, lddn = (uint32_t)a.lddn;
   auto rows_of = [&](int t, const T* (&rows)[4]) {
-    rows[0] = row_at(static_cast<const T*>(a.x), t, ldx);
+    // (r hat, for which x is read, counts through dn alone)
+    rows[0] = kFull || a.dn != nullptr ? row_at(static_cast<const T*>(a.x), t, ldx) : nullptr;
     rows[1] = kFull || a.y != nullptr ? row_at(static_cast<const T*>(a.y), t, ldy) : nullptr;
     rows[2] = kFull || a.dr != nullptr ? row_at(static_cast<const T*>(a.dr), t, lddr) : nullptr;
     rows[3] = kFull || a.dn != nullptr ? row_at(static_cast<const T*>(a.dn), t, lddn) : nullptr;
