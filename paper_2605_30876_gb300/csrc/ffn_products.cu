@@ -1133,10 +1133,11 @@ cudaError_t rows_product(const FfnArgs& a, const void* w0, const void* w1, const
     h = std::max(16, (h / 2 + 15) / 16 * 16);
   }
   if (!ok) return cudaErrorInvalidValue;
-  const int64_t units = (a.n_groups == 1 ? (a.R + p.n_max - 1) / p.n_max
-                                         : a.R / p.n_max + std::min<int64_t>(a.n_groups, a.R)) * p.m_tiles;
-  p.split = pairs_of_unit(units, p.parts * ((p.K + 127) / 128));
-  return launch<kMode, kHalf>(m, p, units, s);
+  // as many as there can be, and if groups overlap: a cluster of several pairs takes one unit, no more
+  const int64_t most = a.n_groups * ((a.R + p.n_max - 1) / p.n_max) * p.m_tiles;
+  p.split = pairs_of_unit(most, p.parts * ((p.K + 127) / 128));
+  const int64_t units = (a.R / p.n_max + std::min<int64_t>(a.n_groups, a.R)) * p.m_tiles;
+  return launch<kMode, kHalf>(m, p, p.split > 1 ? most : units, s);
 }
 
 // Gradients of weights: sums over the groups' rows of out [R][parts][M] and in [R][N].

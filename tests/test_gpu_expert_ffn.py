@@ -198,6 +198,19 @@ def test_offsets_that_are_cut(offsets):
         assert dm.dmoe_expert_device_error()[0] == 0
 
 
+def test_groups_that_overlap_in_calls_of_few_units():
+    """More units than rows that are apart would make, where several pairs of CTAs share a unit's sum."""
+    c = case(torch.bfloat16, 3, 2048, 264, [600, 0, 0], 0)
+    c["offsets"] = torch.tensor([0, 600, 10, 600], dtype=torch.int32, device="cuda")
+    pre, h, y = run_forward(c)
+    got = run_backward(c, pre, h)
+    assert dm.dmoe_expert_device_error()[0] == 0
+    want = O.forward(c["x"][:10], [0, 10, 10, 10], *weights(c))       # (rows that one group has alone)
+    O.check("h", h[:10], want["h"])
+    O.check("y", y[:10], want["y"])
+    assert all(torch.isfinite(t).all() for t in (h, y, got["dx"], got["dw_gate"], got["dw_down"]))
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_other_experts_rows_and_weights_stay_out(bad):
     """Rows of other groups, rows of none and other experts' weights do not reach a group's results."""
