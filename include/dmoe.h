@@ -436,7 +436,10 @@ typedef struct {
  *              dmoe_dispatch's offsets: its unique_ids. A group whose id is outside
  *              [0, n_experts) is left out; an id may stand in several groups
  *   w_gate, w_up  [E, I, d];  w_down  [E, d, I]
- *   pre        [R, 2, I] out: g and u, for the backward pass; or NULL
+ *   pre        [R, 2, I] out: g and u, for the backward pass; or NULL. What is beyond the type's
+ *              finite range (65504 in fp16) is kept as its largest value, so that gradients through
+ *              silu(g) = 0 and of rows with dy = 0 are 0. Where g is cut and silu(g) is g, du is too
+ *              small by as much, and so is dg where u is cut
  *   h          [R, I] out: also the second product's input, so it is always needed
  *   y          [R, d] out, row stride ldy
  *   zero_rest  nonzero: rows of y that are in no group become zeros; 0: they are not written

@@ -65,6 +65,15 @@ __device__ __forceinline__ void store_16(void* p, int64_t at, float v) {
   else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
 }
 
+// g and u for the gradients: cut to the type's finite range, as the form for more rows does
+template <bool kHalf>
+__device__ __forceinline__ void store_16_finite(void* p, int64_t at, float v) {
+  uint16_t w;
+  if constexpr (kHalf) asm("cvt.rn.satfinite.f16.f32 %0, %1;" : "=h"(w) : "f"(v));
+  else asm("cvt.rn.satfinite.bf16.f32 %0, %1;" : "=h"(w) : "f"(v));
+  static_cast<uint16_t*>(p)[at] = w;
+}
+
 __device__ __forceinline__ int few_rows(const FewParams& p, int g, int* row0) {
   int lo = 0, hi = p.R;
   if (p.offsets != nullptr) {
@@ -221,8 +230,8 @@ ffn_few_kernel(const FewParams p) {
           if (r < p.M) {
             store_16<kHalf>(p.out, row * p.ldo + r, v[j] / (1.f + __expf(-v[j])) * v[2 + j]);
             if (p.pre != nullptr) {
-              store_16<kHalf>(p.pre, row * 2 * p.M + r, v[j]);
-              store_16<kHalf>(p.pre, row * 2 * p.M + p.M + r, v[2 + j]);
+              store_16_finite<kHalf>(p.pre, row * 2 * p.M + r, v[j]);
+              store_16_finite<kHalf>(p.pre, row * 2 * p.M + p.M + r, v[2 + j]);
             }
           }
         } else {

@@ -131,6 +131,15 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&b);
   }
 }
+// g and u for the gradients: what the type cannot hold becomes its largest value (and NaN stays NaN). A gate of
+// -70000 is an exact 0 in h, and with -inf in its place dg and du were 0 * inf in fp16, as they were for rows with dy = 0.
+template <bool kHalf>
+__device__ __forceinline__ uint32_t pack2_finite(float lo, float hi) {
+  uint32_t w;
+  if constexpr (kHalf) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
 template <bool kHalf>
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
   if constexpr (kHalf) return __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -781,18 +790,17 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) hv[j] *= u[j];
           const bool in = c0 + (is_gate ? 0 : 8) + (lane >> 2) < nvalid && f < p.I;
-          auto store = [&](const float (&w)[8], uint16_t* to) {
+          auto store = [&](const float (&w)[8], uint16_t* to, auto pack) {
             __syncwarp();                        // (the words before have been read)
-            ptx::stmatrix4_trans(put, pack2<kHalf>(w[0], w[1]), pack2<kHalf>(w[2], w[3]),
-                                 pack2<kHalf>(w[4], w[5]), pack2<kHalf>(w[6], w[7]));
+            ptx::stmatrix4_trans(put, pack(w[0], w[1]), pack(w[2], w[3]), pack(w[4], w[5]), pack(w[6], w[7]));
             __syncwarp();
             const uint4 words8 = *take_words;
             if (in) *reinterpret_cast<uint4*>(to) = words8;
           };
-          store(hv, h + (int64_t)c0 * p.I);
+          store(hv, h + (int64_t)c0 * p.I, pack2<kHalf>);
           if (p.pre != nullptr) {
-            store(g, pre + (int64_t)c0 * 2 * p.I);
-            store(u, pre + (int64_t)c0 * 2 * p.I + p.I);
+            store(g, pre + (int64_t)c0 * 2 * p.I, pack2_finite<kHalf>);
+            store(u, pre + (int64_t)c0 * 2 * p.I + p.I, pack2_finite<kHalf>);
           }
         }
       } else if constexpr (kMode == kGradH) {
