@@ -104,10 +104,12 @@ struct Params {
 // stage costs loads: kGradW's stages are one step, given back two at a time.
 template <int kMode> constexpr int sub_steps() { return kMode == kGradW ? 1 : 2; }
 template <int kMode> constexpr int per_commit() { return kMode == kGradW ? 2 : 1; }
-// The launch before is one of the same call: it was released once what that call was given was there,
-// and nothing of it but the rows of B is waited for. The weights are on their way before that.
-// kGradW behind kGradX waits only before it ends: kGradX writes nothing that it reads, and released it
-// when kGradH's results were there. Its units begin where kGradX's have run out.
+// The launch before is one of the same call. It was released when its own wait had returned, with all work before the
+// call complete: what the call was given (the weights, the offsets) is read before this launch's wait (a token's
+// eight experts 14.8 us, 17.9 with all reads behind it; a small training step 129 and 139). What another launch
+// of the call made is read behind it: rows of B, and all that kGradW reads. kGradX, before kGradW, writes nothing that
+// kGradW reads and has waited for kGradH, but that kGradH's dpre is visible to a third launch is promised by that
+// launch's own wait alone. (Without it kGradW began where kGradX's units had run out: 126 us instead of 129.)
 template <int kMode> constexpr bool early() { return kMode == kDown || kMode == kGradX; }
 // Warps of the epilogue: sixteen take half as long as eight with a launch's last tile (a small training
 // step of 6186 rows 143 us with eight, 133 with sixteen), but kGradW's words in shared memory would take
@@ -331,6 +333,10 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
       uint32_t phase = 0;
       bool ok = true;
       const int part0 = stage0 >= part_stages ? 1 : 0, first_k = (stage0 - part0 * part_stages) * 128;
+      if (kMode == kGradW && p.after_x) {
+        pdl_wait();
+        pdl_launch_dependents();
+      }
       for (int i = 0; ok; ++i) {
         const Unit un = unit_at(i, false);
         if (un.e < 0) break;
@@ -434,10 +440,6 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
         }
       }
       if (early<kMode>()) pdl_wait();   // (a pair without units ends no earlier than the launch before)
-      if (kMode == kGradW && p.after_x) {
-        pdl_wait();
-        pdl_launch_dependents();
-      }
       // the issuer's last commit arrives in this CTA, too
       wait(drain, 0, -1);
     }
