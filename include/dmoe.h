@@ -443,7 +443,7 @@ typedef struct {
  *   h          [R, I] out: also the second product's input, so it is always needed
  *   y          [R, d] out, row stride ldy
  *   zero_rest  nonzero: rows of y that are in no group become zeros; 0: they are not written
- * No output overlaps another one or an input.
+ * No output overlaps another one or an input; one that begins where those do is refused.
  * Rows of pre and h that are in no group are not written. Groups do not overlap: an element of a
  * row that two have is either's. A row's values do not depend on what the call's other rows hold, nor
  * on the groups they are in; R and n_groups choose the kernel, and with it the order of a row's sums. */
@@ -465,7 +465,7 @@ dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_g
  *   dw_gate, dw_up  [E, I, d] out, or NULL for both;  dw_down  [E, d, I] out, or NULL. Experts
  *              without rows get zeros. One output at least is wanted
  *   zero_rest  as above, for the rows of dx
- * No output overlaps another one or an input. */
+ * No output overlaps another one or an input that is read; one that begins where those do is refused. */
 dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, const void* dy,
                                      int64_t lddy, const void* x, int64_t ldx,
                                      const int32_t* offsets, const void* w_gate, const void* w_up,
@@ -502,7 +502,7 @@ typedef struct {
  *   n      [T, d] out (ldn) where w_pre is given, else NULL; may be y itself (with its stride)
  *   stats  fp32 [2, T] out: ry and rr (1 where there is no such norm), for the backward pass; or
  *          NULL
- * No output overlaps another one or an input otherwise. */
+ * No output overlaps another one or an input otherwise; one that begins where those do is refused. */
 dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_t ldx, const void* y,
                                int64_t ldy, const float* w_post, const void* gate, int64_t ldgate,
                                const float* w_pre, void* r, int64_t ldr, void* n, int64_t ldn,
@@ -521,7 +521,8 @@ dmoe_status dmoe_norm_workspace_size(const dmoe_norm_desc* desc, size_t* bytes /
  *   dx, dy     [T, d] out (lddx, lddy);  dgate  out, of the gate's shape (lddgate): sums over the
  *              tokens of a gate row, in fp32, rounded once
  *   dw_post, dw_pre  fp32 [d] out: sums over all tokens
- *              Any of the five may be NULL, but not all; none overlaps an input or another one
+ *              Any of the five may be NULL, but not all; none overlaps an input, the workspace or
+ *              another one (refused where it begins where those do)
  *   workspace  16-byte aligned; NULL is allowed for dx and dy alone
  * Sums over tokens are taken in an order that follows from the sizes: the same call gives the same
  * bits. */

@@ -128,6 +128,16 @@ bool matrix16(const void* p, int64_t ld, int32_t d) {
   return given16(p) && ld >= d && ld % 8 == 0 && ld < (int64_t)1 << 38;
 }
 
+// no output is an input that is read, or another output (NULL: there is none)
+bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (*o == nullptr) continue;
+    if (std::find(ins.begin(), ins.end(), *o) != ins.end() || std::find(o + 1, outs.end(), *o) != outs.end())
+      return false;
+  }
+  return true;
+}
+
 FfnArgs expert_args(const dmoe_expert_desc* d, int64_t R, int32_t n_groups, const int32_t* offsets,
                     const void* w_gate, const void* w_up, const void* w_down) {
   FfnArgs a{};
@@ -368,8 +378,8 @@ dmoe_status dmoe_expert_ffn(const dmoe_expert_desc* desc, int64_t R, int32_t n_g
   if (R == 0) return DMOE_OK;
   if (!matrix16(x, ldx, desc->d_model) || !matrix16(y, ldy, desc->d_model) || !given16(h) ||
       !null_or16(pre) || !given16(w_gate) || !given16(w_up) || !given16(w_down) ||
-      !null_or16(offsets) || !null_or16(expert_ids) || y == x || h == x || h == y ||
-      (pre != nullptr && (pre == x || pre == h || pre == y)))
+      !null_or16(offsets) || !null_or16(expert_ids) ||
+      !apart({pre, h, y}, {x, offsets, expert_ids, w_gate, w_up, w_down}))
     return DMOE_ERR_INVALID_ARG;
   FfnArgs a = expert_args(desc, R, n_groups, offsets, w_gate, w_up, w_down);
   a.expert_ids = expert_ids;
@@ -395,8 +405,7 @@ dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, co
   const bool inner = dx != nullptr || dw_gate != nullptr;
   if ((offsets == nullptr && n_groups != 1) || (!inner && dw_down == nullptr) ||
       (dw_gate == nullptr) != (dw_up == nullptr) || !null_or16(dw_gate) || !null_or16(dw_up) ||
-      !null_or16(dw_down) ||
-      (dw_gate != nullptr && (dw_gate == dw_up || dw_gate == dw_down || dw_up == dw_down)))
+      !null_or16(dw_down) || !apart({dw_gate, dw_up, dw_down}, {}))
     return DMOE_ERR_INVALID_ARG;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (R == 0) {   // no rows: the weights' gradients are zeros
@@ -409,12 +418,16 @@ dmoe_status dmoe_expert_ffn_backward(const dmoe_expert_desc* desc, int64_t R, co
     return DMOE_OK;
   }
   if (!matrix16(dy, lddy, desc->d_model) || !null_or16(offsets) ||
-      (inner && (!given16(w_down) || !given16(pre) || !given16(dpre) || dpre == pre || dpre == h ||
-                 dpre == dy || dpre == x || dpre == dx)) ||
-      (dx != nullptr && (!matrix16(dx, lddx, desc->d_model) || !given16(w_gate) ||
-                         !given16(w_up) || dx == dy || dx == x)) ||
+      (inner && (!given16(w_down) || !given16(pre) || !given16(dpre) || dpre == h || dpre == x)) ||
+      (dx != nullptr && (!matrix16(dx, lddx, desc->d_model) || !given16(w_gate) || !given16(w_up) || dx == x)) ||
       (dw_gate != nullptr && !matrix16(x, ldx, desc->d_model)) ||
       (dw_down != nullptr && !given16(h)))
+    return DMOE_ERR_INVALID_ARG;
+  // (what this call does not read may well be an output's place: h where dw_down is not wanted)
+  auto where = [](bool read, const void* p) { return read ? p : nullptr; };
+  if (!apart({inner ? dpre : nullptr, dx, dw_gate, dw_up, dw_down},
+             {dy, offsets, where(dw_gate != nullptr, x), where(inner, w_down), where(inner, pre),
+              where(dx != nullptr, w_gate), where(dx != nullptr, w_up), where(dw_down != nullptr, h)}))
     return DMOE_ERR_INVALID_ARG;
   FfnArgs a = expert_args(desc, R, n_groups, offsets, w_gate, w_up, w_down);
   a.dy = dy;
@@ -459,9 +472,8 @@ dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_
   if (!norm_inputs(desc, x, ldx, y, ldy, w_post, gate, ldgate, w_pre, &a) ||
       (w_pre == nullptr) != (n == nullptr) || (r == nullptr && n == nullptr) ||
       (r != nullptr && !matrix(r, ldr, dt, d)) || (n != nullptr && !matrix(n, ldn, dt, d)) ||
-      !null_or16(stats) || (r != nullptr && (r == n || r == y || r == gate)) ||
-      (n != nullptr && (n == x || n == gate)) || (r == x && ldr != ldx) ||
-      (n != nullptr && n == y && ldn != ldy))
+      !null_or16(stats) || !apart({r, n, stats}, {w_post, gate, w_pre}) || !apart({r, stats}, {y}) ||
+      !apart({n, stats}, {x}) || (r == x && ldr != ldx) || (n != nullptr && n == y && ldn != ldy))
     return DMOE_ERR_INVALID_ARG;
   if (!strides_fit({ldx, y != nullptr ? ldy : 0, r != nullptr ? ldr : 0, n != nullptr ? ldn : 0}))
     return DMOE_ERR_UNSUPPORTED;
@@ -511,14 +523,8 @@ dmoe_status dmoe_norm_residual_backward(
       (dgate != nullptr && (!matrix(dgate, lddgate, dt, d) || gate == nullptr)) ||
       (dw_post != nullptr && w_post == nullptr) || (dw_pre != nullptr && w_pre == nullptr))
     return DMOE_ERR_INVALID_ARG;
-  void* const outs[] = {dx, dy, dgate};
-  for (int i = 0; i < 3; ++i)
-    if (outs[i] != nullptr) {
-      for (const void* in : {x, y, gate, dr, dn})
-        if (outs[i] == in) return DMOE_ERR_INVALID_ARG;
-      for (int j = 0; j < i; ++j)
-        if (outs[i] == outs[j]) return DMOE_ERR_INVALID_ARG;
-    }
+  if (!apart({dx, dy, dgate, dw_post, dw_pre}, {x, y, w_post, gate, w_pre, stats, dr, dn, workspace}))
+    return DMOE_ERR_INVALID_ARG;
   if (dw_post != nullptr || dw_pre != nullptr || (dgate != nullptr && a.gate_tokens > 1)) {
     if (workspace == nullptr || !aligned(workspace, 16)) return DMOE_ERR_INVALID_ARG;
     if (workspace_bytes < norm_workspace_bytes(desc->T, d, a.gate_tokens)) return DMOE_ERR_WORKSPACE;

@@ -160,6 +160,19 @@ def test_captured_and_replayed():
         assert all(torch.equal(a, b) for a, b in zip((pre[:n], h[:n], y, dpre[:n], dx, *dw), want))
 
 
+def test_dx_in_the_place_of_what_is_not_read():
+    """h is an input for dw_down alone: without it dx may take its memory."""
+    c = case(torch.bfloat16, E, D, D, *MORE, seed=10)
+    pre, h, _ = run_forward(c)
+    want = run_backward(c, pre, h, skip=("dw_down",))
+    got = dict(want, dx=h, **{n: torch.empty_like(want[n]) for n in ("dpre", "dw_gate", "dw_up")})
+    args = (c["dy"], c["x"], c["offsets"], *weights(c), pre, h)
+    dm.dmoe_expert_ffn_backward(*args, *got.values())
+    assert torch.equal(h[:645], want["dx"][:645]) and torch.equal(got["dw_gate"], want["dw_gate"])
+    with pytest.raises(dm.DmoeError):
+        dm.dmoe_expert_ffn_backward(*args, *dict(got, dw_down=torch.empty_like(c["w_down"])).values())
+
+
 def units(shape, gen):
     """-1, 0 and 1."""
     return torch.randint(-1, 2, shape, dtype=torch.int8, device="cuda", generator=gen).to(torch.bfloat16)
