@@ -30,7 +30,7 @@
 // are the next product's operands, and the tensor cores take 16 bits (two operands for each, high and low
 // part, would be twice the work). The weights' gradients of 59000 rows in bf16 are off by 0.0031 of
 // their size so, and by 0.0017 with g, u and h in fp32.
-// Waits are bounded (1 s), record a timeout and unwind.
+// Waits are bounded, record a timeout and unwind.
 //
 // What bounds it, in bf16 with inputs larger than L2: 1024 rows for each of 64 experts of 2048 x 1024 take
 // 525 us forward (1.57 PFLOP/s, 0.83 of a large library product's rate) and 1083 backward (1.52): the
@@ -57,7 +57,10 @@ constexpr int kQueue = 4;
 constexpr int kLevels = 4;                  // heights of the boxes of rows
 constexpr int kMaxGroups = kMaxFfnExperts;
 constexpr int kNMax = 256;
+// A wait lasts as long as a unit at most: microseconds, but for the weights' gradients of very many rows, 317 ns for 64
+// of them (with 1 s for all waits 203 M rows of one expert ran out of time). They have a second, and 1 us for 64 rows.
 constexpr uint64_t kWaitNs = 1000000000ull;
+constexpr uint64_t kStageNs = 1000;
 
 enum Mode { kUp, kDown, kGradH, kGradX, kGradW };
 
@@ -268,11 +271,12 @@ ffn_products_kernel(const __grid_constant__ Maps tm, const Params p) {
   auto wait_for = [&](auto try_wait, int value) -> bool {
     if (try_wait()) return true;
     const uint64_t t0 = ptx::globaltimer_ns();
+    const uint64_t limit = kWaitNs + (kMode == kGradW ? (uint64_t)p.R / 64 * kStageNs : 0);
     for (uint32_t i = 1;; ++i) {
       if (try_wait()) return true;
       if ((i & 63u) == 0u) {
         if (*s_abort) return false;
-        if (ptx::globaltimer_ns() - t0 > kWaitNs) {
+        if (ptx::globaltimer_ns() - t0 > limit) {
           record_error(&ffn_fault, kErrTimeout, kAtFfn, value);
           *s_abort = 1;
           return false;

@@ -234,3 +234,21 @@ def test_every_element_of_a_long_call():
                 assert torch.equal(got[e], s.float().bfloat16())
     finally:
         torch.backends.cuda.matmul.allow_tf32 = tf32
+
+
+def test_a_sum_that_takes_longer_than_a_second():
+    """dw_down of 2^28 + 77 rows of one expert (of more than share a sum): a wait is bounded by what it waits for. Sums of
+    -1, 0 and 1, exact in fp32."""
+    E, d, I, R = 37, 8, 8, (1 << 28) + 77
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    dy, h = units((R, d), gen), units((R, I), gen)
+    offsets = torch.tensor([0] + [R] * E, dtype=torch.int32, device="cuda")
+    w = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((E, I, d), (E, I, d), (E, d, I))]
+    dw_down = torch.full((E, d, I), 7.0, dtype=torch.bfloat16, device="cuda")
+    dm.dmoe_expert_ffn_backward(dy, None, offsets, *w, None, h, None, None, None, None, dw_down)
+    assert dm.dmoe_expert_device_error()[0] == 0
+    want = torch.zeros((d, I), dtype=torch.float64, device="cuda")
+    for lo in range(0, R, 1 << 22):
+        at = slice(lo, lo + (1 << 22))
+        want += products(dy[at].t(), h[at].t()).double()       # (whole numbers up to 2^22)
+    assert torch.equal(dw_down[0], want.float().bfloat16()) and (dw_down[1:] == 0).all()
