@@ -509,8 +509,8 @@ dmoe_status dmoe_norm_residual(const dmoe_norm_desc* desc, const void* x, int64_
                                float* stats, void* stream);
 
 /* Bytes of the workspace of dmoe_norm_residual_backward (host only). They grow with T and d, and a
- * workspace for a desc with a gate serves one without. It needs no preparation, and nothing in it
- * has to last from call to call. */
+ * workspace for a desc with a gate serves one without; a gate's part is needed for dgate of rows that
+ * tokens share. It needs no preparation, and nothing in it has to last from call to call. */
 dmoe_status dmoe_norm_workspace_size(const dmoe_norm_desc* desc, size_t* bytes /* host */);
 
 /* The gradients by x, y, the gate and the weights, from those by r (dr) and by n (dn), either of

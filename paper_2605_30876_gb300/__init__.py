@@ -674,7 +674,8 @@ def _norm_args(x, y, w_post, gate, w_pre, scale, eps, gate_tokens):
 def dmoe_norm_residual(x, y, w_post, gate, w_pre, r, n, stats=None, scale=1.0, eps=1e-6, gate_tokens=0,
                        stream=None) -> None:
     """r = scale * x + gate * norm(y) * w_post, n = norm(r) * w_pre. y, w_post, gate, w_pre (with n) and r
-    may be None; gate [ceil(T / gate_tokens), d]: row t // gate_tokens holds for token t."""
+    may be None; gate [ceil(T / gate_tokens), d]: row t // gate_tokens holds for token t (gate_tokens 0: a row
+    for each token)."""
     desc, dev, args = _norm_args(x, y, w_post, gate, w_pre, scale, eps, gate_tokens)
     T, d, t = desc.T, desc.d, x.dtype
     pr, ldr = (None, 0) if r is None else _matrix(r, "r", T, d, t, dev)

@@ -525,9 +525,11 @@ dmoe_status dmoe_norm_residual_backward(
     return DMOE_ERR_INVALID_ARG;
   if (!apart({dx, dy, dgate, dw_post, dw_pre}, {x, y, w_post, gate, w_pre, stats, dr, dn, workspace}))
     return DMOE_ERR_INVALID_ARG;
-  if (dw_post != nullptr || dw_pre != nullptr || (dgate != nullptr && a.gate_tokens > 1)) {
+  // (a gate row of one token is complete where its token is)
+  const bool gate_parts = dgate != nullptr && a.gate_tokens > 1;
+  if (dw_post != nullptr || dw_pre != nullptr || gate_parts) {
     if (workspace == nullptr || !aligned(workspace, 16)) return DMOE_ERR_INVALID_ARG;
-    if (workspace_bytes < norm_workspace_bytes(desc->T, d, a.gate_tokens)) return DMOE_ERR_WORKSPACE;
+    if (workspace_bytes < norm_workspace_bytes(desc->T, d, gate_parts ? 1 : 0)) return DMOE_ERR_WORKSPACE;
   }
   if (!strides_fit({ldx, y != nullptr ? ldy : 0, dr != nullptr ? lddr : 0, dn != nullptr ? lddn : 0,
                     dx != nullptr ? lddx : 0, dy != nullptr ? lddy : 0}))
