@@ -191,15 +191,21 @@ def products(x, w):
     return x.float() @ w.float().t()
 
 
-def test_every_element_of_a_long_call():
-    """Rows whose offsets pass 2^31 elements, with values of which every product and sum is exact: x is 1 in its
-    first column and -1, 0 or 1 in the others, w_gate 64 in the first and 0 elsewhere, so that g = 64, silu(g) = 64 and its
-    derivative 1 (exp(-64) is less than half a step of 1 in fp32). w_up and w_down have one element of size 1 a
-    row: u is -1, 0 or 1, h and du are multiples of 64, all sums are whole numbers below 2^24."""
-    E, d, I = 3, 1096, 520
+# rows whose offsets pass 2^31 elements; the widest experts, with one row, with a few and with more than one unit has; the
+# most experts
+EXACT = [(1096, 520, [0, 1200007, 1200020, 2099990], 10), (16384, 16384, [0, 1], 0), (16384, 16384, [0, 5, 5, 300], 1),
+         (8, 16384, [0, 700], 3), (16384, 8, [0, 30, 1030], 0), (136, 72, [7 * i for i in range(513)], 9)]
+
+
+@pytest.mark.parametrize("d,I,ends,rest", EXACT, ids=lambda v: str(v)[:24])
+def test_every_element(d, I, ends, rest):
+    """Values of which every product and sum is exact: x is 1 in its first column and -1, 0 or 1 in the others, w_gate
+    64 in the first and 0 elsewhere, so that g = 64, silu(g) = 64 and its derivative 1 (exp(-64) is less than half a
+    step of 1 in fp32). w_up and w_down have one element of size 1 a row: u is -1, 0 or 1, h and du are multiples of
+    64, all sums are whole numbers below 2^24."""
+    E = len(ends) - 1
     gen = torch.Generator(device="cuda").manual_seed(9)
-    ends = [0, 1200007, 1200020, 2099990]
-    R = ends[-1] + 10
+    R = ends[-1] + rest
     x, dy = units((R, d), gen), units((R, d), gen)
     x[:, 0] = 1
     w_gate = torch.zeros((E, I, d), dtype=torch.bfloat16, device="cuda")
@@ -212,8 +218,8 @@ def test_every_element_of_a_long_call():
     dm.dmoe_expert_ffn(x, offsets, w_gate, w_up, w_down, h, y, pre=pre, zero_rest=True)
     dm.dmoe_expert_ffn_backward(dy, x, offsets, w_gate, w_up, w_down, pre, h, dpre, dx, *dw, zero_rest=True)
     assert dm.dmoe_expert_device_error()[0] == 0
-    assert (y[-10:] == 0).all() and (dx[-10:] == 0).all()
-    assert all((t[-10:] == 7).all() for t in (pre, h, dpre))
+    assert (y[ends[-1]:] == 0).all() and (dx[ends[-1]:] == 0).all()
+    assert all((t[ends[-1]:] == 7).all() for t in (pre, h, dpre))
     tf32 = torch.backends.cuda.matmul.allow_tf32
     torch.backends.cuda.matmul.allow_tf32 = False
     try:
@@ -225,7 +231,8 @@ def test_every_element_of_a_long_call():
                 assert (pre[at, 0] == 64).all() and torch.equal(pre[at, 1], u.bfloat16())
                 assert torch.equal(h[at], (64 * u).bfloat16())
                 assert torch.equal(y[at], products(64 * u, w_down[e]).bfloat16())
-                dg, du = (dh * u).bfloat16(), (64 * dh).bfloat16()       # (dh: few units, exact in 8 bits)
+                assert dh.abs().max() <= 256                             # (exact in bf16)
+                dg, du = (dh * u).bfloat16(), (64 * dh).bfloat16()
                 assert torch.equal(dpre[at, 0], dg) and torch.equal(dpre[at, 1], du)
                 assert torch.equal(dx[at], (products(dg, w_gate[e].t()) + products(du, w_up[e].t())).bfloat16())
                 for s, a, b in zip(sums, (dg, du, dy[at]), (x[at], x[at], h[at])):
