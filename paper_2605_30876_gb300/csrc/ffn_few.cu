@@ -479,8 +479,8 @@ cudaError_t few(const FfnArgs& a, cudaStream_t s) {
 //   one expert of 2048 x 512: 8 rows 14.8 / 7.4, 128 rows 17.5 / 15.3, 256 rows 21.4 / 20.6; of 4096 x 4096:
 //   8 rows 32.8 / 28.6; of 2048 x 2048: 32 rows 22.0 / 16.4; of 512 x 512: 512 rows 14.3 / 13.5
 //   4 experts of 4096 x 2048: 8 rows 43.8 / 39.4, 16 rows 42 / 63 (room in L1)
-//   8 of 2048 x 512: 8 rows 23.9 / 14.2, 64 rows 23.7 / 15.4, 256 rows 23.5 / 20.0 if each has 32, but 25.3 / 30.7
-//   if they have 13 to 61 (two chunks for some, one for others)
+//   8 of 2048 x 512: 8 rows 23.9 / 14.2, 64 rows 23.7 / 15.4, 256 rows 25.9 / 23.1 if each has 32 (a block routed as
+//   one), but 25.9 / 29.2 if they have 13 to 61 (two chunks for some, one for others)
 //   128 of 1024 x 512: 128 rows 70.3 / 71.7; 256 of 2048 x 512: 128 rows 128.9 / 131.6; 191 of 168 x 1632:
 //   191 rows 84.5 / 65.9; 75 of 72 x 2480: 75 rows 48.3 / 24.1
 bool expert_ffn_few_ok(const FfnArgs& a) {

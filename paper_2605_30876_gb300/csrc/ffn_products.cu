@@ -28,14 +28,14 @@
 // pairs' sums from their shared memory and adds them in the order of the pairs.
 // Sums are fp32 throughout. g, u, dg, du and h are rounded to the rows' type between products: they
 // are the next product's operands, and the tensor cores take 16 bits (two operands for each, high and low
-// part, would be twice the work). The weights' gradients of 59000 rows in bf16 are off by 0.0031 of
-// their size so, and by 0.0017 with g, u and h in fp32.
+// part, would be twice the work). In bf16, 59000 rows: y and dWd are off by 0.0023 of their size so, dx, dWg and dWu by
+// 0.0031, and by 0.0017, the rounding of the result, with g, u and h in fp32.
 // Waits are bounded, record a timeout and unwind.
 //
 // What bounds it, in bf16 with inputs larger than L2: 1024 rows for each of 64 experts of 2048 x 1024 take
-// 525 us forward (1.57 PFLOP/s, 0.83 of a large library product's rate) and 1083 backward (1.52): the
-// tensor pipe, epilogues at the ends. 230 rows each of 256 experts of 2048 x 512: 406 (5.8 TB/s) and
-// 794 us (5.4 TB/s): weights and rows from HBM, with MMAs of N < 256, which take 60 ns from N = 32 to 160,
+// 510 us forward (1.62 PFLOP/s, 0.85 of a large library product's rate) and 1080 backward (1.53): the
+// tensor pipe, epilogues at the ends. 230 rows each of 256 experts of 2048 x 512: 414 (5.6 TB/s) and
+// 792 us (5.4 TB/s): weights and rows from HBM, with MMAs of N < 256, which take 60 ns from N = 32 to 160,
 // close behind. Small calls: 5 us a launch before the first bytes and after the last.
 #include <cuda_fp16.h>
 

@@ -11,8 +11,9 @@ namespace {
 
 // A group of `width` threads takes the run of `run` rows from group * run on; the next depth - 1 are on
 // their way. kFull: x, y, r and n are all there, a row is exactly what its group holds, and a group is a
-// warp or more. (Asking for each of them every time is a fifth of the instructions: 16384 rows of 2048 in bf16,
-// cold, take 45.2 us without this form and 43.6 with it, 6.1 TB/s; the backward pass 77.8 and 67.9, 5.9 TB/s.)
+// warp or more. (Asking for each of them every time is a fifth of the instructions: 16384 rows of 2048 in bf16 without
+// a gate, cold, a launch's own time: 45.2 us without this form and 43.6 with it, 6.1 TB/s; the backward pass's first launch
+// 77.8 and 68, 5.9 TB/s.)
 template <typename T, int VB, int kE, int kBlock, bool kFull>
 __global__ void __launch_bounds__(kBlock, kBlock <= 256 ? 2 : 1)
 norm_kernel(const NormArgs a, int width, int depth, int run) {

@@ -23,7 +23,7 @@ __device__ __forceinline__ void from_f(float v, __nv_bfloat16* o) { *o = __float
 
 // Two fp32 values in a register pair, for the instructions that take two at once (a row's arithmetic
 // is as long as its bytes otherwise: with one value an instruction and unpacked conversions the
-// forward pass of 16384 rows of 2048 took 61 us, the backward 94, and issue slots were 70 % busy).
+// forward launch of 16384 rows of 2048 took 61 us, the backward one 94, and issue slots were 70 % busy).
 struct F2 {
   unsigned long long v;
   __device__ __forceinline__ F2() {}
@@ -309,8 +309,8 @@ cudaError_t with_type(int dtype, int piece, F f) {
 int esize(int dtype) { return dtype == DMOE_FP32 ? 4 : 2; }
 
 // Bytes that every row can be read and written at a time: 16, 4 or 2. The smaller, the more instructions a
-// row takes: 16384 rows in bf16, cold, forward and backward, of 2048 (16 bytes) 53 and 81 us, of 2050 (4) 72
-// and 177, of 2049 (2) 154 and 474.
+// row takes: 16384 rows in bf16 with a gate row for 32 tokens, cold, a call between two events, forward and backward, of
+// 2048 (16 bytes) 52 and 82 us, of 2050 (4) 72 and 175, of 2049 (2) 158 and 479.
 int piece_of_rows(const NormArgs& a) {
   const uint64_t es = esize(a.dtype);
   uint64_t bits = a.d * es;
